@@ -155,7 +155,7 @@ def _own(s):
     loss, lse, z = tr.head_distill(s["x"], s["W"], s["top_values"], s["top_ids"], case["tau"])
     if op == "distill":
         return loss, lse, z
-    return (loss, lse, z, *tr.head_distill_grad(s["x"], s["W"], s["top_values"], s["top_ids"], case["tau"], lse, z, s["grad_loss"]))
+    return (loss, lse, z, *tr.head_distill_grad(s["x"], s["W"], s["top_values"], s["top_ids"], case["tau"], lse, s["grad_loss"]))
 
 
 def _plain_project_grad(s):
