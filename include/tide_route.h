@@ -258,6 +258,64 @@ int tide_exit_project(const void* hidden, int dtype, int64_t C, int64_t T, int64
                       const float* norm_gain, float eps, void* out, int64_t out_row_stride,
                       void* stream);
 
+/* Gradient of the exit projection: with n_t = src_t / sqrt(mean(src_t^2) + eps), u_t = grad_out_t * norm_gain and src_t as above,
+ *   grad_rows[t,:] = (u_t - n_t * mean(u_t * n_t)) / sqrt(mean(src_t^2) + eps)     the gradient to the row that token t exited with
+ *   grad_gain      = sum over t of grad_out_t * n_t
+ * in fp32, grad_rows rounded once to `dtype`.  A token without a source (final_hidden == NULL and no exit) gets a row of zeros and
+ * adds nothing to grad_gain.  The sums are taken in a fixed order.
+ *   grad_out     device [T rows] of `dtype`: the gradient to tide_exit_project's out
+ *   grad_rows    device [T rows] of `dtype` out; bases and row strides as for tide_exit_project
+ *   grad_gain    device [d] fp32 out, 16-byte aligned, or NULL
+ *   workspace    device, 16-byte aligned, tide_exit_project_grad_bytes(T, d) bytes; it needs no initialisation.  NULL where grad_gain is    */
+size_t tide_exit_project_grad_bytes(int64_t T, int64_t d);
+int tide_exit_project_grad(const void* hidden, int dtype, int64_t C, int64_t T, int64_t d, int64_t ckpt_stride,
+                           int64_t row_stride, const void* final_hidden, int64_t final_row_stride,
+                           const int32_t* exit_layer, const int32_t* layer_ids, const float* norm_gain, float eps,
+                           const void* grad_out, int64_t grad_out_row_stride, void* grad_rows, int64_t grad_row_stride,
+                           float* grad_gain, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- Head operators: what the rows of tide_exit_project are scored with and trained on under the LM head W [V, d].
+ * z[t,v] = x_t . W_v is never stored; products of 16-bit values are exact and summed in fp32, fp32 operands are multiplied to about 22 bits.
+ *
+ * tide_head_loss: softmax cross entropy of every row,
+ *   lse[t] = log sum_v exp(z[t,v]),   loss[t] = lse[t] - z[t, target[t]],   0 where target[t] is not one of 0 .. V-1
+ * tide_head_loss_grad: with grad_loss[t] the gradient to loss[t] and lse from the forward call,
+ *   G[t,v] = grad_loss[t] * (exp(z[t,v] - lse[t]) - [v == target[t]]),   dx = G W,   dW = G^T x
+ * tide_head_distill: divergence from a teacher of which K logits per row are kept (top_values at the tokens top_ids; entries with a
+ *   token outside 0 .. V-1 or a value of -inf do not count, entries with equal tokens add up), at temperature tau,
+ *   q[t,k] = softmax_k(top_values[t,:] / tau),   lse[t] = log sum_v exp(z[t,v] / tau),   z_top[t,k] = z[t, top_ids[t,k]] (0 where no token)
+ *   loss[t] = tau^2 * sum_k q[t,k] * (log q[t,k] - z_top[t,k] / tau + lse[t]),   0 where the teacher has no entry
+ * tide_head_distill_grad:
+ *   G[t,v] = grad_loss[t] * tau * (exp(z[t,v] / tau - lse[t]) - sum of q[t,k] over top_ids[t,k] == v),   dx = G W,   dW = G^T x
+ *
+ * Rows without a target (or whose teacher has no entry) and rows with grad_loss[t] == 0 get dx = 0 and add nothing to dW, whatever
+ * they hold.  G is rounded once, to `dtype` (fp16 under a common power of two; fp32 to about 22 bits); dx and dW are summed in fp32 and
+ * rounded once.  dx or dW may be NULL: that product is left out.  T == 0: dW is filled with zeros.  The results do not depend on timing.
+ *
+ *   x          device [T rows] of `dtype`;  W device [V rows] of `dtype`;  strides in elements, at most 4194304
+ *              rows of whole 16-byte chunks: bases and strides multiples of 16 bytes; other hidden sizes: of an element (the call copies x and W)
+ *   1 <= d <= 16384, T <= 4194304, 1 <= K <= 1024, 1e-30 <= tau <= 1e30
+ *   target     device [T] int32;  top_values device [T,K] fp32;  top_ids device [T,K] int32
+ *   loss, lse, grad_loss  device [T] fp32;  z_top device [T,K] fp32
+ *   dx device [T rows], dW device [V rows] of `dtype`, aligned as x and W
+ *   workspace  device, 256-byte aligned, tide_head_workspace_bytes(dtype, T, d, V, K, gradient) bytes (K = 0: the loss; gradient != 0: the _grad call).  It needs no
+ *              initialisation and keeps nothing: calls on different workspaces may overlap.  The size is host arithmetic; 0 with tide_last_error() set if unsupported. */
+size_t tide_head_workspace_bytes(int dtype, int64_t T, int64_t d, int64_t V, int64_t K, int gradient);
+int tide_head_loss(const void* x, int dtype, int64_t T, int64_t d, int64_t V, int64_t x_row_stride, const void* W,
+                   int64_t w_row_stride, const int32_t* target, float* loss, float* lse, void* workspace,
+                   size_t workspace_bytes, void* stream);
+int tide_head_loss_grad(const void* x, int dtype, int64_t T, int64_t d, int64_t V, int64_t x_row_stride, const void* W,
+                        int64_t w_row_stride, const int32_t* target, const float* lse, const float* grad_loss, void* dx,
+                        int64_t dx_row_stride, void* dW, int64_t dw_row_stride, void* workspace, size_t workspace_bytes,
+                        void* stream);
+int tide_head_distill(const void* x, int dtype, int64_t T, int64_t d, int64_t V, int64_t x_row_stride, const void* W,
+                      int64_t w_row_stride, const float* top_values, const int32_t* top_ids, int64_t K, float tau,
+                      float* loss, float* lse, float* z_top, void* workspace, size_t workspace_bytes, void* stream);
+int tide_head_distill_grad(const void* x, int dtype, int64_t T, int64_t d, int64_t V, int64_t x_row_stride, const void* W,
+                           int64_t w_row_stride, const float* top_values, const int32_t* top_ids, int64_t K, float tau,
+                           const float* lse, const float* grad_loss, void* dx, int64_t dx_row_stride, void* dW,
+                           int64_t dw_row_stride, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Batch compaction (Sec. 3.4 kernel 2): the tokens that have exited at or before `layer`
  * (exit_layer[t] <= layer) and those that continue, as two index lists in ascending token order --
  * what a layer-skipping runtime needs to gather the continuing tokens after a checkpoint.

@@ -1,0 +1,435 @@
+// The matrix products of the head operators: z = x W^T of rows x [T, d] under an LM head W [V, d], what a softmax over the V
+// columns needs of z, and the two products of its gradient.  The logits are never kept: they are made a tile at a time, in
+// registers, and leave as
+//   kHeadStats   per row and 32 kBP columns the maximum and the sum of exponentials, and the logits of the row's own few tokens;
+//   kHeadGrad    G = (softmax - wanted) * scale of a piece of the vocabulary, in 16 bits, for the two products that follow;
+//   kHeadRows    dx += G W over that piece (fp32, a buffer per k slice);
+//   kHeadWeights dW = G^T x of that piece, complete.
+// The gradient makes the logits a second time, so a training step is four products where one that keeps T x V logits has three.
+//
+// One tile of kQ x kP output elements per workgroup of eight waves, k in stages of 32 elements.  "q" is the operand whose rows are
+// the output's rows, "p" the one whose rows are its columns: a matrix-core step takes the p fragment first, so a lane holds ONE
+// output row and, in its registers, runs of four consecutive columns (softmax: sums over columns stay in the lane).
+//
+// Both operands go through LDS by direct transfers (16 bytes a lane, no registers), a ring of kStages stages; what lies outside the operand is
+// fetched as zeros by the buffer descriptor's bound, so ragged rows, columns and k cost no instruction in the loop.  An operand
+// whose k runs along memory rows (x, W in the logits; G in dx) is read as fragments of 16 bytes; one whose k runs ACROSS memory rows
+// (W in dx; G and x in dW) lies in LDS as it lies in memory and is read by the transposing LDS loads, so no transposed copy of
+// W, x or G is ever made.
+//
+// The transfers are inline assembly: of the builtin the compiler makes every LDS read wait for all outstanding transfers, as it cannot
+// tell the ring's slots apart.  They have no output registers; they are ordered by explicit counts and the barrier in the MIDDLE of a stage,
+// which says that stage k + 1 has landed for every wave and that stage k - 1 has been read by every wave (its slot is filled next).
+//
+// fp32 operands are taken apart into two fp16 planes, x * 2^s = hi + lo + O(2^-23 x) with one power of two per tensor, and a product is three
+// passes over k: hi hi + hi lo + lo hi (what is dropped is 2^-22 of a term at most).  The fp32 matrix instructions have 1/16 of the 16-bit rate.
+#pragma once
+#include <type_traits>
+
+#include "device_utils.hpp"
+#include "prefill_dma_kernel.hpp"
+
+namespace tide {
+
+enum : int { kHeadStats = 0, kHeadGrad = 1, kHeadRows = 2, kHeadWeights = 3 };
+
+// What one call finds out on the device before its products (head_rows_kernel.hpp).
+struct HeadCtl {
+    int live;                      // rows that have a gradient
+    float x_scale, w_scale;        // powers of two that fp32 operands are multiplied by
+    float logit_scale;             // what the products of the logits are multiplied by (the planes' scales taken back)
+    float row_back, weight_back;   // the same for dx and dW
+};
+
+struct HeadOperand {
+    const char* plane[2];
+    int64_t row_bytes;
+};
+
+struct HeadGemmParams {
+    HeadOperand q, p;
+    int q_rows, p_rows, k;     // of these the one that counts live rows is replaced by ctl->live
+    int segments;              // 1, or 3 for two planes
+    int tiles_q, tiles_p, k_slices;
+    const HeadCtl* ctl;        // null where nothing is scaled and every row counts (16-bit statistics)
+    // statistics and G
+    float c1;                  // log2(e) / tau
+    const int32_t* ids;        // [T][K] the tokens' own entries of the vocabulary; others than 0 .. V - 1: none
+    const int32_t* source;     // G: the token of each row
+    int K, V, v0;              // p row 0 is token v0
+    float2* part;              // statistics: [tiles_p * kWP][q_rows]
+    float* z_out;              // statistics: [q_rows][K]
+    const float2* row_const;   // G: (lse * log2 e, scale) of each row
+    const float* wanted;       // G: [T][K] or null (one)
+    char* g_out;               // G
+    int64_t g_row_bytes, g_plane_bytes;
+    // dx
+    float* acc_out;            // [k_slices][acc_rows][acc_ld]
+    int64_t acc_slice;         // elements
+    int acc_ld, accumulate;
+    // dW
+    char* out;
+    int64_t out_row_elems;
+    int out_aligned;           // rows of whole 16-byte chunks
+};
+
+template <int WQ, int WP, int BQ, int BP, int S> struct HeadTile {
+    static constexpr int kWQ = WQ, kWP = WP, kBQ = BQ, kBP = BP, kStages = S;
+    static constexpr int kQ = WQ * BQ * 32, kP = WP * BP * 32;
+    static constexpr int kQBytes = kQ * 64, kPBytes = kP * 64, kStageBytes = kQBytes + kPBytes;
+    static constexpr int kCols = BP * 32, kLd = kCols + 4;       // a wave's columns; its rows in LDS after the loop, padded against bank conflicts
+    static constexpr int kEpiBytes = 8 * 32 * kLd * 4;
+    static constexpr int kLdsBytes = S * kStageBytes > kEpiBytes ? S * kStageBytes : kEpiBytes;
+    static_assert(WQ * WP == 8, "eight waves");
+    static_assert(kLdsBytes <= 160 * 1024, "LDS of a CU");
+};
+constexpr int kHeadThreads = 512;
+constexpr uint32_t kHeadNowhere = 0x80000000u;       // an offset at the descriptor's bound: fetched as zeros
+
+// 64 lanes x 16 bytes from memory (offsets voff from the descriptor's base) to 1 KiB of LDS at byte `lds`.
+__device__ __forceinline__ void head_dma(uint32_t lds, uint32_t voff, u32x4 rsrc) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(voff), "s"(rsrc) : "memory");
+}
+template <int n> __device__ __forceinline__ void head_wait_vm() { asm volatile("s_waitcnt vmcnt(%0)" ::"i"(n) : "memory"); }
+
+// One operand's transfers: kRows tile rows, instruction n = wave + 8 i of kRows / 16.
+template <int kRows, bool kAcross> struct HeadFeed {
+    static constexpr int kInstr = kRows / 16, kN = (kInstr + 7) / 8;
+    uint32_t voff[kN];
+    int along[kN];             // first k element of this lane's chunk within a stage (along), or its k row (across)
+    const char* base;
+    int64_t step;
+
+    // Position of chunk c of a memory row in LDS.  Along: 64-byte rows, chunk ^ (row / 4) % 4, so that the 16 rows a quarter wave reads cover all
+    // banks.  Across: rows of kRows * 2 bytes, 64-byte pieces moved by the row's number where that leaves banks unused.
+    static __device__ __forceinline__ int place_along(int row, int c) { return c ^ ((row >> 2) & 3); }
+    static __device__ __forceinline__ int place_across(int kr, int c) {
+        if constexpr (kRows >= 128) return c ^ ((kr & 3) << 2);
+        else if constexpr (kRows == 64) return c ^ (((kr >> 1) & 1) << 2);
+        else return c;
+    }
+
+    __device__ __forceinline__ void init(const HeadOperand& o, int row0, int rows, int wave, int lane) {
+#pragma unroll
+        for (int i = 0; i < kN; ++i) {
+            const int n = wave + 8 * i;
+            if constexpr (!kAcross) {
+                const int r = 16 * n + (lane >> 2), c = place_along(r, lane & 3);
+                voff[i] = row0 + r < rows ? (uint32_t)r * (uint32_t)o.row_bytes + c * 16 : kHeadNowhere;
+                along[i] = c * 8;
+            } else {
+                constexpr int kRowBytes = kRows * 2;
+                const int byte = n * 1024 + lane * 16, kr = byte / kRowBytes, c = place_across(kr, (byte % kRowBytes) >> 4);
+                voff[i] = row0 + c * 8 < rows ? (uint32_t)kr * (uint32_t)o.row_bytes + c * 16 : kHeadNowhere;
+                along[i] = kr;
+            }
+        }
+        step = kAcross ? 32 * o.row_bytes : 64;
+    }
+    __device__ __forceinline__ void seek(const HeadOperand& o, int plane, int row0, int stage) {
+        base = o.plane[plane] + (kAcross ? (int64_t)row0 * 2 : (int64_t)row0 * o.row_bytes) + stage * step;
+    }
+    // left: k elements from this stage's start to the operand's end (0 or less: nothing is fetched)
+    __device__ __forceinline__ void issue(uint32_t lds, int left, int wave) {
+        u32x4 rsrc;
+        rsrc[0] = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)base);
+        rsrc[1] = __builtin_amdgcn_readfirstlane((uint32_t)((uintptr_t)base >> 32) & 0xffffu);
+        rsrc[2] = left > 0 ? kHeadNowhere : 0u;
+        rsrc[3] = 0x00020000u;
+#pragma unroll
+        for (int i = 0; i < kN; ++i) {
+            if (kInstr % 8 != 0 && wave + 8 * i >= kInstr) break;
+            uint32_t v = voff[i];
+            if (left < 32) v = along[i] < left ? v : kHeadNowhere;
+            head_dma(lds + (wave + 8 * i) * 1024, v, rsrc);
+        }
+        base += step;
+    }
+};
+
+typedef __attribute__((address_space(3))) char head_lds;
+typedef __attribute__((ext_vector_type(4))) short s16x4;
+typedef __attribute__((address_space(3))) s16x4 head_lds_s16x4;
+typedef __attribute__((address_space(3))) u32x4 head_lds_u32x4;
+
+// The fragment of block b (32 tile rows) and k group g (16 elements) of an operand at `at`: lane l gets row l % 32, the 8 k values of half l / 32.
+template <int kRows, bool kAcross> __device__ __forceinline__ u32x4 head_fragment(head_lds* at, int b, int g, int lane) {
+    typedef HeadFeed<kRows, kAcross> Feed;
+    if constexpr (!kAcross) {
+        const int row = lane & 31, c = Feed::place_along(row, 2 * g + (lane >> 5));        // (32 b moves the place by nothing: a multiple of 16 rows)
+        return *(head_lds_u32x4*)(at + 32 * b * 64 + row * 64 + c * 16);
+    } else {
+        // two loads of four k rows: a group of 16 lanes supplies 4 rows x 16 columns and each lane receives one column
+        const int i = lane & 15, c = 4 * b + 2 * ((lane >> 4) & 1) + ((i & 3) >> 1);
+        s16x4 v[2];
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const int kr = 16 * g + 8 * (lane >> 5) + 4 * s + (i >> 2);
+            v[s] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((head_lds_s16x4*)(at + kr * (kRows * 2) + Feed::place_across(kr, c) * 16 + (i & 1) * 8));
+        }
+        typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
+        const u32x2 a = __builtin_bit_cast(u32x2, v[0]), d = __builtin_bit_cast(u32x2, v[1]);
+        return u32x4{a[0], a[1], d[0], d[1]};
+    }
+}
+
+// Tile `id` of tiles_q x tiles_p: every XCD (workgroup id mod 8) takes a contiguous eighth of a list that goes through groups of 8 row tiles column by
+// column, so that the 32 tiles an XCD works on at a time share 8 row tiles and 4 column tiles in its L2.
+__device__ __forceinline__ bool head_tile(int id, int tiles_q, int tiles_p, int& tq, int& tp) {
+    const int total = tiles_q * tiles_p, per_xcd = (total + 7) >> 3;
+    const int t = (id & 7) * per_xcd + (id >> 3);
+    if ((id >> 3) >= per_xcd || t >= total) return false;
+    const int group = t / (8 * tiles_p), q0 = group * 8, nq = min(8, tiles_q - q0), in = t - q0 * tiles_p;
+    tp = in / nq;
+    tq = q0 + (in - tp * nq);
+    return true;
+}
+
+template <int DT> __device__ __forceinline__ uint32_t head_round2(float a, float b) {
+    if constexpr (DT == kF16) {
+        const f16x2 h = {static_cast<_Float16>(a), static_cast<_Float16>(b)};
+        return __builtin_bit_cast(uint32_t, h);
+    } else {
+        const bf16x2 h = {static_cast<__bf16>(a), static_cast<__bf16>(b)};
+        return __builtin_bit_cast(uint32_t, h);
+    }
+}
+
+// DT: the operands' element type, kF16 or kBF16.  OutDT: the type dW is written in.  grid = (8 * ceil(tiles / 8), k_slices).
+template <int DT, int OutDT, int kMode, class Tile>
+__global__ __launch_bounds__(kHeadThreads) void tide_head_gemm_kernel(const HeadGemmParams p) {
+    constexpr bool kQAcross = kMode == kHeadWeights, kPAcross = kMode == kHeadRows || kMode == kHeadWeights;
+    constexpr int kBQ = Tile::kBQ, kBP = Tile::kBP, S = Tile::kStages, kCols = Tile::kCols, kLd = Tile::kLd;
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int wq = wave % Tile::kWQ, wp = wave / Tile::kWQ;
+    int tq, tp;
+    if (!head_tile(blockIdx.x, p.tiles_q, p.tiles_p, tq, tp)) return;
+    const int live = kMode == kHeadStats ? 0 : p.ctl->live;
+    const int q_rows = kMode == kHeadGrad || kMode == kHeadRows ? live : p.q_rows;
+    const int k_elems = kMode == kHeadWeights ? live : p.k;
+    const int q0 = tq * Tile::kQ, p0 = tp * Tile::kP;
+    if (q0 >= q_rows) return;
+
+    // ---- k loop: n stages, the slice's part of every segment
+    const int per = (k_elems + 31) >> 5;
+    const int first = (int)((int64_t)per * blockIdx.y / p.k_slices), last = (int)((int64_t)per * (blockIdx.y + 1) / p.k_slices);
+    const int nk = last - first, n = nk * p.segments;
+    HeadFeed<Tile::kQ, kQAcross> fq;
+    HeadFeed<Tile::kP, kPAcross> fp;
+    fq.init(p.q, q0, q_rows, wave, lane);
+    fp.init(p.p, p0, p.p_rows, wave, lane);
+    fq.seek(p.q, 0, q0, first);
+    fp.seek(p.p, 0, p0, first);
+    const uint32_t lds0 = (uint32_t)(size_t)(head_lds*)smem;
+    int issued = 0, kk = 0, fill = 0;                     // stages issued, the next one's number within its segment, and its slot's byte
+    auto issue = [&] {
+        const int left = issued < n ? k_elems - (first + kk) * 32 : 0;
+        fq.issue(lds0 + fill, left, wave);
+        fp.issue(lds0 + fill + Tile::kQBytes, left, wave);
+        fill = fill + Tile::kStageBytes == S * Tile::kStageBytes ? 0 : fill + Tile::kStageBytes;
+        ++issued;
+        if (++kk == nk && issued < n) {                   // the next segment: (hi, hi), (hi, lo), (lo, hi)
+            kk = 0;
+            fq.seek(p.q, issued == 2 * nk ? 1 : 0, q0, first);
+            fp.seek(p.p, issued == nk ? 1 : 0, p0, first);
+        }
+    };
+    // Waits until all but the kYounger last stages issued by this wave have landed.
+    auto landed = [&](auto younger_c) {
+        constexpr int kYounger = decltype(younger_c)::value;
+        constexpr int kFull = Tile::kQ / 128 + Tile::kP / 128, kRest = Tile::kQ / 16 % 8;
+        static_assert(Tile::kP % 128 == 0, "");
+        if (kRest != 0 && wave < kRest) head_wait_vm<kYounger * (kFull + 1)>();
+        else head_wait_vm<kYounger * kFull>();
+    };
+
+    f32x16 acc[kBP][kBQ];
+#pragma unroll
+    for (int i = 0; i < kBP; ++i)
+#pragma unroll
+        for (int j = 0; j < kBQ; ++j) acc[i][j] = f32x16{0};
+    u32x4 aq[2][kBQ], ap[2][kBP];
+    auto read = [&](auto g_c, int slot) {
+        constexpr int g = decltype(g_c)::value;
+        head_lds* at = (head_lds*)smem + slot;
+#pragma unroll
+        for (int j = 0; j < kBQ; ++j) aq[g][j] = head_fragment<Tile::kQ, kQAcross>(at, wq * kBQ + j, g, lane);
+#pragma unroll
+        for (int i = 0; i < kBP; ++i) ap[g][i] = head_fragment<Tile::kP, kPAcross>(at + Tile::kQBytes, wp * kBP + i, g, lane);
+    };
+    auto multiply = [&](auto g_c) {
+        constexpr int g = decltype(g_c)::value;
+#pragma unroll
+        for (int i = 0; i < kBP; ++i)
+#pragma unroll
+            for (int j = 0; j < kBQ; ++j) acc[i][j] = mma_k16<DT>(ap[g][i], aq[g][j], acc[i][j]);
+    };
+    constexpr std::integral_constant<int, 0> g0;
+    constexpr std::integral_constant<int, 1> g1;
+    constexpr std::integral_constant<int, S - 3> steady;
+
+#pragma unroll
+    for (int s = 0; s < S - 1; ++s) issue();
+    landed(std::integral_constant<int, S - 2>{});
+    ring_barrier();
+    read(g0, 0);
+    int slot = 0;
+    for (int k = 0; k < n; ++k) {
+        const int next = slot + Tile::kStageBytes == S * Tile::kStageBytes ? 0 : slot + Tile::kStageBytes;
+        read(g1, slot);
+        multiply(g0);
+        landed(steady);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // this wave has read all of stage k
+        ring_barrier();
+        issue();
+        read(g0, next);
+        multiply(g1);
+        slot = next;
+    }
+    head_wait_vm<0>();
+    __syncthreads();
+
+    // ---- what becomes of the tile
+    typedef __attribute__((address_space(3))) float lds_float;
+    typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
+    lds_float* stage = (lds_float*)((head_lds*)smem + wave * 32 * kLd * 4);
+    const int row = lane & 31, h = lane >> 5;
+    const int col0 = p0 + wp * kCols;                     // the wave's first column
+    // this wave's block of 32 rows into LDS, row by row; f(value, column within the wave's)
+    auto to_lds = [&](int j, auto f) {
+#pragma unroll
+        for (int i = 0; i < kBP; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                f32x4 v;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = f(acc[i][j][4 * q + e], 32 * i + 8 * q + 4 * h + e);
+                *(lds_f32x4*)(stage + row * kLd + 32 * i + 8 * q + 4 * h) = v;
+            }
+    };
+    auto lds_fence = [] {                                  // the wave's own LDS accesses stay in order
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    };
+
+#pragma unroll
+    for (int j = 0; j < kBQ; ++j) {
+        const int t0 = q0 + (wq * kBQ + j) * 32, t = t0 + row;
+        if constexpr (kMode == kHeadStats) {
+            const float scale = p.ctl ? p.ctl->logit_scale : 1.0f, c1 = p.c1 * scale;
+            const bool ragged = col0 + kCols > p.p_rows;
+            float m = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < kBP; ++i)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) {
+                    if (ragged && col0 + 32 * i + 8 * (v >> 2) + 4 * h + (v & 3) >= p.p_rows) acc[i][j][v] = -INFINITY;
+                    m = fmaxf(m, acc[i][j][v]);
+                }
+            m = fmaxf(m, __shfl_xor(m, 32, kWave));
+            const float m2 = m * c1, shift = m2 == -INFINITY ? 0.0f : m2;
+            float s = 0.0f;
+#pragma unroll
+            for (int i = 0; i < kBP; ++i)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) s += __builtin_amdgcn_exp2f(fmaf(acc[i][j][v], c1, -shift));
+            s += __shfl_xor(s, 32, kWave);
+            if (h == 0 && t < q_rows) p.part[(int64_t)(tp * Tile::kWP + wp) * q_rows + t] = float2{m2, s};
+            // the row's own tokens among these columns: lane halves take every second one
+            bool any = false;
+            if (t < q_rows)
+                for (int k = h; k < p.K; k += 2) any |= (uint32_t)p.ids[(int64_t)t * p.K + k] - (uint32_t)col0 < (uint32_t)kCols;
+            if (__any(any)) {
+                to_lds(j, [](float z, int) { return z; });
+                lds_fence();
+                if (any)
+                    for (int k = h; k < p.K; k += 2) {
+                        const int id = p.ids[(int64_t)t * p.K + k];
+                        if ((uint32_t)id - (uint32_t)col0 < (uint32_t)kCols && id < p.V) p.z_out[(int64_t)t * p.K + k] = stage[row * kLd + id - col0] * scale;
+                    }
+                lds_fence();
+            }
+        } else if constexpr (kMode == kHeadGrad) {
+            const float c1 = p.c1 * p.ctl->logit_scale;
+            const float2 rc = t < q_rows ? p.row_const[t] : float2{0.0f, 0.0f};
+            const int64_t own = t < q_rows ? (int64_t)p.source[t] * p.K : 0;
+            to_lds(j, [&](float z, int c) { return col0 + c < p.p_rows ? rc.y * __builtin_amdgcn_exp2f(fmaf(z, c1, -rc.x)) : 0.0f; });
+            lds_fence();
+            if (t < q_rows)
+                for (int k = 0; k < p.K; ++k) {           // each half of the lanes its own columns: a token that is given twice is subtracted in order
+                    const int c = (int)((uint32_t)p.ids[own + k] - (uint32_t)(p.v0 + col0));
+                    if ((uint32_t)c < (uint32_t)kCols && ((c >> 4) & 1) == h && col0 + c < p.p_rows) {
+                        const float w = p.wanted ? p.wanted[own + k] : 1.0f;
+                        stage[row * kLd + c] = fmaf(-w, rc.y, stage[row * kLd + c]);
+                    }
+                }
+            lds_fence();
+            constexpr int kLanes = kCols / 8, kRowsAtOnce = 64 / kLanes;      // 16 bytes of G a lane
+#pragma unroll
+            for (int r0 = 0; r0 < 32; r0 += kRowsAtOnce) {
+                const int r = r0 + lane / kLanes, c = lane % kLanes * 8;
+                if (t0 + r >= q_rows) continue;
+                const f32x4 a = *(lds_f32x4*)(stage + r * kLd + c), b = *(lds_f32x4*)(stage + r * kLd + c + 4);
+                char* dst = p.g_out + (int64_t)(t0 + r) * p.g_row_bytes + (int64_t)(col0 + c) * 2;
+                *reinterpret_cast<u32x4*>(dst) = u32x4{head_round2<DT>(a[0], a[1]), head_round2<DT>(a[2], a[3]), head_round2<DT>(b[0], b[1]), head_round2<DT>(b[2], b[3])};
+                if constexpr (OutDT == kF32) {
+                    f32x4 x = a, y = b;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        x[e] = a[e] - (float)static_cast<_Float16>(a[e]);
+                        y[e] = b[e] - (float)static_cast<_Float16>(b[e]);
+                    }
+                    *reinterpret_cast<u32x4*>(dst + p.g_plane_bytes) = u32x4{head_round2<DT>(x[0], x[1]), head_round2<DT>(x[2], x[3]), head_round2<DT>(y[0], y[1]), head_round2<DT>(y[2], y[3])};
+                }
+            }
+            lds_fence();
+        } else if constexpr (kMode == kHeadRows) {
+            if (t < q_rows) {
+                float* dst = p.acc_out + blockIdx.y * p.acc_slice + (int64_t)t * p.acc_ld;
+#pragma unroll
+                for (int i = 0; i < kBP; ++i)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const int c = col0 + 32 * i + 8 * q + 4 * h;
+                        if (c >= p.acc_ld) continue;
+                        f32x4 v = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+                        f32x4* at = reinterpret_cast<f32x4*>(dst + c);
+                        if (p.accumulate) v += *at;
+                        *at = v;
+                    }
+            }
+        } else {
+            const float back = p.ctl->weight_back;
+            to_lds(j, [&](float v, int) { return v * back; });
+            lds_fence();
+            constexpr int kBytes = Storage<OutDT>::kBytes, kE = 16 / kBytes, kLanes = kCols / kE, kRowsAtOnce = 64 / kLanes;
+#pragma unroll
+            for (int r0 = 0; r0 < 32; r0 += kRowsAtOnce) {
+                const int r = r0 + lane / kLanes, c = lane % kLanes * kE;
+                if (t0 + r >= q_rows || col0 + c >= p.p_rows) continue;
+                float v[kE];
+#pragma unroll
+                for (int e = 0; e < kE; ++e) v[e] = stage[r * kLd + c + e];
+                char* dst = p.out + ((int64_t)(t0 + r) * p.out_row_elems + col0 + c) * kBytes;
+                if (p.out_aligned) {
+                    if constexpr (kBytes == 2)
+                        *reinterpret_cast<u32x4*>(dst) = u32x4{head_round2<OutDT>(v[0], v[1]), head_round2<OutDT>(v[2], v[3]), head_round2<OutDT>(v[4], v[5]), head_round2<OutDT>(v[6], v[7])};
+                    else
+                        *reinterpret_cast<f32x4*>(dst) = f32x4{v[0], v[1], v[2], v[3]};
+                } else {
+#pragma unroll
+                    for (int e = 0; e < kE; ++e)
+                        if (col0 + c + e < p.p_rows) {
+                            if constexpr (OutDT == kF16) reinterpret_cast<_Float16*>(dst)[e] = static_cast<_Float16>(v[e]);
+                            else if constexpr (OutDT == kBF16) reinterpret_cast<__bf16*>(dst)[e] = static_cast<__bf16>(v[e]);
+                            else reinterpret_cast<float*>(dst)[e] = v[e];
+                        }
+                }
+            }
+            lds_fence();
+        }
+    }
+}
+
+}  // namespace tide

@@ -1,0 +1,525 @@
+// Host side of the head operators (include/tide_route.h): argument checks, the division of the work, the workspace's layout and the launches.
+// Included by tide_route.hip, whose error reporting and device queries it uses.
+#pragma once
+
+namespace {
+
+// The tile that the rows of a call take.  The vocabulary side is always 256 wide.
+using HeadTile32 = HeadTile<1, 8, 1, 1, 8>;
+using HeadTile64 = HeadTile<2, 4, 1, 2, 7>;
+using HeadTile128 = HeadTile<2, 4, 2, 2, 6>;
+using HeadTile256 = HeadTile<4, 2, 2, 4, 5>;
+constexpr int kHeadCols = 256;
+constexpr int64_t kHeadMostRows = (int64_t)1 << 22, kHeadMostVocab = ((int64_t)1 << 31) - 1024;
+constexpr int kHeadMostTop = 1024;
+constexpr size_t kHeadPieceBytes = (size_t)256 << 20;      // G of a piece of the vocabulary: as much as stays in the last-level cache
+
+template <typename F> int by_head_tile(int rows, F&& f) {
+    switch (rows) {
+    case 32: return f(HeadTile32{});
+    case 64: return f(HeadTile64{});
+    case 128: return f(HeadTile128{});
+    default: return f(HeadTile256{});
+    }
+}
+
+struct HeadShape {
+    int dtype;
+    int64_t T, d, V, K;
+    int64_t dp() const { return (d + 7) / 8 * 8; }                      // elements of a padded row of 16-bit values
+    int planes() const { return dtype == TIDE_F32 ? 2 : 1; }
+    bool copied() const { return dtype == TIDE_F32 || d % 8 != 0; }     // the products read copies of x and W
+    int64_t plane_bytes(int64_t rows) const { return rows * dp() * 2; }
+    int rows_per_tile() const {
+        if (T <= 32) return 32;
+        if (T <= 64) return 64;
+        // 128-row tiles need a third more time per row; what a last, partly filled tile wastes decides
+        const int64_t small = (T + 127) / 128 * 128, large = (T + 255) / 256 * 256;
+        return 4 * small < 3 * large || T <= 128 ? 128 : 256;
+    }
+    int64_t row_tiles() const { return (T + rows_per_tile() - 1) / rows_per_tile(); }
+    int64_t col_tiles() const { return (V + kHeadCols - 1) / kHeadCols; }
+    int64_t parts() const { return col_tiles() * (rows_per_tile() == 32 ? 8 : rows_per_tile() == 256 ? 2 : 4); }
+    // columns of a piece of the vocabulary in the gradient: equal pieces whose G is at most kHeadPieceBytes
+    int64_t piece() const {
+        const int64_t tiles = std::max<int64_t>(1, (int64_t)(kHeadPieceBytes / ((size_t)std::max<int64_t>(T, 1) * planes() * 2 * kHeadCols)));
+        const int64_t pieces = (col_tiles() + tiles - 1) / tiles;
+        return (col_tiles() + pieces - 1) / pieces * kHeadCols;
+    }
+    // workgroups that share a tile's piece of the vocabulary in dx = G W: what fills the chip once
+    int dx_slices(unsigned cus) const {
+        const int64_t tiles = row_tiles() * ((d + kHeadCols - 1) / kHeadCols);
+        return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(cus / std::max<int64_t>(tiles, 1), 64), piece() / kHeadCols));
+    }
+};
+
+// The workspace of a call: counted with a null base, laid out with the caller's.
+struct HeadSpace {
+    char* base;
+    size_t at = 0;
+    template <typename T> T* take(size_t n) {
+        T* p = base ? reinterpret_cast<T*>(base + at) : nullptr;
+        at += (n * sizeof(T) + 255) & ~size_t(255);
+        return p;
+    }
+};
+struct HeadWork {
+    HeadCtl* ctl;
+    uint32_t *x_max, *w_max;
+    char *x, *w;               // copies: the rows (of the gradient: the live ones), the weights
+    float2* part;
+    float* z;
+    int32_t *source, *place;
+    float2* row_const;
+    float* wanted;
+    uint8_t* taught;
+    char* g;
+    float* acc;
+};
+size_t head_layout(const HeadShape& s, bool grads, unsigned cus, void* base, HeadWork* out) {
+    HeadSpace sp{(char*)base};
+    HeadWork w{};
+    w.ctl = sp.take<HeadCtl>(1);
+    if (s.dtype == TIDE_F32) {
+        w.x_max = sp.take<uint32_t>(kHeadMaxBlocks);
+        w.w_max = sp.take<uint32_t>(kHeadMaxBlocks);
+    }
+    if (s.copied()) w.w = sp.take<char>((size_t)s.plane_bytes(s.V) * s.planes());
+    if (s.copied() || grads) w.x = sp.take<char>((size_t)s.plane_bytes(s.T) * s.planes());
+    if (!grads) {
+        w.part = sp.take<float2>((size_t)s.parts() * s.T);
+        if (!s.K) w.z = sp.take<float>((size_t)s.T);
+    } else {
+        w.source = sp.take<int32_t>((size_t)s.T);
+        w.place = sp.take<int32_t>((size_t)s.T);
+        w.row_const = sp.take<float2>((size_t)s.T);
+        if (s.K) {
+            w.wanted = sp.take<float>((size_t)s.T * s.K);
+            w.taught = sp.take<uint8_t>((size_t)s.T);
+        }
+        w.g = sp.take<char>((size_t)s.T * s.piece() * 2 * s.planes());
+        w.acc = sp.take<float>((size_t)s.dx_slices(cus) * s.T * s.dp());
+    }
+    if (out) *out = w;
+    return sp.at;
+}
+
+template <int DT, int OutDT, int kMode, class Tile> int launch_head(int64_t q_rows, int64_t p_rows, hipStream_t st, HeadGemmParams& p) {
+    static std::atomic<bool> raised[kMaxDevices];
+    int dev = 0;
+    const int rc = current_device(&dev);
+    if (rc) return rc;
+    if (!raised[dev].load(std::memory_order_relaxed)) {
+        TIDE_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(&tide_head_gemm_kernel<DT, OutDT, kMode, Tile>), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                     Tile::kLdsBytes));
+        raised[dev].store(true, std::memory_order_relaxed);
+    }
+    const int64_t tq = (q_rows + Tile::kQ - 1) / Tile::kQ, tp = (p_rows + Tile::kP - 1) / Tile::kP;
+    p.tiles_q = (int)tq;
+    p.tiles_p = (int)tp;
+    if (tq * tp == 0) return TIDE_OK;
+    hipLaunchKernelGGL((tide_head_gemm_kernel<DT, OutDT, kMode, Tile>), dim3(8u * (unsigned)((tq * tp + 7) / 8), (unsigned)p.k_slices), dim3(kHeadThreads),
+                       Tile::kLdsBytes, st, p);
+    return TIDE_OK;
+}
+// The products of fp32 operands run on fp16 planes.
+template <int DT> constexpr int kHeadElem = DT == kF32 ? (int)kF16 : DT;
+
+struct HeadCall {
+    HeadShape s;
+    const void *x, *W;
+    int64_t x_stride, w_stride;
+    const int32_t* ids;        // targets, or the teacher's tokens
+    const float* values;       // teacher's values, or null
+    float tau;
+    float *loss, *lse, *z;     // forward
+    const float *lse_in, *grad;
+    void *dx, *dW;
+    int64_t dx_stride, dw_stride;
+    void* workspace;
+    size_t workspace_bytes;
+    hipStream_t st;
+};
+
+int check_head(const HeadCall& c, bool grads) {
+    const HeadShape& s = c.s;
+    if (s.dtype != TIDE_F32 && s.dtype != TIDE_F16 && s.dtype != TIDE_BF16) return fail(TIDE_ERR_INVALID_ARG, "dtype %d is not a tide_dtype_t", s.dtype);
+    if (s.T < 0) return fail(TIDE_ERR_INVALID_ARG, "T = %lld is negative", (long long)s.T);
+    if (s.T > kHeadMostRows) return fail(TIDE_ERR_UNSUPPORTED, "T = %lld exceeds %lld", (long long)s.T, (long long)kHeadMostRows);
+    if (s.d <= 0) return fail(TIDE_ERR_INVALID_ARG, "d = %lld must be positive", (long long)s.d);
+    if (s.d > kMaxHidden) return fail(TIDE_ERR_UNSUPPORTED, "d = %lld: hidden sizes from 1 to 16384", (long long)s.d);
+    if (s.V <= 0) return fail(TIDE_ERR_INVALID_ARG, "V = %lld must be positive", (long long)s.V);
+    if (s.V > kHeadMostVocab) return fail(TIDE_ERR_UNSUPPORTED, "V = %lld exceeds %lld", (long long)s.V, (long long)kHeadMostVocab);
+    if (s.K < 0 || s.K > kHeadMostTop) return fail(TIDE_ERR_UNSUPPORTED, "K = %lld: 1 to %d entries of a teacher", (long long)s.K, kHeadMostTop);
+    if (!(c.tau > 0.0f) || !(c.tau <= 1e30f) || c.tau < 1e-30f) return fail(TIDE_ERR_INVALID_ARG, "tau = %g must be positive and finite", (double)c.tau);
+    if (c.x_stride < s.d || c.w_stride < s.d) return fail(TIDE_ERR_INVALID_ARG, "row strides of x and W must be at least d");
+    const int64_t most = (int64_t)1 << 22;             // elements: 256 rows of a tile at 32-bit offsets
+    if (c.x_stride > most || c.w_stride > most) return fail(TIDE_ERR_UNSUPPORTED, "row strides of x and W must be at most %lld", (long long)most);
+    const size_t eb = elem_bytes(s.dtype);
+    auto check_rows = [&](const void* p, int64_t stride, const char* name) {
+        const size_t unit = chunked_rows(s.dtype, s.d) ? 16 : eb;
+        if (((uintptr_t)p % unit) || ((size_t)stride * eb % unit)) return fail(TIDE_ERR_ALIGNMENT, "%s: base and row stride must be multiples of %zu bytes", name, unit);
+        return (int)TIDE_OK;
+    };
+    if (!c.W || (s.T > 0 && (!c.x || !c.ids))) return fail(TIDE_ERR_INVALID_ARG, "x, W and the targets / top_ids must not be NULL");
+    if (s.K && s.T > 0 && !c.values) return fail(TIDE_ERR_INVALID_ARG, "top_values must not be NULL");
+    int rc;
+    if ((rc = check_rows(c.x, c.x_stride, "x")) || (rc = check_rows(c.W, c.w_stride, "W"))) return rc;
+    if (!grads) {
+        if (s.T > 0 && (!c.loss || !c.lse || (s.K && !c.z))) return fail(TIDE_ERR_INVALID_ARG, "loss, lse and z must not be NULL");
+    } else {
+        if (s.T > 0 && (!c.lse_in || !c.grad)) return fail(TIDE_ERR_INVALID_ARG, "lse and grad_loss must not be NULL");
+        if ((c.dx && c.dx_stride < s.d) || (c.dW && c.dw_stride < s.d)) return fail(TIDE_ERR_INVALID_ARG, "row strides of dx and dW must be at least d");
+        if ((rc = check_rows(c.dx, c.dx ? c.dx_stride : 0, "dx")) || (rc = check_rows(c.dW, c.dW ? c.dw_stride : 0, "dW"))) return rc;
+    }
+    if (((uintptr_t)c.ids | (uintptr_t)c.values | (uintptr_t)c.loss | (uintptr_t)c.lse | (uintptr_t)c.z | (uintptr_t)c.lse_in | (uintptr_t)c.grad) & 3)
+        return fail(TIDE_ERR_ALIGNMENT, "4-byte arrays must be aligned to their elements");
+    return TIDE_OK;
+}
+
+int head_space(const HeadCall& c, bool grads, unsigned cus, HeadWork* w) {
+    const size_t need = head_layout(c.s, grads, cus, nullptr, nullptr);
+    if (!c.workspace || c.workspace_bytes < need) return fail(TIDE_ERR_WORKSPACE, "this call needs %zu bytes of workspace, %zu given", need, c.workspace ? c.workspace_bytes : 0);
+    if ((uintptr_t)c.workspace & 255) return fail(TIDE_ERR_ALIGNMENT, "the workspace must be 256-byte aligned");
+    head_layout(c.s, grads, cus, c.workspace, w);
+    return TIDE_OK;
+}
+
+template <int DT> void head_max(const void* rows, int64_t stride, int64_t n, int64_t d, uint32_t* out, int* blocks, hipStream_t st) {
+    *blocks = (int)std::min<int64_t>(n, kHeadMaxBlocks);
+    if (*blocks) hipLaunchKernelGGL(tide_head_max_kernel, dim3(*blocks), dim3(kHeadRowThreads), 0, st, (const char*)rows, stride * 4, n, (int)d, out);
+}
+template <int DT> void head_copy(const HeadShape& s, const void* rows, int64_t stride, int64_t n, const int32_t* source, const HeadCtl* ctl, int weights, char* out, hipStream_t st) {
+    if (n == 0) return;
+    hipLaunchKernelGGL((tide_head_copy_kernel<DT>), dim3((unsigned)std::min<int64_t>(n, 4096)), dim3(kHeadRowThreads), 0, st, (const char*)rows, stride * Storage<DT>::kBytes, n,
+                       (int)s.d, source, ctl, weights, out, s.dp() * 2, s.plane_bytes(n));
+}
+// x or W as an operand: the caller's rows, or the copy's planes of n rows.
+HeadOperand head_operand(const HeadShape& s, const void* rows, int64_t stride, const char* copy, int64_t n) {
+    if (copy) return HeadOperand{{copy, copy + (s.planes() - 1) * s.plane_bytes(n)}, s.dp() * 2};
+    return HeadOperand{{(const char*)rows, (const char*)rows}, stride * 2};
+}
+
+int head_forward(const HeadCall& c) {
+    int rc = check_head(c, false);
+    if (rc || c.s.T == 0) return rc;
+    unsigned cus = 0;
+    if ((rc = resident_cus(&cus))) return rc;
+    const HeadShape& s = c.s;
+    HeadWork w;
+    if ((rc = head_space(c, false, cus, &w))) return rc;
+    rc = by_dtype(s.dtype, [&](auto dt) -> int {
+        constexpr int DT = decltype(dt)::value;
+        HeadCtlParams cp{};
+        if constexpr (DT == kF32) {
+            cp.ctl = w.ctl;
+            cp.x_max = w.x_max;
+            cp.w_max = w.w_max;
+            head_max<DT>(c.x, c.x_stride, s.T, s.d, w.x_max, &cp.x_blocks, c.st);
+            head_max<DT>(c.W, c.w_stride, s.V, s.d, w.w_max, &cp.w_blocks, c.st);
+            hipLaunchKernelGGL(tide_head_ctl_kernel, dim3(1), dim3(kHeadCtlThreads), 0, c.st, cp);
+        }
+        if (s.copied()) {
+            head_copy<DT>(s, c.x, c.x_stride, s.T, nullptr, w.ctl, 0, w.x, c.st);
+            head_copy<DT>(s, c.W, c.w_stride, s.V, nullptr, w.ctl, 1, w.w, c.st);
+        }
+        HeadGemmParams p{};
+        p.q = head_operand(s, c.x, c.x_stride, w.x, s.T);
+        p.p = head_operand(s, c.W, c.w_stride, w.w, s.V);
+        p.q_rows = (int)s.T;
+        p.p_rows = (int)s.V;
+        p.k = s.copied() ? (int)s.dp() : (int)s.d;
+        p.segments = DT == kF32 ? 3 : 1;
+        p.k_slices = 1;
+        p.ctl = DT == kF32 ? w.ctl : nullptr;
+        p.c1 = 1.4426950408889634f / c.tau;
+        p.ids = c.ids;
+        p.K = s.K ? (int)s.K : 1;
+        p.V = (int)s.V;
+        p.part = w.part;
+        p.z_out = s.K ? c.z : w.z;
+        const int rc2 = by_head_tile(s.rows_per_tile(), [&](auto tile) { return launch_head<kHeadElem<DT>, DT, kHeadStats, decltype(tile)>(s.T, s.V, c.st, p); });
+        if (rc2) return rc2;
+        HeadFinishParams f{};
+        f.part = w.part;
+        f.parts = (int)s.parts();
+        f.T = (int)s.T;
+        f.K = p.K;
+        f.V = (int)s.V;
+        f.tau = c.tau;
+        f.ids = c.ids;
+        f.values = c.values;
+        f.z = p.z_out;
+        f.loss = c.loss;
+        f.lse = c.lse;
+        hipLaunchKernelGGL(tide_head_finish_kernel, dim3((unsigned)((s.T + 15) / 16)), dim3(1024), 0, c.st, f);
+        return TIDE_OK;
+    });
+    if (rc) return rc;
+    TIDE_HIP(hipGetLastError());
+    return TIDE_OK;
+}
+
+int head_backward(const HeadCall& c) {
+    int rc = check_head(c, true);
+    if (rc || (!c.dx && !c.dW)) return rc;
+    unsigned cus = 0;
+    if ((rc = resident_cus(&cus))) return rc;
+    const HeadShape& s = c.s;
+    HeadWork w;
+    if ((rc = head_space(c, true, cus, &w))) return rc;
+    rc = by_dtype(s.dtype, [&](auto dt) -> int {
+        constexpr int DT = decltype(dt)::value, E = kHeadElem<DT>;
+        HeadCtlParams cp{};
+        cp.ctl = w.ctl;
+        cp.x_max = w.x_max;
+        cp.w_max = w.w_max;
+        if constexpr (DT == kF32) {
+            head_max<DT>(c.x, c.x_stride, s.T, s.d, w.x_max, &cp.x_blocks, c.st);
+            head_max<DT>(c.W, c.w_stride, s.V, s.d, w.w_max, &cp.w_blocks, c.st);
+        }
+        if (s.K && s.T)
+            hipLaunchKernelGGL(tide_head_teacher_kernel, dim3((unsigned)((s.T + 3) / 4)), dim3(kHeadRowThreads), 0, c.st, c.values, c.ids, (int)s.T, (int)s.K, (int)s.V,
+                               1.0f / c.tau, w.wanted, w.taught);
+        cp.grads = 1;
+        cp.scale_grad = E == kF16;
+        cp.T = (int)s.T;
+        cp.V = (int)s.V;
+        cp.target = s.K ? nullptr : c.ids;
+        cp.taught = w.taught;
+        cp.grad = c.grad;
+        cp.lse = c.lse_in;
+        cp.tau = c.tau;
+        cp.source = w.source;
+        cp.place = w.place;
+        cp.row_const = w.row_const;
+        hipLaunchKernelGGL(tide_head_ctl_kernel, dim3(1), dim3(kHeadCtlThreads), 0, c.st, cp);
+        head_copy<DT>(s, c.x, c.x_stride, s.T, w.source, w.ctl, 0, w.x, c.st);
+        if (s.copied()) head_copy<DT>(s, c.W, c.w_stride, s.V, nullptr, w.ctl, 1, w.w, c.st);
+        const HeadOperand x = head_operand(s, nullptr, 0, w.x, s.T), W = head_operand(s, c.W, c.w_stride, w.w, s.V);
+        const int64_t piece = s.piece(), g_plane = s.T * piece * 2;
+        const HeadOperand g{{w.g, w.g + (s.planes() - 1) * g_plane}, piece * 2};
+        const int slices = s.dx_slices(cus);
+        for (int64_t v0 = 0; v0 < s.V; v0 += piece) {
+            const int64_t width = std::min(piece, s.V - v0);
+            const HeadOperand Wv{{W.plane[0] + v0 * W.row_bytes, W.plane[1] + v0 * W.row_bytes}, W.row_bytes};
+            HeadGemmParams p{};
+            p.ctl = w.ctl;
+            p.segments = DT == kF32 ? 3 : 1;
+            p.k_slices = 1;
+            int rc2 = TIDE_OK;
+            if (s.T) {
+                HeadGemmParams a = p;
+                a.q = x;
+                a.p = Wv;
+                a.q_rows = (int)s.T;
+                a.p_rows = (int)width;
+                a.k = (int)s.dp();
+                a.c1 = 1.4426950408889634f / c.tau;
+                a.ids = c.ids;
+                a.source = w.source;
+                a.K = s.K ? (int)s.K : 1;
+                a.V = (int)s.V;
+                a.v0 = (int)v0;
+                a.row_const = w.row_const;
+                a.wanted = w.wanted;
+                a.g_out = w.g;
+                a.g_row_bytes = g.row_bytes;
+                a.g_plane_bytes = g_plane;
+                rc2 = by_head_tile(s.rows_per_tile(), [&](auto tile) { return launch_head<E, DT, kHeadGrad, decltype(tile)>(s.T, width, c.st, a); });
+                if (rc2) return rc2;
+            }
+            if (s.T && c.dx) {
+                HeadGemmParams a = p;
+                a.q = g;
+                a.p = Wv;
+                a.q_rows = (int)s.T;
+                a.p_rows = (int)s.dp();
+                a.k = (int)width;
+                a.k_slices = slices;
+                a.acc_out = w.acc;
+                a.acc_slice = s.T * s.dp();
+                a.acc_ld = (int)s.dp();
+                a.accumulate = v0 != 0;
+                rc2 = by_head_tile(s.rows_per_tile(), [&](auto tile) { return launch_head<E, E, kHeadRows, decltype(tile)>(s.T, s.dp(), c.st, a); });
+                if (rc2) return rc2;
+            }
+            if (c.dW) {
+                HeadGemmParams a = p;
+                a.q = g;
+                a.p = x;
+                a.q_rows = (int)width;
+                a.p_rows = (int)s.d;
+                a.k = (int)s.T;
+                a.out = (char*)c.dW + v0 * c.dw_stride * Storage<DT>::kBytes;
+                a.out_row_elems = c.dw_stride;
+                a.out_aligned = chunked_rows(s.dtype, s.d);
+                if ((rc2 = launch_head<E, DT, kHeadWeights, HeadTile256>(width, s.d, c.st, a))) return rc2;
+            }
+        }
+        if (s.T && c.dx)
+            hipLaunchKernelGGL((tide_head_dx_kernel<DT>), dim3((unsigned)std::min<int64_t>(s.T, 4096)), dim3(kHeadRowThreads), 0, c.st, w.acc, slices, s.T * s.dp(), (int)s.dp(), w.place,
+                               w.ctl, (int)s.T, (int)s.d, (char*)c.dx, c.dx_stride * Storage<DT>::kBytes);
+        return TIDE_OK;
+    });
+    if (rc) return rc;
+    TIDE_HIP(hipGetLastError());
+    return TIDE_OK;
+}
+
+constexpr int kProjectGradMaxBlocks = 1024;
+int project_grad_blocks(int64_t T, unsigned cus) { return (int)std::min<int64_t>(T, std::min<int64_t>(2 * cus, kProjectGradMaxBlocks)); }
+
+}  // namespace
+
+extern "C" {
+
+size_t tide_head_workspace_bytes(int dtype, int64_t T, int64_t d, int64_t V, int64_t K, int gradient) {
+    g_err[0] = 0;
+    HeadCall c{};
+    c.s = HeadShape{dtype, T, d, V, K};
+    c.tau = 1.0f;
+    c.x_stride = c.w_stride = (d + 7) / 8 * 8;
+    alignas(256) static char some[256];                // checks of pointers that are not asked about
+    c.x = c.W = some;
+    c.ids = (const int32_t*)some;
+    c.values = c.lse_in = c.grad = (const float*)some;
+    c.loss = c.lse = c.z = (float*)some;
+    if (check_head(c, gradient != 0)) return 0;
+    unsigned cus = 256;             // without a device: the answer for a 256-CU one
+    int dev = 0;
+    if (hipGetDevice(&dev) == hipSuccess) {
+        if (resident_cus(&cus) != TIDE_OK) cus = 256;
+    } else {
+        (void)hipGetLastError();
+    }
+    return head_layout(c.s, gradient != 0, cus, nullptr, nullptr);
+}
+
+int tide_head_loss(const void* x, int dtype, int64_t T, int64_t d, int64_t V, int64_t x_row_stride, const void* W, int64_t w_row_stride, const int32_t* target, float* loss,
+                   float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+    g_err[0] = 0;
+    HeadCall c{};
+    c.s = HeadShape{dtype, T, d, V, 0};
+    c.x = x, c.W = W, c.x_stride = x_row_stride, c.w_stride = w_row_stride;
+    c.ids = target, c.tau = 1.0f, c.loss = loss, c.lse = lse;
+    c.workspace = workspace, c.workspace_bytes = workspace_bytes, c.st = (hipStream_t)stream;
+    return head_forward(c);
+}
+
+int tide_head_loss_grad(const void* x, int dtype, int64_t T, int64_t d, int64_t V, int64_t x_row_stride, const void* W, int64_t w_row_stride, const int32_t* target,
+                        const float* lse, const float* grad_loss, void* dx, int64_t dx_row_stride, void* dW, int64_t dw_row_stride, void* workspace, size_t workspace_bytes,
+                        void* stream) {
+    g_err[0] = 0;
+    HeadCall c{};
+    c.s = HeadShape{dtype, T, d, V, 0};
+    c.x = x, c.W = W, c.x_stride = x_row_stride, c.w_stride = w_row_stride;
+    c.ids = target, c.tau = 1.0f, c.lse_in = lse, c.grad = grad_loss;
+    c.dx = dx, c.dx_stride = dx_row_stride, c.dW = dW, c.dw_stride = dw_row_stride;
+    c.workspace = workspace, c.workspace_bytes = workspace_bytes, c.st = (hipStream_t)stream;
+    return head_backward(c);
+}
+
+int tide_head_distill(const void* x, int dtype, int64_t T, int64_t d, int64_t V, int64_t x_row_stride, const void* W, int64_t w_row_stride, const float* top_values,
+                      const int32_t* top_ids, int64_t K, float tau, float* loss, float* lse, float* z, void* workspace, size_t workspace_bytes, void* stream) {
+    g_err[0] = 0;
+    if (K < 1) return fail(TIDE_ERR_INVALID_ARG, "K = %lld must be at least 1", (long long)K);
+    HeadCall c{};
+    c.s = HeadShape{dtype, T, d, V, K};
+    c.x = x, c.W = W, c.x_stride = x_row_stride, c.w_stride = w_row_stride;
+    c.ids = top_ids, c.values = top_values, c.tau = tau, c.loss = loss, c.lse = lse, c.z = z;
+    c.workspace = workspace, c.workspace_bytes = workspace_bytes, c.st = (hipStream_t)stream;
+    return head_forward(c);
+}
+
+int tide_head_distill_grad(const void* x, int dtype, int64_t T, int64_t d, int64_t V, int64_t x_row_stride, const void* W, int64_t w_row_stride, const float* top_values,
+                           const int32_t* top_ids, int64_t K, float tau, const float* lse, const float* grad_loss, void* dx, int64_t dx_row_stride, void* dW,
+                           int64_t dw_row_stride, void* workspace, size_t workspace_bytes, void* stream) {
+    g_err[0] = 0;
+    if (K < 1) return fail(TIDE_ERR_INVALID_ARG, "K = %lld must be at least 1", (long long)K);
+    HeadCall c{};
+    c.s = HeadShape{dtype, T, d, V, K};
+    c.x = x, c.W = W, c.x_stride = x_row_stride, c.w_stride = w_row_stride;
+    c.ids = top_ids, c.values = top_values, c.tau = tau, c.lse_in = lse, c.grad = grad_loss;
+    c.dx = dx, c.dx_stride = dx_row_stride, c.dW = dW, c.dw_stride = dw_row_stride;
+    c.workspace = workspace, c.workspace_bytes = workspace_bytes, c.st = (hipStream_t)stream;
+    return head_backward(c);
+}
+
+size_t tide_exit_project_grad_bytes(int64_t T, int64_t d) {
+    if (T < 0 || d < 1 || d > kMaxHidden) return 0;
+    return ((size_t)std::min<int64_t>(std::max<int64_t>(T, 1), kProjectGradMaxBlocks) * d * sizeof(float) + 255) & ~size_t(255);
+}
+
+int tide_exit_project_grad(const void* hidden, int dtype, int64_t C, int64_t T, int64_t d, int64_t ckpt_stride, int64_t row_stride, const void* final_hidden,
+                           int64_t final_row_stride, const int32_t* exit_layer, const int32_t* layer_ids, const float* norm_gain, float eps, const void* grad_out,
+                           int64_t grad_out_row_stride, void* grad_rows, int64_t grad_row_stride, float* grad_gain, void* workspace, size_t workspace_bytes, void* stream) {
+    g_err[0] = 0;
+    int rc = check_common(hidden, dtype, C, T, d, kBottleneck, ckpt_stride, row_stride, hidden, reinterpret_cast<const float*>(hidden), eps, true);
+    if (rc) return rc;
+    if (!layer_ids || (T > 0 && (!exit_layer || !grad_out || !grad_rows)))
+        return fail(TIDE_ERR_INVALID_ARG, "exit_layer, layer_ids (host), grad_out and grad_rows must not be NULL");
+    if (grad_out_row_stride < d || grad_row_stride < d || (final_hidden && final_row_stride < d))
+        return fail(TIDE_ERR_INVALID_ARG, "row strides of grad_out, grad_rows and final_hidden must be at least d");
+    const size_t eb = elem_bytes(dtype);
+    if (((uintptr_t)grad_out | (uintptr_t)grad_rows | (uintptr_t)final_hidden | (uintptr_t)norm_gain | ((size_t)grad_out_row_stride * eb) | ((size_t)grad_row_stride * eb) |
+         (final_hidden ? (size_t)final_row_stride * eb : 0)) & 15)
+        return fail(TIDE_ERR_ALIGNMENT, "grad_out, grad_rows, final_hidden and norm_gain bases and the row strides must be multiples of 16 bytes");
+    if ((uintptr_t)grad_gain & 3) return fail(TIDE_ERR_ALIGNMENT, "grad_gain must be aligned to a float");
+    ProjectGradParams p;
+    std::memset(&p, 0, sizeof(p));
+    for (int64_t c = 0; c < C; ++c) {
+        if (c > 0 && layer_ids[c] <= layer_ids[c - 1]) return fail(TIDE_ERR_INVALID_ARG, "layer_ids must be strictly ascending");
+        p.layer_id[c] = layer_ids[c];
+    }
+    if (T == 0 && !grad_gain) return TIDE_OK;
+    unsigned cus = 0;
+    if ((rc = resident_cus(&cus))) return rc;
+    const int blocks = project_grad_blocks(T, cus);
+    const bool joined = grad_gain && blocks != 1;      // one workgroup's sums are the gradient
+    if (joined && blocks) {
+        const size_t need = (size_t)blocks * d * sizeof(float);
+        if (!workspace || workspace_bytes < need) return fail(TIDE_ERR_WORKSPACE, "this call needs %zu bytes of workspace, %zu given", need, workspace ? workspace_bytes : 0);
+        if ((uintptr_t)workspace & 15) return fail(TIDE_ERR_ALIGNMENT, "the workspace must be 16-byte aligned");
+    }
+    if (!joined && ((uintptr_t)grad_gain & 15)) return fail(TIDE_ERR_ALIGNMENT, "grad_gain must be 16-byte aligned");
+    p.hidden = (const char*)hidden;
+    p.ckpt_stride_bytes = ckpt_stride * (int64_t)eb;
+    p.row_stride_bytes = row_stride * (int64_t)eb;
+    p.final_hidden = (const char*)final_hidden;
+    p.final_row_stride_bytes = final_row_stride * (int64_t)eb;
+    p.exit_layer = exit_layer;
+    p.gain = norm_gain;
+    p.grad_out = (const char*)grad_out;
+    p.grad_out_row_bytes = grad_out_row_stride * (int64_t)eb;
+    p.grad = (char*)grad_rows;
+    p.grad_row_bytes = grad_row_stride * (int64_t)eb;
+    p.part = joined ? (float*)workspace : grad_gain;
+    p.C = (int)C;
+    p.T = (int)T;
+    p.d = (int)d;
+    p.eps = eps;
+    hipStream_t st = (hipStream_t)stream;
+    const int64_t per_thread = (d * (int64_t)eb / 16 + kProjectThreads - 1) / kProjectThreads;
+    if (blocks)
+        by_dtype(dtype, [&](auto dt) {
+            constexpr int DT = decltype(dt)::value;
+            auto go = [&](auto chunks) {
+                hipLaunchKernelGGL((tide_project_grad_kernel<DT, decltype(chunks)::value>), dim3(blocks), dim3(kProjectThreads), 0, st, p);
+                return 0;
+            };
+            using std::integral_constant;
+            if (per_thread <= 1) return go(integral_constant<int, 1>{});
+            if (per_thread <= 2) return go(integral_constant<int, 2>{});
+            if (per_thread <= 4) return go(integral_constant<int, 4>{});
+            if constexpr (DT == kF32) {                // rows above 32 KiB
+                if (per_thread > 8) return go(integral_constant<int, 16>{});
+            }
+            return go(integral_constant<int, 8>{});
+        });
+    if (joined) hipLaunchKernelGGL(tide_project_gain_kernel, dim3((unsigned)((d + 31) / 32)), dim3(256), 0, st, (const float*)workspace, blocks, (int)d, grad_gain);
+    TIDE_HIP(hipGetLastError());
+    return TIDE_OK;
+}
+
+}  // extern "C"

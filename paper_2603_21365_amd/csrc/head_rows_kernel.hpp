@@ -1,0 +1,318 @@
+// What stands around the products of the head operators (head_gemm_kernel.hpp): the rows that have a gradient, the teacher's
+// probabilities, the scales of 16-bit planes, padded or split copies, and the sums that finish a call.
+//
+// Rows without a gradient -- no target, a teacher without entries, an upstream gradient of zero -- are left out of the three products of
+// the gradient: the others are gathered, which makes their number the products' size (a tenth of a training batch is typically masked) and keeps
+// whatever such rows hold (NaN, infinities) out of dW, where a zero weight would not (0 * NaN).
+#pragma once
+#include "head_gemm_kernel.hpp"
+
+namespace tide {
+
+constexpr int kHeadRowThreads = 256;
+constexpr int kHeadCtlThreads = 1024;
+constexpr int kHeadMaxBlocks = 512;        // workgroups that search for the largest magnitude
+
+template <int DT> __device__ __forceinline__ float head_load(const char* row, int i) {
+    if constexpr (DT == kF32) return reinterpret_cast<const float*>(row)[i];
+    else if constexpr (DT == kF16) return (float)reinterpret_cast<const _Float16*>(row)[i];
+    else return bf16_bits_to_f32(reinterpret_cast<const uint16_t*>(row)[i]);
+}
+template <int DT> __device__ __forceinline__ void head_store(char* row, int64_t i, float v) {
+    if constexpr (DT == kF32) reinterpret_cast<float*>(row)[i] = v;
+    else if constexpr (DT == kF16) reinterpret_cast<_Float16*>(row)[i] = static_cast<_Float16>(v);
+    else reinterpret_cast<__bf16*>(row)[i] = static_cast<__bf16>(v);
+}
+
+// Largest finite magnitude of fp32 rows, one per workgroup (as bits: the order of non-negative floats).  Infinities and NaN are passed
+// over: they give what they give whatever the scale, and must not cost the other rows theirs.
+__global__ __launch_bounds__(kHeadRowThreads) void tide_head_max_kernel(const char* rows, int64_t row_bytes, int64_t n_rows, int d, uint32_t* out) {
+    __shared__ uint32_t part[4];
+    uint32_t m = 0;
+    const bool chunks = ((uintptr_t)rows | (uintptr_t)row_bytes) % 16 == 0 && d % 4 == 0;
+    auto take = [&](uint32_t b) { b &= 0x7fffffffu; m = b < 0x7f800000u && b > m ? b : m; };
+    for (int64_t r = blockIdx.x; r < n_rows; r += gridDim.x) {
+        const char* row = rows + r * row_bytes;
+        if (chunks) {
+            for (int i = threadIdx.x; i < d / 4; i += kHeadRowThreads) {
+                const u32x4 v = reinterpret_cast<const u32x4*>(row)[i];
+                take(v[0]), take(v[1]), take(v[2]), take(v[3]);
+            }
+        } else {
+            for (int i = threadIdx.x; i < d; i += kHeadRowThreads) take(reinterpret_cast<const uint32_t*>(row)[i]);
+        }
+    }
+#pragma unroll
+    for (int s = 1; s < kWave; s <<= 1) m = max(m, (uint32_t)__shfl_xor((int)m, s, kWave));
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = m;
+    __syncthreads();
+    if (threadIdx.x == 0) out[blockIdx.x] = max(max(part[0], part[1]), max(part[2], part[3]));
+}
+
+// The power of two that brings a largest magnitude into [2^14, 2^15): the upper end of fp16, so that small elements keep their bits.
+__device__ __forceinline__ float head_scale(uint32_t max_bits) {
+    const int e = (int)(max_bits >> 23) - 127;
+    if (max_bits == 0 || e > 127) return 1.0f;
+    return ldexpf(1.0f, min(110, 14 - e));
+}
+
+struct HeadCtlParams {
+    HeadCtl* ctl;
+    const uint32_t *x_max, *w_max;   // fp32: the workgroups' maxima
+    int x_blocks, w_blocks;
+    int grads;                 // 0: scales only
+    int scale_grad;            // G is held in fp16
+    int T, V;
+    const int32_t* target;     // [T], or null and
+    const uint8_t* taught;     // [T] whether the teacher has entries
+    const float* grad;         // [T] upstream
+    const float* lse;          // [T]
+    float tau;
+    int32_t* source;           // [T] out: the live rows' tokens, ascending
+    int32_t* place;            // [T] out: a token's live row, or -1
+    float2* row_const;         // [T] out, of live rows: (lse * log2 e, grad * tau * grad_scale)
+};
+
+// One workgroup: the scales, and the list of live rows in token order (each thread a run of tokens).
+__global__ __launch_bounds__(kHeadCtlThreads) void tide_head_ctl_kernel(const HeadCtlParams p) {
+    __shared__ uint32_t max_of[3][16];
+    __shared__ int count_of[16];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    uint32_t m[3] = {0, 0, 0};
+    for (int i = tid; i < p.x_blocks; i += kHeadCtlThreads) m[0] = max(m[0], p.x_max[i]);
+    for (int i = tid; i < p.w_blocks; i += kHeadCtlThreads) m[1] = max(m[1], p.w_max[i]);
+    const int per = p.grads ? (p.T + kHeadCtlThreads - 1) / kHeadCtlThreads : 0;
+    const int t0 = min(p.T, tid * per), t1 = min(p.T, t0 + per);
+    auto live = [&](int t) {
+        const float g = p.grad[t];
+        const bool there = p.target ? (uint32_t)p.target[t] < (uint32_t)p.V : p.taught[t] != 0;
+        return there && g != 0.0f;
+    };
+    int n = 0;
+    for (int t = t0; t < t1; ++t)
+        if (live(t)) {
+            ++n;
+            m[2] = max(m[2], __float_as_uint(fabsf(p.grad[t] * p.tau)));
+        }
+#pragma unroll
+    for (int j = 0; j < 3; ++j) {
+#pragma unroll
+        for (int s = 1; s < kWave; s <<= 1) m[j] = max(m[j], (uint32_t)__shfl_xor((int)m[j], s, kWave));
+        if (lane == 0) max_of[j][wave] = m[j];
+    }
+    int upto = n;                                      // live rows of this wave's lanes up to this one
+#pragma unroll
+    for (int s = 1; s < kWave; s <<= 1) {
+        const int o = __shfl_up(upto, s, kWave);
+        if (lane >= s) upto += o;
+    }
+    if (lane == 63) count_of[wave] = upto;
+    __syncthreads();
+    int before = upto - n, all = 0;
+    for (int w = 0; w < 16; ++w) {
+        all += count_of[w];
+        if (w < wave) before += count_of[w];
+        for (int j = 0; j < 3; ++j) m[j] = max(m[j], max_of[j][w]);
+    }
+    const float sx = head_scale(m[0]), sw = head_scale(m[1]), sg = p.scale_grad ? head_scale(m[2]) : 1.0f;
+    for (int t = t0; t < t1; ++t) {
+        const bool l = live(t);
+        p.place[t] = l ? before : -1;
+        if (l) {
+            p.source[before] = t;
+            p.row_const[before] = float2{p.lse[t] * 1.4426950408889634f, p.grad[t] * p.tau * sg};
+            ++before;
+        }
+    }
+    if (tid == 0) {
+        HeadCtl c;
+        c.live = all;
+        c.x_scale = sx;
+        c.w_scale = sw;
+        c.logit_scale = (float)fmin(1.0 / ((double)sx * sw), 1e38);
+        c.row_back = (float)fmin(1.0 / ((double)sg * sw), 1e38);
+        c.weight_back = (float)fmin(1.0 / ((double)sg * sx), 1e38);
+        *p.ctl = c;
+    }
+}
+
+// Rows into the form the products read: gathered (source != null), padded with zeros to whole 16-byte chunks, fp32 ones as two fp16 planes.
+// A workgroup per row in turn.
+template <int DT>
+__global__ __launch_bounds__(kHeadRowThreads) void tide_head_copy_kernel(const char* rows, int64_t row_bytes, int64_t n_rows, int d, const int32_t* source,
+                                                                         const HeadCtl* ctl, int weights, char* out, int64_t out_row_bytes, int64_t plane_bytes) {
+    const int64_t n = source ? ctl->live : n_rows;
+    const float scale = DT == kF32 ? (weights ? ctl->w_scale : ctl->x_scale) : 1.0f;
+    const bool chunks = ((uintptr_t)rows | (uintptr_t)row_bytes) % 16 == 0 && d % 8 == 0;
+    for (int64_t r = blockIdx.x; r < n; r += gridDim.x) {
+        const char* row = rows + (source ? (int64_t)source[r] : r) * row_bytes;
+        char* to = out + r * out_row_bytes;
+        for (int c = threadIdx.x; c < (int)(out_row_bytes / 16); c += kHeadRowThreads) {
+            if constexpr (DT != kF32) {
+                u32x4 v;
+                if (chunks) {
+                    v = reinterpret_cast<const u32x4*>(row)[c];
+                } else {
+                    const uint16_t* e = reinterpret_cast<const uint16_t*>(row) + 8 * c;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const uint32_t lo = 8 * c + 2 * i < d ? e[2 * i] : 0, hi = 8 * c + 2 * i + 1 < d ? e[2 * i + 1] : 0;
+                        v[i] = lo | hi << 16;
+                    }
+                }
+                reinterpret_cast<u32x4*>(to)[c] = v;
+            } else {
+                f16x8 hi, lo;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float v = 8 * c + i < d ? reinterpret_cast<const float*>(row)[8 * c + i] * scale : 0.0f;
+                    hi[i] = static_cast<_Float16>(v);
+                    lo[i] = static_cast<_Float16>(v - (float)hi[i]);       // the difference is exact
+                }
+                reinterpret_cast<u32x4*>(to)[c] = __builtin_bit_cast(u32x4, hi);
+                reinterpret_cast<u32x4*>(to + plane_bytes)[c] = __builtin_bit_cast(u32x4, lo);
+            }
+        }
+    }
+}
+
+// The teacher of one row: a wave, lanes over its K entries.  An entry counts if its token is one of the vocabulary's and its value is not -inf.
+struct HeadTeacher {
+    float m, log_sum;          // largest value / tau and log of the sum of exp(value / tau - m)
+    bool any;
+};
+__device__ __forceinline__ float head_wave_max(float v) {
+#pragma unroll
+    for (int s = 1; s < kWave; s <<= 1) v = fmaxf(v, __shfl_xor(v, s, kWave));
+    return v;
+}
+__device__ __forceinline__ HeadTeacher head_teacher(const float* values, const int32_t* ids, int K, int V, float inv_tau, int lane) {
+    float m = -INFINITY;
+    bool any = false;
+    for (int k = lane; k < K; k += kWave)
+        if ((uint32_t)ids[k] < (uint32_t)V && values[k] != -INFINITY) {
+            any = true;
+            m = fmaxf(m, values[k] * inv_tau);
+        }
+    m = head_wave_max(m);
+    float s = 0.0f;
+    for (int k = lane; k < K; k += kWave)
+        if ((uint32_t)ids[k] < (uint32_t)V && values[k] != -INFINITY) s += expf(values[k] * inv_tau - m);
+    return HeadTeacher{m, logf(wave_sum(s)), __any(any) != 0};
+}
+
+// [T][K] probabilities of the teacher (zero where it has no entry), and which rows have any.
+__global__ __launch_bounds__(kHeadRowThreads) void tide_head_teacher_kernel(const float* values, const int32_t* ids, int T, int K, int V, float inv_tau,
+                                                                            float* wanted, uint8_t* taught) {
+    const int t = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+    if (t >= T) return;
+    values += (int64_t)t * K, ids += (int64_t)t * K, wanted += (int64_t)t * K;
+    const HeadTeacher h = head_teacher(values, ids, K, V, inv_tau, lane);
+    for (int k = lane; k < K; k += kWave) {
+        const bool there = (uint32_t)ids[k] < (uint32_t)V && values[k] != -INFINITY;
+        wanted[k] = there ? expf(values[k] * inv_tau - h.m - h.log_sum) : 0.0f;
+    }
+    if (lane == 0) taught[t] = h.any;
+}
+
+struct HeadFinishParams {
+    const float2* part;        // [parts][T]
+    int parts, T, K, V;
+    float tau;
+    const int32_t* ids;        // [T][K]
+    const float* values;       // [T][K] teacher's values, or null: one hard target
+    float* z;                  // [T][K] logits of the row's own tokens; with a teacher an output, zeros where there is no token
+    float *loss, *lse;         // [T] out
+};
+
+// 16 rows per workgroup: 64 threads join a row's partial maxima and sums, then a wave takes its loss.
+__global__ __launch_bounds__(1024) void tide_head_finish_kernel(const HeadFinishParams p) {
+    __shared__ float2 part[64][17];
+    const int tid = threadIdx.x, r = tid & 15, slice = tid >> 4, t = blockIdx.x * 16 + r;
+    float m = -INFINITY, s = 0.0f;
+    auto join = [](float& m, float& s, float m1, float s1) {
+        const float top = fmaxf(m, m1), at = top == -INFINITY ? 0.0f : top;
+        s = s * __builtin_amdgcn_exp2f(m - at) + s1 * __builtin_amdgcn_exp2f(m1 - at);
+        m = top;
+    };
+    if (t < p.T)
+        for (int i = slice; i < p.parts; i += 64) {
+            const float2 v = p.part[(int64_t)i * p.T + t];
+            join(m, s, v.x, v.y);
+        }
+    part[slice][r] = float2{m, s};
+    __syncthreads();
+    const int wave = tid >> 6, lane = tid & 63, row = blockIdx.x * 16 + wave;      // wave w finishes row w
+    const float2 v = part[lane][wave];
+    m = v.x, s = v.y;
+#pragma unroll
+    for (int x = 1; x < kWave; x <<= 1) {
+        const float m1 = __shfl_xor(m, x, kWave), s1 = __shfl_xor(s, x, kWave);
+        join(m, s, m1, s1);
+    }
+    if (row >= p.T) return;
+    const float lse = (m + log2f(s)) * 0.6931471805599453f;
+    const int32_t* ids = p.ids + (int64_t)row * p.K;
+    float* z = p.z + (int64_t)row * p.K;
+    if (!p.values) {
+        if (lane == 0) {
+            p.lse[row] = lse;
+            p.loss[row] = (uint32_t)ids[0] < (uint32_t)p.V ? lse - z[0] / p.tau : 0.0f;
+        }
+        return;
+    }
+    const float inv_tau = 1.0f / p.tau;
+    const float* values = p.values + (int64_t)row * p.K;
+    const HeadTeacher h = head_teacher(values, ids, p.K, p.V, inv_tau, lane);
+    float sum = 0.0f;
+    for (int k = lane; k < p.K; k += kWave) {
+        if ((uint32_t)ids[k] >= (uint32_t)p.V) {
+            z[k] = 0.0f;
+        } else if (values[k] != -INFINITY) {
+            const float log_q = values[k] * inv_tau - h.m - h.log_sum, q = expf(log_q);
+            sum += q > 0.0f ? q * (log_q - z[k] * inv_tau + lse) : 0.0f;
+        }
+    }
+    sum = wave_sum(sum);
+    if (lane == 0) {
+        p.lse[row] = lse;
+        p.loss[row] = h.any ? p.tau * p.tau * sum : 0.0f;
+    }
+}
+
+// dx: the k slices' sums in order, scaled back, rounded once to the storage type; zeros in the rows that have no gradient.
+template <int DT>
+__global__ __launch_bounds__(kHeadRowThreads) void tide_head_dx_kernel(const float* acc, int slices, int64_t slice, int acc_ld, const int32_t* place, const HeadCtl* ctl, int T, int d,
+                                                                       char* out, int64_t out_row_bytes) {
+    const float back = ctl->row_back;
+    const bool chunks = ((uintptr_t)out | (uintptr_t)out_row_bytes) % 16 == 0 && d % 8 == 0;
+    for (int t = blockIdx.x; t < T; t += gridDim.x) {
+        const int i = place[t];
+        char* to = out + (int64_t)t * out_row_bytes;
+        for (int c = threadIdx.x; c < acc_ld / 8; c += kHeadRowThreads) {
+            f32x4 a = {0, 0, 0, 0}, b = a;
+            if (i >= 0)
+                for (int s = 0; s < slices; ++s) {
+                    const f32x4* from = reinterpret_cast<const f32x4*>(acc + s * slice + (int64_t)i * acc_ld + 8 * c);
+                    a += from[0];
+                    b += from[1];
+                }
+            a *= back;
+            b *= back;
+            if (chunks) {
+                if constexpr (DT == kF32) {
+                    reinterpret_cast<f32x4*>(to)[2 * c] = a;
+                    reinterpret_cast<f32x4*>(to)[2 * c + 1] = b;
+                } else {
+                    reinterpret_cast<u32x4*>(to)[c] = u32x4{head_round2<DT>(a[0], a[1]), head_round2<DT>(a[2], a[3]), head_round2<DT>(b[0], b[1]), head_round2<DT>(b[2], b[3])};
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (8 * c + e < d) head_store<DT>(to, 8 * c + e, e < 4 ? a[e & 3] : b[e & 3]);
+            }
+        }
+    }
+}
+
+}  // namespace tide

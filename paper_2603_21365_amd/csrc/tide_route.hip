@@ -20,6 +20,8 @@
 #include "cosine_kernel.hpp"
 #include "decode_kernel.hpp"
 #include "few_rows_kernel.hpp"
+#include "head_gemm_kernel.hpp"
+#include "head_rows_kernel.hpp"
 #include "pack_kernel.hpp"
 #include "prefill_dma_kernel.hpp"
 #include "prefill_kernel.hpp"
@@ -31,6 +33,7 @@
 #include "prefill_band32_kernel.hpp"
 #include "mfma_probe_kernel.hpp"
 #include "prefill_wide32_kernel.hpp"
+#include "project_grad_kernel.hpp"
 #include "project_kernel.hpp"
 #include "repack_kernel.hpp"
 
@@ -2133,3 +2136,5 @@ int tide_release(void) {
 }
 
 }  // extern "C"
+
+#include "head_route.hpp"

@@ -29,6 +29,8 @@ EXPORTS = (
     "tide_select_exit_packed", "tide_exit_project", "tide_batch_exit", "tide_cosine_labels", "tide_batch_compact", "tide_set_variant", "tide_set_prefill_form", "tide_prefill_plan", "tide_stream_schedule", "tide_band_schedule", "tide_band_f32_schedule", "tide_call_route", "tide_release",
     "tide_workspace_bytes", "tide_workspace_init", "tide_workspace_forget", "tide_router_eval_ws", "tide_select_exit_ws",
     "tide_select_exit_packed_noalloc", "tide_noalloc_scratch_bytes", "tide_workspace_allocations", "tide_mfma_probe",
+    "tide_exit_project_grad_bytes", "tide_exit_project_grad", "tide_head_workspace_bytes", "tide_head_loss", "tide_head_loss_grad",
+    "tide_head_distill", "tide_head_distill_grad",
 )
 
 _lib = None
@@ -85,6 +87,18 @@ def load_library() -> ctypes.CDLL:
     lib.tide_call_route.argtypes = [ci, i64, i64, i64, i64, ci, ci, sz, vp]
     lib.tide_mfma_probe.argtypes = [ci, ci, ci, ci, vp]
     lib.tide_mfma_probe.restype = ci
+    lib.tide_exit_project_grad_bytes.argtypes = [i64, i64]
+    lib.tide_exit_project_grad_bytes.restype = sz
+    lib.tide_exit_project_grad.argtypes = [vp, ci, i64, i64, i64, i64, i64, vp, i64, vp, vp, vp, f32, vp, i64, vp, i64, vp, vp, sz, vp]
+    lib.tide_head_workspace_bytes.argtypes = [ci, i64, i64, i64, i64, ci]
+    lib.tide_head_workspace_bytes.restype = sz
+    head = [vp, ci, i64, i64, i64, i64, vp, i64]
+    lib.tide_head_loss.argtypes = [*head, vp, vp, vp, vp, sz, vp]
+    lib.tide_head_loss_grad.argtypes = [*head, vp, vp, vp, vp, i64, vp, i64, vp, sz, vp]
+    lib.tide_head_distill.argtypes = [*head, vp, vp, i64, f32, vp, vp, vp, vp, sz, vp]
+    lib.tide_head_distill_grad.argtypes = [*head, vp, vp, i64, f32, vp, vp, vp, i64, vp, i64, vp, sz, vp]
+    for name in ("tide_exit_project_grad", "tide_head_loss", "tide_head_loss_grad", "tide_head_distill", "tide_head_distill_grad"):
+        getattr(lib, name).restype = ci
     for name in ("tide_router_eval", "tide_router_eval_packed", "tide_select_exit", "tide_select_exit_packed",
                  "tide_router_pack", "tide_exit_project", "tide_batch_exit", "tide_cosine_labels", "tide_batch_compact", "tide_set_variant", "tide_set_prefill_form", "tide_release",
                  "tide_router_eval_ws", "tide_select_exit_ws", "tide_select_exit_packed_noalloc", "tide_workspace_init", "tide_workspace_forget"):
@@ -521,6 +535,133 @@ def batch_exit(fire_mask, C, layer_ids, min_layer, no_exit_layer):
                                           _ptr(layer), _ptr(allm), _ptr(counts), _stream()))
     del idh
     return layer, allm, counts
+
+
+def _dev(t, dtype, shape, name):
+    """A contiguous CUDA tensor of this type and shape."""
+    if t.dtype != dtype or not t.is_cuda or not t.is_contiguous() or tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be a contiguous CUDA {dtype} tensor of shape {tuple(shape)}")
+    return t
+
+
+def _scratch(workspace, nbytes, device):
+    """The workspace of a call that needs no initialised one: the caller's (a CUDA uint8 tensor), or one of torch's allocator for this call."""
+    if workspace is None:
+        workspace = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    return workspace, workspace.numel() * workspace.element_size()
+
+
+def exit_project_grad(hidden, final_hidden, exit_layer, layer_ids, norm_gain, eps, grad_out, *, want_gain=True, workspace=None):
+    """The gradient of exit_project: hidden [C,T,>=d], final_hidden [T,>=d] | None, exit_layer int32 [T], layer_ids host [C],
+    norm_gain [d] | None, grad_out [T,d] of hidden's dtype -> (grad_rows [T,d]: to the row each token exited with; grad_gain fp32 [d] | None)."""
+    (C, T, width), (cs, rs, _) = _rows(hidden, 3)
+    (Tg, d), (gs, _) = _rows(grad_out, 2)
+    if Tg != T or width < d or grad_out.dtype != hidden.dtype:
+        raise ValueError("grad_out must be [T, <=d] of hidden's dtype")
+    _f32dev(norm_gain, (d,), "norm_gain")
+    _dev(exit_layer, torch.int32, (T,), "exit_layer")
+    frs = d
+    if final_hidden is not None:
+        (Tf, wf), (frs, _) = _rows(final_hidden, 2)
+        if Tf != T or wf < d or final_hidden.dtype != hidden.dtype:
+            raise ValueError("final_hidden must be [T, >=d] of hidden's dtype")
+        frs = frs if T > 1 else max(frs, d)
+    idh, idp = _host(layer_ids, C, np.int32)
+    grad = torch.empty((T, d), dtype=hidden.dtype, device=hidden.device)
+    gain = torch.empty(d, dtype=torch.float32, device=hidden.device) if want_gain else None
+    lib = load_library()
+    nbytes = 0
+    if want_gain:
+        workspace, nbytes = _scratch(workspace, int(lib.tide_exit_project_grad_bytes(T, d)), hidden.device)
+    _check(lib.tide_exit_project_grad(_ptr(hidden), _dtype_code(hidden), C, T, d, cs if (C > 1 and T > 0) else max(cs, 0), rs if T > 1 else max(rs, d),
+                                      _ptr(final_hidden), frs, _ptr(exit_layer), idp, _ptr(norm_gain), float(eps), _ptr(grad_out),
+                                      gs if T > 1 else max(gs, d), _ptr(grad), d, _ptr(gain), _ptr(workspace) if want_gain else None, nbytes, _stream()))
+    del idh
+    return grad, gain
+
+
+def head_workspace_bytes(dtype: int, T: int, d: int, V: int, K: int = 0, *, gradient: bool = False) -> int:
+    """Bytes of workspace a head call needs (K = 0: the loss, else the distillation; 0 and last_error() if unsupported)."""
+    return int(load_library().tide_head_workspace_bytes(int(dtype), int(T), int(d), int(V), int(K), 1 if gradient else 0))
+
+
+def _head_args(x, W):
+    (T, d), (xs, _) = _rows(x, 2)
+    (V, dw), (ws, _) = _rows(W, 2)
+    if dw != d or W.dtype != x.dtype:
+        raise ValueError("W must be [V, d] of x's dtype, x [T, d]")
+    return T, d, V, (_ptr(x), _dtype_code(x), T, d, V, xs if T > 1 else max(xs, d), _ptr(W), ws if V > 1 else max(ws, d))
+
+
+def _head_scratch(x, T, d, V, K, gradient, workspace):
+    if workspace is None:
+        need = head_workspace_bytes(_dtype_code(x), T, d, V, K, gradient=gradient)
+        if need == 0:
+            raise TideError(-2, last_error())
+        workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
+    return workspace, workspace.numel() * workspace.element_size()
+
+
+def _head_grads(x, W, want_dx, want_dw):
+    T, d = x.shape
+    dx = torch.empty((T, d), dtype=x.dtype, device=x.device) if want_dx else None
+    dW = torch.empty((W.shape[0], d), dtype=W.dtype, device=W.device) if want_dw else None
+    return dx, dW
+
+
+def head_loss(x, W, target, *, workspace=None):
+    """Softmax cross entropy of rows under an LM head: x [T,d], W [V,d] of one dtype, target int32 [T] (outside 0..V-1: none)
+    -> (loss f32 [T], 0 without a target; lse f32 [T]).  The logits are not kept."""
+    T, d, V, rows = _head_args(x, W)
+    _dev(target, torch.int32, (T,), "target")
+    loss = torch.empty(T, dtype=torch.float32, device=x.device)
+    lse = torch.empty(T, dtype=torch.float32, device=x.device)
+    workspace, nbytes = _head_scratch(x, T, d, V, 0, False, workspace)
+    _check(load_library().tide_head_loss(*rows, _ptr(target), _ptr(loss), _ptr(lse), _ptr(workspace), nbytes, _stream()))
+    return loss, lse
+
+
+def head_loss_grad(x, W, target, lse, grad_loss, *, want_dx=True, want_dw=True, workspace=None):
+    """Gradients of head_loss for grad_loss f32 [T] and its lse -> (dx [T,d] | None, dW [V,d] | None) of x's dtype."""
+    T, d, V, rows = _head_args(x, W)
+    _dev(target, torch.int32, (T,), "target")
+    _dev(lse, torch.float32, (T,), "lse"), _dev(grad_loss, torch.float32, (T,), "grad_loss")
+    dx, dW = _head_grads(x, W, want_dx, want_dw)
+    workspace, nbytes = _head_scratch(x, T, d, V, 0, True, workspace)
+    _check(load_library().tide_head_loss_grad(*rows, _ptr(target), _ptr(lse), _ptr(grad_loss), _ptr(dx), d, _ptr(dW), d, _ptr(workspace), nbytes, _stream()))
+    return dx, dW
+
+
+def _head_top(x, T, top_values, top_ids):
+    K = int(top_ids.shape[-1])
+    _dev(top_values, torch.float32, (T, K), "top_values"), _dev(top_ids, torch.int32, (T, K), "top_ids")
+    return K
+
+
+def head_distill(x, W, top_values, top_ids, tau, *, workspace=None):
+    """Divergence of rows under an LM head from a teacher's K kept logits: top_values f32 [T,K] at the tokens top_ids int32 [T,K]
+    (outside 0..V-1, or a value of -inf: no entry) -> (loss f32 [T], lse f32 [T] of z / tau, z f32 [T,K] at top_ids)."""
+    T, d, V, rows = _head_args(x, W)
+    K = _head_top(x, T, top_values, top_ids)
+    loss = torch.empty(T, dtype=torch.float32, device=x.device)
+    lse = torch.empty(T, dtype=torch.float32, device=x.device)
+    z = torch.empty((T, K), dtype=torch.float32, device=x.device)
+    workspace, nbytes = _head_scratch(x, T, d, V, K, False, workspace)
+    _check(load_library().tide_head_distill(*rows, _ptr(top_values), _ptr(top_ids), K, float(tau), _ptr(loss), _ptr(lse), _ptr(z), _ptr(workspace), nbytes,
+                                            _stream()))
+    return loss, lse, z
+
+
+def head_distill_grad(x, W, top_values, top_ids, tau, lse, grad_loss, *, want_dx=True, want_dw=True, workspace=None):
+    """Gradients of head_distill for grad_loss f32 [T] and its lse -> (dx [T,d] | None, dW [V,d] | None) of x's dtype."""
+    T, d, V, rows = _head_args(x, W)
+    K = _head_top(x, T, top_values, top_ids)
+    _dev(lse, torch.float32, (T,), "lse"), _dev(grad_loss, torch.float32, (T,), "grad_loss")
+    dx, dW = _head_grads(x, W, want_dx, want_dw)
+    workspace, nbytes = _head_scratch(x, T, d, V, K, True, workspace)
+    _check(load_library().tide_head_distill_grad(*rows, _ptr(top_values), _ptr(top_ids), K, float(tau), _ptr(lse), _ptr(grad_loss), _ptr(dx), d, _ptr(dW), d,
+                                                 _ptr(workspace), nbytes, _stream()))
+    return dx, dW
 
 
 class PreparedCall:
