@@ -7,7 +7,7 @@
 //   kHeadWeights dW = G^T x of that piece, complete.
 // The gradient makes the logits a second time, so a training step is four products where one that keeps T x V logits has three.
 //
-// One tile of kQ x kP output elements per workgroup of eight waves, k in stages of 32 elements.  "q" is the operand whose rows are
+// One tile of kQ x kP output elements per workgroup of eight waves, k in stages of 64 elements.  "q" is the operand whose rows are
 // the output's rows, "p" the one whose rows are its columns: a matrix-core step takes the p fragment first, so a lane holds ONE
 // output row and, in its registers, runs of four consecutive columns (softmax: sums over columns stay in the lane).
 //
@@ -17,9 +17,14 @@
 // (W in dx; G and x in dW) lies in LDS as it lies in memory and is read by the transposing LDS loads, so no transposed copy of
 // W, x or G is ever made.
 //
+// The waves work as two groups of four, one wave of each per SIMD, that take turns: while one group's matrix steps run (a phase of 32 k elements, 512 cycles),
+// the other reads its fragments for the next phase and issues transfers; every phase ends in a barrier.  Left to itself (both groups in step, reads and
+// steps mixed by the compiler) the same kernel is 6 % slower (T = 4096, d = 4096, V = 128000: 3.50 / 3.27 ms).  A stage's slot is free when the group that
+// is behind has read its second half, so the transfers issued in stage k fill the slots of stage k - 1.
+//
 // The transfers are inline assembly: of the builtin the compiler makes every LDS read wait for all outstanding transfers, as it cannot
-// tell the ring's slots apart.  They have no output registers; they are ordered by explicit counts and the barrier in the MIDDLE of a stage,
-// which says that stage k + 1 has landed for every wave and that stage k - 1 has been read by every wave (its slot is filled next).
+// tell the ring's slots apart.  They have no output registers; they are ordered by explicit counts and the phases' barriers.  A stage is 128 bytes of
+// a memory row: with 64 every cache line came twice from L2, and the CU's load path was the bound (4.0 ms).
 //
 // fp32 operands are taken apart into two fp16 planes, x * 2^s = hi + lo + O(2^-23 x) with one power of two per tensor, and a product is three
 // passes over k: hi hi + hi lo + lo hi (what is dropped is 2^-22 of a term at most).  The fp32 matrix instructions have 1/16 of the 16-bit rate.
@@ -40,6 +45,8 @@ struct HeadCtl {
     float logit_scale;             // what the products of the logits are multiplied by (the planes' scales taken back)
     float row_back, weight_back;   // the same for dx and dW
 };
+
+constexpr int kHeadStageK = 64;                      // k elements of a stage: a whole cache line of a row
 
 struct HeadOperand {
     const char* plane[2];
@@ -73,17 +80,18 @@ struct HeadGemmParams {
     int out_aligned;           // rows of whole 16-byte chunks
 };
 
-template <int WQ, int WP, int BQ, int BP, int S> struct HeadTile {
-    static constexpr int kWQ = WQ, kWP = WP, kBQ = BQ, kBP = BP, kStages = S;
-    static constexpr int kQ = WQ * BQ * 32, kP = WP * BP * 32;
-    static constexpr int kQBytes = kQ * 64, kPBytes = kP * 64, kStageBytes = kQBytes + kPBytes;
-    static constexpr int kCols = BP * 32, kLd = kCols + 4;       // a wave's columns; its rows in LDS after the loop, padded against bank conflicts
-    static constexpr int kEpiBytes = 8 * 32 * kLd * 4;
-    static constexpr int kLdsBytes = S * kStageBytes > kEpiBytes ? S * kStageBytes : kEpiBytes;
-    static_assert(WQ * WP == 8, "eight waves");
+// kSQ, kSP: stages of each operand that its part of LDS holds.
+template <int WQ, int WP, int BQ, int BP, int SQ, int SP> struct HeadTile {
+    static constexpr int kWQ = WQ, kWP = WP, kBQ = BQ, kBP = BP, kSQ = SQ, kSP = SP;
+    static constexpr int kWaves = WQ * WP, kThreads = kWaves * kWave;
+    static constexpr int kQ = WQ * BQ * 16, kP = WP * BP * 16;
+    static constexpr int kQBytes = kQ * kHeadStageK * 2, kPBytes = kP * kHeadStageK * 2, kRingBytes = SQ * kQBytes + SP * kPBytes;
+    static constexpr int kCols = BP * 16, kLd = kCols + 4;       // a wave's columns; its rows in LDS after the loop, padded against bank conflicts
+    static constexpr int kEpiBytes = kWaves * 16 * kLd * 4;
+    static constexpr int kLdsBytes = kRingBytes > kEpiBytes ? kRingBytes : kEpiBytes;
+    static_assert(kWaves == 8 && SP >= 2 && SQ >= SP, "two groups of four waves");
     static_assert(kLdsBytes <= 160 * 1024, "LDS of a CU");
 };
-constexpr int kHeadThreads = 512;
 constexpr uint32_t kHeadNowhere = 0x80000000u;       // an offset at the descriptor's bound: fetched as zeros
 
 // 64 lanes x 16 bytes from memory (offsets voff from the descriptor's base) to 1 KiB of LDS at byte `lds`.
@@ -92,29 +100,29 @@ __device__ __forceinline__ void head_dma(uint32_t lds, uint32_t voff, u32x4 rsrc
 }
 template <int n> __device__ __forceinline__ void head_wait_vm() { asm volatile("s_waitcnt vmcnt(%0)" ::"i"(n) : "memory"); }
 
-// One operand's transfers: kRows tile rows, instruction n = wave + 8 i of kRows / 16.
-template <int kRows, bool kAcross> struct HeadFeed {
-    static constexpr int kInstr = kRows / 16, kN = (kInstr + 7) / 8;
+// One operand's transfers: kRows tile rows, instruction n = wave + 8 i of kRows / 8 a stage, a ring of kSlots stages at byte `lds`.
+template <int kRows, bool kAcross, int kWaves> struct HeadFeed {
+    static constexpr int kInstr = kRows / 8, kN = (kInstr + kWaves - 1) / kWaves, kBytes = kRows * kHeadStageK * 2;
     uint32_t voff[kN];
     int along[kN];             // first k element of this lane's chunk within a stage (along), or its k row (across)
     const char* base;
     int64_t step;
+    int issued, kk, fill;      // stages issued, the next one's number within its segment, its slot's byte
 
-    // Position of chunk c of a memory row in LDS.  Along: 64-byte rows, chunk ^ (row / 4) % 4, so that the 16 rows a quarter wave reads cover all
-    // banks.  Across: rows of kRows * 2 bytes, 64-byte pieces moved by the row's number where that leaves banks unused.
-    static __device__ __forceinline__ int place_along(int row, int c) { return c ^ ((row >> 2) & 3); }
+    // Position of chunk c of a memory row in LDS, chosen so that the lanes that read at a time cover all banks.  Along: 128-byte rows, 16 of them at one
+    // chunk.  Across: rows of 512 bytes, 32 bytes of each of eight.
+    static __device__ __forceinline__ int place_along(int row, int c) { return c ^ ((row >> 1) & 7); }
     static __device__ __forceinline__ int place_across(int kr, int c) {
-        if constexpr (kRows >= 128) return c ^ ((kr & 3) << 2);
-        else if constexpr (kRows == 64) return c ^ (((kr >> 1) & 1) << 2);
-        else return c;
+        static_assert(!kAcross || kRows == 256, "");
+        return c ^ ((kr & 3) << 1 | (kr >> 3 & 1) << 3);
     }
 
-    __device__ __forceinline__ void init(const HeadOperand& o, int row0, int rows, int wave, int lane) {
+    __device__ __forceinline__ void init(const HeadOperand& o, int row0, int rows, int first, int wave, int lane) {
 #pragma unroll
         for (int i = 0; i < kN; ++i) {
-            const int n = wave + 8 * i;
+            const int n = wave + kWaves * i;
             if constexpr (!kAcross) {
-                const int r = 16 * n + (lane >> 2), c = place_along(r, lane & 3);
+                const int r = 8 * n + (lane >> 3), c = place_along(r, lane & 7);
                 voff[i] = row0 + r < rows ? (uint32_t)r * (uint32_t)o.row_bytes + c * 16 : kHeadNowhere;
                 along[i] = c * 8;
             } else {
@@ -124,13 +132,18 @@ template <int kRows, bool kAcross> struct HeadFeed {
                 along[i] = kr;
             }
         }
-        step = kAcross ? 32 * o.row_bytes : 64;
+        step = kAcross ? kHeadStageK * o.row_bytes : kHeadStageK * 2;
+        issued = kk = fill = 0;
+        seek(o, 0, row0, first);
     }
     __device__ __forceinline__ void seek(const HeadOperand& o, int plane, int row0, int stage) {
         base = o.plane[plane] + (kAcross ? (int64_t)row0 * 2 : (int64_t)row0 * o.row_bytes) + stage * step;
     }
-    // left: k elements from this stage's start to the operand's end (0 or less: nothing is fetched)
-    __device__ __forceinline__ void issue(uint32_t lds, int left, int wave) {
+    // The next stage's transfers: `n` stages in segments of `nk`, k_elems elements of k from stage `first` on; `second`: the segment that takes the second
+    // plane.  Beyond the last stage zeros are fetched all the same, so that the counts of outstanding transfers hold.
+    template <int kSlots>
+    __device__ __forceinline__ void issue(uint32_t lds, const HeadOperand& o, int second, int row0, int n, int nk, int first, int k_elems, int wave) {
+        const int left = issued < n ? k_elems - (first + kk) * kHeadStageK : 0;
         u32x4 rsrc;
         rsrc[0] = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)base);
         rsrc[1] = __builtin_amdgcn_readfirstlane((uint32_t)((uintptr_t)base >> 32) & 0xffffu);
@@ -138,12 +151,18 @@ template <int kRows, bool kAcross> struct HeadFeed {
         rsrc[3] = 0x00020000u;
 #pragma unroll
         for (int i = 0; i < kN; ++i) {
-            if (kInstr % 8 != 0 && wave + 8 * i >= kInstr) break;
+            if (kInstr % kWaves != 0 && wave + kWaves * i >= kInstr) break;
             uint32_t v = voff[i];
-            if (left < 32) v = along[i] < left ? v : kHeadNowhere;
-            head_dma(lds + (wave + 8 * i) * 1024, v, rsrc);
+            if (left < kHeadStageK) v = along[i] < left ? v : kHeadNowhere;
+            head_dma(lds + fill + (wave + kWaves * i) * 1024, v, rsrc);
         }
         base += step;
+        fill = fill + kBytes == kSlots * kBytes ? 0 : fill + kBytes;
+        ++issued;
+        if (++kk == nk && issued < n) {                   // the next segment
+            kk = 0;
+            seek(o, issued == second * nk ? 1 : 0, row0, first);
+        }
     }
 };
 
@@ -152,25 +171,32 @@ typedef __attribute__((ext_vector_type(4))) short s16x4;
 typedef __attribute__((address_space(3))) s16x4 head_lds_s16x4;
 typedef __attribute__((address_space(3))) u32x4 head_lds_u32x4;
 
-// The fragment of block b (32 tile rows) and k group g (16 elements) of an operand at `at`: lane l gets row l % 32, the 8 k values of half l / 32.
+// The fragment of block b (16 tile rows) and k group g (32 elements) of an operand at `at`: lane l gets row l % 16, the 8 k values of quarter l / 16.
 template <int kRows, bool kAcross> __device__ __forceinline__ u32x4 head_fragment(head_lds* at, int b, int g, int lane) {
-    typedef HeadFeed<kRows, kAcross> Feed;
+    typedef HeadFeed<kRows, kAcross, 8> Feed;      // (the places do not depend on the number of waves)
     if constexpr (!kAcross) {
-        const int row = lane & 31, c = Feed::place_along(row, 2 * g + (lane >> 5));        // (32 b moves the place by nothing: a multiple of 16 rows)
-        return *(head_lds_u32x4*)(at + 32 * b * 64 + row * 64 + c * 16);
+        const int row = lane & 15, c = Feed::place_along(row, 4 * g + (lane >> 4));        // (16 b changes nothing: places repeat every 16 rows)
+        return *(head_lds_u32x4*)(at + (16 * b + row) * 128 + c * 16);
     } else {
         // two loads of four k rows: a group of 16 lanes supplies 4 rows x 16 columns and each lane receives one column
-        const int i = lane & 15, c = 4 * b + 2 * ((lane >> 4) & 1) + ((i & 3) >> 1);
+        const int i = lane & 15, c = 2 * b + ((i & 3) >> 1);
         s16x4 v[2];
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-            const int kr = 16 * g + 8 * (lane >> 5) + 4 * s + (i >> 2);
+            const int kr = 32 * g + 8 * (lane >> 4) + 4 * s + (i >> 2);
             v[s] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((head_lds_s16x4*)(at + kr * (kRows * 2) + Feed::place_across(kr, c) * 16 + (i & 1) * 8));
         }
         typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
         const u32x2 a = __builtin_bit_cast(u32x2, v[0]), d = __builtin_bit_cast(u32x2, v[1]);
         return u32x4{a[0], a[1], d[0], d[1]};
     }
+}
+
+// acc[16x16] += A[16 x 32] * B[32 x 16].  With operands that are not zeros the chip runs into its power limit before its rate: back to back from registers this
+// shape does 2.09 PFLOP/s where 32 x 32 x 16 does 1.84 (2.42 / 2.45 on zeros), as it moves half the accumulators per product.
+template <int DT> __device__ __forceinline__ f32x4 head_mma(u32x4 a, u32x4 b, f32x4 acc) {
+    if constexpr (DT == kBF16) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), acc, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), acc, 0, 0, 0);
 }
 
 // Tile `id` of tiles_q x tiles_p: every XCD (workgroup id mod 8) takes a contiguous eighth of a list that goes through groups of 8 row tiles column by
@@ -197,9 +223,9 @@ template <int DT> __device__ __forceinline__ uint32_t head_round2(float a, float
 
 // DT: the operands' element type, kF16 or kBF16.  OutDT: the type dW is written in.  grid = (8 * ceil(tiles / 8), k_slices).
 template <int DT, int OutDT, int kMode, class Tile>
-__global__ __launch_bounds__(kHeadThreads) void tide_head_gemm_kernel(const HeadGemmParams p) {
+__global__ __launch_bounds__(Tile::kThreads) void tide_head_gemm_kernel(const HeadGemmParams p) {
     constexpr bool kQAcross = kMode == kHeadWeights, kPAcross = kMode == kHeadRows || kMode == kHeadWeights;
-    constexpr int kBQ = Tile::kBQ, kBP = Tile::kBP, S = Tile::kStages, kCols = Tile::kCols, kLd = Tile::kLd;
+    constexpr int kBQ = Tile::kBQ, kBP = Tile::kBP, kCols = Tile::kCols, kLd = Tile::kLd;
     extern __shared__ __attribute__((aligned(16))) char smem[];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int wq = wave % Tile::kWQ, wp = wave / Tile::kWQ;
@@ -211,102 +237,104 @@ __global__ __launch_bounds__(kHeadThreads) void tide_head_gemm_kernel(const Head
     const int q0 = tq * Tile::kQ, p0 = tp * Tile::kP;
     if (q0 >= q_rows) return;
 
-    // ---- k loop: n stages, the slice's part of every segment
-    const int per = (k_elems + 31) >> 5;
+    // ---- k loop: n stages, the slice's part of every segment: (hi, hi), (hi, lo), (lo, hi)
+    const int per = (k_elems + kHeadStageK - 1) / kHeadStageK;
     const int first = (int)((int64_t)per * blockIdx.y / p.k_slices), last = (int)((int64_t)per * (blockIdx.y + 1) / p.k_slices);
     const int nk = last - first, n = nk * p.segments;
-    HeadFeed<Tile::kQ, kQAcross> fq;
-    HeadFeed<Tile::kP, kPAcross> fp;
-    fq.init(p.q, q0, q_rows, wave, lane);
-    fp.init(p.p, p0, p.p_rows, wave, lane);
-    fq.seek(p.q, 0, q0, first);
-    fp.seek(p.p, 0, p0, first);
-    const uint32_t lds0 = (uint32_t)(size_t)(head_lds*)smem;
-    int issued = 0, kk = 0, fill = 0;                     // stages issued, the next one's number within its segment, and its slot's byte
-    auto issue = [&] {
-        const int left = issued < n ? k_elems - (first + kk) * 32 : 0;
-        fq.issue(lds0 + fill, left, wave);
-        fp.issue(lds0 + fill + Tile::kQBytes, left, wave);
-        fill = fill + Tile::kStageBytes == S * Tile::kStageBytes ? 0 : fill + Tile::kStageBytes;
-        ++issued;
-        if (++kk == nk && issued < n) {                   // the next segment: (hi, hi), (hi, lo), (lo, hi)
-            kk = 0;
-            fq.seek(p.q, issued == 2 * nk ? 1 : 0, q0, first);
-            fp.seek(p.p, issued == nk ? 1 : 0, p0, first);
-        }
-    };
-    // Waits until all but the kYounger last stages issued by this wave have landed.
-    auto landed = [&](auto younger_c) {
-        constexpr int kYounger = decltype(younger_c)::value;
-        constexpr int kFull = Tile::kQ / 128 + Tile::kP / 128, kRest = Tile::kQ / 16 % 8;
-        static_assert(Tile::kP % 128 == 0, "");
-        if (kRest != 0 && wave < kRest) head_wait_vm<kYounger * (kFull + 1)>();
-        else head_wait_vm<kYounger * kFull>();
+    typedef HeadFeed<Tile::kQ, kQAcross, Tile::kWaves> FeedQ;
+    typedef HeadFeed<Tile::kP, kPAcross, Tile::kWaves> FeedP;
+    FeedQ fq;
+    FeedP fp;
+    fq.init(p.q, q0, q_rows, first, wave, lane);
+    fp.init(p.p, p0, p.p_rows, first, wave, lane);
+    const uint32_t lds_q = (uint32_t)(size_t)(head_lds*)smem, lds_p = lds_q + Tile::kSQ * Tile::kQBytes;
+    // Step s issues stage s + kSP of p, then stage s + kSQ of q.
+    auto issue_p = [&] { fp.template issue<Tile::kSP>(lds_p, p.p, 1, p0, n, nk, first, k_elems, wave); };
+    auto issue_q = [&] { fq.template issue<Tile::kSQ>(lds_q, p.q, 2, q0, n, nk, first, k_elems, wave); };
+    // Waits until all but the last kSteps steps of this wave's transfers, and the q transfers of the step before those where q is further ahead than
+    // p, have landed.
+    auto landed = [&](auto steps_c) {
+        constexpr int kSteps = decltype(steps_c)::value, kAhead = Tile::kSQ > Tile::kSP ? 1 : 0;
+        constexpr int kNP = FeedP::kN, kNQ = FeedQ::kInstr / Tile::kWaves, kRest = FeedQ::kInstr % Tile::kWaves;
+        static_assert(FeedP::kInstr % Tile::kWaves == 0, "");
+        if (kRest != 0 && wave < kRest) head_wait_vm<kSteps * kNP + (kSteps + kAhead) * (kNQ + 1)>();
+        else head_wait_vm<kSteps * kNP + (kSteps + kAhead) * kNQ>();
     };
 
-    f32x16 acc[kBP][kBQ];
+    f32x4 acc[kBP][kBQ];
 #pragma unroll
     for (int i = 0; i < kBP; ++i)
 #pragma unroll
-        for (int j = 0; j < kBQ; ++j) acc[i][j] = f32x16{0};
-    u32x4 aq[2][kBQ], ap[2][kBP];
-    auto read = [&](auto g_c, int slot) {
+        for (int j = 0; j < kBQ; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    u32x4 aq[kBQ], ap[kBP];
+    auto read = [&](auto g_c, int slot_q, int slot_p) {
         constexpr int g = decltype(g_c)::value;
-        head_lds* at = (head_lds*)smem + slot;
+        head_lds* at = (head_lds*)smem;
 #pragma unroll
-        for (int j = 0; j < kBQ; ++j) aq[g][j] = head_fragment<Tile::kQ, kQAcross>(at, wq * kBQ + j, g, lane);
+        for (int j = 0; j < kBQ; ++j) aq[j] = head_fragment<Tile::kQ, kQAcross>(at + slot_q, wq * kBQ + j, g, lane);
 #pragma unroll
-        for (int i = 0; i < kBP; ++i) ap[g][i] = head_fragment<Tile::kP, kPAcross>(at + Tile::kQBytes, wp * kBP + i, g, lane);
+        for (int i = 0; i < kBP; ++i) ap[i] = head_fragment<Tile::kP, kPAcross>(at + Tile::kSQ * Tile::kQBytes + slot_p, wp * kBP + i, g, lane);
     };
-    auto multiply = [&](auto g_c) {
-        constexpr int g = decltype(g_c)::value;
+    auto multiply = [&] {
 #pragma unroll
         for (int i = 0; i < kBP; ++i)
 #pragma unroll
-            for (int j = 0; j < kBQ; ++j) acc[i][j] = mma_k16<DT>(ap[g][i], aq[g][j], acc[i][j]);
+            for (int j = 0; j < kBQ; ++j) acc[i][j] = head_mma<DT>(ap[i], aq[j], acc[i][j]);
     };
     constexpr std::integral_constant<int, 0> g0;
     constexpr std::integral_constant<int, 1> g1;
-    constexpr std::integral_constant<int, S - 3> steady;
-
+    constexpr std::integral_constant<int, Tile::kSP - 2> steady;
+    int slot_q = 0, slot_p = 0;
 #pragma unroll
-    for (int s = 0; s < S - 1; ++s) issue();
-    landed(std::integral_constant<int, S - 2>{});
-    ring_barrier();
-    read(g0, 0);
-    int slot = 0;
-    for (int k = 0; k < n; ++k) {
-        const int next = slot + Tile::kStageBytes == S * Tile::kStageBytes ? 0 : slot + Tile::kStageBytes;
-        read(g1, slot);
-        multiply(g0);
-        landed(steady);
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // this wave has read all of stage k
-        ring_barrier();
-        issue();
-        read(g0, next);
-        multiply(g1);
-        slot = next;
+    for (int s = -Tile::kSQ; s < -1; ++s) {
+        if (s + Tile::kSP >= 0) issue_p();
+        issue_q();
     }
+    landed(steady);
+    ring_barrier();
+    const int group = wave >> 2;
+    if (group == 1) ring_barrier();
+    for (int k = 0; k < n; ++k) {
+        const int next_q = slot_q + Tile::kQBytes == Tile::kSQ * Tile::kQBytes ? 0 : slot_q + Tile::kQBytes;
+        const int next_p = slot_p + Tile::kPBytes == Tile::kSP * Tile::kPBytes ? 0 : slot_p + Tile::kPBytes;
+        auto edge = [] { __builtin_amdgcn_sched_barrier(0); ring_barrier(); __builtin_amdgcn_sched_barrier(0); };
+        read(g0, slot_q, slot_p);
+        issue_p();
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        edge();
+        multiply();
+        edge();
+        read(g1, slot_q, slot_p);
+        issue_q();
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (group == 1) landed(steady);
+        edge();
+        multiply();
+        __builtin_amdgcn_sched_barrier(0);
+        if (group == 0) landed(steady);
+        edge();
+        slot_q = next_q;
+        slot_p = next_p;
+    }
+    if (group == 0) ring_barrier();
     head_wait_vm<0>();
     __syncthreads();
 
     // ---- what becomes of the tile
     typedef __attribute__((address_space(3))) float lds_float;
     typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
-    lds_float* stage = (lds_float*)((head_lds*)smem + wave * 32 * kLd * 4);
-    const int row = lane & 31, h = lane >> 5;
+    lds_float* stage = (lds_float*)((head_lds*)smem + wave * 16 * kLd * 4);
+    const int row = lane & 15, h = lane >> 4;
     const int col0 = p0 + wp * kCols;                     // the wave's first column
-    // this wave's block of 32 rows into LDS, row by row; f(value, column within the wave's)
+    // this wave's block of 16 rows into LDS, row by row; f(value, column within the wave's)
     auto to_lds = [&](int j, auto f) {
 #pragma unroll
-        for (int i = 0; i < kBP; ++i)
+        for (int i = 0; i < kBP; ++i) {
+            f32x4 v;
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                f32x4 v;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = f(acc[i][j][4 * q + e], 32 * i + 8 * q + 4 * h + e);
-                *(lds_f32x4*)(stage + row * kLd + 32 * i + 8 * q + 4 * h) = v;
-            }
+            for (int e = 0; e < 4; ++e) v[e] = f(acc[i][j][e], 16 * i + 4 * h + e);
+            *(lds_f32x4*)(stage + row * kLd + 16 * i + 4 * h) = v;
+        }
     };
     auto lds_fence = [] {                                  // the wave's own LDS accesses stay in order
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -315,7 +343,7 @@ __global__ __launch_bounds__(kHeadThreads) void tide_head_gemm_kernel(const Head
 
 #pragma unroll
     for (int j = 0; j < kBQ; ++j) {
-        const int t0 = q0 + (wq * kBQ + j) * 32, t = t0 + row;
+        const int t0 = q0 + (wq * kBQ + j) * 16, t = t0 + row;
         if constexpr (kMode == kHeadStats) {
             const float scale = p.ctl ? p.ctl->logit_scale : 1.0f, c1 = p.c1 * scale;
             const bool ragged = col0 + kCols > p.p_rows;
@@ -323,28 +351,29 @@ __global__ __launch_bounds__(kHeadThreads) void tide_head_gemm_kernel(const Head
 #pragma unroll
             for (int i = 0; i < kBP; ++i)
 #pragma unroll
-                for (int v = 0; v < 16; ++v) {
-                    if (ragged && col0 + 32 * i + 8 * (v >> 2) + 4 * h + (v & 3) >= p.p_rows) acc[i][j][v] = -INFINITY;
+                for (int v = 0; v < 4; ++v) {
+                    if (ragged && col0 + 16 * i + 4 * h + v >= p.p_rows) acc[i][j][v] = -INFINITY;
                     m = fmaxf(m, acc[i][j][v]);
                 }
+            m = fmaxf(m, __shfl_xor(m, 16, kWave));
             m = fmaxf(m, __shfl_xor(m, 32, kWave));
             const float m2 = m * c1, shift = m2 == -INFINITY ? 0.0f : m2;
             float s = 0.0f;
 #pragma unroll
             for (int i = 0; i < kBP; ++i)
 #pragma unroll
-                for (int v = 0; v < 16; ++v) s += __builtin_amdgcn_exp2f(fmaf(acc[i][j][v], c1, -shift));
-            s += __shfl_xor(s, 32, kWave);
+                for (int v = 0; v < 4; ++v) s += __builtin_amdgcn_exp2f(fmaf(acc[i][j][v], c1, -shift));
+            s = add_xor<32>(add_xor<16>(s));
             if (h == 0 && t < q_rows) p.part[(int64_t)(tp * Tile::kWP + wp) * q_rows + t] = float2{m2, s};
-            // the row's own tokens among these columns: lane halves take every second one
+            // the row's own tokens among these columns: quarters of the lanes take every fourth one
             bool any = false;
             if (t < q_rows)
-                for (int k = h; k < p.K; k += 2) any |= (uint32_t)p.ids[(int64_t)t * p.K + k] - (uint32_t)col0 < (uint32_t)kCols;
+                for (int k = h; k < p.K; k += 4) any |= (uint32_t)p.ids[(int64_t)t * p.K + k] - (uint32_t)col0 < (uint32_t)kCols;
             if (__any(any)) {
                 to_lds(j, [](float z, int) { return z; });
                 lds_fence();
                 if (any)
-                    for (int k = h; k < p.K; k += 2) {
+                    for (int k = h; k < p.K; k += 4) {
                         const int id = p.ids[(int64_t)t * p.K + k];
                         if ((uint32_t)id - (uint32_t)col0 < (uint32_t)kCols && id < p.V) p.z_out[(int64_t)t * p.K + k] = stage[row * kLd + id - col0] * scale;
                     }
@@ -357,9 +386,9 @@ __global__ __launch_bounds__(kHeadThreads) void tide_head_gemm_kernel(const Head
             to_lds(j, [&](float z, int c) { return col0 + c < p.p_rows ? rc.y * __builtin_amdgcn_exp2f(fmaf(z, c1, -rc.x)) : 0.0f; });
             lds_fence();
             if (t < q_rows)
-                for (int k = 0; k < p.K; ++k) {           // each half of the lanes its own columns: a token that is given twice is subtracted in order
+                for (int k = 0; k < p.K; ++k) {           // each quarter of the lanes its own columns: a token that is given twice is subtracted in order
                     const int c = (int)((uint32_t)p.ids[own + k] - (uint32_t)(p.v0 + col0));
-                    if ((uint32_t)c < (uint32_t)kCols && ((c >> 4) & 1) == h && col0 + c < p.p_rows) {
+                    if ((uint32_t)c < (uint32_t)kCols && ((c >> 4) & 3) == h && col0 + c < p.p_rows) {
                         const float w = p.wanted ? p.wanted[own + k] : 1.0f;
                         stage[row * kLd + c] = fmaf(-w, rc.y, stage[row * kLd + c]);
                     }
@@ -367,7 +396,7 @@ __global__ __launch_bounds__(kHeadThreads) void tide_head_gemm_kernel(const Head
             lds_fence();
             constexpr int kLanes = kCols / 8, kRowsAtOnce = 64 / kLanes;      // 16 bytes of G a lane
 #pragma unroll
-            for (int r0 = 0; r0 < 32; r0 += kRowsAtOnce) {
+            for (int r0 = 0; r0 < 16; r0 += kRowsAtOnce) {
                 const int r = r0 + lane / kLanes, c = lane % kLanes * 8;
                 if (t0 + r >= q_rows) continue;
                 const f32x4 a = *(lds_f32x4*)(stage + r * kLd + c), b = *(lds_f32x4*)(stage + r * kLd + c + 4);
@@ -388,16 +417,12 @@ __global__ __launch_bounds__(kHeadThreads) void tide_head_gemm_kernel(const Head
             if (t < q_rows) {
                 float* dst = p.acc_out + blockIdx.y * p.acc_slice + (int64_t)t * p.acc_ld;
 #pragma unroll
-                for (int i = 0; i < kBP; ++i)
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        const int c = col0 + 32 * i + 8 * q + 4 * h;
-                        if (c >= p.acc_ld) continue;
-                        f32x4 v = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
-                        f32x4* at = reinterpret_cast<f32x4*>(dst + c);
-                        if (p.accumulate) v += *at;
-                        *at = v;
-                    }
+                for (int i = 0; i < kBP; ++i) {
+                    const int c = col0 + 16 * i + 4 * h;
+                    if (c >= p.acc_ld) continue;
+                    f32x4* at = reinterpret_cast<f32x4*>(dst + c);
+                    *at = p.accumulate ? acc[i][j] + *at : acc[i][j];
+                }
             }
         } else {
             const float back = p.ctl->weight_back;
@@ -405,7 +430,7 @@ __global__ __launch_bounds__(kHeadThreads) void tide_head_gemm_kernel(const Head
             lds_fence();
             constexpr int kBytes = Storage<OutDT>::kBytes, kE = 16 / kBytes, kLanes = kCols / kE, kRowsAtOnce = 64 / kLanes;
 #pragma unroll
-            for (int r0 = 0; r0 < 32; r0 += kRowsAtOnce) {
+            for (int r0 = 0; r0 < 16; r0 += kRowsAtOnce) {
                 const int r = r0 + lane / kLanes, c = lane % kLanes * kE;
                 if (t0 + r >= q_rows || col0 + c >= p.p_rows) continue;
                 float v[kE];

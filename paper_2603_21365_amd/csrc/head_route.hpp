@@ -5,10 +5,10 @@
 namespace {
 
 // The tile that the rows of a call take.  The vocabulary side is always 256 wide.
-using HeadTile32 = HeadTile<1, 8, 1, 1, 8>;
-using HeadTile64 = HeadTile<2, 4, 1, 2, 7>;
-using HeadTile128 = HeadTile<2, 4, 2, 2, 6>;
-using HeadTile256 = HeadTile<4, 2, 2, 4, 5>;
+using HeadTile32 = HeadTile<1, 8, 2, 2, 4, 4>;
+using HeadTile64 = HeadTile<2, 4, 2, 4, 4, 4>;
+using HeadTile128 = HeadTile<2, 4, 4, 4, 4, 3>;
+using HeadTile256 = HeadTile<4, 2, 4, 8, 3, 2>;
 constexpr int kHeadCols = 256;
 constexpr int64_t kHeadMostRows = (int64_t)1 << 22, kHeadMostVocab = ((int64_t)1 << 31) - 1024;
 constexpr int kHeadMostTop = 1024;
@@ -118,7 +118,7 @@ template <int DT, int OutDT, int kMode, class Tile> int launch_head(int64_t q_ro
     p.tiles_q = (int)tq;
     p.tiles_p = (int)tp;
     if (tq * tp == 0) return TIDE_OK;
-    hipLaunchKernelGGL((tide_head_gemm_kernel<DT, OutDT, kMode, Tile>), dim3(8u * (unsigned)((tq * tp + 7) / 8), (unsigned)p.k_slices), dim3(kHeadThreads),
+    hipLaunchKernelGGL((tide_head_gemm_kernel<DT, OutDT, kMode, Tile>), dim3(8u * (unsigned)((tq * tp + 7) / 8), (unsigned)p.k_slices), dim3(Tile::kThreads),
                        Tile::kLdsBytes, st, p);
     return TIDE_OK;
 }
