@@ -368,7 +368,17 @@ int head_backward(const HeadCall& c) {
 }
 
 constexpr int kProjectGradMaxBlocks = 1024;
-int project_grad_blocks(int64_t T, unsigned cus) { return (int)std::min<int64_t>(T, std::min<int64_t>(2 * cus, kProjectGradMaxBlocks)); }
+// Rows of up to 4 KiB: four at a time, a wave each.
+bool project_grad_wave_rows(int64_t row_bytes) { return row_bytes <= 4096; }
+// As many workgroups as have rows in equal rounds: at most two per CU, four where each then has four rounds or more, which is where the requests in flight
+// outweigh the sums that each leaves (two / four, us, bf16: T = 1000, d = 4096 11.2 / 15.2, 4000 27.4 / 27.2, 8192 47.8 / 43.1; d = 768, T = 16384 23.5 / 18.5;
+// d = 2048, T = 3000 12.0 / 13.1).
+int project_grad_blocks(int64_t T, int64_t row_bytes, unsigned cus) {
+    const int64_t turns = project_grad_wave_rows(row_bytes) ? (T + 3) / 4 : T;
+    const int64_t most = std::min<int64_t>((turns >= 16 * (int64_t)cus ? 4 : 2) * cus, kProjectGradMaxBlocks);
+    const int64_t rounds = std::max<int64_t>(1, (turns + most - 1) / most);
+    return (int)((turns + rounds - 1) / rounds);
+}
 
 }  // namespace
 
@@ -475,7 +485,7 @@ int tide_exit_project_grad(const void* hidden, int dtype, int64_t C, int64_t T, 
     if (T == 0 && !grad_gain) return TIDE_OK;
     unsigned cus = 0;
     if ((rc = resident_cus(&cus))) return rc;
-    const int blocks = project_grad_blocks(T, cus);
+    const int blocks = project_grad_blocks(T, d * (int64_t)eb, cus);
     const bool joined = grad_gain && blocks != 1;      // one workgroup's sums are the gradient
     if (joined && blocks) {
         const size_t need = (size_t)blocks * d * sizeof(float);
@@ -500,24 +510,28 @@ int tide_exit_project_grad(const void* hidden, int dtype, int64_t C, int64_t T, 
     p.d = (int)d;
     p.eps = eps;
     hipStream_t st = (hipStream_t)stream;
-    const int64_t per_thread = (d * (int64_t)eb / 16 + kProjectThreads - 1) / kProjectThreads;
+    const bool wave_rows = project_grad_wave_rows(d * (int64_t)eb);
+    const int64_t step = wave_rows ? kWave : kProjectThreads, per_thread = (d * (int64_t)eb / 16 + step - 1) / step;
     if (blocks)
         by_dtype(dtype, [&](auto dt) {
             constexpr int DT = decltype(dt)::value;
-            auto go = [&](auto chunks) {
-                hipLaunchKernelGGL((tide_project_grad_kernel<DT, decltype(chunks)::value>), dim3(blocks), dim3(kProjectThreads), 0, st, p);
+            auto go = [&](auto chunks, auto wave) {
+                hipLaunchKernelGGL((tide_project_grad_kernel<DT, decltype(chunks)::value, decltype(wave)::value>), dim3(blocks), dim3(kProjectThreads), 0, st, p);
                 return 0;
             };
             using std::integral_constant;
-            if (per_thread <= 1) return go(integral_constant<int, 1>{});
-            if (per_thread <= 2) return go(integral_constant<int, 2>{});
-            if (per_thread <= 4) return go(integral_constant<int, 4>{});
-            if constexpr (DT == kF32) {                // rows above 32 KiB
-                if (per_thread > 8) return go(integral_constant<int, 16>{});
+            if (wave_rows) {
+                if (per_thread <= 2) return go(integral_constant<int, 2>{}, std::true_type{});
+                return go(integral_constant<int, 4>{}, std::true_type{});
             }
-            return go(integral_constant<int, 8>{});
+            if (per_thread <= 2) return go(integral_constant<int, 2>{}, std::false_type{});
+            if (per_thread <= 4) return go(integral_constant<int, 4>{}, std::false_type{});
+            if constexpr (DT == kF32) {                // rows above 32 KiB
+                if (per_thread > 8) return go(integral_constant<int, 16>{}, std::false_type{});
+            }
+            return go(integral_constant<int, 8>{}, std::false_type{});
         });
-    if (joined) hipLaunchKernelGGL(tide_project_gain_kernel, dim3((unsigned)((d + 31) / 32)), dim3(256), 0, st, (const float*)workspace, blocks, (int)d, grad_gain);
+    if (joined) hipLaunchKernelGGL(tide_project_gain_kernel, dim3((unsigned)((d + 31) / 32)), dim3(kProjectGainThreads), 0, st, (const float*)workspace, blocks, (int)d, grad_gain);
     TIDE_HIP(hipGetLastError());
     return TIDE_OK;
 }

@@ -566,16 +566,17 @@ def exit_project_grad(hidden, final_hidden, exit_layer, layer_ids, norm_gain, ep
         if Tf != T or wf < d or final_hidden.dtype != hidden.dtype:
             raise ValueError("final_hidden must be [T, >=d] of hidden's dtype")
         frs = frs if T > 1 else max(frs, d)
-    idh, idp = _host(layer_ids, C, np.int32)
-    grad = torch.empty((T, d), dtype=hidden.dtype, device=hidden.device)
-    gain = torch.empty(d, dtype=torch.float32, device=hidden.device) if want_gain else None
+    idh, idp = _host_once(layer_ids, C, np.int32)
+    dev = hidden.device
+    grad = torch.empty((T, d), dtype=hidden.dtype, device=dev)
+    gain = torch.empty(d, dtype=torch.float32, device=dev) if want_gain else None
     lib = load_library()
     nbytes = 0
-    if want_gain:
-        workspace, nbytes = _scratch(workspace, int(lib.tide_exit_project_grad_bytes(T, d)), hidden.device)
+    if want_gain and T > 1:                        # (one row's products are the gradient to the gain)
+        workspace, nbytes = _scratch(workspace, lib.tide_exit_project_grad_bytes(T, d), dev)
     _check(lib.tide_exit_project_grad(_ptr(hidden), _dtype_code(hidden), C, T, d, cs if (C > 1 and T > 0) else max(cs, 0), rs if T > 1 else max(rs, d),
                                       _ptr(final_hidden), frs, _ptr(exit_layer), idp, _ptr(norm_gain), float(eps), _ptr(grad_out),
-                                      gs if T > 1 else max(gs, d), _ptr(grad), d, _ptr(gain), _ptr(workspace) if want_gain else None, nbytes, _stream()))
+                                      gs if T > 1 else max(gs, d), _ptr(grad), d, _ptr(gain), _ptr(workspace) if nbytes else None, nbytes, _stream()))
     del idh
     return grad, gain
 
