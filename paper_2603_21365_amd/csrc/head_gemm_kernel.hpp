@@ -46,7 +46,7 @@ struct HeadCtl {
     float row_back, weight_back;   // the same for dx and dW
 };
 
-constexpr int kHeadStageK = 64;                      // k elements of a stage: a whole cache line of a row
+constexpr int kHeadRowBytes = 128;                   // of a row along k in a stage: a whole cache line
 
 struct HeadOperand {
     const char* plane[2];
@@ -58,6 +58,7 @@ struct HeadGemmParams {
     int q_rows, p_rows, k;     // of these the one that counts live rows is replaced by ctl->live
     int segments;              // 1, or 3 for two planes
     int tiles_q, tiles_p, k_slices;
+    int pitch;                 // columns of a tile: kP, or fewer (statistics) where that gives every CU as many
     const HeadCtl* ctl;        // null where nothing is scaled and every row counts (16-bit statistics)
     // statistics and G
     float c1;                  // log2(e) / tau
@@ -80,15 +81,18 @@ struct HeadGemmParams {
     int out_aligned;           // rows of whole 16-byte chunks
 };
 
-// kSQ, kSP: stages of each operand that its part of LDS holds.
-template <int WQ, int WP, int BQ, int BP, int SQ, int SP> struct HeadTile {
-    static constexpr int kWQ = WQ, kWP = WP, kBQ = BQ, kBP = BP, kSQ = SQ, kSP = SP;
-    static constexpr int kWaves = WQ * WP, kThreads = kWaves * kWave;
+// kSQ, kSP: stages of each operand that its part of LDS holds.  EB: bytes of an element (4: fp32 rows as they are).
+template <int WQ, int WP, int BQ, int BP, int SQ, int SP, int EB = 2> struct HeadTile {
+    static constexpr int kWQ = WQ, kWP = WP, kBQ = BQ, kBP = BP, kSQ = SQ, kSP = SP, kEB = EB;
+    static constexpr int kWaves = WQ * WP, kThreads = kWaves * kWave, kK = kHeadRowBytes / EB;
+    static constexpr bool kTurns = BQ * BP >= 16;                // two groups of waves that take turns (few rows: bound by memory, one barrier a stage)
     static constexpr int kQ = WQ * BQ * 16, kP = WP * BP * 16;
-    static constexpr int kQBytes = kQ * kHeadStageK * 2, kPBytes = kP * kHeadStageK * 2, kRingBytes = SQ * kQBytes + SP * kPBytes;
+    static constexpr int kQBytes = kQ * kHeadRowBytes, kPBytes = kP * kHeadRowBytes, kRingBytes = SQ * kQBytes + SP * kPBytes;
     static constexpr int kCols = BP * 16, kLd = kCols + 4;       // a wave's columns; its rows in LDS after the loop, padded against bank conflicts
     static constexpr int kEpiBytes = kWaves * 16 * kLd * 4;
-    static constexpr int kLdsBytes = kRingBytes > kEpiBytes ? kRingBytes : kEpiBytes;
+    static constexpr bool kJoined = WP > 2;                      // the statistics of a tile's columns leave as one
+    static constexpr int kParts = kJoined ? 1 : WP, kJoinBytes = kJoined ? WP * kQ * 8 : 0;
+    static constexpr int kLdsBytes = kRingBytes > kEpiBytes + kJoinBytes ? kRingBytes : kEpiBytes + kJoinBytes;
     static_assert(kWaves == 8 && SP >= 2 && SQ >= SP, "two groups of four waves");
     static_assert(kLdsBytes <= 160 * 1024, "LDS of a CU");
 };
@@ -100,9 +104,9 @@ __device__ __forceinline__ void head_dma(uint32_t lds, uint32_t voff, u32x4 rsrc
 }
 template <int n> __device__ __forceinline__ void head_wait_vm() { asm volatile("s_waitcnt vmcnt(%0)" ::"i"(n) : "memory"); }
 
-// One operand's transfers: kRows tile rows, instruction n = wave + 8 i of kRows / 8 a stage, a ring of kSlots stages at byte `lds`.
-template <int kRows, bool kAcross, int kWaves> struct HeadFeed {
-    static constexpr int kInstr = kRows / 8, kN = (kInstr + kWaves - 1) / kWaves, kBytes = kRows * kHeadStageK * 2;
+// One operand's transfers: kRows tile rows of a stage, instruction n = wave + kWaves i of kInstr, a ring of kSlots stages at byte `lds`.
+template <int kRows, bool kAcross, int kWaves, int kEB = 2> struct HeadFeed {
+    static constexpr int kK = kHeadRowBytes / kEB, kBytes = kRows * kHeadRowBytes, kInstr = kBytes / 1024, kN = (kInstr + kWaves - 1) / kWaves;
     uint32_t voff[kN];
     int along[kN];             // first k element of this lane's chunk within a stage (along), or its k row (across)
     const char* base;
@@ -113,7 +117,7 @@ template <int kRows, bool kAcross, int kWaves> struct HeadFeed {
     // chunk.  Across: rows of 512 bytes, 32 bytes of each of eight.
     static __device__ __forceinline__ int place_along(int row, int c) { return c ^ ((row >> 1) & 7); }
     static __device__ __forceinline__ int place_across(int kr, int c) {
-        static_assert(!kAcross || kRows == 256, "");
+        static_assert(!kAcross || (kRows == 256 && kEB == 2), "");
         return c ^ ((kr & 3) << 1 | (kr >> 3 & 1) << 3);
     }
 
@@ -124,15 +128,14 @@ template <int kRows, bool kAcross, int kWaves> struct HeadFeed {
             if constexpr (!kAcross) {
                 const int r = 8 * n + (lane >> 3), c = place_along(r, lane & 7);
                 voff[i] = row0 + r < rows ? (uint32_t)r * (uint32_t)o.row_bytes + c * 16 : kHeadNowhere;
-                along[i] = c * 8;
+                along[i] = c * (16 / kEB);
             } else {
-                constexpr int kRowBytes = kRows * 2;
-                const int byte = n * 1024 + lane * 16, kr = byte / kRowBytes, c = place_across(kr, (byte % kRowBytes) >> 4);
+                const int byte = n * 1024 + lane * 16, kr = byte / (kRows * 2), c = place_across(kr, byte % (kRows * 2) >> 4);
                 voff[i] = row0 + c * 8 < rows ? (uint32_t)kr * (uint32_t)o.row_bytes + c * 16 : kHeadNowhere;
                 along[i] = kr;
             }
         }
-        step = kAcross ? kHeadStageK * o.row_bytes : kHeadStageK * 2;
+        step = kAcross ? kK * o.row_bytes : kHeadRowBytes;
         issued = kk = fill = 0;
         seek(o, 0, row0, first);
     }
@@ -143,7 +146,7 @@ template <int kRows, bool kAcross, int kWaves> struct HeadFeed {
     // plane.  Beyond the last stage zeros are fetched all the same, so that the counts of outstanding transfers hold.
     template <int kSlots>
     __device__ __forceinline__ void issue(uint32_t lds, const HeadOperand& o, int second, int row0, int n, int nk, int first, int k_elems, int wave) {
-        const int left = issued < n ? k_elems - (first + kk) * kHeadStageK : 0;
+        const int left = issued < n ? k_elems - (first + kk) * kK : 0;
         u32x4 rsrc;
         rsrc[0] = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)base);
         rsrc[1] = __builtin_amdgcn_readfirstlane((uint32_t)((uintptr_t)base >> 32) & 0xffffu);
@@ -153,7 +156,7 @@ template <int kRows, bool kAcross, int kWaves> struct HeadFeed {
         for (int i = 0; i < kN; ++i) {
             if (kInstr % kWaves != 0 && wave + kWaves * i >= kInstr) break;
             uint32_t v = voff[i];
-            if (left < kHeadStageK) v = along[i] < left ? v : kHeadNowhere;
+            if (left < kK) v = along[i] < left ? v : kHeadNowhere;
             head_dma(lds + fill + (wave + kWaves * i) * 1024, v, rsrc);
         }
         base += step;
@@ -171,9 +174,19 @@ typedef __attribute__((ext_vector_type(4))) short s16x4;
 typedef __attribute__((address_space(3))) s16x4 head_lds_s16x4;
 typedef __attribute__((address_space(3))) u32x4 head_lds_u32x4;
 
+template <int DT> __device__ __forceinline__ uint32_t head_round2(float a, float b) {
+    if constexpr (DT == kF16) {
+        const f16x2 h = {static_cast<_Float16>(a), static_cast<_Float16>(b)};
+        return __builtin_bit_cast(uint32_t, h);
+    } else {
+        const bf16x2 h = {static_cast<__bf16>(a), static_cast<__bf16>(b)};
+        return __builtin_bit_cast(uint32_t, h);
+    }
+}
+
 // The fragment of block b (16 tile rows) and k group g (32 elements) of an operand at `at`: lane l gets row l % 16, the 8 k values of quarter l / 16.
 template <int kRows, bool kAcross> __device__ __forceinline__ u32x4 head_fragment(head_lds* at, int b, int g, int lane) {
-    typedef HeadFeed<kRows, kAcross, 8> Feed;      // (the places do not depend on the number of waves)
+    typedef HeadFeed<kRows, kAcross, 8> Feed;
     if constexpr (!kAcross) {
         const int row = lane & 15, c = Feed::place_along(row, 4 * g + (lane >> 4));        // (16 b changes nothing: places repeat every 16 rows)
         return *(head_lds_u32x4*)(at + (16 * b + row) * 128 + c * 16);
@@ -192,11 +205,44 @@ template <int kRows, bool kAcross> __device__ __forceinline__ u32x4 head_fragmen
     }
 }
 
+// The same of fp32 rows: eight values, each as three bf16 terms, x = hi + mid + lo to 2^-24 x.
+struct HeadSplit {
+    u32x4 hi, mid, lo;
+};
+template <int kRows> __device__ __forceinline__ HeadSplit head_fragment_f32(head_lds* at, int b, int lane) {
+    typedef HeadFeed<kRows, false, 8, 4> Feed;
+    const int row = lane & 15, c = 2 * (lane >> 4);
+    const u32x4 v[2] = {*(head_lds_u32x4*)(at + (16 * b + row) * 128 + Feed::place_along(row, c) * 16), *(head_lds_u32x4*)(at + (16 * b + row) * 128 + Feed::place_along(row, c + 1) * 16)};
+    HeadSplit s;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float a = __uint_as_float(v[i >> 1][2 * (i & 1)]), d = __uint_as_float(v[i >> 1][2 * (i & 1) + 1]);
+        uint32_t t[3];
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {                  // (each difference is exact)
+            t[k] = head_round2<kBF16>(a, d);
+            a -= __uint_as_float(t[k] << 16);
+            d -= __uint_as_float(t[k] & 0xffff0000u);
+        }
+        s.hi[i] = t[0], s.mid[i] = t[1], s.lo[i] = t[2];
+    }
+    return s;
+}
+
 // acc[16x16] += A[16 x 32] * B[32 x 16].  With operands that are not zeros the chip runs into its power limit before its rate: back to back from registers this
 // shape does 2.09 PFLOP/s where 32 x 32 x 16 does 1.84 (2.42 / 2.45 on zeros), as it moves half the accumulators per product.
 template <int DT> __device__ __forceinline__ f32x4 head_mma(u32x4 a, u32x4 b, f32x4 acc) {
     if constexpr (DT == kBF16) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), acc, 0, 0, 0);
     else return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), acc, 0, 0, 0);
+}
+// fp32: the products of the terms down to 2^-24, small ones first.
+template <int DT> __device__ __forceinline__ f32x4 head_mma(const HeadSplit& a, const HeadSplit& b, f32x4 acc) {
+    acc = head_mma<kBF16>(a.lo, b.hi, acc);
+    acc = head_mma<kBF16>(a.hi, b.lo, acc);
+    acc = head_mma<kBF16>(a.mid, b.mid, acc);
+    acc = head_mma<kBF16>(a.mid, b.hi, acc);
+    acc = head_mma<kBF16>(a.hi, b.mid, acc);
+    return head_mma<kBF16>(a.hi, b.hi, acc);
 }
 
 // Tile `id` of tiles_q x tiles_p: every XCD (workgroup id mod 8) takes a contiguous eighth of a list that goes through groups of 8 row tiles column by
@@ -211,17 +257,7 @@ __device__ __forceinline__ bool head_tile(int id, int tiles_q, int tiles_p, int&
     return true;
 }
 
-template <int DT> __device__ __forceinline__ uint32_t head_round2(float a, float b) {
-    if constexpr (DT == kF16) {
-        const f16x2 h = {static_cast<_Float16>(a), static_cast<_Float16>(b)};
-        return __builtin_bit_cast(uint32_t, h);
-    } else {
-        const bf16x2 h = {static_cast<__bf16>(a), static_cast<__bf16>(b)};
-        return __builtin_bit_cast(uint32_t, h);
-    }
-}
-
-// DT: the operands' element type, kF16 or kBF16.  OutDT: the type dW is written in.  grid = (8 * ceil(tiles / 8), k_slices).
+// DT: the operands' element type, kF16 or kBF16 (kF32: fp32 rows as they are, statistics of few rows only).  OutDT: the type dW is written in.  grid = (8 * ceil(tiles / 8), k_slices).
 template <int DT, int OutDT, int kMode, class Tile>
 __global__ __launch_bounds__(Tile::kThreads) void tide_head_gemm_kernel(const HeadGemmParams p) {
     constexpr bool kQAcross = kMode == kHeadWeights, kPAcross = kMode == kHeadRows || kMode == kHeadWeights;
@@ -234,19 +270,20 @@ __global__ __launch_bounds__(Tile::kThreads) void tide_head_gemm_kernel(const He
     const int live = kMode == kHeadStats ? 0 : p.ctl->live;
     const int q_rows = kMode == kHeadGrad || kMode == kHeadRows ? live : p.q_rows;
     const int k_elems = kMode == kHeadWeights ? live : p.k;
-    const int q0 = tq * Tile::kQ, p0 = tp * Tile::kP;
+    const int q0 = tq * Tile::kQ, p0 = tp * p.pitch, p_end = min(p.p_rows, p0 + p.pitch);
     if (q0 >= q_rows) return;
 
     // ---- k loop: n stages, the slice's part of every segment: (hi, hi), (hi, lo), (lo, hi)
-    const int per = (k_elems + kHeadStageK - 1) / kHeadStageK;
+    const int per = (k_elems + Tile::kK - 1) / Tile::kK;
     const int first = (int)((int64_t)per * blockIdx.y / p.k_slices), last = (int)((int64_t)per * (blockIdx.y + 1) / p.k_slices);
     const int nk = last - first, n = nk * p.segments;
-    typedef HeadFeed<Tile::kQ, kQAcross, Tile::kWaves> FeedQ;
-    typedef HeadFeed<Tile::kP, kPAcross, Tile::kWaves> FeedP;
+    typedef HeadFeed<Tile::kQ, kQAcross, Tile::kWaves, Tile::kEB> FeedQ;
+    typedef HeadFeed<Tile::kP, kPAcross, Tile::kWaves, Tile::kEB> FeedP;
+    static_assert((DT == kF32) == (Tile::kEB == 4) && (DT != kF32 || kMode == kHeadStats), "");
     FeedQ fq;
     FeedP fp;
     fq.init(p.q, q0, q_rows, first, wave, lane);
-    fp.init(p.p, p0, p.p_rows, first, wave, lane);
+    fp.init(p.p, p0, p_end, first, wave, lane);
     const uint32_t lds_q = (uint32_t)(size_t)(head_lds*)smem, lds_p = lds_q + Tile::kSQ * Tile::kQBytes;
     // Step s issues stage s + kSP of p, then stage s + kSQ of q.
     auto issue_p = [&] { fp.template issue<Tile::kSP>(lds_p, p.p, 1, p0, n, nk, first, k_elems, wave); };
@@ -266,14 +303,20 @@ __global__ __launch_bounds__(Tile::kThreads) void tide_head_gemm_kernel(const He
     for (int i = 0; i < kBP; ++i)
 #pragma unroll
         for (int j = 0; j < kBQ; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    u32x4 aq[kBQ], ap[kBP];
+    std::conditional_t<DT == kF32, HeadSplit, u32x4> aq[kBQ], ap[kBP];
     auto read = [&](auto g_c, int slot_q, int slot_p) {
         constexpr int g = decltype(g_c)::value;
         head_lds* at = (head_lds*)smem;
 #pragma unroll
-        for (int j = 0; j < kBQ; ++j) aq[j] = head_fragment<Tile::kQ, kQAcross>(at + slot_q, wq * kBQ + j, g, lane);
+        for (int j = 0; j < kBQ; ++j) {
+            if constexpr (DT == kF32) aq[j] = head_fragment_f32<Tile::kQ>(at + slot_q, wq * kBQ + j, lane);
+            else aq[j] = head_fragment<Tile::kQ, kQAcross>(at + slot_q, wq * kBQ + j, g, lane);
+        }
 #pragma unroll
-        for (int i = 0; i < kBP; ++i) ap[i] = head_fragment<Tile::kP, kPAcross>(at + Tile::kSQ * Tile::kQBytes + slot_p, wp * kBP + i, g, lane);
+        for (int i = 0; i < kBP; ++i) {
+            if constexpr (DT == kF32) ap[i] = head_fragment_f32<Tile::kP>(at + Tile::kSQ * Tile::kQBytes + slot_p, wp * kBP + i, lane);
+            else ap[i] = head_fragment<Tile::kP, kPAcross>(at + Tile::kSQ * Tile::kQBytes + slot_p, wp * kBP + i, g, lane);
+        }
     };
     auto multiply = [&] {
 #pragma unroll
@@ -290,33 +333,52 @@ __global__ __launch_bounds__(Tile::kThreads) void tide_head_gemm_kernel(const He
         if (s + Tile::kSP >= 0) issue_p();
         issue_q();
     }
-    landed(steady);
-    ring_barrier();
-    const int group = wave >> 2;
-    if (group == 1) ring_barrier();
-    for (int k = 0; k < n; ++k) {
-        const int next_q = slot_q + Tile::kQBytes == Tile::kSQ * Tile::kQBytes ? 0 : slot_q + Tile::kQBytes;
-        const int next_p = slot_p + Tile::kPBytes == Tile::kSP * Tile::kPBytes ? 0 : slot_p + Tile::kPBytes;
-        auto edge = [] { __builtin_amdgcn_sched_barrier(0); ring_barrier(); __builtin_amdgcn_sched_barrier(0); };
-        read(g0, slot_q, slot_p);
-        issue_p();
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        edge();
-        multiply();
-        edge();
-        read(g1, slot_q, slot_p);
-        issue_q();
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        if (group == 1) landed(steady);
-        edge();
-        multiply();
-        __builtin_amdgcn_sched_barrier(0);
-        if (group == 0) landed(steady);
-        edge();
-        slot_q = next_q;
-        slot_p = next_p;
+    if constexpr (Tile::kTurns) {
+        landed(steady);
+        ring_barrier();
+        const int group = wave >> 2;
+        if (group == 1) ring_barrier();
+        for (int k = 0; k < n; ++k) {
+            const int next_q = slot_q + Tile::kQBytes == Tile::kSQ * Tile::kQBytes ? 0 : slot_q + Tile::kQBytes;
+            const int next_p = slot_p + Tile::kPBytes == Tile::kSP * Tile::kPBytes ? 0 : slot_p + Tile::kPBytes;
+            auto edge = [] { __builtin_amdgcn_sched_barrier(0); ring_barrier(); __builtin_amdgcn_sched_barrier(0); };
+            read(g0, slot_q, slot_p);
+            issue_p();
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            edge();
+            multiply();
+            edge();
+            read(g1, slot_q, slot_p);
+            issue_q();
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            if (group == 1) landed(steady);
+            edge();
+            multiply();
+            __builtin_amdgcn_sched_barrier(0);
+            if (group == 0) landed(steady);
+            edge();
+            slot_q = next_q;
+            slot_p = next_p;
+        }
+        if (group == 0) ring_barrier();
+    } else {
+        static_assert(Tile::kTurns || Tile::kSQ == Tile::kSP, "");
+        for (int k = 0; k < n; ++k) {
+            landed(steady);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");          // this wave has read all of stage k - 1, whose slot is filled next
+            ring_barrier();
+            issue_p();
+            issue_q();
+            read(g0, slot_q, slot_p);
+            multiply();
+            if constexpr (Tile::kK == 64) {
+                read(g1, slot_q, slot_p);
+                multiply();
+            }
+            slot_q = slot_q + Tile::kQBytes == Tile::kSQ * Tile::kQBytes ? 0 : slot_q + Tile::kQBytes;
+            slot_p = slot_p + Tile::kPBytes == Tile::kSP * Tile::kPBytes ? 0 : slot_p + Tile::kPBytes;
+        }
     }
-    if (group == 0) ring_barrier();
     head_wait_vm<0>();
     __syncthreads();
 
@@ -326,6 +388,9 @@ __global__ __launch_bounds__(Tile::kThreads) void tide_head_gemm_kernel(const He
     lds_float* stage = (lds_float*)((head_lds*)smem + wave * 16 * kLd * 4);
     const int row = lane & 15, h = lane >> 4;
     const int col0 = p0 + wp * kCols;                     // the wave's first column
+    typedef __attribute__((ext_vector_type(2))) float f32x2;
+    typedef __attribute__((address_space(3))) f32x2 lds_f32x2;
+    lds_f32x2* joined = (lds_f32x2*)((head_lds*)smem + Tile::kEpiBytes);      // statistics: [kWP][kQ] maxima and sums
     // this wave's block of 16 rows into LDS, row by row; f(value, column within the wave's)
     auto to_lds = [&](int j, auto f) {
 #pragma unroll
@@ -346,13 +411,13 @@ __global__ __launch_bounds__(Tile::kThreads) void tide_head_gemm_kernel(const He
         const int t0 = q0 + (wq * kBQ + j) * 16, t = t0 + row;
         if constexpr (kMode == kHeadStats) {
             const float scale = p.ctl ? p.ctl->logit_scale : 1.0f, c1 = p.c1 * scale;
-            const bool ragged = col0 + kCols > p.p_rows;
+            const bool ragged = col0 + kCols > p_end;
             float m = -INFINITY;
 #pragma unroll
             for (int i = 0; i < kBP; ++i)
 #pragma unroll
                 for (int v = 0; v < 4; ++v) {
-                    if (ragged && col0 + 16 * i + 4 * h + v >= p.p_rows) acc[i][j][v] = -INFINITY;
+                    if (ragged && col0 + 16 * i + 4 * h + v >= p_end) acc[i][j][v] = -INFINITY;
                     m = fmaxf(m, acc[i][j][v]);
                 }
             m = fmaxf(m, __shfl_xor(m, 16, kWave));
@@ -364,7 +429,11 @@ __global__ __launch_bounds__(Tile::kThreads) void tide_head_gemm_kernel(const He
 #pragma unroll
                 for (int v = 0; v < 4; ++v) s += __builtin_amdgcn_exp2f(fmaf(acc[i][j][v], c1, -shift));
             s = add_xor<32>(add_xor<16>(s));
-            if (h == 0 && t < q_rows) p.part[(int64_t)(tp * Tile::kWP + wp) * q_rows + t] = float2{m2, s};
+            if constexpr (Tile::kJoined) {                // with the other waves' columns, below
+                if (h == 0) joined[wp * Tile::kQ + (wq * kBQ + j) * 16 + row] = f32x2{m2, s};
+            } else {
+                if (h == 0 && t < q_rows) p.part[(int64_t)(tp * Tile::kWP + wp) * q_rows + t] = float2{m2, s};
+            }
             // the row's own tokens among these columns: quarters of the lanes take every fourth one
             bool any = false;
             if (t < q_rows)
@@ -375,7 +444,7 @@ __global__ __launch_bounds__(Tile::kThreads) void tide_head_gemm_kernel(const He
                 if (any)
                     for (int k = h; k < p.K; k += 4) {
                         const int id = p.ids[(int64_t)t * p.K + k];
-                        if ((uint32_t)id - (uint32_t)col0 < (uint32_t)kCols && id < p.V) p.z_out[(int64_t)t * p.K + k] = stage[row * kLd + id - col0] * scale;
+                        if ((uint32_t)id - (uint32_t)col0 < (uint32_t)kCols && id < p_end) p.z_out[(int64_t)t * p.K + k] = stage[row * kLd + id - col0] * scale;
                     }
                 lds_fence();
             }
@@ -453,6 +522,18 @@ __global__ __launch_bounds__(Tile::kThreads) void tide_head_gemm_kernel(const He
                 }
             }
             lds_fence();
+        }
+    }
+    if constexpr (kMode == kHeadStats && Tile::kJoined) {
+        __syncthreads();
+        const int r = threadIdx.x;
+        if (r < Tile::kQ && q0 + r < q_rows) {
+            float m = -INFINITY, s = 0.0f;
+#pragma unroll
+            for (int w = 0; w < Tile::kWP; ++w) m = fmaxf(m, joined[w * Tile::kQ + r][0]);
+#pragma unroll
+            for (int w = 0; w < Tile::kWP; ++w) s += joined[w * Tile::kQ + r][1] * __builtin_amdgcn_exp2f(joined[w * Tile::kQ + r][0] - (m == -INFINITY ? 0.0f : m));
+            p.part[(int64_t)tp * q_rows + q0 + r] = float2{m, s};
         }
     }
 }

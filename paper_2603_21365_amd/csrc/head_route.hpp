@@ -4,11 +4,18 @@
 
 namespace {
 
-// The tile that the rows of a call take.  The vocabulary side is always 256 wide.
-using HeadTile32 = HeadTile<1, 8, 2, 2, 4, 4>;
-using HeadTile64 = HeadTile<2, 4, 2, 4, 4, 4>;
+// The tile that the rows of a call take.  Few rows: the products with x W^T are bound by reading W, so their tiles are 128 columns wide and leave half of a
+// CU's LDS, so that two workgroups are there and one's first and last stages overlap with the other's (256 columns, one workgroup: 44 us for 32003 x 768 in
+// fp32, 125 tiles on 256 CUs, 34 as 251 of 128).  dx reads W across and stays 256 wide.
+using HeadTile32 = HeadTile<1, 8, 2, 1, 4, 4>;
+using HeadTile64 = HeadTile<2, 4, 2, 2, 3, 3>;
+using HeadTile32F = HeadTile<1, 8, 2, 1, 4, 4, 4>;      // fp32 rows as they are
+using HeadTile64F = HeadTile<2, 4, 2, 2, 3, 3, 4>;
 using HeadTile128 = HeadTile<2, 4, 4, 4, 4, 3>;
 using HeadTile256 = HeadTile<4, 2, 4, 8, 3, 2>;
+using HeadRows32 = HeadTile<1, 8, 2, 2, 4, 4>;
+using HeadRows64 = HeadTile<2, 4, 2, 4, 4, 4>;
+constexpr int kHeadDirectRows = 64;
 constexpr int kHeadCols = 256;
 constexpr int64_t kHeadMostRows = (int64_t)1 << 22, kHeadMostVocab = ((int64_t)1 << 31) - 1024;
 constexpr int kHeadMostTop = 1024;
@@ -22,13 +29,21 @@ template <typename F> int by_head_tile(int rows, F&& f) {
     default: return f(HeadTile256{});
     }
 }
+template <typename F> int by_head_rows(int rows, F&& f) {
+    switch (rows) {
+    case 32: return f(HeadRows32{});
+    case 64: return f(HeadRows64{});
+    case 128: return f(HeadTile128{});
+    default: return f(HeadTile256{});
+    }
+}
 
 struct HeadShape {
     int dtype;
     int64_t T, d, V, K;
     int64_t dp() const { return (d + 7) / 8 * 8; }                      // elements of a padded row of 16-bit values
     int planes() const { return dtype == TIDE_F32 ? 2 : 1; }
-    bool copied() const { return dtype == TIDE_F32 || d % 8 != 0; }     // the products read copies of x and W
+    bool copied(bool grads) const { return direct(grads) ? false : dtype == TIDE_F32 || d % 8 != 0; }     // the products read copies of x and W
     int64_t plane_bytes(int64_t rows) const { return rows * dp() * 2; }
     int rows_per_tile() const {
         if (T <= 32) return 32;
@@ -39,7 +54,18 @@ struct HeadShape {
     }
     int64_t row_tiles() const { return (T + rows_per_tile() - 1) / rows_per_tile(); }
     int64_t col_tiles() const { return (V + kHeadCols - 1) / kHeadCols; }
-    int64_t parts() const { return col_tiles() * (rows_per_tile() == 32 ? 8 : rows_per_tile() == 256 ? 2 : 4); }
+    // Columns of a tile of the statistics.  Few rows: as many tiles as the narrowest multiple of the CUs that holds them, so that each CU reads as much of W
+    // (bf16, d = 4096, V = 128000: 1000 tiles of 128 columns 186 us / 1024 of 125 180; fp32, T = 17, d = 768, V = 32003: 251 of 128 32.0 / 256 of 126 31.1).
+    int pitch(unsigned cus) const {
+        const int rows = rows_per_tile();
+        if (rows > 64) return kHeadCols;
+        const int64_t tiles = ((V + HeadTile32::kP - 1) / HeadTile32::kP + cus - 1) / cus * cus;
+        return (int)((V + tiles - 1) / tiles);
+    }
+    int64_t parts(unsigned cus) const { return (V + pitch(cus) - 1) / pitch(cus) * (rows_per_tile() == 256 ? HeadTile256::kParts : 1); }
+    static_assert(HeadTile32::kP == HeadTile64::kP && HeadTile32::kP == HeadTile32F::kP && HeadTile32::kP == HeadTile64F::kP && HeadTile128::kParts == 1, "");
+    // fp32 rows without planes: the forward call on few rows, which is bound by reading W once
+    bool direct(bool grads) const { return dtype == TIDE_F32 && !grads && T <= kHeadDirectRows && d % 4 == 0; }
     // columns of a piece of the vocabulary in the gradient: equal pieces whose G is at most kHeadPieceBytes
     int64_t piece() const {
         const int64_t tiles = std::max<int64_t>(1, (int64_t)(kHeadPieceBytes / ((size_t)std::max<int64_t>(T, 1) * planes() * 2 * kHeadCols)));
@@ -80,14 +106,14 @@ size_t head_layout(const HeadShape& s, bool grads, unsigned cus, void* base, Hea
     HeadSpace sp{(char*)base};
     HeadWork w{};
     w.ctl = sp.take<HeadCtl>(1);
-    if (s.dtype == TIDE_F32) {
+    if (s.dtype == TIDE_F32 && !s.direct(grads)) {
         w.x_max = sp.take<uint32_t>(kHeadMaxBlocks);
         w.w_max = sp.take<uint32_t>(kHeadMaxBlocks);
     }
-    if (s.copied()) w.w = sp.take<char>((size_t)s.plane_bytes(s.V) * s.planes());
-    if (s.copied() || grads) w.x = sp.take<char>((size_t)s.plane_bytes(s.T) * s.planes());
+    if (s.copied(grads)) w.w = sp.take<char>((size_t)s.plane_bytes(s.V) * s.planes());
+    if (s.copied(grads) || grads) w.x = sp.take<char>((size_t)s.plane_bytes(s.T) * s.planes());
     if (!grads) {
-        w.part = sp.take<float2>((size_t)s.parts() * s.T);
+        w.part = sp.take<float2>((size_t)s.parts(cus) * s.T);
         if (!s.K) w.z = sp.take<float>((size_t)s.T);
     } else {
         w.source = sp.take<int32_t>((size_t)s.T);
@@ -114,7 +140,8 @@ template <int DT, int OutDT, int kMode, class Tile> int launch_head(int64_t q_ro
                                      Tile::kLdsBytes));
         raised[dev].store(true, std::memory_order_relaxed);
     }
-    const int64_t tq = (q_rows + Tile::kQ - 1) / Tile::kQ, tp = (p_rows + Tile::kP - 1) / Tile::kP;
+    if (!p.pitch) p.pitch = Tile::kP;
+    const int64_t tq = (q_rows + Tile::kQ - 1) / Tile::kQ, tp = (p_rows + p.pitch - 1) / p.pitch;
     p.tiles_q = (int)tq;
     p.tiles_p = (int)tp;
     if (tq * tp == 0) return TIDE_OK;
@@ -197,7 +224,7 @@ template <int DT> void head_copy(const HeadShape& s, const void* rows, int64_t s
 // x or W as an operand: the caller's rows, or the copy's planes of n rows.
 HeadOperand head_operand(const HeadShape& s, const void* rows, int64_t stride, const char* copy, int64_t n) {
     if (copy) return HeadOperand{{copy, copy + (s.planes() - 1) * s.plane_bytes(n)}, s.dp() * 2};
-    return HeadOperand{{(const char*)rows, (const char*)rows}, stride * 2};
+    return HeadOperand{{(const char*)rows, (const char*)rows}, stride * (int64_t)elem_bytes(s.dtype)};
 }
 
 int head_forward(const HeadCall& c) {
@@ -210,8 +237,9 @@ int head_forward(const HeadCall& c) {
     if ((rc = head_space(c, false, cus, &w))) return rc;
     rc = by_dtype(s.dtype, [&](auto dt) -> int {
         constexpr int DT = decltype(dt)::value;
-        HeadCtlParams cp{};
-        if constexpr (DT == kF32) {
+        const bool direct = s.direct(false);
+        if (DT == kF32 && !direct) {
+            HeadCtlParams cp{};
             cp.ctl = w.ctl;
             cp.x_max = w.x_max;
             cp.w_max = w.w_max;
@@ -219,7 +247,7 @@ int head_forward(const HeadCall& c) {
             head_max<DT>(c.W, c.w_stride, s.V, s.d, w.w_max, &cp.w_blocks, c.st);
             hipLaunchKernelGGL(tide_head_ctl_kernel, dim3(1), dim3(kHeadCtlThreads), 0, c.st, cp);
         }
-        if (s.copied()) {
+        if (s.copied(false)) {
             head_copy<DT>(s, c.x, c.x_stride, s.T, nullptr, w.ctl, 0, w.x, c.st);
             head_copy<DT>(s, c.W, c.w_stride, s.V, nullptr, w.ctl, 1, w.w, c.st);
         }
@@ -228,21 +256,28 @@ int head_forward(const HeadCall& c) {
         p.p = head_operand(s, c.W, c.w_stride, w.w, s.V);
         p.q_rows = (int)s.T;
         p.p_rows = (int)s.V;
-        p.k = s.copied() ? (int)s.dp() : (int)s.d;
-        p.segments = DT == kF32 ? 3 : 1;
+        p.k = s.copied(false) ? (int)s.dp() : (int)s.d;
+        p.segments = DT == kF32 && !direct ? 3 : 1;
         p.k_slices = 1;
-        p.ctl = DT == kF32 ? w.ctl : nullptr;
+        p.ctl = DT == kF32 && !direct ? w.ctl : nullptr;
         p.c1 = 1.4426950408889634f / c.tau;
         p.ids = c.ids;
         p.K = s.K ? (int)s.K : 1;
         p.V = (int)s.V;
         p.part = w.part;
+        p.pitch = s.pitch(cus);
         p.z_out = s.K ? c.z : w.z;
-        const int rc2 = by_head_tile(s.rows_per_tile(), [&](auto tile) { return launch_head<kHeadElem<DT>, DT, kHeadStats, decltype(tile)>(s.T, s.V, c.st, p); });
+        int rc2 = TIDE_OK;
+        if (direct) {
+            if constexpr (DT == kF32)
+                rc2 = s.T <= 32 ? launch_head<kF32, kF32, kHeadStats, HeadTile32F>(s.T, s.V, c.st, p) : launch_head<kF32, kF32, kHeadStats, HeadTile64F>(s.T, s.V, c.st, p);
+        } else {
+            rc2 = by_head_tile(s.rows_per_tile(), [&](auto tile) { return launch_head<kHeadElem<DT>, DT, kHeadStats, decltype(tile)>(s.T, s.V, c.st, p); });
+        }
         if (rc2) return rc2;
         HeadFinishParams f{};
         f.part = w.part;
-        f.parts = (int)s.parts();
+        f.parts = (int)s.parts(cus);
         f.T = (int)s.T;
         f.K = p.K;
         f.V = (int)s.V;
@@ -295,7 +330,7 @@ int head_backward(const HeadCall& c) {
         cp.row_const = w.row_const;
         hipLaunchKernelGGL(tide_head_ctl_kernel, dim3(1), dim3(kHeadCtlThreads), 0, c.st, cp);
         head_copy<DT>(s, c.x, c.x_stride, s.T, w.source, w.ctl, 0, w.x, c.st);
-        if (s.copied()) head_copy<DT>(s, c.W, c.w_stride, s.V, nullptr, w.ctl, 1, w.w, c.st);
+        if (s.copied(true)) head_copy<DT>(s, c.W, c.w_stride, s.V, nullptr, w.ctl, 1, w.w, c.st);
         const HeadOperand x = head_operand(s, nullptr, 0, w.x, s.T), W = head_operand(s, c.W, c.w_stride, w.w, s.V);
         const int64_t piece = s.piece(), g_plane = s.T * piece * 2;
         const HeadOperand g{{w.g, w.g + (s.planes() - 1) * g_plane}, piece * 2};
@@ -341,7 +376,7 @@ int head_backward(const HeadCall& c) {
                 a.acc_slice = s.T * s.dp();
                 a.acc_ld = (int)s.dp();
                 a.accumulate = v0 != 0;
-                rc2 = by_head_tile(s.rows_per_tile(), [&](auto tile) { return launch_head<E, E, kHeadRows, decltype(tile)>(s.T, s.dp(), c.st, a); });
+                rc2 = by_head_rows(s.rows_per_tile(), [&](auto tile) { return launch_head<E, E, kHeadRows, decltype(tile)>(s.T, s.dp(), c.st, a); });
                 if (rc2) return rc2;
             }
             if (c.dW) {
