@@ -100,7 +100,7 @@ constexpr uint32_t kHeadNowhere = 0x80000000u;       // an offset at the descrip
 
 // 64 lanes x 16 bytes from memory (offsets voff from the descriptor's base) to 1 KiB of LDS at byte `lds`.
 __device__ __forceinline__ void head_dma(uint32_t lds, uint32_t voff, u32x4 rsrc) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(voff), "s"(rsrc) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(voff), "s"(rsrc) : "memory");
 }
 template <int n> __device__ __forceinline__ void head_wait_vm() { asm volatile("s_waitcnt vmcnt(%0)" ::"i"(n) : "memory"); }
 
@@ -108,7 +108,7 @@ template <int n> __device__ __forceinline__ void head_wait_vm() { asm volatile("
 template <int kRows, bool kAcross, int kWaves, int kEB = 2> struct HeadFeed {
     static constexpr int kK = kHeadRowBytes / kEB, kBytes = kRows * kHeadRowBytes, kInstr = kBytes / 1024, kN = (kInstr + kWaves - 1) / kWaves;
     uint32_t voff[kN];
-    int along[kN];             // first k element of this lane's chunk within a stage (along), or its k row (across)
+    int along;                 // first k element of this lane's chunks within a stage (along), or the first one's k row (across)
     const char* base;
     int64_t step;
     int issued, kk, fill;      // stages issued, the next one's number within its segment, its slot's byte
@@ -128,11 +128,11 @@ template <int kRows, bool kAcross, int kWaves, int kEB = 2> struct HeadFeed {
             if constexpr (!kAcross) {
                 const int r = 8 * n + (lane >> 3), c = place_along(r, lane & 7);
                 voff[i] = row0 + r < rows ? (uint32_t)r * (uint32_t)o.row_bytes + c * 16 : kHeadNowhere;
-                along[i] = c * (16 / kEB);
+                if (i == 0) along = c * (16 / kEB);        // (the same for all: their rows differ by multiples of 16)
             } else {
                 const int byte = n * 1024 + lane * 16, kr = byte / (kRows * 2), c = place_across(kr, byte % (kRows * 2) >> 4);
                 voff[i] = row0 + c * 8 < rows ? (uint32_t)kr * (uint32_t)o.row_bytes + c * 16 : kHeadNowhere;
-                along[i] = kr;
+                if (i == 0) along = kr;
             }
         }
         step = kAcross ? kK * o.row_bytes : kHeadRowBytes;
@@ -150,14 +150,13 @@ template <int kRows, bool kAcross, int kWaves, int kEB = 2> struct HeadFeed {
         u32x4 rsrc;
         rsrc[0] = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)base);
         rsrc[1] = __builtin_amdgcn_readfirstlane((uint32_t)((uintptr_t)base >> 32) & 0xffffu);
-        rsrc[2] = left > 0 ? kHeadNowhere : 0u;
+        rsrc[2] = __builtin_amdgcn_readfirstlane(left > 0 ? kHeadNowhere : 0u);
         rsrc[3] = 0x00020000u;
 #pragma unroll
         for (int i = 0; i < kN; ++i) {
             if (kInstr % kWaves != 0 && wave + kWaves * i >= kInstr) break;
-            uint32_t v = voff[i];
-            if (left < kK) v = along[i] < left ? v : kHeadNowhere;
-            head_dma(lds + fill + (wave + kWaves * i) * 1024, v, rsrc);
+            const int at = kAcross ? along + kWaves * i * (1024 / (kRows * 2)) : along;
+            head_dma(lds + fill + (wave + kWaves * i) * 1024, at < left ? voff[i] : kHeadNowhere, rsrc);
         }
         base += step;
         fill = fill + kBytes == kSlots * kBytes ? 0 : fill + kBytes;
@@ -267,7 +266,7 @@ __global__ __launch_bounds__(Tile::kThreads) void tide_head_gemm_kernel(const He
     const int wq = wave % Tile::kWQ, wp = wave / Tile::kWQ;
     int tq, tp;
     if (!head_tile(blockIdx.x, p.tiles_q, p.tiles_p, tq, tp)) return;
-    const int live = kMode == kHeadStats ? 0 : p.ctl->live;
+    const int live = kMode == kHeadStats ? 0 : __builtin_amdgcn_readfirstlane(p.ctl->live);
     const int q_rows = kMode == kHeadGrad || kMode == kHeadRows ? live : p.q_rows;
     const int k_elems = kMode == kHeadWeights ? live : p.k;
     const int q0 = tq * Tile::kQ, p0 = tp * p.pitch, p_end = min(p.p_rows, p0 + p.pitch);

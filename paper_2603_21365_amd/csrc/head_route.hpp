@@ -12,6 +12,7 @@ using HeadTile64 = HeadTile<2, 4, 2, 2, 3, 3>;
 using HeadTile32F = HeadTile<1, 8, 2, 1, 4, 4, 4>;      // fp32 rows as they are
 using HeadTile64F = HeadTile<2, 4, 2, 2, 3, 3, 4>;
 using HeadTile128 = HeadTile<2, 4, 4, 4, 4, 3>;
+using HeadTile192 = HeadTile<4, 2, 3, 8, 3, 2>;
 using HeadTile256 = HeadTile<4, 2, 4, 8, 3, 2>;
 using HeadRows32 = HeadTile<1, 8, 2, 2, 4, 4>;
 using HeadRows64 = HeadTile<2, 4, 2, 4, 4, 4>;
@@ -19,13 +20,14 @@ constexpr int kHeadDirectRows = 64;
 constexpr int kHeadCols = 256;
 constexpr int64_t kHeadMostRows = (int64_t)1 << 22, kHeadMostVocab = ((int64_t)1 << 31) - 1024;
 constexpr int kHeadMostTop = 1024;
-constexpr size_t kHeadPieceBytes = (size_t)256 << 20;      // G of a piece of the vocabulary: as much as stays in the last-level cache
+constexpr size_t kHeadPieceBytes = (size_t)256 << 20;      // G of a piece of the vocabulary: as much as stays in the last-level cache (256 MiB to 4 GiB: no difference)
 
 template <typename F> int by_head_tile(int rows, F&& f) {
     switch (rows) {
     case 32: return f(HeadTile32{});
     case 64: return f(HeadTile64{});
     case 128: return f(HeadTile128{});
+    case 192: return f(HeadTile192{});
     default: return f(HeadTile256{});
     }
 }
@@ -34,6 +36,7 @@ template <typename F> int by_head_rows(int rows, F&& f) {
     case 32: return f(HeadRows32{});
     case 64: return f(HeadRows64{});
     case 128: return f(HeadTile128{});
+    case 192: return f(HeadTile192{});
     default: return f(HeadTile256{});
     }
 }
@@ -48,9 +51,12 @@ struct HeadShape {
     int rows_per_tile() const {
         if (T <= 32) return 32;
         if (T <= 64) return 64;
-        // 128-row tiles need a third more time per row; what a last, partly filled tile wastes decides
-        const int64_t small = (T + 127) / 128 * 128, large = (T + 255) / 256 * 256;
-        return 4 * small < 3 * large || T <= 128 ? 128 : 256;
+        // A tile of 128 / 192 rows takes 60 / 80 % of the time of one of 256 (d = 4096, V = 65536, us a tile row: 66-108); the least of those decides
+        int best = 256;
+        int64_t least = (T + 255) / 256 * 100;
+        if ((T + 191) / 192 * 80 < least) best = 192, least = (T + 191) / 192 * 80;
+        if ((T + 127) / 128 * 60 < least) best = 128;
+        return best;
     }
     int64_t row_tiles() const { return (T + rows_per_tile() - 1) / rows_per_tile(); }
     int64_t col_tiles() const { return (V + kHeadCols - 1) / kHeadCols; }
@@ -62,8 +68,8 @@ struct HeadShape {
         const int64_t tiles = ((V + HeadTile32::kP - 1) / HeadTile32::kP + cus - 1) / cus * cus;
         return (int)((V + tiles - 1) / tiles);
     }
-    int64_t parts(unsigned cus) const { return (V + pitch(cus) - 1) / pitch(cus) * (rows_per_tile() == 256 ? HeadTile256::kParts : 1); }
-    static_assert(HeadTile32::kP == HeadTile64::kP && HeadTile32::kP == HeadTile32F::kP && HeadTile32::kP == HeadTile64F::kP && HeadTile128::kParts == 1, "");
+    int64_t parts(unsigned cus) const { return (V + pitch(cus) - 1) / pitch(cus) * (rows_per_tile() >= 192 ? HeadTile256::kParts : 1); }
+    static_assert(HeadTile32::kP == HeadTile64::kP && HeadTile32::kP == HeadTile32F::kP && HeadTile32::kP == HeadTile64F::kP && HeadTile128::kParts == 1 && HeadTile192::kParts == HeadTile256::kParts, "");
     // fp32 rows without planes: the forward call on few rows, which is bound by reading W once
     bool direct(bool grads) const { return dtype == TIDE_F32 && !grads && T <= kHeadDirectRows && d % 4 == 0; }
     // columns of a piece of the vocabulary in the gradient: equal pieces whose G is at most kHeadPieceBytes
@@ -212,13 +218,16 @@ int head_space(const HeadCall& c, bool grads, unsigned cus, HeadWork* w) {
     return TIDE_OK;
 }
 
+// Rows per workgroup of the copies: 2048 chunks of eight elements, eight a thread.
+int64_t head_copy_rows(int64_t chunks) { return std::max<int64_t>(1, 8 * kHeadRowThreads / chunks); }
 template <int DT> void head_max(const void* rows, int64_t stride, int64_t n, int64_t d, uint32_t* out, int* blocks, hipStream_t st) {
     *blocks = (int)std::min<int64_t>(n, kHeadMaxBlocks);
     if (*blocks) hipLaunchKernelGGL(tide_head_max_kernel, dim3(*blocks), dim3(kHeadRowThreads), 0, st, (const char*)rows, stride * 4, n, (int)d, out);
 }
 template <int DT> void head_copy(const HeadShape& s, const void* rows, int64_t stride, int64_t n, const int32_t* source, const HeadCtl* ctl, int weights, char* out, hipStream_t st) {
     if (n == 0) return;
-    hipLaunchKernelGGL((tide_head_copy_kernel<DT>), dim3((unsigned)std::min<int64_t>(n, 4096)), dim3(kHeadRowThreads), 0, st, (const char*)rows, stride * Storage<DT>::kBytes, n,
+    const int64_t rows_each = head_copy_rows(s.dp() / 8);
+    hipLaunchKernelGGL((tide_head_copy_kernel<DT>), dim3((unsigned)((n + rows_each - 1) / rows_each)), dim3(kHeadRowThreads), 0, st, (const char*)rows, stride * Storage<DT>::kBytes, n, (int)rows_each,
                        (int)s.d, source, ctl, weights, out, s.dp() * 2, s.plane_bytes(n));
 }
 // x or W as an operand: the caller's rows, or the copy's planes of n rows.

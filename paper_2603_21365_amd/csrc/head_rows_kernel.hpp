@@ -11,7 +11,7 @@ namespace tide {
 
 constexpr int kHeadRowThreads = 256;
 constexpr int kHeadCtlThreads = 1024;
-constexpr int kHeadMaxBlocks = 512;        // workgroups that search for the largest magnitude
+constexpr int kHeadMaxBlocks = 2048;       // workgroups that search for the largest magnitude
 
 template <int DT> __device__ __forceinline__ float head_load(const char* row, int i) {
     if constexpr (DT == kF32) return reinterpret_cast<const float*>(row)[i];
@@ -31,16 +31,22 @@ __global__ __launch_bounds__(kHeadRowThreads) void tide_head_max_kernel(const ch
     uint32_t m = 0;
     const bool chunks = ((uintptr_t)rows | (uintptr_t)row_bytes) % 16 == 0 && d % 4 == 0;
     auto take = [&](uint32_t b) { b &= 0x7fffffffu; m = b < 0x7f800000u && b > m ? b : m; };
-    for (int64_t r = blockIdx.x; r < n_rows; r += gridDim.x) {
-        const char* row = rows + r * row_bytes;
-        if (chunks) {
-            for (int i = threadIdx.x; i < d / 4; i += kHeadRowThreads) {
-                const u32x4 v = reinterpret_cast<const u32x4*>(row)[i];
-                take(v[0]), take(v[1]), take(v[2]), take(v[3]);
+    if (chunks) {                                      // contiguous rows as one, four chunks a thread at a time
+        const bool flat = row_bytes == (int64_t)d * 4;
+        const int64_t n = flat ? 1 : n_rows, per_row = flat ? n_rows * (d / 4) : d / 4, step = (int64_t)gridDim.x * kHeadRowThreads;
+        for (int64_t r = 0; r < n; ++r) {
+            const u32x4* row = reinterpret_cast<const u32x4*>(rows + r * row_bytes);
+            for (int64_t i = (int64_t)blockIdx.x * kHeadRowThreads + threadIdx.x; i < per_row; i += 4 * step) {
+                u32x4 v[4];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) v[u] = row[min(i + u * step, per_row - 1)];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) take(v[u][0]), take(v[u][1]), take(v[u][2]), take(v[u][3]);
             }
-        } else {
-            for (int i = threadIdx.x; i < d; i += kHeadRowThreads) take(reinterpret_cast<const uint32_t*>(row)[i]);
         }
+    } else {
+        for (int64_t r = blockIdx.x; r < n_rows; r += gridDim.x)
+            for (int i = threadIdx.x; i < d; i += kHeadRowThreads) take(reinterpret_cast<const uint32_t*>(rows + r * row_bytes)[i]);
     }
 #pragma unroll
     for (int s = 1; s < kWave; s <<= 1) m = max(m, (uint32_t)__shfl_xor((int)m, s, kWave));
@@ -137,40 +143,57 @@ __global__ __launch_bounds__(kHeadCtlThreads) void tide_head_ctl_kernel(const He
 }
 
 // Rows into the form the products read: gathered (source != null), padded with zeros to whole 16-byte chunks, fp32 ones as two fp16 planes.
-// A workgroup per row in turn.
+// A workgroup has rows_each rows, taken as one list of chunks, four a thread at a time.
 template <int DT>
-__global__ __launch_bounds__(kHeadRowThreads) void tide_head_copy_kernel(const char* rows, int64_t row_bytes, int64_t n_rows, int d, const int32_t* source,
+__global__ __launch_bounds__(kHeadRowThreads) void tide_head_copy_kernel(const char* rows, int64_t row_bytes, int64_t n_rows, int rows_each, int d, const int32_t* source,
                                                                          const HeadCtl* ctl, int weights, char* out, int64_t out_row_bytes, int64_t plane_bytes) {
-    const int64_t n = source ? ctl->live : n_rows;
+    const int64_t n = source ? ctl->live : n_rows, r0 = (int64_t)blockIdx.x * rows_each;
+    if (r0 >= n) return;
     const float scale = DT == kF32 ? (weights ? ctl->w_scale : ctl->x_scale) : 1.0f;
     const bool chunks = ((uintptr_t)rows | (uintptr_t)row_bytes) % 16 == 0 && d % 8 == 0;
-    for (int64_t r = blockIdx.x; r < n; r += gridDim.x) {
-        const char* row = rows + (source ? (int64_t)source[r] : r) * row_bytes;
-        char* to = out + r * out_row_bytes;
-        for (int c = threadIdx.x; c < (int)(out_row_bytes / 16); c += kHeadRowThreads) {
-            if constexpr (DT != kF32) {
-                u32x4 v;
-                if (chunks) {
-                    v = reinterpret_cast<const u32x4*>(row)[c];
-                } else {
-                    const uint16_t* e = reinterpret_cast<const uint16_t*>(row) + 8 * c;
+    const int per_row = (int)(out_row_bytes / 16), total = (int)min((int64_t)rows_each, n - r0) * per_row;
+    constexpr int kU = 4, kW = DT == kF32 ? 2 : 1;     // 16-byte pieces of a chunk's source
+    for (int i0 = threadIdx.x; i0 < total; i0 += kU * kHeadRowThreads) {
+        u32x4 v[kU][kW];
+        int64_t r[kU];
+        int c[kU];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const uint32_t lo = 8 * c + 2 * i < d ? e[2 * i] : 0, hi = 8 * c + 2 * i + 1 < d ? e[2 * i + 1] : 0;
-                        v[i] = lo | hi << 16;
-                    }
+        for (int u = 0; u < kU; ++u) {
+            const int i = min(i0 + u * kHeadRowThreads, total - 1), q = i / per_row;
+            r[u] = r0 + q;
+            c[u] = i - q * per_row;
+            const char* row = rows + (source ? (int64_t)source[r[u]] : r[u]) * row_bytes;
+            if (chunks) {
+#pragma unroll
+                for (int w = 0; w < kW; ++w) v[u][w] = reinterpret_cast<const u32x4*>(row)[c[u] * kW + w];
+            } else if constexpr (DT == kF32) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[u][e / 4][e & 3] = 8 * c[u] + e < d ? reinterpret_cast<const uint32_t*>(row)[8 * c[u] + e] : 0u;
+            } else {
+                const uint16_t* e = reinterpret_cast<const uint16_t*>(row) + 8 * c[u];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const uint32_t lo = 8 * c[u] + 2 * k < d ? e[2 * k] : 0, hi = 8 * c[u] + 2 * k + 1 < d ? e[2 * k + 1] : 0;
+                    v[u][0][k] = lo | hi << 16;
                 }
-                reinterpret_cast<u32x4*>(to)[c] = v;
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kU; ++u) {
+            if (i0 + u * kHeadRowThreads >= total) break;
+            char* to = out + r[u] * out_row_bytes;
+            if constexpr (DT != kF32) {
+                reinterpret_cast<u32x4*>(to)[c[u]] = v[u][0];
             } else {
                 f16x8 hi, lo;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float v = 8 * c + i < d ? reinterpret_cast<const float*>(row)[8 * c + i] * scale : 0.0f;
-                    hi[i] = static_cast<_Float16>(v);
-                    lo[i] = static_cast<_Float16>(v - (float)hi[i]);       // the difference is exact
+                for (int e = 0; e < 8; ++e) {
+                    const float x = __uint_as_float(v[u][e / 4][e & 3]) * scale;
+                    hi[e] = static_cast<_Float16>(x);
+                    lo[e] = static_cast<_Float16>(x - (float)hi[e]);       // the difference is exact
                 }
-                reinterpret_cast<u32x4*>(to)[c] = __builtin_bit_cast(u32x4, hi);
-                reinterpret_cast<u32x4*>(to + plane_bytes)[c] = __builtin_bit_cast(u32x4, lo);
+                reinterpret_cast<u32x4*>(to)[c[u]] = __builtin_bit_cast(u32x4, hi);
+                reinterpret_cast<u32x4*>(to + plane_bytes)[c[u]] = __builtin_bit_cast(u32x4, lo);
             }
         }
     }
@@ -236,9 +259,12 @@ __global__ __launch_bounds__(1024) void tide_head_finish_kernel(const HeadFinish
         m = top;
     };
     if (t < p.T)
-        for (int i = slice; i < p.parts; i += 64) {
-            const float2 v = p.part[(int64_t)i * p.T + t];
-            join(m, s, v.x, v.y);
+        for (int i = slice; i < p.parts; i += 8 * 64) {        // eight loads at a time
+            float2 v[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) v[u] = i + u * 64 < p.parts ? p.part[(int64_t)(i + u * 64) * p.T + t] : float2{-INFINITY, 0.0f};
+#pragma unroll
+            for (int u = 0; u < 8; ++u) join(m, s, v[u].x, v[u].y);
         }
     part[slice][r] = float2{m, s};
     __syncthreads();
