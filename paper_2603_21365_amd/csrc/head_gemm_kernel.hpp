@@ -57,17 +57,16 @@ struct HeadGemmParams {
     HeadOperand q, p;
     int q_rows, p_rows, k;     // of these the one that counts live rows is replaced by ctl->live
     int segments;              // 1, or 3 for two planes
-    int tiles_q, tiles_p, k_slices;
+    int tiles_p, k_slices;
     int pitch;                 // columns of a tile: kP, or fewer (statistics) where that gives every CU as many
     const HeadCtl* ctl;        // null where nothing is scaled and every row counts (16-bit statistics)
     // statistics and G
     float c1;                  // log2(e) / tau
     const int32_t* ids;        // [T][K] the tokens' own entries of the vocabulary; others than 0 .. V - 1: none
-    const int32_t* source;     // G: the token of each row
     int K, V, v0;              // p row 0 is token v0
     float2* part;              // statistics: [tiles_p * kWP][q_rows]
     float* z_out;              // statistics: [q_rows][K]
-    const float2* row_const;   // G: (lse * log2 e, scale) of each row
+    const float4* row_const;   // G: lse * log2 e, scale, and as an integer the target (wanted == null) or the token, of each row
     const float* wanted;       // G: [T][K] or null (one)
     char* g_out;               // G
     int64_t g_row_bytes, g_plane_bytes;
@@ -89,10 +88,10 @@ template <int WQ, int WP, int BQ, int BP, int SQ, int SP, int EB = 2> struct Hea
     static constexpr int kQ = WQ * BQ * 16, kP = WP * BP * 16;
     static constexpr int kQBytes = kQ * kHeadRowBytes, kPBytes = kP * kHeadRowBytes, kRingBytes = SQ * kQBytes + SP * kPBytes;
     static constexpr int kCols = BP * 16, kLd = kCols + 4;       // a wave's columns; its rows in LDS after the loop, padded against bank conflicts
-    static constexpr int kEpiBytes = kWaves * 16 * kLd * 4;
+    static constexpr int kStageBytes = kWaves * 16 * kLd * 4;    // 16 rows of every wave
     static constexpr bool kJoined = WP > 2;                      // the statistics of a tile's columns leave as one
     static constexpr int kParts = kJoined ? 1 : WP, kJoinBytes = kJoined ? WP * kQ * 8 : 0;
-    static constexpr int kLdsBytes = kRingBytes > kEpiBytes + kJoinBytes ? kRingBytes : kEpiBytes + kJoinBytes;
+    static constexpr int kLdsBytes = kRingBytes > kStageBytes + kJoinBytes ? kRingBytes : kStageBytes + kJoinBytes;
     static_assert(kWaves == 8 && SP >= 2 && SQ >= SP, "two groups of four waves");
     static_assert(kLdsBytes <= 160 * 1024, "LDS of a CU");
 };
@@ -183,6 +182,12 @@ template <int DT> __device__ __forceinline__ uint32_t head_round2(float a, float
     }
 }
 
+template <int DT> __device__ __forceinline__ void head_put(char* row, int i, float v) {
+    if constexpr (DT == kF32) reinterpret_cast<float*>(row)[i] = v;
+    else if constexpr (DT == kF16) reinterpret_cast<_Float16*>(row)[i] = static_cast<_Float16>(v);
+    else reinterpret_cast<__bf16*>(row)[i] = static_cast<__bf16>(v);
+}
+
 // The fragment of block b (16 tile rows) and k group g (32 elements) of an operand at `at`: lane l gets row l % 16, the 8 k values of quarter l / 16.
 template <int kRows, bool kAcross> __device__ __forceinline__ u32x4 head_fragment(head_lds* at, int b, int g, int lane) {
     typedef HeadFeed<kRows, kAcross, 8> Feed;
@@ -244,64 +249,82 @@ template <int DT> __device__ __forceinline__ f32x4 head_mma(const HeadSplit& a, 
     return head_mma<kBF16>(a.hi, b.hi, acc);
 }
 
-// Tile `id` of tiles_q x tiles_p: every XCD (workgroup id mod 8) takes a contiguous eighth of a list that goes through groups of 8 row tiles column by
-// column, so that the 32 tiles an XCD works on at a time share 8 row tiles and 4 column tiles in its L2.
-__device__ __forceinline__ bool head_tile(int id, int tiles_q, int tiles_p, int& tq, int& tp) {
-    const int total = tiles_q * tiles_p, per_xcd = (total + 7) >> 3;
-    const int t = (id & 7) * per_xcd + (id >> 3);
-    if ((id >> 3) >= per_xcd || t >= total) return false;
+// Item `at` of the eighth of the work that XCD `xcd` (workgroup id mod 8) has: the work is a list of k_slices x tiles_q x tiles_p tiles that goes through groups
+// of 8 row tiles column by column, so that the 32 tiles an XCD works on at a time share 8 row tiles and 4 column tiles in its L2.
+__device__ __forceinline__ bool head_item(int xcd, int at, int tiles_q, int tiles_p, int k_slices, int& tq, int& tp, int& slice) {
+    const int tiles = tiles_q * tiles_p, total = tiles * k_slices, per_xcd = (total + 7) >> 3;
+    int t = xcd * per_xcd + at;
+    if (at >= per_xcd || t >= total) return false;
+    slice = t / tiles;
+    t -= slice * tiles;
     const int group = t / (8 * tiles_p), q0 = group * 8, nq = min(8, tiles_q - q0), in = t - q0 * tiles_p;
     tp = in / nq;
     tq = q0 + (in - tp * nq);
     return true;
 }
 
-// DT: the operands' element type, kF16 or kBF16 (kF32: fp32 rows as they are, statistics of few rows only).  OutDT: the type dW is written in.  grid = (8 * ceil(tiles / 8), k_slices).
+// Two blocks of 16 x 16 in 16 bits, as the matrix steps leave them (lane quarter h: columns 4 h .. 4 h + 3 of a row of each), exchanged so that a lane has eight
+// consecutive columns: 8 h .. 8 h + 7 of the 32.
+__device__ __forceinline__ u32x4 head_gather8(uint32_t a0, uint32_t a1, uint32_t b0, uint32_t b1) {
+    asm("s_nop 1\n\tv_permlane32_swap_b32 %0, %1\n\tv_permlane32_swap_b32 %2, %3\n\ts_nop 1\n\tv_permlane16_swap_b32 %0, %1\n\tv_permlane16_swap_b32 %2, %3"
+        : "+v"(a0), "+v"(b0), "+v"(a1), "+v"(b1));
+    return u32x4{a0, a1, b0, b1};
+}
+
+// DT: the operands' element type, kF16 or kBF16 (kF32: fp32 rows as they are, statistics of few rows only).  OutDT: the type dW is written in.
+// dx and dW: a workgroup per CU, which goes through its share of the tiles and requests the first stages of the next one before it deals with the results of
+// the last (dW of 290 live rows, d = 4096, V = 128000: 627 / 596 us).  The others: a workgroup per tile; their results need LDS and loads, and gathering them in
+// registers with the next stages under way is 3 to 6 % slower.
+template <int kMode, class Tile> constexpr bool kLoops = Tile::kTurns && (kMode == kHeadRows || kMode == kHeadWeights);
 template <int DT, int OutDT, int kMode, class Tile>
 __global__ __launch_bounds__(Tile::kThreads) void tide_head_gemm_kernel(const HeadGemmParams p) {
     constexpr bool kQAcross = kMode == kHeadWeights, kPAcross = kMode == kHeadRows || kMode == kHeadWeights;
-    constexpr int kBQ = Tile::kBQ, kBP = Tile::kBP, kCols = Tile::kCols, kLd = Tile::kLd;
-    extern __shared__ __attribute__((aligned(16))) char smem[];
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-    const int wq = wave % Tile::kWQ, wp = wave / Tile::kWQ;
-    int tq, tp;
-    if (!head_tile(blockIdx.x, p.tiles_q, p.tiles_p, tq, tp)) return;
-    const int live = kMode == kHeadStats ? 0 : __builtin_amdgcn_readfirstlane(p.ctl->live);
-    const int q_rows = kMode == kHeadGrad || kMode == kHeadRows ? live : p.q_rows;
-    const int k_elems = kMode == kHeadWeights ? live : p.k;
-    const int q0 = tq * Tile::kQ, p0 = tp * p.pitch, p_end = min(p.p_rows, p0 + p.pitch);
-    if (q0 >= q_rows) return;
-
-    // ---- k loop: n stages, the slice's part of every segment: (hi, hi), (hi, lo), (lo, hi)
-    const int per = (k_elems + Tile::kK - 1) / Tile::kK;
-    const int first = (int)((int64_t)per * blockIdx.y / p.k_slices), last = (int)((int64_t)per * (blockIdx.y + 1) / p.k_slices);
-    const int nk = last - first, n = nk * p.segments;
+    constexpr int kBQ = Tile::kBQ, kBP = Tile::kBP, kCols = Tile::kCols;
     typedef HeadFeed<Tile::kQ, kQAcross, Tile::kWaves, Tile::kEB> FeedQ;
     typedef HeadFeed<Tile::kP, kPAcross, Tile::kWaves, Tile::kEB> FeedP;
     static_assert((DT == kF32) == (Tile::kEB == 4) && (DT != kF32 || kMode == kHeadStats), "");
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int wq = wave % Tile::kWQ, wp = wave / Tile::kWQ;
+    const int live = kMode == kHeadStats ? 0 : __builtin_amdgcn_readfirstlane(p.ctl->live);
+    const int q_rows = kMode == kHeadGrad || kMode == kHeadRows ? live : p.q_rows;
+    const int k_elems = kMode == kHeadWeights ? live : p.k;
+    const int tiles_q = (q_rows + Tile::kQ - 1) / Tile::kQ;
+    const uint32_t lds_q = (uint32_t)(size_t)(head_lds*)smem, lds_p = lds_q + Tile::kSQ * Tile::kQBytes;
+
+    // ---- one tile's k loop: n stages, the slice's part of every segment: (hi, hi), (hi, lo), (lo, hi)
+    int tq, tp, slice, q0, p0, p_end, first, nk, n;
     FeedQ fq;
     FeedP fp;
-    fq.init(p.q, q0, q_rows, first, wave, lane);
-    fp.init(p.p, p0, p_end, first, wave, lane);
-    const uint32_t lds_q = (uint32_t)(size_t)(head_lds*)smem, lds_p = lds_q + Tile::kSQ * Tile::kQBytes;
+    auto set_item = [&] {
+        q0 = tq * Tile::kQ, p0 = tp * p.pitch, p_end = min(p.p_rows, p0 + p.pitch);
+        const int per = (k_elems + Tile::kK - 1) / Tile::kK;
+        first = (int)((int64_t)per * slice / p.k_slices);
+        nk = (int)((int64_t)per * (slice + 1) / p.k_slices) - first;
+        n = nk * p.segments;
+        fq.init(p.q, q0, q_rows, first, wave, lane);
+        fp.init(p.p, p0, p_end, first, wave, lane);
+    };
     // Step s issues stage s + kSP of p, then stage s + kSQ of q.
     auto issue_p = [&] { fp.template issue<Tile::kSP>(lds_p, p.p, 1, p0, n, nk, first, k_elems, wave); };
     auto issue_q = [&] { fq.template issue<Tile::kSQ>(lds_q, p.q, 2, q0, n, nk, first, k_elems, wave); };
-    // Waits until all but the last kSteps steps of this wave's transfers, and the q transfers of the step before those where q is further ahead than
-    // p, have landed.
-    auto landed = [&](auto steps_c) {
-        constexpr int kSteps = decltype(steps_c)::value, kAhead = Tile::kSQ > Tile::kSP ? 1 : 0;
+    auto issue_first = [&] {
+#pragma unroll
+        for (int s = -Tile::kSQ; s < -1; ++s) {
+            if (s + Tile::kSP >= 0) issue_p();
+            issue_q();
+        }
+    };
+    // Waits until all but the last kSP - 2 steps of this wave's transfers, and the q transfers of the step before those where q is further ahead than p,
+    // have landed: the next stage, in the loop.  (Memory operations of the last tile's results that are still outstanding are waited for too.)
+    auto landed = [&] {
+        constexpr int kSteps = Tile::kSP - 2, kAhead = Tile::kSQ > Tile::kSP ? 1 : 0;
         constexpr int kNP = FeedP::kN, kNQ = FeedQ::kInstr / Tile::kWaves, kRest = FeedQ::kInstr % Tile::kWaves;
         static_assert(FeedP::kInstr % Tile::kWaves == 0, "");
         if (kRest != 0 && wave < kRest) head_wait_vm<kSteps * kNP + (kSteps + kAhead) * (kNQ + 1)>();
         else head_wait_vm<kSteps * kNP + (kSteps + kAhead) * kNQ>();
     };
-
     f32x4 acc[kBP][kBQ];
-#pragma unroll
-    for (int i = 0; i < kBP; ++i)
-#pragma unroll
-        for (int j = 0; j < kBQ; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     std::conditional_t<DT == kF32, HeadSplit, u32x4> aq[kBQ], ap[kBP];
     auto read = [&](auto g_c, int slot_q, int slot_p) {
         constexpr int g = decltype(g_c)::value;
@@ -325,215 +348,277 @@ __global__ __launch_bounds__(Tile::kThreads) void tide_head_gemm_kernel(const He
     };
     constexpr std::integral_constant<int, 0> g0;
     constexpr std::integral_constant<int, 1> g1;
-    constexpr std::integral_constant<int, Tile::kSP - 2> steady;
-    int slot_q = 0, slot_p = 0;
+    auto k_loop = [&] {
+        int slot_q = 0, slot_p = 0;
 #pragma unroll
-    for (int s = -Tile::kSQ; s < -1; ++s) {
-        if (s + Tile::kSP >= 0) issue_p();
-        issue_q();
-    }
-    if constexpr (Tile::kTurns) {
-        landed(steady);
-        ring_barrier();
-        const int group = wave >> 2;
-        if (group == 1) ring_barrier();
-        for (int k = 0; k < n; ++k) {
-            const int next_q = slot_q + Tile::kQBytes == Tile::kSQ * Tile::kQBytes ? 0 : slot_q + Tile::kQBytes;
-            const int next_p = slot_p + Tile::kPBytes == Tile::kSP * Tile::kPBytes ? 0 : slot_p + Tile::kPBytes;
-            auto edge = [] { __builtin_amdgcn_sched_barrier(0); ring_barrier(); __builtin_amdgcn_sched_barrier(0); };
-            read(g0, slot_q, slot_p);
-            issue_p();
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            edge();
-            multiply();
-            edge();
-            read(g1, slot_q, slot_p);
-            issue_q();
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            if (group == 1) landed(steady);
-            edge();
-            multiply();
-            __builtin_amdgcn_sched_barrier(0);
-            if (group == 0) landed(steady);
-            edge();
-            slot_q = next_q;
-            slot_p = next_p;
-        }
-        if (group == 0) ring_barrier();
-    } else {
-        static_assert(Tile::kTurns || Tile::kSQ == Tile::kSP, "");
-        for (int k = 0; k < n; ++k) {
-            landed(steady);
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");          // this wave has read all of stage k - 1, whose slot is filled next
+        for (int i = 0; i < kBP; ++i)
+#pragma unroll
+            for (int j = 0; j < kBQ; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        if constexpr (Tile::kTurns) {
+            landed();
             ring_barrier();
-            issue_p();
-            issue_q();
-            read(g0, slot_q, slot_p);
-            multiply();
-            if constexpr (Tile::kK == 64) {
-                read(g1, slot_q, slot_p);
+            const int group = wave >> 2;
+            if (group == 1) ring_barrier();
+            for (int k = 0; k < n; ++k) {
+                const int next_q = slot_q + Tile::kQBytes == Tile::kSQ * Tile::kQBytes ? 0 : slot_q + Tile::kQBytes;
+                const int next_p = slot_p + Tile::kPBytes == Tile::kSP * Tile::kPBytes ? 0 : slot_p + Tile::kPBytes;
+                auto edge = [] { __builtin_amdgcn_sched_barrier(0); ring_barrier(); __builtin_amdgcn_sched_barrier(0); };
+                read(g0, slot_q, slot_p);
+                issue_p();
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                edge();
                 multiply();
+                edge();
+                read(g1, slot_q, slot_p);
+                issue_q();
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                if (group == 1) landed();
+                edge();
+                multiply();
+                __builtin_amdgcn_sched_barrier(0);
+                if (group == 0) landed();
+                edge();
+                slot_q = next_q;
+                slot_p = next_p;
             }
-            slot_q = slot_q + Tile::kQBytes == Tile::kSQ * Tile::kQBytes ? 0 : slot_q + Tile::kQBytes;
-            slot_p = slot_p + Tile::kPBytes == Tile::kSP * Tile::kPBytes ? 0 : slot_p + Tile::kPBytes;
+            if (group == 0) ring_barrier();
+        } else {
+            static_assert(Tile::kTurns || Tile::kSQ == Tile::kSP, "");
+            for (int k = 0; k < n; ++k) {
+                landed();
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // this wave has read all of stage k - 1, whose slot is filled next
+                ring_barrier();
+                issue_p();
+                issue_q();
+                read(g0, slot_q, slot_p);
+                multiply();
+                if constexpr (Tile::kK == 64) {
+                    read(g1, slot_q, slot_p);
+                    multiply();
+                }
+                slot_q = slot_q + Tile::kQBytes == Tile::kSQ * Tile::kQBytes ? 0 : slot_q + Tile::kQBytes;
+                slot_p = slot_p + Tile::kPBytes == Tile::kSP * Tile::kPBytes ? 0 : slot_p + Tile::kPBytes;
+            }
         }
-    }
-    head_wait_vm<0>();
-    __syncthreads();
+        head_wait_vm<0>();                                 // (zeros beyond the last stage)
+        __syncthreads();                                   // every wave has read the ring
+    };
 
-    // ---- what becomes of the tile
-    typedef __attribute__((address_space(3))) float lds_float;
-    typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
-    lds_float* stage = (lds_float*)((head_lds*)smem + wave * 16 * kLd * 4);
-    const int row = lane & 15, h = lane >> 4;
-    const int col0 = p0 + wp * kCols;                     // the wave's first column
+    // ---- what becomes of a tile of which this lane has row `row` of each 16 and columns 16 i + 4 h + (0 .. 3) of each 16
     typedef __attribute__((ext_vector_type(2))) float f32x2;
     typedef __attribute__((address_space(3))) f32x2 lds_f32x2;
-    lds_f32x2* joined = (lds_f32x2*)((head_lds*)smem + Tile::kEpiBytes);      // statistics: [kWP][kQ] maxima and sums
-    // this wave's block of 16 rows into LDS, row by row; f(value, column within the wave's)
-    auto to_lds = [&](int j, auto f) {
+    typedef __attribute__((address_space(3))) float lds_float;
+    typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
+    lds_float* stage = (lds_float*)((head_lds*)smem + wave * 16 * Tile::kLd * 4);        // statistics and G: 16 of the wave's rows
+    lds_f32x2* joined = (lds_f32x2*)((head_lds*)smem + Tile::kStageBytes);                // statistics: [kWP][kQ] maxima and sums
+    const int row = lane & 15, h = lane >> 4;
+    auto to_lds = [&](int j) {
 #pragma unroll
-        for (int i = 0; i < kBP; ++i) {
-            f32x4 v;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = f(acc[i][j][e], 16 * i + 4 * h + e);
-            *(lds_f32x4*)(stage + row * kLd + 16 * i + 4 * h) = v;
-        }
+        for (int i = 0; i < kBP; ++i) *(lds_f32x4*)(stage + row * Tile::kLd + 16 * i + 4 * h) = acc[i][j];
     };
     auto lds_fence = [] {                                  // the wave's own LDS accesses stay in order
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
     };
-
+    // Which of the row's own tokens ids[k0 .. k0 + 32) are among the first `there` columns from token `base` on: bit k - k0.  Each of the four lanes that
+    // share a row looks at every fourth, eight loads at a time.
+    auto own_tokens = [&](const int32_t* ids, int k0, int base, int there) {
+        uint32_t mine = 0, id[8];
 #pragma unroll
-    for (int j = 0; j < kBQ; ++j) {
-        const int t0 = q0 + (wq * kBQ + j) * 16, t = t0 + row;
-        if constexpr (kMode == kHeadStats) {
-            const float scale = p.ctl ? p.ctl->logit_scale : 1.0f, c1 = p.c1 * scale;
-            const bool ragged = col0 + kCols > p_end;
-            float m = -INFINITY;
+        for (int u = 0; u < 8; ++u) id[u] = (uint32_t)ids[min(k0 + 4 * u + h, p.K - 1)];
 #pragma unroll
-            for (int i = 0; i < kBP; ++i)
+        for (int u = 0; u < 8; ++u) {
+            const int c = (int)(id[u] - (uint32_t)base);
+            mine |= k0 + 4 * u + h < p.K && c >= 0 && c < there ? 1u << (4 * u + h) : 0u;
+        }
+        return mine;
+    };
+    auto results = [&](int q0, int p0, int p_end, int slice) {
+        const int col0 = p0 + wp * kCols;                  // the wave's first column
+        const bool ragged = col0 + kCols > p_end;
 #pragma unroll
-                for (int v = 0; v < 4; ++v) {
-                    if (ragged && col0 + 16 * i + 4 * h + v >= p_end) acc[i][j][v] = -INFINITY;
-                    m = fmaxf(m, acc[i][j][v]);
+        for (int j = 0; j < kBQ; ++j) {
+            const int t = q0 + (wq * kBQ + j) * 16 + row;
+            if constexpr (kMode == kHeadStats) {
+                const float scale = p.ctl ? p.ctl->logit_scale : 1.0f, c1 = p.c1 * scale;
+                if (ragged) {
+#pragma unroll
+                    for (int i = 0; i < kBP; ++i)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[i][j][e] = col0 + 16 * i + 4 * h + e >= p_end ? -INFINITY : acc[i][j][e];
                 }
-            m = fmaxf(m, __shfl_xor(m, 16, kWave));
-            m = fmaxf(m, __shfl_xor(m, 32, kWave));
-            const float m2 = m * c1, shift = m2 == -INFINITY ? 0.0f : m2;
-            float s = 0.0f;
+                float m = -INFINITY;
 #pragma unroll
-            for (int i = 0; i < kBP; ++i)
+                for (int i = 0; i < kBP; ++i)
 #pragma unroll
-                for (int v = 0; v < 4; ++v) s += __builtin_amdgcn_exp2f(fmaf(acc[i][j][v], c1, -shift));
-            s = add_xor<32>(add_xor<16>(s));
-            if constexpr (Tile::kJoined) {                // with the other waves' columns, below
-                if (h == 0) joined[wp * Tile::kQ + (wq * kBQ + j) * 16 + row] = f32x2{m2, s};
+                    for (int e = 0; e < 4; ++e) m = fmaxf(m, acc[i][j][e]);
+                m = fmaxf(m, __shfl_xor(m, 16, kWave));
+                m = fmaxf(m, __shfl_xor(m, 32, kWave));
+                const float m2 = m * c1, shift = m2 == -INFINITY ? 0.0f : m2;
+                float s = 0.0f;
+#pragma unroll
+                for (int i = 0; i < kBP; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s += __builtin_amdgcn_exp2f(fmaf(acc[i][j][e], c1, -shift));
+                s = add_xor<32>(add_xor<16>(s));
+                if constexpr (Tile::kJoined) {
+                    if (h == 0) joined[wp * Tile::kQ + (wq * kBQ + j) * 16 + row] = f32x2{m2, s};
+                } else {
+                    if (h == 0 && t < q_rows) p.part[(int64_t)((p0 / p.pitch) * Tile::kWP + wp) * q_rows + t] = float2{m2, s};
+                }
+                const int32_t* ids = p.ids + (int64_t)min(t, q_rows - 1) * p.K;
+                const int there = t < q_rows ? min(kCols, p_end - col0) : 0;
+                bool staged = false;
+                for (int k0 = 0; k0 < p.K; k0 += 32) {
+                    uint32_t mine = 0;
+                    if (p.K == 1) {
+                        const int c = (int)((uint32_t)ids[0] - (uint32_t)col0);
+                        mine = h == 0 && c >= 0 && c < there ? 1u : 0u;
+                    } else {
+                        mine = own_tokens(ids, k0, col0, there);
+                    }
+                    if (!__any(mine != 0)) continue;
+                    if (!staged) to_lds(j);
+                    staged = true;
+                    lds_fence();
+                    for (; mine != 0; mine &= mine - 1) {
+                        const int k = k0 + __builtin_ctz(mine);
+                        p.z_out[(int64_t)t * p.K + k] = stage[row * Tile::kLd + ids[k] - col0] * scale;
+                    }
+                    lds_fence();
+                }
+            } else if constexpr (kMode == kHeadGrad) {
+                const float c1 = p.c1 * p.ctl->logit_scale;
+                const int t_in = min(t, q_rows - 1);
+                const float4 rc = p.row_const[t_in];
+                const int own = __float_as_int(rc.z);
+#pragma unroll
+                for (int i = 0; i < kBP; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[i][j][e] = rc.y * __builtin_amdgcn_exp2f(fmaf(acc[i][j][e], c1, -rc.x));
+                if (ragged) {
+#pragma unroll
+                    for (int i = 0; i < kBP; ++i)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[i][j][e] = col0 + 16 * i + 4 * h + e >= p_end ? 0.0f : acc[i][j][e];
+                }
+                to_lds(j);
+                lds_fence();
+                const int there = min(kCols, p_end - col0);
+                auto subtract = [&](int c, float w) { stage[row * Tile::kLd + c] = fmaf(-w, rc.y, stage[row * Tile::kLd + c]); };
+                if (!p.wanted) {
+                    const int c = own - p.v0 - col0;
+                    if (c >= 0 && c < there && (c >> 2 & 3) == h) subtract(c, 1.0f);
+                } else {
+                    const int64_t at = (int64_t)own * p.K;
+                    for (int k0 = 0; k0 < p.K; k0 += 32) {
+                        uint32_t mine = own_tokens(p.ids + at, k0, p.v0 + col0, there);
+                        if (!__any(mine != 0)) continue;
+                        mine |= __shfl_xor(mine, 16, kWave);           // all of the row's; each lane then deals with its own columns, in order
+                        mine |= __shfl_xor(mine, 32, kWave);
+                        for (; mine != 0; mine &= mine - 1) {
+                            const int k = k0 + __builtin_ctz(mine), c = p.ids[at + k] - p.v0 - col0;
+                            if ((c >> 2 & 3) == h) subtract(c, p.wanted[at + k]);
+                        }
+                    }
+                }
+                lds_fence();
+                constexpr int kLanes = kCols / 8, kRowsAtOnce = 64 / kLanes;      // 16 bytes of G a lane
+#pragma unroll
+                for (int r0 = 0; r0 < 16; r0 += kRowsAtOnce) {
+                    const int r = r0 + lane / kLanes, c = lane % kLanes * 8, tr = t - row + r;
+                    if (r >= 16 || tr >= q_rows) continue;
+                    const f32x4 a = *(lds_f32x4*)(stage + r * Tile::kLd + c), b = *(lds_f32x4*)(stage + r * Tile::kLd + c + 4);
+                    char* dst = p.g_out + (int64_t)tr * p.g_row_bytes + (int64_t)(col0 + c) * 2;
+                    *reinterpret_cast<u32x4*>(dst) = u32x4{head_round2<DT>(a[0], a[1]), head_round2<DT>(a[2], a[3]), head_round2<DT>(b[0], b[1]), head_round2<DT>(b[2], b[3])};
+                    if constexpr (OutDT == kF32) {
+                        f32x4 x, y;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            x[e] = a[e] - (float)static_cast<_Float16>(a[e]);
+                            y[e] = b[e] - (float)static_cast<_Float16>(b[e]);
+                        }
+                        *reinterpret_cast<u32x4*>(dst + p.g_plane_bytes) = u32x4{head_round2<DT>(x[0], x[1]), head_round2<DT>(x[2], x[3]), head_round2<DT>(y[0], y[1]), head_round2<DT>(y[2], y[3])};
+                    }
+                }
+                lds_fence();
+            } else if constexpr (kMode == kHeadRows) {
+                if (t < q_rows) {
+                    float* dst = p.acc_out + slice * p.acc_slice + (int64_t)t * p.acc_ld;
+#pragma unroll
+                    for (int i = 0; i < kBP; ++i) {
+                        const int c = col0 + 16 * i + 4 * h;
+                        if (c >= p.acc_ld) continue;
+                        f32x4* at = reinterpret_cast<f32x4*>(dst + c);
+                        *at = p.accumulate ? acc[i][j] + *at : acc[i][j];
+                    }
+                }
             } else {
-                if (h == 0 && t < q_rows) p.part[(int64_t)(tp * Tile::kWP + wp) * q_rows + t] = float2{m2, s};
-            }
-            // the row's own tokens among these columns: quarters of the lanes take every fourth one
-            bool any = false;
-            if (t < q_rows)
-                for (int k = h; k < p.K; k += 4) any |= (uint32_t)p.ids[(int64_t)t * p.K + k] - (uint32_t)col0 < (uint32_t)kCols;
-            if (__any(any)) {
-                to_lds(j, [](float z, int) { return z; });
-                lds_fence();
-                if (any)
-                    for (int k = h; k < p.K; k += 4) {
-                        const int id = p.ids[(int64_t)t * p.K + k];
-                        if ((uint32_t)id - (uint32_t)col0 < (uint32_t)kCols && id < p_end) p.z_out[(int64_t)t * p.K + k] = stage[row * kLd + id - col0] * scale;
-                    }
-                lds_fence();
-            }
-        } else if constexpr (kMode == kHeadGrad) {
-            const float c1 = p.c1 * p.ctl->logit_scale;
-            const float2 rc = t < q_rows ? p.row_const[t] : float2{0.0f, 0.0f};
-            const int64_t own = t < q_rows ? (int64_t)p.source[t] * p.K : 0;
-            to_lds(j, [&](float z, int c) { return col0 + c < p.p_rows ? rc.y * __builtin_amdgcn_exp2f(fmaf(z, c1, -rc.x)) : 0.0f; });
-            lds_fence();
-            if (t < q_rows)
-                for (int k = 0; k < p.K; ++k) {           // each quarter of the lanes its own columns: a token that is given twice is subtracted in order
-                    const int c = (int)((uint32_t)p.ids[own + k] - (uint32_t)(p.v0 + col0));
-                    if ((uint32_t)c < (uint32_t)kCols && ((c >> 4) & 3) == h && col0 + c < p.p_rows) {
-                        const float w = p.wanted ? p.wanted[own + k] : 1.0f;
-                        stage[row * kLd + c] = fmaf(-w, rc.y, stage[row * kLd + c]);
-                    }
-                }
-            lds_fence();
-            constexpr int kLanes = kCols / 8, kRowsAtOnce = 64 / kLanes;      // 16 bytes of G a lane
-#pragma unroll
-            for (int r0 = 0; r0 < 16; r0 += kRowsAtOnce) {
-                const int r = r0 + lane / kLanes, c = lane % kLanes * 8;
-                if (t0 + r >= q_rows) continue;
-                const f32x4 a = *(lds_f32x4*)(stage + r * kLd + c), b = *(lds_f32x4*)(stage + r * kLd + c + 4);
-                char* dst = p.g_out + (int64_t)(t0 + r) * p.g_row_bytes + (int64_t)(col0 + c) * 2;
-                *reinterpret_cast<u32x4*>(dst) = u32x4{head_round2<DT>(a[0], a[1]), head_round2<DT>(a[2], a[3]), head_round2<DT>(b[0], b[1]), head_round2<DT>(b[2], b[3])};
-                if constexpr (OutDT == kF32) {
-                    f32x4 x = a, y = b;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        x[e] = a[e] - (float)static_cast<_Float16>(a[e]);
-                        y[e] = b[e] - (float)static_cast<_Float16>(b[e]);
-                    }
-                    *reinterpret_cast<u32x4*>(dst + p.g_plane_bytes) = u32x4{head_round2<DT>(x[0], x[1]), head_round2<DT>(x[2], x[3]), head_round2<DT>(y[0], y[1]), head_round2<DT>(y[2], y[3])};
-                }
-            }
-            lds_fence();
-        } else if constexpr (kMode == kHeadRows) {
-            if (t < q_rows) {
-                float* dst = p.acc_out + blockIdx.y * p.acc_slice + (int64_t)t * p.acc_ld;
-#pragma unroll
-                for (int i = 0; i < kBP; ++i) {
-                    const int c = col0 + 16 * i + 4 * h;
-                    if (c >= p.acc_ld) continue;
-                    f32x4* at = reinterpret_cast<f32x4*>(dst + c);
-                    *at = p.accumulate ? acc[i][j] + *at : acc[i][j];
-                }
-            }
-        } else {
-            const float back = p.ctl->weight_back;
-            to_lds(j, [&](float v, int) { return v * back; });
-            lds_fence();
-            constexpr int kBytes = Storage<OutDT>::kBytes, kE = 16 / kBytes, kLanes = kCols / kE, kRowsAtOnce = 64 / kLanes;
-#pragma unroll
-            for (int r0 = 0; r0 < 16; r0 += kRowsAtOnce) {
-                const int r = r0 + lane / kLanes, c = lane % kLanes * kE;
-                if (t0 + r >= q_rows || col0 + c >= p.p_rows) continue;
-                float v[kE];
-#pragma unroll
-                for (int e = 0; e < kE; ++e) v[e] = stage[r * kLd + c + e];
-                char* dst = p.out + ((int64_t)(t0 + r) * p.out_row_elems + col0 + c) * kBytes;
+                const float back = p.ctl->weight_back;
+                constexpr int kBytes = Storage<OutDT>::kBytes;
+                char* dst = p.out + (int64_t)t * p.out_row_elems * kBytes;
                 if (p.out_aligned) {
-                    if constexpr (kBytes == 2)
-                        *reinterpret_cast<u32x4*>(dst) = u32x4{head_round2<OutDT>(v[0], v[1]), head_round2<OutDT>(v[2], v[3]), head_round2<OutDT>(v[4], v[5]), head_round2<OutDT>(v[6], v[7])};
-                    else
-                        *reinterpret_cast<f32x4*>(dst) = f32x4{v[0], v[1], v[2], v[3]};
+                    if constexpr (kBytes == 4) {
+#pragma unroll
+                        for (int i = 0; i < kBP; ++i) {
+                            const int c = col0 + 16 * i + 4 * h;
+                            if (t < q_rows && c < p.p_rows) *reinterpret_cast<f32x4*>(dst + c * 4) = acc[i][j] * back;
+                        }
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < kBP; i += 2) {
+                            const f32x4 a = acc[i][j] * back, b = acc[i + 1][j] * back;
+                            const u32x4 v = head_gather8(head_round2<OutDT>(a[0], a[1]), head_round2<OutDT>(a[2], a[3]), head_round2<OutDT>(b[0], b[1]), head_round2<OutDT>(b[2], b[3]));
+                            const int c = col0 + 16 * i + 8 * h;
+                            if (t < q_rows && c < p.p_rows) *reinterpret_cast<u32x4*>(dst + c * 2) = v;
+                        }
+                    }
                 } else {
 #pragma unroll
-                    for (int e = 0; e < kE; ++e)
-                        if (col0 + c + e < p.p_rows) {
-                            if constexpr (OutDT == kF16) reinterpret_cast<_Float16*>(dst)[e] = static_cast<_Float16>(v[e]);
-                            else if constexpr (OutDT == kBF16) reinterpret_cast<__bf16*>(dst)[e] = static_cast<__bf16>(v[e]);
-                            else reinterpret_cast<float*>(dst)[e] = v[e];
+                    for (int i = 0; i < kBP; ++i)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const int c = col0 + 16 * i + 4 * h + e;
+                            if (t < q_rows && c < p.p_rows) head_put<OutDT>(dst, c, acc[i][j][e] * back);
                         }
                 }
             }
-            lds_fence();
         }
-    }
-    if constexpr (kMode == kHeadStats && Tile::kJoined) {
-        __syncthreads();
-        const int r = threadIdx.x;
-        if (r < Tile::kQ && q0 + r < q_rows) {
-            float m = -INFINITY, s = 0.0f;
+        if constexpr (kMode == kHeadStats && Tile::kJoined) {
+            __syncthreads();
+            const int r = threadIdx.x;
+            if (r < Tile::kQ && q0 + r < q_rows) {
+                float m = -INFINITY, s = 0.0f;
 #pragma unroll
-            for (int w = 0; w < Tile::kWP; ++w) m = fmaxf(m, joined[w * Tile::kQ + r][0]);
+                for (int w = 0; w < Tile::kWP; ++w) m = fmaxf(m, joined[w * Tile::kQ + r][0]);
 #pragma unroll
-            for (int w = 0; w < Tile::kWP; ++w) s += joined[w * Tile::kQ + r][1] * __builtin_amdgcn_exp2f(joined[w * Tile::kQ + r][0] - (m == -INFINITY ? 0.0f : m));
-            p.part[(int64_t)tp * q_rows + q0 + r] = float2{m, s};
+                for (int w = 0; w < Tile::kWP; ++w) s += joined[w * Tile::kQ + r][1] * __builtin_amdgcn_exp2f(joined[w * Tile::kQ + r][0] - (m == -INFINITY ? 0.0f : m));
+                p.part[(int64_t)(p0 / p.pitch) * q_rows + q0 + r] = float2{m, s};
+            }
         }
+    };
+
+    const int xcd = blockIdx.x & 7;
+    int at = blockIdx.x >> 3;
+    if (!head_item(xcd, at, tiles_q, p.tiles_p, p.k_slices, tq, tp, slice)) return;
+    set_item();
+    issue_first();
+    if constexpr (kLoops<kMode, Tile>) {
+        for (;;) {
+            k_loop();
+            const int done_q0 = q0, done_p0 = p0, done_end = p_end, done_slice = slice;
+            at += gridDim.x >> 3;
+            const bool more = head_item(xcd, at, tiles_q, p.tiles_p, p.k_slices, tq, tp, slice);
+            if (more) {
+                set_item();
+                issue_first();
+            }
+            results(done_q0, done_p0, done_end, done_slice);
+            if (!more) break;
+        }
+    } else {
+        k_loop();
+        results(q0, p0, p_end, slice);
     }
 }
 

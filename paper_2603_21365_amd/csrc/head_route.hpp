@@ -68,8 +68,9 @@ struct HeadShape {
         const int64_t tiles = ((V + HeadTile32::kP - 1) / HeadTile32::kP + cus - 1) / cus * cus;
         return (int)((V + tiles - 1) / tiles);
     }
-    int64_t parts(unsigned cus) const { return (V + pitch(cus) - 1) / pitch(cus) * (rows_per_tile() >= 192 ? HeadTile256::kParts : 1); }
-    static_assert(HeadTile32::kP == HeadTile64::kP && HeadTile32::kP == HeadTile32F::kP && HeadTile32::kP == HeadTile64F::kP && HeadTile128::kParts == 1 && HeadTile192::kParts == HeadTile256::kParts, "");
+    int64_t parts(unsigned cus) const { return (V + pitch(cus) - 1) / pitch(cus) * (rows_per_tile() <= 64 ? 1 : rows_per_tile() == 128 ? HeadTile128::kParts : HeadTile256::kParts); }
+    static_assert(HeadTile192::kParts == HeadTile256::kParts, "");
+    static_assert(HeadTile32::kP == HeadTile64::kP && HeadTile32::kP == HeadTile32F::kP && HeadTile32::kP == HeadTile64F::kP && HeadTile32::kParts == 1 && HeadTile64::kParts == 1, "");
     // fp32 rows without planes: the forward call on few rows, which is bound by reading W once
     bool direct(bool grads) const { return dtype == TIDE_F32 && !grads && T <= kHeadDirectRows && d % 4 == 0; }
     // columns of a piece of the vocabulary in the gradient: equal pieces whose G is at most kHeadPieceBytes
@@ -102,7 +103,7 @@ struct HeadWork {
     float2* part;
     float* z;
     int32_t *source, *place;
-    float2* row_const;
+    float4* row_const;
     float* wanted;
     uint8_t* taught;
     char* g;
@@ -124,7 +125,7 @@ size_t head_layout(const HeadShape& s, bool grads, unsigned cus, void* base, Hea
     } else {
         w.source = sp.take<int32_t>((size_t)s.T);
         w.place = sp.take<int32_t>((size_t)s.T);
-        w.row_const = sp.take<float2>((size_t)s.T);
+        w.row_const = sp.take<float4>((size_t)s.T);
         if (s.K) {
             w.wanted = sp.take<float>((size_t)s.T * s.K);
             w.taught = sp.take<uint8_t>((size_t)s.T);
@@ -139,7 +140,7 @@ size_t head_layout(const HeadShape& s, bool grads, unsigned cus, void* base, Hea
 template <int DT, int OutDT, int kMode, class Tile> int launch_head(int64_t q_rows, int64_t p_rows, hipStream_t st, HeadGemmParams& p) {
     static std::atomic<bool> raised[kMaxDevices];
     int dev = 0;
-    const int rc = current_device(&dev);
+    int rc = current_device(&dev);
     if (rc) return rc;
     if (!raised[dev].load(std::memory_order_relaxed)) {
         TIDE_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(&tide_head_gemm_kernel<DT, OutDT, kMode, Tile>), hipFuncAttributeMaxDynamicSharedMemorySize,
@@ -147,12 +148,14 @@ template <int DT, int OutDT, int kMode, class Tile> int launch_head(int64_t q_ro
         raised[dev].store(true, std::memory_order_relaxed);
     }
     if (!p.pitch) p.pitch = Tile::kP;
-    const int64_t tq = (q_rows + Tile::kQ - 1) / Tile::kQ, tp = (p_rows + p.pitch - 1) / p.pitch;
-    p.tiles_q = (int)tq;
-    p.tiles_p = (int)tp;
-    if (tq * tp == 0) return TIDE_OK;
-    hipLaunchKernelGGL((tide_head_gemm_kernel<DT, OutDT, kMode, Tile>), dim3(8u * (unsigned)((tq * tp + 7) / 8), (unsigned)p.k_slices), dim3(Tile::kThreads),
-                       Tile::kLdsBytes, st, p);
+    const int64_t tq = (q_rows + Tile::kQ - 1) / Tile::kQ;
+    p.tiles_p = (int)((p_rows + p.pitch - 1) / p.pitch);
+    if (tq * p.tiles_p == 0) return TIDE_OK;
+    unsigned cus = 0;
+    if ((rc = resident_cus(&cus))) return rc;
+    int64_t grid = (tq * p.tiles_p * p.k_slices + 7) / 8 * 8;
+    if (kLoops<kMode, Tile>) grid = std::min<int64_t>(grid, cus);
+    hipLaunchKernelGGL((tide_head_gemm_kernel<DT, OutDT, kMode, Tile>), dim3((unsigned)grid), dim3(Tile::kThreads), Tile::kLdsBytes, st, p);
     return TIDE_OK;
 }
 // The products of fp32 operands run on fp16 planes.
@@ -361,7 +364,6 @@ int head_backward(const HeadCall& c) {
                 a.k = (int)s.dp();
                 a.c1 = 1.4426950408889634f / c.tau;
                 a.ids = c.ids;
-                a.source = w.source;
                 a.K = s.K ? (int)s.K : 1;
                 a.V = (int)s.V;
                 a.v0 = (int)v0;

@@ -13,17 +13,6 @@ constexpr int kHeadRowThreads = 256;
 constexpr int kHeadCtlThreads = 1024;
 constexpr int kHeadMaxBlocks = 2048;       // workgroups that search for the largest magnitude
 
-template <int DT> __device__ __forceinline__ float head_load(const char* row, int i) {
-    if constexpr (DT == kF32) return reinterpret_cast<const float*>(row)[i];
-    else if constexpr (DT == kF16) return (float)reinterpret_cast<const _Float16*>(row)[i];
-    else return bf16_bits_to_f32(reinterpret_cast<const uint16_t*>(row)[i]);
-}
-template <int DT> __device__ __forceinline__ void head_store(char* row, int64_t i, float v) {
-    if constexpr (DT == kF32) reinterpret_cast<float*>(row)[i] = v;
-    else if constexpr (DT == kF16) reinterpret_cast<_Float16*>(row)[i] = static_cast<_Float16>(v);
-    else reinterpret_cast<__bf16*>(row)[i] = static_cast<__bf16>(v);
-}
-
 // Largest finite magnitude of fp32 rows, one per workgroup (as bits: the order of non-negative floats).  Infinities and NaN are passed
 // over: they give what they give whatever the scale, and must not cost the other rows theirs.
 __global__ __launch_bounds__(kHeadRowThreads) void tide_head_max_kernel(const char* rows, int64_t row_bytes, int64_t n_rows, int d, uint32_t* out) {
@@ -76,7 +65,7 @@ struct HeadCtlParams {
     float tau;
     int32_t* source;           // [T] out: the live rows' tokens, ascending
     int32_t* place;            // [T] out: a token's live row, or -1
-    float2* row_const;         // [T] out, of live rows: (lse * log2 e, grad * tau * grad_scale)
+    float4* row_const;         // [T] out, of live rows: lse * log2 e, grad * tau * grad_scale, the target or the token, -
 };
 
 // One workgroup: the scales, and the list of live rows in token order (each thread a run of tokens).
@@ -126,7 +115,7 @@ __global__ __launch_bounds__(kHeadCtlThreads) void tide_head_ctl_kernel(const He
         p.place[t] = l ? before : -1;
         if (l) {
             p.source[before] = t;
-            p.row_const[before] = float2{p.lse[t] * 1.4426950408889634f, p.grad[t] * p.tau * sg};
+            p.row_const[before] = float4{p.lse[t] * 1.4426950408889634f, p.grad[t] * p.tau * sg, __int_as_float(p.target ? p.target[t] : t), 0.0f};
             ++before;
         }
     }
@@ -335,7 +324,7 @@ __global__ __launch_bounds__(kHeadRowThreads) void tide_head_dx_kernel(const flo
             } else {
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
-                    if (8 * c + e < d) head_store<DT>(to, 8 * c + e, e < 4 ? a[e & 3] : b[e & 3]);
+                    if (8 * c + e < d) head_put<DT>(to, 8 * c + e, e < 4 ? a[e & 3] : b[e & 3]);
             }
         }
     }
