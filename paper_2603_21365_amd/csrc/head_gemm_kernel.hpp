@@ -64,7 +64,7 @@ struct HeadGemmParams {
     float c1;                  // log2(e) / tau
     const int32_t* ids;        // [T][K] the tokens' own entries of the vocabulary; others than 0 .. V - 1: none
     int K, V, v0;              // p row 0 is token v0
-    float2* part;              // statistics: [tiles_p * kWP][q_rows]
+    float2* part;              // statistics: [tiles_p * kParts][q_rows] largest logit and sum of exp((logit - it) / tau)
     float* z_out;              // statistics: [q_rows][K]
     const float4* row_const;   // G: lse * log2 e, scale, and as an integer the target (wanted == null) or the token, of each row
     const float* wanted;       // G: [T][K] or null (one)
@@ -209,28 +209,16 @@ template <int kRows, bool kAcross> __device__ __forceinline__ u32x4 head_fragmen
     }
 }
 
-// The same of fp32 rows: eight values, each as three bf16 terms, x = hi + mid + lo to 2^-24 x.
-struct HeadSplit {
-    u32x4 hi, mid, lo;
+// The same of fp32 rows: lane l gets the 8 k values of quarter l / 16 of 32.
+struct HeadFloats {
+    f32x4 v[2];
 };
-template <int kRows> __device__ __forceinline__ HeadSplit head_fragment_f32(head_lds* at, int b, int lane) {
+template <int kRows> __device__ __forceinline__ HeadFloats head_fragment_f32(head_lds* at, int b, int lane) {
+    typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
     typedef HeadFeed<kRows, false, 8, 4> Feed;
     const int row = lane & 15, c = 2 * (lane >> 4);
-    const u32x4 v[2] = {*(head_lds_u32x4*)(at + (16 * b + row) * 128 + Feed::place_along(row, c) * 16), *(head_lds_u32x4*)(at + (16 * b + row) * 128 + Feed::place_along(row, c + 1) * 16)};
-    HeadSplit s;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        float a = __uint_as_float(v[i >> 1][2 * (i & 1)]), d = __uint_as_float(v[i >> 1][2 * (i & 1) + 1]);
-        uint32_t t[3];
-#pragma unroll
-        for (int k = 0; k < 3; ++k) {                  // (each difference is exact)
-            t[k] = head_round2<kBF16>(a, d);
-            a -= __uint_as_float(t[k] << 16);
-            d -= __uint_as_float(t[k] & 0xffff0000u);
-        }
-        s.hi[i] = t[0], s.mid[i] = t[1], s.lo[i] = t[2];
-    }
-    return s;
+    head_lds* from = at + (16 * b + row) * 128;
+    return HeadFloats{{*(lds_f32x4*)(from + Feed::place_along(row, c) * 16), *(lds_f32x4*)(from + Feed::place_along(row, c + 1) * 16)}};
 }
 
 // acc[16x16] += A[16 x 32] * B[32 x 16].  With operands that are not zeros the chip runs into its power limit before its rate: back to back from registers this
@@ -239,14 +227,13 @@ template <int DT> __device__ __forceinline__ f32x4 head_mma(u32x4 a, u32x4 b, f3
     if constexpr (DT == kBF16) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), acc, 0, 0, 0);
     else return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), acc, 0, 0, 0);
 }
-// fp32: the products of the terms down to 2^-24, small ones first.
-template <int DT> __device__ __forceinline__ f32x4 head_mma(const HeadSplit& a, const HeadSplit& b, f32x4 acc) {
-    acc = head_mma<kBF16>(a.lo, b.hi, acc);
-    acc = head_mma<kBF16>(a.hi, b.lo, acc);
-    acc = head_mma<kBF16>(a.mid, b.mid, acc);
-    acc = head_mma<kBF16>(a.mid, b.hi, acc);
-    acc = head_mma<kBF16>(a.hi, b.mid, acc);
-    return head_mma<kBF16>(a.hi, b.hi, acc);
+// fp32: eight steps of four k values, one from each quarter of the lanes.  (At most 64 rows are bound by reading W; three bf16 terms a value, split as the
+// fragments are read, cost as many cycles in the vector ALU as these in the matrix cores, and
+// the fragments of x in every wave: 32003 x 768 32.2 / 26.6 us at T = 17, 100000 x 4096 418 / 328 at T = 20.)
+template <int DT> __device__ __forceinline__ f32x4 head_mma(const HeadFloats& a, const HeadFloats& b, f32x4 acc) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(a.v[i >> 2][i & 3], b.v[i >> 2][i & 3], acc, 0, 0, 0);
+    return acc;
 }
 
 // Item `at` of the eighth of the work that XCD `xcd` (workgroup id mod 8) has: the work is a list of k_slices x tiles_q x tiles_p tiles that goes through groups
@@ -325,7 +312,7 @@ __global__ __launch_bounds__(Tile::kThreads) void tide_head_gemm_kernel(const He
         else head_wait_vm<kSteps * kNP + (kSteps + kAhead) * kNQ>();
     };
     f32x4 acc[kBP][kBQ];
-    std::conditional_t<DT == kF32, HeadSplit, u32x4> aq[kBQ], ap[kBP];
+    std::conditional_t<DT == kF32, HeadFloats, u32x4> aq[kBQ], ap[kBP];
     auto read = [&](auto g_c, int slot_q, int slot_p) {
         constexpr int g = decltype(g_c)::value;
         head_lds* at = (head_lds*)smem;
@@ -454,17 +441,19 @@ __global__ __launch_bounds__(Tile::kThreads) void tide_head_gemm_kernel(const He
                     for (int e = 0; e < 4; ++e) m = fmaxf(m, acc[i][j][e]);
                 m = fmaxf(m, __shfl_xor(m, 16, kWave));
                 m = fmaxf(m, __shfl_xor(m, 32, kWave));
-                const float m2 = m * c1, shift = m2 == -INFINITY ? 0.0f : m2;
+                // The maximum stays a logit: the differences from it are exact where they count, so neither its size nor a factor's rounding gets into the sum.
+                const float shift = m == -INFINITY ? 0.0f : m;
                 float s = 0.0f;
 #pragma unroll
                 for (int i = 0; i < kBP; ++i)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) s += __builtin_amdgcn_exp2f(fmaf(acc[i][j][e], c1, -shift));
+                    for (int e = 0; e < 4; ++e) s += __builtin_amdgcn_exp2f((acc[i][j][e] - shift) * c1);
                 s = add_xor<32>(add_xor<16>(s));
-                if constexpr (Tile::kJoined) {
-                    if (h == 0) joined[wp * Tile::kQ + (wq * kBQ + j) * 16 + row] = f32x2{m2, s};
+                m *= scale;
+                if constexpr (Tile::kJoined) {                // with the other waves' columns, below
+                    if (h == 0) joined[wp * Tile::kQ + (wq * kBQ + j) * 16 + row] = f32x2{m, s};
                 } else {
-                    if (h == 0 && t < q_rows) p.part[(int64_t)((p0 / p.pitch) * Tile::kWP + wp) * q_rows + t] = float2{m2, s};
+                    if (h == 0 && t < q_rows) p.part[(int64_t)((p0 / p.pitch) * Tile::kWP + wp) * q_rows + t] = float2{m, s};
                 }
                 const int32_t* ids = p.ids + (int64_t)min(t, q_rows - 1) * p.K;
                 const int there = t < q_rows ? min(kCols, p_end - col0) : 0;
@@ -592,7 +581,7 @@ __global__ __launch_bounds__(Tile::kThreads) void tide_head_gemm_kernel(const He
 #pragma unroll
                 for (int w = 0; w < Tile::kWP; ++w) m = fmaxf(m, joined[w * Tile::kQ + r][0]);
 #pragma unroll
-                for (int w = 0; w < Tile::kWP; ++w) s += joined[w * Tile::kQ + r][1] * __builtin_amdgcn_exp2f(joined[w * Tile::kQ + r][0] - (m == -INFINITY ? 0.0f : m));
+                for (int w = 0; w < Tile::kWP; ++w) s += joined[w * Tile::kQ + r][1] * __builtin_amdgcn_exp2f((joined[w * Tile::kQ + r][0] - (m == -INFINITY ? 0.0f : m)) * p.c1);
                 p.part[(int64_t)(p0 / p.pitch) * q_rows + q0 + r] = float2{m, s};
             }
         }

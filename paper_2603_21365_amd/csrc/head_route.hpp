@@ -9,7 +9,9 @@ namespace {
 // fp32, 125 tiles on 256 CUs, 34 as 251 of 128).  dx reads W across and stays 256 wide.
 using HeadTile32 = HeadTile<1, 8, 2, 1, 4, 4>;
 using HeadTile64 = HeadTile<2, 4, 2, 2, 3, 3>;
-using HeadTile32F = HeadTile<1, 8, 2, 1, 4, 4, 4>;      // fp32 rows as they are
+using HeadTile16F = HeadTile<1, 8, 1, 1, 4, 4, 4>;      // fp32 rows as they are
+using HeadTile32F = HeadTile<1, 8, 2, 1, 4, 4, 4>;
+using HeadTile48F = HeadTile<1, 8, 3, 1, 3, 3, 4>;
 using HeadTile64F = HeadTile<2, 4, 2, 2, 3, 3, 4>;
 using HeadTile128 = HeadTile<2, 4, 4, 4, 4, 3>;
 using HeadTile192 = HeadTile<4, 2, 3, 8, 3, 2>;
@@ -70,7 +72,7 @@ struct HeadShape {
     }
     int64_t parts(unsigned cus) const { return (V + pitch(cus) - 1) / pitch(cus) * (rows_per_tile() <= 64 ? 1 : rows_per_tile() == 128 ? HeadTile128::kParts : HeadTile256::kParts); }
     static_assert(HeadTile192::kParts == HeadTile256::kParts, "");
-    static_assert(HeadTile32::kP == HeadTile64::kP && HeadTile32::kP == HeadTile32F::kP && HeadTile32::kP == HeadTile64F::kP && HeadTile32::kParts == 1 && HeadTile64::kParts == 1, "");
+    static_assert(HeadTile32::kP == HeadTile64::kP && HeadTile32::kP == HeadTile32F::kP && HeadTile32::kP == HeadTile16F::kP && HeadTile32::kP == HeadTile48F::kP && HeadTile32::kP == HeadTile64F::kP && HeadTile32::kParts == 1 && HeadTile64::kParts == 1, "");
     // fp32 rows without planes: the forward call on few rows, which is bound by reading W once
     bool direct(bool grads) const { return dtype == TIDE_F32 && !grads && T <= kHeadDirectRows && d % 4 == 0; }
     // columns of a piece of the vocabulary in the gradient: equal pieces whose G is at most kHeadPieceBytes
@@ -282,7 +284,8 @@ int head_forward(const HeadCall& c) {
         int rc2 = TIDE_OK;
         if (direct) {
             if constexpr (DT == kF32)
-                rc2 = s.T <= 32 ? launch_head<kF32, kF32, kHeadStats, HeadTile32F>(s.T, s.V, c.st, p) : launch_head<kF32, kF32, kHeadStats, HeadTile64F>(s.T, s.V, c.st, p);
+                rc2 = s.T <= 16 ? launch_head<kF32, kF32, kHeadStats, HeadTile16F>(s.T, s.V, c.st, p) : s.T <= 32 ? launch_head<kF32, kF32, kHeadStats, HeadTile32F>(s.T, s.V, c.st, p) : s.T <= 48 ? launch_head<kF32, kF32, kHeadStats, HeadTile48F>(s.T, s.V, c.st, p)
+                     : launch_head<kF32, kF32, kHeadStats, HeadTile64F>(s.T, s.V, c.st, p);
         } else {
             rc2 = by_head_tile(s.rows_per_tile(), [&](auto tile) { return launch_head<kHeadElem<DT>, DT, kHeadStats, decltype(tile)>(s.T, s.V, c.st, p); });
         }

@@ -242,9 +242,10 @@ __global__ __launch_bounds__(1024) void tide_head_finish_kernel(const HeadFinish
     __shared__ float2 part[64][17];
     const int tid = threadIdx.x, r = tid & 15, slice = tid >> 4, t = blockIdx.x * 16 + r;
     float m = -INFINITY, s = 0.0f;
-    auto join = [](float& m, float& s, float m1, float s1) {
+    const float c1 = 1.4426950408889634f / p.tau;
+    auto join = [c1](float& m, float& s, float m1, float s1) {
         const float top = fmaxf(m, m1), at = top == -INFINITY ? 0.0f : top;
-        s = s * __builtin_amdgcn_exp2f(m - at) + s1 * __builtin_amdgcn_exp2f(m1 - at);
+        s = s * __builtin_amdgcn_exp2f((m - at) * c1) + s1 * __builtin_amdgcn_exp2f((m1 - at) * c1);
         m = top;
     };
     if (t < p.T)
@@ -266,13 +267,13 @@ __global__ __launch_bounds__(1024) void tide_head_finish_kernel(const HeadFinish
         join(m, s, m1, s1);
     }
     if (row >= p.T) return;
-    const float lse = (m + log2f(s)) * 0.6931471805599453f;
+    const float log_s = logf(s), lse = m / p.tau + log_s;
     const int32_t* ids = p.ids + (int64_t)row * p.K;
     float* z = p.z + (int64_t)row * p.K;
     if (!p.values) {
         if (lane == 0) {
             p.lse[row] = lse;
-            p.loss[row] = (uint32_t)ids[0] < (uint32_t)p.V ? lse - z[0] / p.tau : 0.0f;
+            p.loss[row] = (uint32_t)ids[0] < (uint32_t)p.V ? (m - z[0]) / p.tau + log_s : 0.0f;
         }
         return;
     }
@@ -285,7 +286,7 @@ __global__ __launch_bounds__(1024) void tide_head_finish_kernel(const HeadFinish
             z[k] = 0.0f;
         } else if (values[k] != -INFINITY) {
             const float log_q = values[k] * inv_tau - h.m - h.log_sum, q = expf(log_q);
-            sum += q > 0.0f ? q * (log_q - z[k] * inv_tau + lse) : 0.0f;
+            sum += q > 0.0f ? q * (log_q + (m - z[k]) * inv_tau + log_s) : 0.0f;
         }
     }
     sum = wave_sum(sum);
