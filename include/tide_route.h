@@ -294,7 +294,7 @@ int tide_exit_project_grad(const void* hidden, int dtype, int64_t C, int64_t T, 
  *
  *   x          device [T rows] of `dtype`;  W device [V rows] of `dtype`;  strides in elements, at most 4194304
  *              rows of whole 16-byte chunks: bases and strides multiples of 16 bytes; other hidden sizes: of an element (the call copies x and W)
- *   1 <= d <= 16384, T <= 4194304, 1 <= K <= 1024, 1e-30 <= tau <= 1e30
+ *   1 <= d <= 16384, T <= 4194304, V <= 8388608, T * V up to about 2^38, 1 <= K <= 1024, 1e-30 <= tau <= 1e30 (TIDE_ERR_UNSUPPORTED, tau: TIDE_ERR_INVALID_ARG)
  *   target     device [T] int32;  top_values device [T,K] fp32;  top_ids device [T,K] int32
  *   loss, lse, grad_loss  device [T] fp32;  z_top device [T,K] fp32
  *   dx device [T rows], dW device [V rows] of `dtype`, aligned as x and W

@@ -20,7 +20,8 @@ using HeadRows32 = HeadTile<1, 8, 2, 2, 4, 4>;
 using HeadRows64 = HeadTile<2, 4, 2, 4, 4, 4>;
 constexpr int kHeadDirectRows = 64;
 constexpr int kHeadCols = 256;
-constexpr int64_t kHeadMostRows = (int64_t)1 << 22, kHeadMostVocab = ((int64_t)1 << 31) - 1024;
+constexpr int64_t kHeadMostRows = (int64_t)1 << 22, kHeadMostVocab = (int64_t)1 << 23;
+constexpr int64_t kHeadMostTiles = ((int64_t)1 << 23) - 8;      // a launch has fewer than 2^32 threads, a tile 512
 constexpr int kHeadMostTop = 1024;
 constexpr size_t kHeadPieceBytes = (size_t)256 << 20;      // G of a piece of the vocabulary: as much as stays in the last-level cache (256 MiB to 4 GiB: no difference)
 
@@ -188,6 +189,8 @@ int check_head(const HeadCall& c, bool grads) {
     if (s.d > kMaxHidden) return fail(TIDE_ERR_UNSUPPORTED, "d = %lld: hidden sizes from 1 to 16384", (long long)s.d);
     if (s.V <= 0) return fail(TIDE_ERR_INVALID_ARG, "V = %lld must be positive", (long long)s.V);
     if (s.V > kHeadMostVocab) return fail(TIDE_ERR_UNSUPPORTED, "V = %lld exceeds %lld", (long long)s.V, (long long)kHeadMostVocab);
+    if (s.row_tiles() * ((s.V + HeadTile32::kP - 1) / HeadTile32::kP) > kHeadMostTiles)
+        return fail(TIDE_ERR_UNSUPPORTED, "T = %lld rows of V = %lld logits are too many for one call", (long long)s.T, (long long)s.V);
     if (s.K < 0 || s.K > kHeadMostTop) return fail(TIDE_ERR_UNSUPPORTED, "K = %lld: 1 to %d entries of a teacher", (long long)s.K, kHeadMostTop);
     if (!(c.tau > 0.0f) || !(c.tau <= 1e30f) || c.tau < 1e-30f) return fail(TIDE_ERR_INVALID_ARG, "tau = %g must be positive and finite", (double)c.tau);
     if (c.x_stride < s.d || c.w_stride < s.d) return fail(TIDE_ERR_INVALID_ARG, "row strides of x and W must be at least d");

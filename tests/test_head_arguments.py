@@ -28,7 +28,7 @@ def distill_grad(K=3, tau=1.0, lse=FAKE, g=FAKE, values=FAKE):
 @pytest.mark.parametrize("call", [loss, loss_grad])
 @pytest.mark.parametrize("bad,status,word", [
     (dict(dtype=3), INVALID, "dtype"), (dict(T=-1), INVALID, "negative"), (dict(T=1 << 23), UNSUPPORTED, "exceeds"), (dict(d=0), INVALID, "positive"),
-    (dict(d=16392, xs=16392, ws=16392), UNSUPPORTED, "16384"), (dict(V=0), INVALID, "V = 0"), (dict(V=1 << 31), UNSUPPORTED, "V ="), (dict(x=None), INVALID, "NULL"),
+    (dict(d=16392, xs=16392, ws=16392), UNSUPPORTED, "16384"), (dict(V=0), INVALID, "V = 0"), (dict(V=1 << 24), UNSUPPORTED, "V ="), (dict(T=1 << 22, V=1 << 20), UNSUPPORTED, "too many"), (dict(x=None), INVALID, "NULL"),
     (dict(W=None), INVALID, "NULL"), (dict(target=None), INVALID, "NULL"), (dict(lse=None), INVALID, "lse"), (dict(xs=63), INVALID, "strides"), (dict(ws=63), INVALID, "strides"),
     (dict(xs=1 << 23), UNSUPPORTED, "strides"), (dict(x=FAKE + 8), ALIGNMENT, "x:"), (dict(ws=68), ALIGNMENT, "W:"), (dict(d=63, W=FAKE + 1), ALIGNMENT, "W:"),
     (dict(target=FAKE + 2), ALIGNMENT, "4-byte")])
