@@ -56,7 +56,7 @@ struct HeadOperand {
 struct HeadGemmParams {
     HeadOperand q, p;
     int q_rows, p_rows, k;     // of these the one that counts live rows is replaced by ctl->live
-    int segments;              // 1, or 3 for two planes
+    int segments;              // passes over k: 1, or 3 for operands of two planes
     int tiles_p, k_slices;
     int pitch;                 // columns of a tile: kP, or fewer (statistics) where that gives every CU as many
     const HeadCtl* ctl;        // null where nothing is scaled and every row counts (16-bit statistics)
@@ -68,12 +68,13 @@ struct HeadGemmParams {
     float* z_out;              // statistics: [q_rows][K]
     const float4* row_const;   // G: lse * log2 e, scale, and as an integer the target (wanted == null) or the token, of each row
     const float* wanted;       // G: [T][K] or null (one)
-    char* g_out;               // G
+    char* g_out;               // G: rounded to 16 bits, and (g_plane_bytes != 0) what that leaves in a second plane
     int64_t g_row_bytes, g_plane_bytes;
     // dx
     float* acc_out;            // [k_slices][acc_rows][acc_ld]
     int64_t acc_slice;         // elements
     int acc_ld, accumulate;
+    int stacked;               // G's second plane follows its first as further rows, from this one on (0: none; 16-bit operands): rows of dx, of k in dW
     // dW
     char* out;
     int64_t out_row_elems;
@@ -182,6 +183,10 @@ template <int DT> __device__ __forceinline__ uint32_t head_round2(float a, float
     }
 }
 
+template <int DT> __device__ __forceinline__ float head_rounded(float v) {
+    if constexpr (DT == kF16) return (float)static_cast<_Float16>(v);
+    else return (float)static_cast<__bf16>(v);
+}
 template <int DT> __device__ __forceinline__ void head_put(char* row, int i, float v) {
     if constexpr (DT == kF32) reinterpret_cast<float*>(row)[i] = v;
     else if constexpr (DT == kF16) reinterpret_cast<_Float16*>(row)[i] = static_cast<_Float16>(v);
@@ -274,8 +279,8 @@ __global__ __launch_bounds__(Tile::kThreads) void tide_head_gemm_kernel(const He
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int wq = wave % Tile::kWQ, wp = wave / Tile::kWQ;
     const int live = kMode == kHeadStats ? 0 : __builtin_amdgcn_readfirstlane(p.ctl->live);
-    const int q_rows = kMode == kHeadGrad || kMode == kHeadRows ? live : p.q_rows;
-    const int k_elems = kMode == kHeadWeights ? live : p.k;
+    const int q_rows = kMode == kHeadGrad ? live : kMode == kHeadRows ? p.stacked + live : p.q_rows;
+    const int k_elems = kMode == kHeadWeights ? (live ? p.stacked + live : 0) : p.k;
     const int tiles_q = (q_rows + Tile::kQ - 1) / Tile::kQ;
     const uint32_t lds_q = (uint32_t)(size_t)(head_lds*)smem, lds_p = lds_q + Tile::kSQ * Tile::kQBytes;
 
@@ -371,6 +376,20 @@ __global__ __launch_bounds__(Tile::kThreads) void tide_head_gemm_kernel(const He
             if (group == 0) ring_barrier();
         } else {
             static_assert(Tile::kTurns || Tile::kSQ == Tile::kSP, "");
+            f32x4 sum[kBP][kBQ];                           // fp32: sums of 128 products each are added up here, so that the roundings do not pile up over k
+#pragma unroll
+            for (int i = 0; i < kBP; ++i)
+#pragma unroll
+                for (int j = 0; j < kBQ; ++j) sum[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            auto fold = [&] {
+#pragma unroll
+                for (int i = 0; i < kBP; ++i)
+#pragma unroll
+                    for (int j = 0; j < kBQ; ++j) {
+                        sum[i][j] += acc[i][j];
+                        acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+                    }
+            };
             for (int k = 0; k < n; ++k) {
                 landed();
                 asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // this wave has read all of stage k - 1, whose slot is filled next
@@ -382,9 +401,18 @@ __global__ __launch_bounds__(Tile::kThreads) void tide_head_gemm_kernel(const He
                 if constexpr (Tile::kK == 64) {
                     read(g1, slot_q, slot_p);
                     multiply();
+                } else if ((k & 3) == 3) {
+                    fold();
                 }
                 slot_q = slot_q + Tile::kQBytes == Tile::kSQ * Tile::kQBytes ? 0 : slot_q + Tile::kQBytes;
                 slot_p = slot_p + Tile::kPBytes == Tile::kSP * Tile::kPBytes ? 0 : slot_p + Tile::kPBytes;
+            }
+            if constexpr (DT == kF32) {
+                fold();
+#pragma unroll
+                for (int i = 0; i < kBP; ++i)
+#pragma unroll
+                    for (int j = 0; j < kBQ; ++j) acc[i][j] = sum[i][j];
             }
         }
         head_wait_vm<0>();                                 // (zeros beyond the last stage)
@@ -484,7 +512,7 @@ __global__ __launch_bounds__(Tile::kThreads) void tide_head_gemm_kernel(const He
 #pragma unroll
                 for (int i = 0; i < kBP; ++i)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) acc[i][j][e] = rc.y * __builtin_amdgcn_exp2f(fmaf(acc[i][j][e], c1, -rc.x));
+                    for (int e = 0; e < 4; ++e) acc[i][j][e] = t < q_rows ? rc.y * __builtin_amdgcn_exp2f(fmaf(acc[i][j][e], c1, -rc.x)) : 0.0f;
                 if (ragged) {
 #pragma unroll
                     for (int i = 0; i < kBP; ++i)
@@ -493,7 +521,7 @@ __global__ __launch_bounds__(Tile::kThreads) void tide_head_gemm_kernel(const He
                 }
                 to_lds(j);
                 lds_fence();
-                const int there = min(kCols, p_end - col0);
+                const int there = t < q_rows ? min(kCols, p_end - col0) : 0;
                 auto subtract = [&](int c, float w) { stage[row * Tile::kLd + c] = fmaf(-w, rc.y, stage[row * Tile::kLd + c]); };
                 if (!p.wanted) {
                     const int c = own - p.v0 - col0;
@@ -516,16 +544,16 @@ __global__ __launch_bounds__(Tile::kThreads) void tide_head_gemm_kernel(const He
 #pragma unroll
                 for (int r0 = 0; r0 < 16; r0 += kRowsAtOnce) {
                     const int r = r0 + lane / kLanes, c = lane % kLanes * 8, tr = t - row + r;
-                    if (r >= 16 || tr >= q_rows) continue;
+                    if (r >= 16 || tr >= max(q_rows, p.stacked)) continue;      // (stacked: zeros in the rows between the planes)
                     const f32x4 a = *(lds_f32x4*)(stage + r * Tile::kLd + c), b = *(lds_f32x4*)(stage + r * Tile::kLd + c + 4);
                     char* dst = p.g_out + (int64_t)tr * p.g_row_bytes + (int64_t)(col0 + c) * 2;
                     *reinterpret_cast<u32x4*>(dst) = u32x4{head_round2<DT>(a[0], a[1]), head_round2<DT>(a[2], a[3]), head_round2<DT>(b[0], b[1]), head_round2<DT>(b[2], b[3])};
-                    if constexpr (OutDT == kF32) {
+                    if (p.g_plane_bytes) {
                         f32x4 x, y;
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
-                            x[e] = a[e] - (float)static_cast<_Float16>(a[e]);
-                            y[e] = b[e] - (float)static_cast<_Float16>(b[e]);
+                            x[e] = a[e] - head_rounded<DT>(a[e]);
+                            y[e] = b[e] - head_rounded<DT>(b[e]);
                         }
                         *reinterpret_cast<u32x4*>(dst + p.g_plane_bytes) = u32x4{head_round2<DT>(x[0], x[1]), head_round2<DT>(x[2], x[3]), head_round2<DT>(y[0], y[1]), head_round2<DT>(y[2], y[3])};
                     }
@@ -543,6 +571,15 @@ __global__ __launch_bounds__(Tile::kThreads) void tide_head_gemm_kernel(const He
                     }
                 }
             } else {
+                if (p.acc_out) {                           // a k slice's part, as for dx
+                    if (t < q_rows) {
+                        float* dst = p.acc_out + slice * p.acc_slice + (int64_t)t * p.acc_ld;
+#pragma unroll
+                        for (int i = 0; i < kBP; ++i)
+                            if (col0 + 16 * i + 4 * h < p.acc_ld) *reinterpret_cast<f32x4*>(dst + col0 + 16 * i + 4 * h) = acc[i][j];
+                    }
+                    continue;
+                }
                 const float back = p.ctl->weight_back;
                 constexpr int kBytes = Storage<OutDT>::kBytes;
                 char* dst = p.out + (int64_t)t * p.out_row_elems * kBytes;

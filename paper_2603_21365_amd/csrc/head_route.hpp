@@ -18,7 +18,8 @@ using HeadTile192 = HeadTile<4, 2, 3, 8, 3, 2>;
 using HeadTile256 = HeadTile<4, 2, 4, 8, 3, 2>;
 using HeadRows32 = HeadTile<1, 8, 2, 2, 4, 4>;
 using HeadRows64 = HeadTile<2, 4, 2, 4, 4, 4>;
-constexpr int kHeadDirectRows = 64;
+// fp32 rows as they are up to here, planes beyond (V = 100000, d = 4096, us: T = 65 806 / 1429, 96 809 / 1436, 128 1024 / 1445; 192 would be three tiles of 64).
+constexpr int kHeadDirectRows = 128;
 constexpr int kHeadCols = 256;
 constexpr int64_t kHeadMostRows = (int64_t)1 << 22, kHeadMostVocab = (int64_t)1 << 23;
 constexpr int64_t kHeadMostTiles = ((int64_t)1 << 23) - 8;      // a launch has fewer than 2^32 threads, a tile 512
@@ -47,11 +48,12 @@ template <typename F> int by_head_rows(int rows, F&& f) {
 struct HeadShape {
     int dtype;
     int64_t T, d, V, K;
+    unsigned cus = 256;
     int64_t dp() const { return (d + 7) / 8 * 8; }                      // elements of a padded row of 16-bit values
     int planes() const { return dtype == TIDE_F32 ? 2 : 1; }
     bool copied(bool grads) const { return direct(grads) ? false : dtype == TIDE_F32 || d % 8 != 0; }     // the products read copies of x and W
     int64_t plane_bytes(int64_t rows) const { return rows * dp() * 2; }
-    int rows_per_tile() const {
+    static int rows_for(int64_t T) {
         if (T <= 32) return 32;
         if (T <= 64) return 64;
         // A tile of 128 / 192 rows takes 60 / 80 % of the time of one of 256 (d = 4096, V = 65536, us a tile row: 66-108); the least of those decides
@@ -61,31 +63,51 @@ struct HeadShape {
         if ((T + 127) / 128 * 60 < least) best = 128;
         return best;
     }
+    // The products with x W^T: the same, but tiles of 64 rows and 128 columns where the large ones fill less than half of the CUs and these fit one round of two a
+    // CU (with the slices of dW, a step in bf16 at T = 2142, d = 768, V = 1147 141 -> 102 us; fp16, T = 8000, d = 1024, V = 1000 302 -> 181).
+    int rows_per_tile() const {
+        const int rows = rows_for(T);
+        if (rows <= 64) return rows;
+        return 2 * ((T + rows - 1) / rows) * col_tiles() < (int64_t)cus && (T + 63) / 64 * ((V + HeadTile64::kP - 1) / HeadTile64::kP) <= 2 * (int64_t)cus ? 64 : rows;
+    }
     int64_t row_tiles() const { return (T + rows_per_tile() - 1) / rows_per_tile(); }
+    // Few rows: a row of dx can hang on one element of G, whose rounding would then be all of that row's; what it leaves goes into a second plane.  Their products
+    // are bound by reading W and writing dW.
+    int g_planes() const { return dtype == TIDE_F32 || T <= 64 ? 2 : 1; }
+    // 16-bit operands: the second plane follows as further rows -- of dx, so that W is read once, and of k in dW (of x, too), where a stage has room for them
+    int64_t stacked() const { return dtype != TIDE_F32 && g_planes() == 2 ? T : 0; }
+    int rows_of_dx() const { return rows_for(T + stacked()); }
     int64_t col_tiles() const { return (V + kHeadCols - 1) / kHeadCols; }
     // Columns of a tile of the statistics.  Few rows: as many tiles as the narrowest multiple of the CUs that holds them, so that each CU reads as much of W
     // (bf16, d = 4096, V = 128000: 1000 tiles of 128 columns 186 us / 1024 of 125 180; fp32, T = 17, d = 768, V = 32003: 251 of 128 32.0 / 256 of 126 31.1).
-    int pitch(unsigned cus) const {
-        const int rows = rows_per_tile();
+    int stats_rows() const { return direct(false) ? std::min(rows_for(T), 64) : rows_per_tile(); }
+    int pitch() const {
+        const int rows = stats_rows();
         if (rows > 64) return kHeadCols;
+        if (T > 64) return HeadTile64::kP;
         const int64_t tiles = ((V + HeadTile32::kP - 1) / HeadTile32::kP + cus - 1) / cus * cus;
         return (int)((V + tiles - 1) / tiles);
     }
-    int64_t parts(unsigned cus) const { return (V + pitch(cus) - 1) / pitch(cus) * (rows_per_tile() <= 64 ? 1 : rows_per_tile() == 128 ? HeadTile128::kParts : HeadTile256::kParts); }
+    int64_t parts() const { return (V + pitch() - 1) / pitch() * (stats_rows() <= 64 ? 1 : stats_rows() == 128 ? HeadTile128::kParts : HeadTile256::kParts); }
     static_assert(HeadTile192::kParts == HeadTile256::kParts, "");
     static_assert(HeadTile32::kP == HeadTile64::kP && HeadTile32::kP == HeadTile32F::kP && HeadTile32::kP == HeadTile16F::kP && HeadTile32::kP == HeadTile48F::kP && HeadTile32::kP == HeadTile64F::kP && HeadTile32::kParts == 1 && HeadTile64::kParts == 1, "");
     // fp32 rows without planes: the forward call on few rows, which is bound by reading W once
     bool direct(bool grads) const { return dtype == TIDE_F32 && !grads && T <= kHeadDirectRows && d % 4 == 0; }
     // columns of a piece of the vocabulary in the gradient: equal pieces whose G is at most kHeadPieceBytes
     int64_t piece() const {
-        const int64_t tiles = std::max<int64_t>(1, (int64_t)(kHeadPieceBytes / ((size_t)std::max<int64_t>(T, 1) * planes() * 2 * kHeadCols)));
+        const int64_t tiles = std::max<int64_t>(1, (int64_t)(kHeadPieceBytes / ((size_t)std::max<int64_t>(T, 1) * g_planes() * 2 * kHeadCols)));
         const int64_t pieces = (col_tiles() + tiles - 1) / tiles;
         return (col_tiles() + pieces - 1) / pieces * kHeadCols;
     }
     // workgroups that share a tile's piece of the vocabulary in dx = G W: what fills the chip once
-    int dx_slices(unsigned cus) const {
-        const int64_t tiles = row_tiles() * ((d + kHeadCols - 1) / kHeadCols);
+    int dx_slices() const {
+        const int64_t tiles = (T + stacked() + rows_of_dx() - 1) / rows_of_dx() * ((d + kHeadCols - 1) / kHeadCols);
         return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(cus / std::max<int64_t>(tiles, 1), 64), piece() / kHeadCols));
+    }
+    // the same for dW = G^T x, over the rows: at least four stages each (few tiles: a vocabulary of a few thousand tokens)
+    int dw_slices() const {
+        const int64_t tiles = piece() / kHeadCols * ((d + kHeadCols - 1) / kHeadCols);
+        return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(cus / tiles, 32), (T + 255) / 256));
     }
 };
 
@@ -110,9 +132,9 @@ struct HeadWork {
     float* wanted;
     uint8_t* taught;
     char* g;
-    float* acc;
+    float *acc, *dw;
 };
-size_t head_layout(const HeadShape& s, bool grads, unsigned cus, void* base, HeadWork* out) {
+size_t head_layout(const HeadShape& s, bool grads, void* base, HeadWork* out) {
     HeadSpace sp{(char*)base};
     HeadWork w{};
     w.ctl = sp.take<HeadCtl>(1);
@@ -121,9 +143,9 @@ size_t head_layout(const HeadShape& s, bool grads, unsigned cus, void* base, Hea
         w.w_max = sp.take<uint32_t>(kHeadMaxBlocks);
     }
     if (s.copied(grads)) w.w = sp.take<char>((size_t)s.plane_bytes(s.V) * s.planes());
-    if (s.copied(grads) || grads) w.x = sp.take<char>((size_t)s.plane_bytes(s.T) * s.planes());
+    if (s.copied(grads) || grads) w.x = sp.take<char>((size_t)s.plane_bytes(std::max(s.T + (grads ? s.stacked() : 0), grads && s.T > 64 ? (int64_t)128 : 0)) * s.planes());
     if (!grads) {
-        w.part = sp.take<float2>((size_t)s.parts(cus) * s.T);
+        w.part = sp.take<float2>((size_t)s.parts() * s.T);
         if (!s.K) w.z = sp.take<float>((size_t)s.T);
     } else {
         w.source = sp.take<int32_t>((size_t)s.T);
@@ -133,8 +155,9 @@ size_t head_layout(const HeadShape& s, bool grads, unsigned cus, void* base, Hea
             w.wanted = sp.take<float>((size_t)s.T * s.K);
             w.taught = sp.take<uint8_t>((size_t)s.T);
         }
-        w.g = sp.take<char>((size_t)s.T * s.piece() * 2 * s.planes());
-        w.acc = sp.take<float>((size_t)s.dx_slices(cus) * s.T * s.dp());
+        w.g = sp.take<char>((size_t)std::max<int64_t>(s.T * s.g_planes(), s.T > 64 ? 128 : 0) * s.piece() * 2);      // (no less than 64 rows of two planes take)
+        w.acc = sp.take<float>((size_t)s.dx_slices() * std::max(s.T + s.stacked(), s.T > 64 ? (int64_t)128 : 0) * s.dp());
+        if (s.dw_slices() > 1) w.dw = sp.take<float>((size_t)s.dw_slices() * s.piece() * s.dp());
     }
     if (out) *out = w;
     return sp.at;
@@ -218,11 +241,11 @@ int check_head(const HeadCall& c, bool grads) {
     return TIDE_OK;
 }
 
-int head_space(const HeadCall& c, bool grads, unsigned cus, HeadWork* w) {
-    const size_t need = head_layout(c.s, grads, cus, nullptr, nullptr);
+int head_space(const HeadCall& c, bool grads, HeadWork* w) {
+    const size_t need = head_layout(c.s, grads, nullptr, nullptr);
     if (!c.workspace || c.workspace_bytes < need) return fail(TIDE_ERR_WORKSPACE, "this call needs %zu bytes of workspace, %zu given", need, c.workspace ? c.workspace_bytes : 0);
     if ((uintptr_t)c.workspace & 255) return fail(TIDE_ERR_ALIGNMENT, "the workspace must be 256-byte aligned");
-    head_layout(c.s, grads, cus, c.workspace, w);
+    head_layout(c.s, grads, c.workspace, w);
     return TIDE_OK;
 }
 
@@ -232,11 +255,11 @@ template <int DT> void head_max(const void* rows, int64_t stride, int64_t n, int
     *blocks = (int)std::min<int64_t>(n, kHeadMaxBlocks);
     if (*blocks) hipLaunchKernelGGL(tide_head_max_kernel, dim3(*blocks), dim3(kHeadRowThreads), 0, st, (const char*)rows, stride * 4, n, (int)d, out);
 }
-template <int DT> void head_copy(const HeadShape& s, const void* rows, int64_t stride, int64_t n, const int32_t* source, const HeadCtl* ctl, int weights, char* out, hipStream_t st) {
+template <int DT> void head_copy(const HeadShape& s, const void* rows, int64_t stride, int64_t n, const int32_t* source, const HeadCtl* ctl, int weights, char* out, hipStream_t st, int64_t stacked = 0) {
     if (n == 0) return;
     const int64_t rows_each = head_copy_rows(s.dp() / 8);
     hipLaunchKernelGGL((tide_head_copy_kernel<DT>), dim3((unsigned)((n + rows_each - 1) / rows_each)), dim3(kHeadRowThreads), 0, st, (const char*)rows, stride * Storage<DT>::kBytes, n, (int)rows_each,
-                       (int)s.d, source, ctl, weights, out, s.dp() * 2, s.plane_bytes(n));
+                       (int)s.d, source, ctl, weights, (int)stacked, out, s.dp() * 2, s.plane_bytes(n));
 }
 // x or W as an operand: the caller's rows, or the copy's planes of n rows.
 HeadOperand head_operand(const HeadShape& s, const void* rows, int64_t stride, const char* copy, int64_t n) {
@@ -244,14 +267,13 @@ HeadOperand head_operand(const HeadShape& s, const void* rows, int64_t stride, c
     return HeadOperand{{(const char*)rows, (const char*)rows}, stride * (int64_t)elem_bytes(s.dtype)};
 }
 
-int head_forward(const HeadCall& c) {
+int head_forward(HeadCall& c) {
     int rc = check_head(c, false);
     if (rc || c.s.T == 0) return rc;
-    unsigned cus = 0;
-    if ((rc = resident_cus(&cus))) return rc;
+    if ((rc = resident_cus(&c.s.cus))) return rc;
     const HeadShape& s = c.s;
     HeadWork w;
-    if ((rc = head_space(c, false, cus, &w))) return rc;
+    if ((rc = head_space(c, false, &w))) return rc;
     rc = by_dtype(s.dtype, [&](auto dt) -> int {
         constexpr int DT = decltype(dt)::value;
         const bool direct = s.direct(false);
@@ -282,12 +304,12 @@ int head_forward(const HeadCall& c) {
         p.K = s.K ? (int)s.K : 1;
         p.V = (int)s.V;
         p.part = w.part;
-        p.pitch = s.pitch(cus);
+        p.pitch = s.pitch();
         p.z_out = s.K ? c.z : w.z;
         int rc2 = TIDE_OK;
         if (direct) {
             if constexpr (DT == kF32)
-                rc2 = s.T <= 16 ? launch_head<kF32, kF32, kHeadStats, HeadTile16F>(s.T, s.V, c.st, p) : s.T <= 32 ? launch_head<kF32, kF32, kHeadStats, HeadTile32F>(s.T, s.V, c.st, p) : s.T <= 48 ? launch_head<kF32, kF32, kHeadStats, HeadTile48F>(s.T, s.V, c.st, p)
+                rc2 = s.T <= 16 ? launch_head<kF32, kF32, kHeadStats, HeadTile16F>(s.T, s.V, c.st, p) : s.T <= 32 ? launch_head<kF32, kF32, kHeadStats, HeadTile32F>(s.T, s.V, c.st, p) : s.T <= 48 || (s.T > 64 && s.T <= 96) ? launch_head<kF32, kF32, kHeadStats, HeadTile48F>(s.T, s.V, c.st, p)
                      : launch_head<kF32, kF32, kHeadStats, HeadTile64F>(s.T, s.V, c.st, p);
         } else {
             rc2 = by_head_tile(s.rows_per_tile(), [&](auto tile) { return launch_head<kHeadElem<DT>, DT, kHeadStats, decltype(tile)>(s.T, s.V, c.st, p); });
@@ -295,7 +317,7 @@ int head_forward(const HeadCall& c) {
         if (rc2) return rc2;
         HeadFinishParams f{};
         f.part = w.part;
-        f.parts = (int)s.parts(cus);
+        f.parts = (int)s.parts();
         f.T = (int)s.T;
         f.K = p.K;
         f.V = (int)s.V;
@@ -313,14 +335,13 @@ int head_forward(const HeadCall& c) {
     return TIDE_OK;
 }
 
-int head_backward(const HeadCall& c) {
+int head_backward(HeadCall& c) {
     int rc = check_head(c, true);
     if (rc || (!c.dx && !c.dW)) return rc;
-    unsigned cus = 0;
-    if ((rc = resident_cus(&cus))) return rc;
+    if ((rc = resident_cus(&c.s.cus))) return rc;
     const HeadShape& s = c.s;
     HeadWork w;
-    if ((rc = head_space(c, true, cus, &w))) return rc;
+    if ((rc = head_space(c, true, &w))) return rc;
     rc = by_dtype(s.dtype, [&](auto dt) -> int {
         constexpr int DT = decltype(dt)::value, E = kHeadElem<DT>;
         HeadCtlParams cp{};
@@ -347,12 +368,12 @@ int head_backward(const HeadCall& c) {
         cp.place = w.place;
         cp.row_const = w.row_const;
         hipLaunchKernelGGL(tide_head_ctl_kernel, dim3(1), dim3(kHeadCtlThreads), 0, c.st, cp);
-        head_copy<DT>(s, c.x, c.x_stride, s.T, w.source, w.ctl, 0, w.x, c.st);
+        head_copy<DT>(s, c.x, c.x_stride, s.T, w.source, w.ctl, 0, w.x, c.st, s.stacked());
         if (s.copied(true)) head_copy<DT>(s, c.W, c.w_stride, s.V, nullptr, w.ctl, 1, w.w, c.st);
         const HeadOperand x = head_operand(s, nullptr, 0, w.x, s.T), W = head_operand(s, c.W, c.w_stride, w.w, s.V);
         const int64_t piece = s.piece(), g_plane = s.T * piece * 2;
-        const HeadOperand g{{w.g, w.g + (s.planes() - 1) * g_plane}, piece * 2};
-        const int slices = s.dx_slices(cus);
+        const HeadOperand g{{w.g, w.g + (s.g_planes() - 1) * g_plane}, piece * 2};     // (the second plane's rows follow the first's)
+        const int slices = s.dx_slices(), dw_slices = s.dw_slices();
         for (int64_t v0 = 0; v0 < s.V; v0 += piece) {
             const int64_t width = std::min(piece, s.V - v0);
             const HeadOperand Wv{{W.plane[0] + v0 * W.row_bytes, W.plane[1] + v0 * W.row_bytes}, W.row_bytes};
@@ -377,7 +398,8 @@ int head_backward(const HeadCall& c) {
                 a.wanted = w.wanted;
                 a.g_out = w.g;
                 a.g_row_bytes = g.row_bytes;
-                a.g_plane_bytes = g_plane;
+                a.g_plane_bytes = s.g_planes() == 2 ? g_plane : 0;
+                a.stacked = (int)s.stacked();
                 rc2 = by_head_tile(s.rows_per_tile(), [&](auto tile) { return launch_head<E, DT, kHeadGrad, decltype(tile)>(s.T, width, c.st, a); });
                 if (rc2) return rc2;
             }
@@ -385,15 +407,16 @@ int head_backward(const HeadCall& c) {
                 HeadGemmParams a = p;
                 a.q = g;
                 a.p = Wv;
+                a.stacked = (int)s.stacked();
                 a.q_rows = (int)s.T;
                 a.p_rows = (int)s.dp();
                 a.k = (int)width;
                 a.k_slices = slices;
                 a.acc_out = w.acc;
-                a.acc_slice = s.T * s.dp();
+                a.acc_slice = (s.T + s.stacked()) * s.dp();
                 a.acc_ld = (int)s.dp();
                 a.accumulate = v0 != 0;
-                rc2 = by_head_rows(s.rows_per_tile(), [&](auto tile) { return launch_head<E, E, kHeadRows, decltype(tile)>(s.T, s.dp(), c.st, a); });
+                rc2 = by_head_rows(s.rows_of_dx(), [&](auto tile) { return launch_head<E, E, kHeadRows, decltype(tile)>(s.T + s.stacked(), s.dp(), c.st, a); });
                 if (rc2) return rc2;
             }
             if (c.dW) {
@@ -403,14 +426,24 @@ int head_backward(const HeadCall& c) {
                 a.q_rows = (int)width;
                 a.p_rows = (int)s.d;
                 a.k = (int)s.T;
+                a.stacked = (int)s.stacked();
                 a.out = (char*)c.dW + v0 * c.dw_stride * Storage<DT>::kBytes;
                 a.out_row_elems = c.dw_stride;
                 a.out_aligned = chunked_rows(s.dtype, s.d);
+                if (dw_slices > 1) {
+                    a.k_slices = dw_slices;
+                    a.acc_out = w.dw;
+                    a.acc_slice = piece * s.dp();
+                    a.acc_ld = (int)s.dp();
+                }
                 if ((rc2 = launch_head<E, DT, kHeadWeights, HeadTile256>(width, s.d, c.st, a))) return rc2;
+                if (dw_slices > 1)
+                    hipLaunchKernelGGL((tide_head_dx_kernel<DT>), dim3((unsigned)std::min<int64_t>(width, 4096)), dim3(kHeadRowThreads), 0, c.st, w.dw, dw_slices, piece * s.dp(),
+                                       (int)s.dp(), 0, (const int32_t*)nullptr, w.ctl, (int)width, (int)s.d, a.out, c.dw_stride * Storage<DT>::kBytes);
             }
         }
         if (s.T && c.dx)
-            hipLaunchKernelGGL((tide_head_dx_kernel<DT>), dim3((unsigned)std::min<int64_t>(s.T, 4096)), dim3(kHeadRowThreads), 0, c.st, w.acc, slices, s.T * s.dp(), (int)s.dp(), w.place,
+            hipLaunchKernelGGL((tide_head_dx_kernel<DT>), dim3((unsigned)std::min<int64_t>(s.T, 4096)), dim3(kHeadRowThreads), 0, c.st, w.acc, slices, (s.T + s.stacked()) * s.dp(), (int)s.dp(), (int)s.stacked(), w.place,
                                w.ctl, (int)s.T, (int)s.d, (char*)c.dx, c.dx_stride * Storage<DT>::kBytes);
         return TIDE_OK;
     });
@@ -448,14 +481,13 @@ size_t tide_head_workspace_bytes(int dtype, int64_t T, int64_t d, int64_t V, int
     c.values = c.lse_in = c.grad = (const float*)some;
     c.loss = c.lse = c.z = (float*)some;
     if (check_head(c, gradient != 0)) return 0;
-    unsigned cus = 256;             // without a device: the answer for a 256-CU one
-    int dev = 0;
+    int dev = 0;                    // without a device: the answer for a 256-CU one
     if (hipGetDevice(&dev) == hipSuccess) {
-        if (resident_cus(&cus) != TIDE_OK) cus = 256;
+        if (resident_cus(&c.s.cus) != TIDE_OK) c.s.cus = 256;
     } else {
         (void)hipGetLastError();
     }
-    return head_layout(c.s, gradient != 0, cus, nullptr, nullptr);
+    return head_layout(c.s, gradient != 0, nullptr, nullptr);
 }
 
 int tide_head_loss(const void* x, int dtype, int64_t T, int64_t d, int64_t V, int64_t x_row_stride, const void* W, int64_t w_row_stride, const int32_t* target, float* loss,

@@ -20,17 +20,17 @@ __global__ __launch_bounds__(kHeadRowThreads) void tide_head_max_kernel(const ch
     uint32_t m = 0;
     const bool chunks = ((uintptr_t)rows | (uintptr_t)row_bytes) % 16 == 0 && d % 4 == 0;
     auto take = [&](uint32_t b) { b &= 0x7fffffffu; m = b < 0x7f800000u && b > m ? b : m; };
-    if (chunks) {                                      // contiguous rows as one, four chunks a thread at a time
+    if (chunks) {                                      // contiguous rows as one, eight chunks a thread at a time
         const bool flat = row_bytes == (int64_t)d * 4;
         const int64_t n = flat ? 1 : n_rows, per_row = flat ? n_rows * (d / 4) : d / 4, step = (int64_t)gridDim.x * kHeadRowThreads;
         for (int64_t r = 0; r < n; ++r) {
             const u32x4* row = reinterpret_cast<const u32x4*>(rows + r * row_bytes);
-            for (int64_t i = (int64_t)blockIdx.x * kHeadRowThreads + threadIdx.x; i < per_row; i += 4 * step) {
-                u32x4 v[4];
+            for (int64_t i = (int64_t)blockIdx.x * kHeadRowThreads + threadIdx.x; i < per_row; i += 8 * step) {
+                u32x4 v[8];
 #pragma unroll
-                for (int u = 0; u < 4; ++u) v[u] = row[min(i + u * step, per_row - 1)];
+                for (int u = 0; u < 8; ++u) v[u] = row[min(i + u * step, per_row - 1)];
 #pragma unroll
-                for (int u = 0; u < 4; ++u) take(v[u][0]), take(v[u][1]), take(v[u][2]), take(v[u][3]);
+                for (int u = 0; u < 8; ++u) take(v[u][0]), take(v[u][1]), take(v[u][2]), take(v[u][3]);
             }
         }
     } else {
@@ -132,11 +132,12 @@ __global__ __launch_bounds__(kHeadCtlThreads) void tide_head_ctl_kernel(const He
 }
 
 // Rows into the form the products read: gathered (source != null), padded with zeros to whole 16-byte chunks, fp32 ones as two fp16 planes.
+// stacked != 0: every row a second time, `stacked` rows on, and zeros in the rows from the last one to there.
 // A workgroup has rows_each rows, taken as one list of chunks, four a thread at a time.
 template <int DT>
 __global__ __launch_bounds__(kHeadRowThreads) void tide_head_copy_kernel(const char* rows, int64_t row_bytes, int64_t n_rows, int rows_each, int d, const int32_t* source,
-                                                                         const HeadCtl* ctl, int weights, char* out, int64_t out_row_bytes, int64_t plane_bytes) {
-    const int64_t n = source ? ctl->live : n_rows, r0 = (int64_t)blockIdx.x * rows_each;
+                                                                         const HeadCtl* ctl, int weights, int stacked, char* out, int64_t out_row_bytes, int64_t plane_bytes) {
+    const int64_t live = source ? ctl->live : n_rows, n = stacked ? stacked : live, r0 = (int64_t)blockIdx.x * rows_each;
     if (r0 >= n) return;
     const float scale = DT == kF32 ? (weights ? ctl->w_scale : ctl->x_scale) : 1.0f;
     const bool chunks = ((uintptr_t)rows | (uintptr_t)row_bytes) % 16 == 0 && d % 8 == 0;
@@ -151,7 +152,12 @@ __global__ __launch_bounds__(kHeadRowThreads) void tide_head_copy_kernel(const c
             const int i = min(i0 + u * kHeadRowThreads, total - 1), q = i / per_row;
             r[u] = r0 + q;
             c[u] = i - q * per_row;
-            const char* row = rows + (source ? (int64_t)source[r[u]] : r[u]) * row_bytes;
+            const char* row = rows + (source ? (int64_t)source[max((int64_t)0, min(r[u], live - 1))] : r[u]) * row_bytes;
+            if (r[u] >= live) {
+#pragma unroll
+                for (int w = 0; w < kW; ++w) v[u][w] = u32x4{0, 0, 0, 0};
+                continue;
+            }
             if (chunks) {
 #pragma unroll
                 for (int w = 0; w < kW; ++w) v[u][w] = reinterpret_cast<const u32x4*>(row)[c[u] * kW + w];
@@ -173,6 +179,7 @@ __global__ __launch_bounds__(kHeadRowThreads) void tide_head_copy_kernel(const c
             char* to = out + r[u] * out_row_bytes;
             if constexpr (DT != kF32) {
                 reinterpret_cast<u32x4*>(to)[c[u]] = v[u][0];
+                if (stacked) reinterpret_cast<u32x4*>(to + stacked * out_row_bytes)[c[u]] = v[u][0];
             } else {
                 f16x8 hi, lo;
 #pragma unroll
@@ -296,23 +303,36 @@ __global__ __launch_bounds__(1024) void tide_head_finish_kernel(const HeadFinish
     }
 }
 
-// dx: the k slices' sums in order, scaled back, rounded once to the storage type; zeros in the rows that have no gradient.
+// dx, and dW where its k is in slices (place == null: every row is there): the slices' sums in order, scaled back, rounded once to the storage type; zeros in
+// the rows that have no gradient.
 template <int DT>
-__global__ __launch_bounds__(kHeadRowThreads) void tide_head_dx_kernel(const float* acc, int slices, int64_t slice, int acc_ld, const int32_t* place, const HeadCtl* ctl, int T, int d,
+__global__ __launch_bounds__(kHeadRowThreads) void tide_head_dx_kernel(const float* acc, int slices, int64_t slice, int acc_ld, int stacked, const int32_t* place, const HeadCtl* ctl, int T, int d,
                                                                        char* out, int64_t out_row_bytes) {
-    const float back = ctl->row_back;
+    const float back = place ? ctl->row_back : ctl->weight_back;
     const bool chunks = ((uintptr_t)out | (uintptr_t)out_row_bytes) % 16 == 0 && d % 8 == 0;
     for (int t = blockIdx.x; t < T; t += gridDim.x) {
-        const int i = place[t];
+        const int i = place ? place[t] : t;
         char* to = out + (int64_t)t * out_row_bytes;
         for (int c = threadIdx.x; c < acc_ld / 8; c += kHeadRowThreads) {
             f32x4 a = {0, 0, 0, 0}, b = a;
-            if (i >= 0)
-                for (int s = 0; s < slices; ++s) {
-                    const f32x4* from = reinterpret_cast<const f32x4*>(acc + s * slice + (int64_t)i * acc_ld + 8 * c);
-                    a += from[0];
-                    b += from[1];
-                }
+            if (i >= 0) {
+                const float* from = acc + (int64_t)i * acc_ld + 8 * c;
+                auto add = [&](const float* from) {        // eight slices' loads at a time, added in order
+                    for (int s0 = 0; s0 < slices; s0 += 8) {
+                        f32x4 v[8][2];
+#pragma unroll
+                        for (int u = 0; u < 8; ++u) {
+                            const f32x4* at = reinterpret_cast<const f32x4*>(from + min(s0 + u, slices - 1) * slice);
+                            v[u][0] = at[0], v[u][1] = at[1];
+                        }
+#pragma unroll
+                        for (int u = 0; u < 8; ++u)
+                            if (s0 + u < slices) a += v[u][0], b += v[u][1];
+                    }
+                };
+                add(from);
+                if (stacked) add(from + (int64_t)stacked * acc_ld);        // the part of G's second plane
+            }
             a *= back;
             b *= back;
             if (chunks) {
