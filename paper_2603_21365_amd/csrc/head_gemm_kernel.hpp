@@ -1,17 +1,17 @@
 // The matrix products of the head operators: z = x W^T of rows x [T, d] under an LM head W [V, d], what a softmax over the V
 // columns needs of z, and the two products of its gradient.  The logits are never kept: they are made a tile at a time, in
 // registers, and leave as
-//   kHeadStats   per row and 32 kBP columns the maximum and the sum of exponentials, and the logits of the row's own few tokens;
-//   kHeadGrad    G = (softmax - wanted) * scale of a piece of the vocabulary, in 16 bits, for the two products that follow;
+//   kHeadStats   per row, of a tile's or a wave's columns, the maximum and the sum of exponentials relative to it, and the logits of the row's own few tokens;
+//   kHeadGrad    G = (softmax - wanted) * scale of a piece of the vocabulary, in 16 bits (or two planes of 16), for the two products that follow;
 //   kHeadRows    dx += G W over that piece (fp32, a buffer per k slice);
-//   kHeadWeights dW = G^T x of that piece, complete.
+//   kHeadWeights dW = G^T x of that piece, complete, or in k slices where its tiles are few.
 // The gradient makes the logits a second time, so a training step is four products where one that keeps T x V logits has three.
 //
-// One tile of kQ x kP output elements per workgroup of eight waves, k in stages of 64 elements.  "q" is the operand whose rows are
+// One tile of kQ x kP output elements per workgroup of eight waves, k in stages of 64 elements (fp32 rows: 32).  "q" is the operand whose rows are
 // the output's rows, "p" the one whose rows are its columns: a matrix-core step takes the p fragment first, so a lane holds ONE
 // output row and, in its registers, runs of four consecutive columns (softmax: sums over columns stay in the lane).
 //
-// Both operands go through LDS by direct transfers (16 bytes a lane, no registers), a ring of kStages stages; what lies outside the operand is
+// Both operands go through LDS by direct transfers (16 bytes a lane, no registers), a ring of stages for each; what lies outside the operand is
 // fetched as zeros by the buffer descriptor's bound, so ragged rows, columns and k cost no instruction in the loop.  An operand
 // whose k runs along memory rows (x, W in the logits; G in dx) is read as fragments of 16 bytes; one whose k runs ACROSS memory rows
 // (W in dx; G and x in dW) lies in LDS as it lies in memory and is read by the transposing LDS loads, so no transposed copy of
@@ -27,7 +27,8 @@
 // a memory row: with 64 every cache line came twice from L2, and the CU's load path was the bound (4.0 ms).
 //
 // fp32 operands are taken apart into two fp16 planes, x * 2^s = hi + lo + O(2^-23 x) with one power of two per tensor, and a product is three
-// passes over k: hi hi + hi lo + lo hi (what is dropped is 2^-22 of a term at most).  The fp32 matrix instructions have 1/16 of the 16-bit rate.
+// passes over k: hi hi + hi lo + lo hi (what is dropped is 2^-22 of a term at most).  The fp32 matrix instructions have 1/16 of the 16-bit rate;
+// the forward call on few rows takes them all the same, on the rows as they are, as there reading W is the bound.
 #pragma once
 #include <type_traits>
 

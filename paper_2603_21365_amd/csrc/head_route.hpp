@@ -5,8 +5,8 @@
 namespace {
 
 // The tile that the rows of a call take.  Few rows: the products with x W^T are bound by reading W, so their tiles are 128 columns wide and leave half of a
-// CU's LDS, so that two workgroups are there and one's first and last stages overlap with the other's (256 columns, one workgroup: 44 us for 32003 x 768 in
-// fp32, 125 tiles on 256 CUs, 34 as 251 of 128).  dx reads W across and stays 256 wide.
+// CU's LDS, so that two workgroups are there and one's first and last stages overlap with the other's (bf16, T = 33, d = 8192,
+// V = 20000: 110 us as 79 tiles of 256 columns, 83 as 157 of 128).  dx reads W across and stays 256 wide.
 using HeadTile32 = HeadTile<1, 8, 2, 1, 4, 4>;
 using HeadTile64 = HeadTile<2, 4, 2, 2, 3, 3>;
 using HeadTile16F = HeadTile<1, 8, 1, 1, 4, 4, 4>;      // fp32 rows as they are
@@ -78,8 +78,8 @@ struct HeadShape {
     int64_t stacked() const { return dtype != TIDE_F32 && g_planes() == 2 ? T : 0; }
     int rows_of_dx() const { return rows_for(T + stacked()); }
     int64_t col_tiles() const { return (V + kHeadCols - 1) / kHeadCols; }
-    // Columns of a tile of the statistics.  Few rows: as many tiles as the narrowest multiple of the CUs that holds them, so that each CU reads as much of W
-    // (bf16, d = 4096, V = 128000: 1000 tiles of 128 columns 186 us / 1024 of 125 180; fp32, T = 17, d = 768, V = 32003: 251 of 128 32.0 / 256 of 126 31.1).
+    // Rows and columns of a tile of the statistics.  Few rows: as many tiles as the narrowest multiple of the CUs that holds them, so that each CU reads as much of W
+    // (bf16, d = 4096, V = 128000: 1000 tiles of 128 columns 186 us / 1024 of 125 180).
     int stats_rows() const { return direct(false) ? std::min(rows_for(T), 64) : rows_per_tile(); }
     int pitch() const {
         const int rows = stats_rows();
