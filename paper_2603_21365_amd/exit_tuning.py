@@ -31,7 +31,8 @@ def exit_step(hidden, final_hidden, exit_layer, layer_ids, norm_gain, eps, head,
         taught = (target >= 0) & (target < head.shape[0])
         loss, lse = tr.head_loss(rows, head, target)
     else:
-        taught = (teacher[1] >= 0).any(1)
+        values, ids = teacher
+        taught = ((ids >= 0) & (ids < head.shape[0]) & (values != -torch.inf)).any(1)      # the entries that head_distill counts
         loss, lse, _ = tr.head_distill(rows, head, *teacher, tau)
     count = taught.sum().clamp(min=1)
     grad_loss = taught.to(torch.float32) * (loss_scale / count)
