@@ -293,7 +293,7 @@ __global__ __launch_bounds__(1024) void tide_head_finish_kernel(const HeadFinish
             z[k] = 0.0f;
         } else if (values[k] != -INFINITY) {
             const float log_q = values[k] * inv_tau - h.m - h.log_sum, q = expf(log_q);
-            sum += q > 0.0f ? q * (log_q + (m - z[k]) * inv_tau + log_s) : 0.0f;
+            sum += q == 0.0f ? 0.0f : q * (log_q + (m - z[k]) * inv_tau + log_s);      // (a NaN among the values is the row's loss, as it is its gradient)
         }
     }
     sum = wave_sum(sum);
