@@ -195,9 +195,10 @@ __global__ __launch_bounds__(kHeadRowThreads) void tide_head_copy_kernel(const c
     }
 }
 
-// The teacher of one row: a wave, lanes over its K entries.  An entry counts if its token is one of the vocabulary's and its value is not -inf.
+// The teacher of one row: a wave, lanes over its K entries.  An entry counts if its token is one of the vocabulary's and its value is not -inf.  Differences from
+// the largest value are taken before they are divided by tau: a row of the type's lowest value, which masks are made of, would overflow at tau < 1 otherwise.
 struct HeadTeacher {
-    float m, log_sum;          // largest value / tau and log of the sum of exp(value / tau - m)
+    float m, log_sum;          // largest value and log of the sum of exp((value - m) / tau)
     bool any;
 };
 __device__ __forceinline__ float head_wave_max(float v) {
@@ -211,12 +212,12 @@ __device__ __forceinline__ HeadTeacher head_teacher(const float* values, const i
     for (int k = lane; k < K; k += kWave)
         if ((uint32_t)ids[k] < (uint32_t)V && values[k] != -INFINITY) {
             any = true;
-            m = fmaxf(m, values[k] * inv_tau);
+            m = fmaxf(m, values[k]);
         }
     m = head_wave_max(m);
     float s = 0.0f;
     for (int k = lane; k < K; k += kWave)
-        if ((uint32_t)ids[k] < (uint32_t)V && values[k] != -INFINITY) s += expf(values[k] * inv_tau - m);
+        if ((uint32_t)ids[k] < (uint32_t)V && values[k] != -INFINITY) s += expf((values[k] - m) * inv_tau);
     return HeadTeacher{m, logf(wave_sum(s)), __any(any) != 0};
 }
 
@@ -229,7 +230,7 @@ __global__ __launch_bounds__(kHeadRowThreads) void tide_head_teacher_kernel(cons
     const HeadTeacher h = head_teacher(values, ids, K, V, inv_tau, lane);
     for (int k = lane; k < K; k += kWave) {
         const bool there = (uint32_t)ids[k] < (uint32_t)V && values[k] != -INFINITY;
-        wanted[k] = there ? expf(values[k] * inv_tau - h.m - h.log_sum) : 0.0f;
+        wanted[k] = there ? expf((values[k] - h.m) * inv_tau - h.log_sum) : 0.0f;
     }
     if (lane == 0) taught[t] = h.any;
 }
@@ -292,7 +293,7 @@ __global__ __launch_bounds__(1024) void tide_head_finish_kernel(const HeadFinish
         if ((uint32_t)ids[k] >= (uint32_t)p.V) {
             z[k] = 0.0f;
         } else if (values[k] != -INFINITY) {
-            const float log_q = values[k] * inv_tau - h.m - h.log_sum, q = expf(log_q);
+            const float log_q = (values[k] - h.m) * inv_tau - h.log_sum, q = expf(log_q);
             sum += q == 0.0f ? 0.0f : q * (log_q + (m - z[k]) * inv_tau + log_s);      // (a NaN among the values is the row's loss, as it is its gradient)
         }
     }
