@@ -26,8 +26,10 @@
 // tell the ring's slots apart.  They have no output registers; they are ordered by explicit counts and the phases' barriers.  A stage is 128 bytes of
 // a memory row: with 64 every cache line came twice from L2, and the CU's load path was the bound (4.0 ms).
 //
-// fp32 operands are taken apart into two fp16 planes, x * 2^s = hi + lo + O(2^-23 x) with one power of two per tensor, and a product is three
-// passes over k: hi hi + hi lo + lo hi (what is dropped is 2^-22 of a term at most).  The fp32 matrix instructions have 1/16 of the 16-bit rate;
+// fp32 operands are taken apart into two fp16 planes, x * 2^s = hi + lo + O(2^-23 x), and a product is three passes over k: hi hi + hi lo + lo hi
+// (what is dropped is 2^-22 of a term at most).  s is one for W; a row of x has its own in the logits, and a row of G its own, so that no row's size reaches
+// another row's loss or dx.  dW adds up rows of G and x: there a row of x takes 2^c less the power that its row of G has, with one c for the call, so that the
+// largest |g x| sets the scale.  The fp32 matrix instructions have 1/16 of the 16-bit rate;
 // the forward call on few rows takes them all the same, on the rows as they are, as there reading W is the bound.
 #pragma once
 #include <type_traits>
@@ -42,9 +44,8 @@ enum : int { kHeadStats = 0, kHeadGrad = 1, kHeadRows = 2, kHeadWeights = 3 };
 // What one call finds out on the device before its products (head_rows_kernel.hpp).
 struct HeadCtl {
     int live;                      // rows that have a gradient
-    float x_scale, w_scale;        // powers of two that fp32 operands are multiplied by
-    float logit_scale;             // what the products of the logits are multiplied by (the planes' scales taken back)
-    float row_back, weight_back;   // the same for dx and dW
+    int w_exp;                     // the power of two that W was multiplied by (fp32)
+    int dw_exp;                    // the same of dW's sums
 };
 
 constexpr int kHeadRowBytes = 128;                   // of a row along k in a stage: a whole cache line
@@ -61,13 +62,14 @@ struct HeadGemmParams {
     int tiles_p, k_slices;
     int pitch;                 // columns of a tile: kP, or fewer (statistics) where that gives every CU as many
     const HeadCtl* ctl;        // null where nothing is scaled and every row counts (16-bit statistics)
+    const int32_t* q_exp;      // logits of planes: [q_rows] the power of two that a row of x was multiplied by
     // statistics and G
     float c1;                  // log2(e) / tau
     const int32_t* ids;        // [T][K] the tokens' own entries of the vocabulary; others than 0 .. V - 1: none
-    int K, V, v0;              // p row 0 is token v0
+    int K, v0;                 // p row 0 is token v0
     float2* part;              // statistics: [tiles_p * kParts][q_rows] largest logit and sum of exp((logit - it) / tau)
     float* z_out;              // statistics: [q_rows][K]
-    const float4* row_const;   // G: lse * log2 e, scale, and as an integer the target (wanted == null) or the token, of each row
+    const float4* row_const;   // G: of each row lse * log2 e, grad * tau * 2^s, and as integers the target (wanted == null) or the token, and s
     const float* wanted;       // G: [T][K] or null (one)
     char* g_out;               // G: rounded to 16 bits, and (g_plane_bytes != 0) what that leaves in a second plane
     int64_t g_row_bytes, g_plane_bytes;
@@ -184,6 +186,7 @@ template <int DT> __device__ __forceinline__ uint32_t head_round2(float a, float
     }
 }
 
+__device__ __forceinline__ f32x4 head_shifted(f32x4 v, int n) { return f32x4{ldexpf(v[0], n), ldexpf(v[1], n), ldexpf(v[2], n), ldexpf(v[3], n)}; }
 template <int DT> __device__ __forceinline__ float head_rounded(float v) {
     if constexpr (DT == kF16) return (float)static_cast<_Float16>(v);
     else return (float)static_cast<__bf16>(v);
@@ -265,7 +268,7 @@ __device__ __forceinline__ u32x4 head_gather8(uint32_t a0, uint32_t a1, uint32_t
     return u32x4{a0, a1, b0, b1};
 }
 
-// DT: the operands' element type, kF16 or kBF16 (kF32: fp32 rows as they are, statistics of few rows only).  OutDT: the type dW is written in.
+// DT: the operands' element type, kF16 or kBF16 (kF32: fp32 rows as they are, statistics of few rows only).  OutDT: the caller's type (kF32 over kF16: planes).
 // dx and dW: a workgroup per CU, which goes through its share of the tiles and requests the first stages of the next one before it deals with the results of
 // the last (dW of 290 live rows, d = 4096, V = 128000: 627 / 596 us).  The others: a workgroup per tile; their results need LDS and loads, and gathering them in
 // registers with the next stages under way is 3 to 6 % slower.
@@ -273,6 +276,7 @@ template <int kMode, class Tile> constexpr bool kLoops = Tile::kTurns && (kMode 
 template <int DT, int OutDT, int kMode, class Tile>
 __global__ __launch_bounds__(Tile::kThreads) void tide_head_gemm_kernel(const HeadGemmParams p) {
     constexpr bool kQAcross = kMode == kHeadWeights, kPAcross = kMode == kHeadRows || kMode == kHeadWeights;
+    constexpr bool kPlanes = DT != OutDT;
     constexpr int kBQ = Tile::kBQ, kBP = Tile::kBP, kCols = Tile::kCols;
     typedef HeadFeed<Tile::kQ, kQAcross, Tile::kWaves, Tile::kEB> FeedQ;
     typedef HeadFeed<Tile::kP, kPAcross, Tile::kWaves, Tile::kEB> FeedP;
@@ -450,6 +454,14 @@ __global__ __launch_bounds__(Tile::kThreads) void tide_head_gemm_kernel(const He
         }
         return mine;
     };
+    // The logits of row t, of the products of its plane and W's.  (Not a factor: 2^s of a small row under a small W would overflow.)
+    auto planes_back = [&](int j, int t) {
+        const int back = -(p.ctl->w_exp + p.q_exp[min(t, q_rows - 1)]);
+#pragma unroll
+        for (int i = 0; i < kBP; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[i][j][e] = ldexpf(acc[i][j][e], back);
+    };
     auto results = [&](int q0, int p0, int p_end, int slice) {
         const int col0 = p0 + wp * kCols;                  // the wave's first column
         const bool ragged = col0 + kCols > p_end;
@@ -457,7 +469,7 @@ __global__ __launch_bounds__(Tile::kThreads) void tide_head_gemm_kernel(const He
         for (int j = 0; j < kBQ; ++j) {
             const int t = q0 + (wq * kBQ + j) * 16 + row;
             if constexpr (kMode == kHeadStats) {
-                const float scale = p.ctl ? p.ctl->logit_scale : 1.0f, c1 = p.c1 * scale;
+                if constexpr (kPlanes) planes_back(j, t);
                 if (ragged) {
 #pragma unroll
                     for (int i = 0; i < kBP; ++i)
@@ -477,9 +489,8 @@ __global__ __launch_bounds__(Tile::kThreads) void tide_head_gemm_kernel(const He
 #pragma unroll
                 for (int i = 0; i < kBP; ++i)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) s += __builtin_amdgcn_exp2f((acc[i][j][e] - shift) * c1);
+                    for (int e = 0; e < 4; ++e) s += __builtin_amdgcn_exp2f((acc[i][j][e] - shift) * p.c1);
                 s = add_xor<32>(add_xor<16>(s));
-                m *= scale;
                 if constexpr (Tile::kJoined) {                // with the other waves' columns, below
                     if (h == 0) joined[wp * Tile::kQ + (wq * kBQ + j) * 16 + row] = f32x2{m, s};
                 } else {
@@ -502,19 +513,19 @@ __global__ __launch_bounds__(Tile::kThreads) void tide_head_gemm_kernel(const He
                     lds_fence();
                     for (; mine != 0; mine &= mine - 1) {
                         const int k = k0 + __builtin_ctz(mine);
-                        p.z_out[(int64_t)t * p.K + k] = stage[row * Tile::kLd + ids[k] - col0] * scale;
+                        p.z_out[(int64_t)t * p.K + k] = stage[row * Tile::kLd + ids[k] - col0];
                     }
                     lds_fence();
                 }
             } else if constexpr (kMode == kHeadGrad) {
-                const float c1 = p.c1 * p.ctl->logit_scale;
+                if constexpr (kPlanes) planes_back(j, t);
                 const int t_in = min(t, q_rows - 1);
                 const float4 rc = p.row_const[t_in];
                 const int own = __float_as_int(rc.z);
 #pragma unroll
                 for (int i = 0; i < kBP; ++i)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) acc[i][j][e] = t < q_rows ? rc.y * __builtin_amdgcn_exp2f(fmaf(acc[i][j][e], c1, -rc.x)) : 0.0f;
+                    for (int e = 0; e < 4; ++e) acc[i][j][e] = t < q_rows ? rc.y * __builtin_amdgcn_exp2f(fmaf(acc[i][j][e], p.c1, -rc.x)) : 0.0f;
                 if (ragged) {
 #pragma unroll
                     for (int i = 0; i < kBP; ++i)
@@ -582,7 +593,8 @@ __global__ __launch_bounds__(Tile::kThreads) void tide_head_gemm_kernel(const He
                     }
                     continue;
                 }
-                const float back = p.ctl->weight_back;
+                const int shift = -p.ctl->dw_exp;
+                auto back = [shift](f32x4 v) { return OutDT == kBF16 ? v : head_shifted(v, shift); };      // (bf16: G has no scale)
                 constexpr int kBytes = Storage<OutDT>::kBytes;
                 char* dst = p.out + (int64_t)t * p.out_row_elems * kBytes;
                 if (p.out_aligned) {
@@ -590,12 +602,12 @@ __global__ __launch_bounds__(Tile::kThreads) void tide_head_gemm_kernel(const He
 #pragma unroll
                         for (int i = 0; i < kBP; ++i) {
                             const int c = col0 + 16 * i + 4 * h;
-                            if (t < q_rows && c < p.p_rows) *reinterpret_cast<f32x4*>(dst + c * 4) = acc[i][j] * back;
+                            if (t < q_rows && c < p.p_rows) *reinterpret_cast<f32x4*>(dst + c * 4) = back(acc[i][j]);
                         }
                     } else {
 #pragma unroll
                         for (int i = 0; i < kBP; i += 2) {
-                            const f32x4 a = acc[i][j] * back, b = acc[i + 1][j] * back;
+                            const f32x4 a = back(acc[i][j]), b = back(acc[i + 1][j]);
                             const u32x4 v = head_gather8(head_round2<OutDT>(a[0], a[1]), head_round2<OutDT>(a[2], a[3]), head_round2<OutDT>(b[0], b[1]), head_round2<OutDT>(b[2], b[3]));
                             const int c = col0 + 16 * i + 8 * h;
                             if (t < q_rows && c < p.p_rows) *reinterpret_cast<u32x4*>(dst + c * 2) = v;
@@ -603,12 +615,14 @@ __global__ __launch_bounds__(Tile::kThreads) void tide_head_gemm_kernel(const He
                     }
                 } else {
 #pragma unroll
-                    for (int i = 0; i < kBP; ++i)
+                    for (int i = 0; i < kBP; ++i) {
+                        const f32x4 v = back(acc[i][j]);
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
                             const int c = col0 + 16 * i + 4 * h + e;
-                            if (t < q_rows && c < p.p_rows) head_put<OutDT>(dst, c, acc[i][j][e] * back);
+                            if (t < q_rows && c < p.p_rows) head_put<OutDT>(dst, c, v[e]);
                         }
+                    }
                 }
             }
         }

@@ -123,8 +123,10 @@ struct HeadSpace {
 };
 struct HeadWork {
     HeadCtl* ctl;
-    uint32_t *x_max, *w_max;
+    uint32_t* w_max;
+    int32_t *x_exp, *largest;  // fp32 planes: the rows' powers of two, and what the workgroups found for dW's
     char *x, *w;               // copies: the rows (of the gradient: the live ones), the weights
+    char* x_dw;                // the rows as dW's sum takes them
     float2* part;
     float* z;
     int32_t *source, *place;
@@ -139,11 +141,13 @@ size_t head_layout(const HeadShape& s, bool grads, void* base, HeadWork* out) {
     HeadWork w{};
     w.ctl = sp.take<HeadCtl>(1);
     if (s.dtype == TIDE_F32 && !s.direct(grads)) {
-        w.x_max = sp.take<uint32_t>(kHeadMaxBlocks);
         w.w_max = sp.take<uint32_t>(kHeadMaxBlocks);
+        w.x_exp = sp.take<int32_t>((size_t)s.T);
+        if (grads) w.largest = sp.take<int32_t>(kHeadMaxBlocks);
     }
     if (s.copied(grads)) w.w = sp.take<char>((size_t)s.plane_bytes(s.V) * s.planes());
     if (s.copied(grads) || grads) w.x = sp.take<char>((size_t)s.plane_bytes(std::max(s.T + (grads ? s.stacked() : 0), grads && s.T > 64 ? (int64_t)128 : 0)) * s.planes());
+    w.x_dw = s.dtype == TIDE_F32 && grads ? sp.take<char>((size_t)s.plane_bytes(s.T) * 2) : w.x;
     if (!grads) {
         w.part = sp.take<float2>((size_t)s.parts() * s.T);
         if (!s.K) w.z = sp.take<float>((size_t)s.T);
@@ -251,15 +255,26 @@ int head_space(const HeadCall& c, bool grads, HeadWork* w) {
 
 // Rows per workgroup of the copies: 2048 chunks of eight elements, eight a thread.
 int64_t head_copy_rows(int64_t chunks) { return std::max<int64_t>(1, 8 * kHeadRowThreads / chunks); }
-template <int DT> void head_max(const void* rows, int64_t stride, int64_t n, int64_t d, uint32_t* out, int* blocks, hipStream_t st) {
+void head_max(const void* rows, int64_t stride, int64_t n, int64_t d, uint32_t* out, int* blocks, hipStream_t st) {
     *blocks = (int)std::min<int64_t>(n, kHeadMaxBlocks);
     if (*blocks) hipLaunchKernelGGL(tide_head_max_kernel, dim3(*blocks), dim3(kHeadRowThreads), 0, st, (const char*)rows, stride * 4, n, (int)d, out);
 }
-template <int DT> void head_copy(const HeadShape& s, const void* rows, int64_t stride, int64_t n, const int32_t* source, const HeadCtl* ctl, int weights, char* out, hipStream_t st, int64_t stacked = 0) {
+template <int DT> void head_copy(const HeadShape& s, const void* rows, int64_t stride, int64_t n, const int32_t* source, const HeadWork& w, const float4* row_const, int blocks, char* out, hipStream_t st,
+                                 int64_t stacked = 0) {
     if (n == 0) return;
     const int64_t rows_each = head_copy_rows(s.dp() / 8);
     hipLaunchKernelGGL((tide_head_copy_kernel<DT>), dim3((unsigned)((n + rows_each - 1) / rows_each)), dim3(kHeadRowThreads), 0, st, (const char*)rows, stride * Storage<DT>::kBytes, n, (int)rows_each,
-                       (int)s.d, source, ctl, weights, (int)stacked, out, s.dp() * 2, s.plane_bytes(n));
+                       (int)s.d, source, w.ctl, row_const, w.largest, blocks, (int)stacked, out, s.dp() * 2, s.plane_bytes(n));
+}
+// fp32 rows of x as planes for the logits; returns the workgroups, each of which leaves a greatest exponent where there are gradients (row_const).
+int head_rows(const HeadShape& s, const void* x, int64_t stride, const int32_t* source, const HeadWork& w, const float4* row_const, hipStream_t st) {
+    if (s.T == 0) return 0;
+    const bool wave_rows = s.dp() <= 2048;
+    const unsigned blocks = (unsigned)std::min<int64_t>(wave_rows ? (s.T + 3) / 4 : s.T, kHeadMaxBlocks);
+    auto kernel = wave_rows ? &tide_head_rows_kernel<true> : &tide_head_rows_kernel<false>;
+    hipLaunchKernelGGL(kernel, dim3(blocks), dim3(kHeadRowThreads), 0, st, (const char*)x, stride * 4, (int)s.T, (int)s.d, source, w.ctl, row_const, w.x, s.dp() * 2, s.plane_bytes(s.T), w.x_exp,
+                       row_const ? w.largest : nullptr);
+    return (int)blocks;
 }
 // x or W as an operand: the caller's rows, or the copy's planes of n rows.
 HeadOperand head_operand(const HeadShape& s, const void* rows, int64_t stride, const char* copy, int64_t n) {
@@ -280,15 +295,14 @@ int head_forward(HeadCall& c) {
         if (DT == kF32 && !direct) {
             HeadCtlParams cp{};
             cp.ctl = w.ctl;
-            cp.x_max = w.x_max;
             cp.w_max = w.w_max;
-            head_max<DT>(c.x, c.x_stride, s.T, s.d, w.x_max, &cp.x_blocks, c.st);
-            head_max<DT>(c.W, c.w_stride, s.V, s.d, w.w_max, &cp.w_blocks, c.st);
+            head_max(c.W, c.w_stride, s.V, s.d, w.w_max, &cp.w_blocks, c.st);
             hipLaunchKernelGGL(tide_head_ctl_kernel, dim3(1), dim3(kHeadCtlThreads), 0, c.st, cp);
         }
         if (s.copied(false)) {
-            head_copy<DT>(s, c.x, c.x_stride, s.T, nullptr, w.ctl, 0, w.x, c.st);
-            head_copy<DT>(s, c.W, c.w_stride, s.V, nullptr, w.ctl, 1, w.w, c.st);
+            if (DT == kF32) head_rows(s, c.x, c.x_stride, nullptr, w, nullptr, c.st);
+            else head_copy<DT>(s, c.x, c.x_stride, s.T, nullptr, w, nullptr, 0, w.x, c.st);
+            head_copy<DT>(s, c.W, c.w_stride, s.V, nullptr, w, nullptr, 0, w.w, c.st);
         }
         HeadGemmParams p{};
         p.q = head_operand(s, c.x, c.x_stride, w.x, s.T);
@@ -299,10 +313,10 @@ int head_forward(HeadCall& c) {
         p.segments = DT == kF32 && !direct ? 3 : 1;
         p.k_slices = 1;
         p.ctl = DT == kF32 && !direct ? w.ctl : nullptr;
+        p.q_exp = w.x_exp;
         p.c1 = 1.4426950408889634f / c.tau;
         p.ids = c.ids;
         p.K = s.K ? (int)s.K : 1;
-        p.V = (int)s.V;
         p.part = w.part;
         p.pitch = s.pitch();
         p.z_out = s.K ? c.z : w.z;
@@ -346,17 +360,13 @@ int head_backward(HeadCall& c) {
         constexpr int DT = decltype(dt)::value, E = kHeadElem<DT>;
         HeadCtlParams cp{};
         cp.ctl = w.ctl;
-        cp.x_max = w.x_max;
         cp.w_max = w.w_max;
-        if constexpr (DT == kF32) {
-            head_max<DT>(c.x, c.x_stride, s.T, s.d, w.x_max, &cp.x_blocks, c.st);
-            head_max<DT>(c.W, c.w_stride, s.V, s.d, w.w_max, &cp.w_blocks, c.st);
-        }
+        if constexpr (DT == kF32) head_max(c.W, c.w_stride, s.V, s.d, w.w_max, &cp.w_blocks, c.st);
         if (s.K && s.T)
             hipLaunchKernelGGL(tide_head_teacher_kernel, dim3((unsigned)((s.T + 3) / 4)), dim3(kHeadRowThreads), 0, c.st, c.values, c.ids, (int)s.T, (int)s.K, (int)s.V,
                                1.0f / c.tau, w.wanted, w.taught);
         cp.grads = 1;
-        cp.scale_grad = E == kF16;
+        cp.grad_scale = DT == kF32 ? (int)kHeadGradOwn : DT == kF16 ? (int)kHeadGradCommon : (int)kHeadGradAsIs;
         cp.T = (int)s.T;
         cp.V = (int)s.V;
         cp.target = s.K ? nullptr : c.ids;
@@ -368,9 +378,14 @@ int head_backward(HeadCall& c) {
         cp.place = w.place;
         cp.row_const = w.row_const;
         hipLaunchKernelGGL(tide_head_ctl_kernel, dim3(1), dim3(kHeadCtlThreads), 0, c.st, cp);
-        head_copy<DT>(s, c.x, c.x_stride, s.T, w.source, w.ctl, 0, w.x, c.st, s.stacked());
-        if (s.copied(true)) head_copy<DT>(s, c.W, c.w_stride, s.V, nullptr, w.ctl, 1, w.w, c.st);
-        const HeadOperand x = head_operand(s, nullptr, 0, w.x, s.T), W = head_operand(s, c.W, c.w_stride, w.w, s.V);
+        if constexpr (DT == kF32) {
+            const int blocks = head_rows(s, c.x, c.x_stride, w.source, w, w.row_const, c.st);
+            if (c.dW) head_copy<DT>(s, c.x, c.x_stride, s.T, w.source, w, w.row_const, blocks, w.x_dw, c.st);
+        } else {
+            head_copy<DT>(s, c.x, c.x_stride, s.T, w.source, w, nullptr, 0, w.x, c.st, s.stacked());
+        }
+        if (s.copied(true)) head_copy<DT>(s, c.W, c.w_stride, s.V, nullptr, w, nullptr, 0, w.w, c.st);
+        const HeadOperand x = head_operand(s, nullptr, 0, w.x, s.T), x_dw = head_operand(s, nullptr, 0, w.x_dw, s.T), W = head_operand(s, c.W, c.w_stride, w.w, s.V);
         const int64_t piece = s.piece(), g_plane = s.T * piece * 2;
         const HeadOperand g{{w.g, w.g + (s.g_planes() - 1) * g_plane}, piece * 2};     // (the second plane's rows follow the first's)
         const int slices = s.dx_slices(), dw_slices = s.dw_slices();
@@ -392,8 +407,8 @@ int head_backward(HeadCall& c) {
                 a.c1 = 1.4426950408889634f / c.tau;
                 a.ids = c.ids;
                 a.K = s.K ? (int)s.K : 1;
-                a.V = (int)s.V;
                 a.v0 = (int)v0;
+                a.q_exp = w.x_exp;
                 a.row_const = w.row_const;
                 a.wanted = w.wanted;
                 a.g_out = w.g;
@@ -416,13 +431,13 @@ int head_backward(HeadCall& c) {
                 a.acc_slice = (s.T + s.stacked()) * s.dp();
                 a.acc_ld = (int)s.dp();
                 a.accumulate = v0 != 0;
-                rc2 = by_head_rows(s.rows_of_dx(), [&](auto tile) { return launch_head<E, E, kHeadRows, decltype(tile)>(s.T + s.stacked(), s.dp(), c.st, a); });
+                rc2 = by_head_rows(s.rows_of_dx(), [&](auto tile) { return launch_head<E, DT, kHeadRows, decltype(tile)>(s.T + s.stacked(), s.dp(), c.st, a); });
                 if (rc2) return rc2;
             }
             if (c.dW) {
                 HeadGemmParams a = p;
                 a.q = g;
-                a.p = x;
+                a.p = x_dw;
                 a.q_rows = (int)width;
                 a.p_rows = (int)s.d;
                 a.k = (int)s.T;
@@ -439,12 +454,12 @@ int head_backward(HeadCall& c) {
                 if ((rc2 = launch_head<E, DT, kHeadWeights, HeadTile256>(width, s.d, c.st, a))) return rc2;
                 if (dw_slices > 1)
                     hipLaunchKernelGGL((tide_head_dx_kernel<DT>), dim3((unsigned)std::min<int64_t>(width, 4096)), dim3(kHeadRowThreads), 0, c.st, w.dw, dw_slices, piece * s.dp(),
-                                       (int)s.dp(), 0, (const int32_t*)nullptr, w.ctl, (int)width, (int)s.d, a.out, c.dw_stride * Storage<DT>::kBytes);
+                                       (int)s.dp(), 0, (const int32_t*)nullptr, (const float4*)nullptr, w.ctl, (int)width, (int)s.d, a.out, c.dw_stride * Storage<DT>::kBytes);
             }
         }
         if (s.T && c.dx)
             hipLaunchKernelGGL((tide_head_dx_kernel<DT>), dim3((unsigned)std::min<int64_t>(s.T, 4096)), dim3(kHeadRowThreads), 0, c.st, w.acc, slices, (s.T + s.stacked()) * s.dp(), (int)s.dp(), (int)s.stacked(), w.place,
-                               w.ctl, (int)s.T, (int)s.d, (char*)c.dx, c.dx_stride * Storage<DT>::kBytes);
+                               w.row_const, w.ctl, (int)s.T, (int)s.d, (char*)c.dx, c.dx_stride * Storage<DT>::kBytes);
         return TIDE_OK;
     });
     if (rc) return rc;

@@ -13,7 +13,7 @@ constexpr int kHeadRowThreads = 256;
 constexpr int kHeadCtlThreads = 1024;
 constexpr int kHeadMaxBlocks = 2048;       // workgroups that search for the largest magnitude
 
-// Largest finite magnitude of fp32 rows, one per workgroup (as bits: the order of non-negative floats).  Infinities and NaN are passed
+// Largest finite magnitude of W, one per workgroup (as bits: the order of non-negative floats).  Infinities and NaN are passed
 // over: they give what they give whatever the scale, and must not cost the other rows theirs.
 __global__ __launch_bounds__(kHeadRowThreads) void tide_head_max_kernel(const char* rows, int64_t row_bytes, int64_t n_rows, int d, uint32_t* out) {
     __shared__ uint32_t part[4];
@@ -44,19 +44,16 @@ __global__ __launch_bounds__(kHeadRowThreads) void tide_head_max_kernel(const ch
     if (threadIdx.x == 0) out[blockIdx.x] = max(max(part[0], part[1]), max(part[2], part[3]));
 }
 
-// The power of two that brings a largest magnitude into [2^14, 2^15): the upper end of fp16, so that small elements keep their bits.
-__device__ __forceinline__ float head_scale(uint32_t max_bits) {
-    const int e = (int)(max_bits >> 23) - 127;
-    if (max_bits == 0 || e > 127) return 1.0f;
-    return ldexpf(1.0f, min(110, 14 - e));
-}
+// The power of two that brings a largest magnitude into [2^14, 2^15): the upper end of fp16, so that small elements keep their bits.  (0 for none, or none finite.)
+__device__ __forceinline__ int head_exponent(uint32_t max_bits) { return max_bits == 0 || max_bits >= 0x7f800000u ? 0 : 141 - max(1, (int)(max_bits >> 23)); }
 
+enum : int { kHeadGradAsIs = 0, kHeadGradCommon = 1, kHeadGradOwn = 2 };      // the power of two that a row of G is multiplied by: none, one for all, its own
 struct HeadCtlParams {
     HeadCtl* ctl;
-    const uint32_t *x_max, *w_max;   // fp32: the workgroups' maxima
-    int x_blocks, w_blocks;
-    int grads;                 // 0: scales only
-    int scale_grad;            // G is held in fp16
+    const uint32_t* w_max;     // fp32: the workgroups' maxima
+    int w_blocks;
+    int grads;                 // 0: W's scale only
+    int grad_scale;            // kHeadGrad..., as G is held in bf16, in fp16, or in planes
     int T, V;
     const int32_t* target;     // [T], or null and
     const uint8_t* taught;     // [T] whether the teacher has entries
@@ -65,17 +62,16 @@ struct HeadCtlParams {
     float tau;
     int32_t* source;           // [T] out: the live rows' tokens, ascending
     int32_t* place;            // [T] out: a token's live row, or -1
-    float4* row_const;         // [T] out, of live rows: lse * log2 e, grad * tau * grad_scale, the target or the token, -
+    float4* row_const;         // [T] out, of live rows: lse * log2 e, grad * tau * 2^s, and as integers the target or the token, and s
 };
 
-// One workgroup: the scales, and the list of live rows in token order (each thread a run of tokens).
+// One workgroup: W's and the gradients' scales, and the list of live rows in token order (each thread a run of tokens).
 __global__ __launch_bounds__(kHeadCtlThreads) void tide_head_ctl_kernel(const HeadCtlParams p) {
-    __shared__ uint32_t max_of[3][16];
+    __shared__ uint32_t max_of[2][16];
     __shared__ int count_of[16];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    uint32_t m[3] = {0, 0, 0};
-    for (int i = tid; i < p.x_blocks; i += kHeadCtlThreads) m[0] = max(m[0], p.x_max[i]);
-    for (int i = tid; i < p.w_blocks; i += kHeadCtlThreads) m[1] = max(m[1], p.w_max[i]);
+    uint32_t m[2] = {0, 0};
+    for (int i = tid; i < p.w_blocks; i += kHeadCtlThreads) m[0] = max(m[0], p.w_max[i]);
     const int per = p.grads ? (p.T + kHeadCtlThreads - 1) / kHeadCtlThreads : 0;
     const int t0 = min(p.T, tid * per), t1 = min(p.T, t0 + per);
     auto live = [&](int t) {
@@ -87,10 +83,10 @@ __global__ __launch_bounds__(kHeadCtlThreads) void tide_head_ctl_kernel(const He
     for (int t = t0; t < t1; ++t)
         if (live(t)) {
             ++n;
-            m[2] = max(m[2], __float_as_uint(fabsf(p.grad[t] * p.tau)));
+            m[1] = max(m[1], __float_as_uint(fabsf(p.grad[t] * p.tau)));
         }
 #pragma unroll
-    for (int j = 0; j < 3; ++j) {
+    for (int j = 0; j < 2; ++j) {
 #pragma unroll
         for (int s = 1; s < kWave; s <<= 1) m[j] = max(m[j], (uint32_t)__shfl_xor((int)m[j], s, kWave));
         if (lane == 0) max_of[j][wave] = m[j];
@@ -107,39 +103,87 @@ __global__ __launch_bounds__(kHeadCtlThreads) void tide_head_ctl_kernel(const He
     for (int w = 0; w < 16; ++w) {
         all += count_of[w];
         if (w < wave) before += count_of[w];
-        for (int j = 0; j < 3; ++j) m[j] = max(m[j], max_of[j][w]);
+        for (int j = 0; j < 2; ++j) m[j] = max(m[j], max_of[j][w]);
     }
-    const float sx = head_scale(m[0]), sw = head_scale(m[1]), sg = p.scale_grad ? head_scale(m[2]) : 1.0f;
+    const int common = p.grad_scale == kHeadGradCommon ? head_exponent(m[1]) : 0;
     for (int t = t0; t < t1; ++t) {
         const bool l = live(t);
         p.place[t] = l ? before : -1;
         if (l) {
+            const float g = p.grad[t] * p.tau;
+            const int s = p.grad_scale == kHeadGradOwn ? head_exponent(__float_as_uint(fabsf(g))) : common;
             p.source[before] = t;
-            p.row_const[before] = float4{p.lse[t] * 1.4426950408889634f, p.grad[t] * p.tau * sg, __int_as_float(p.target ? p.target[t] : t), 0.0f};
+            p.row_const[before] = float4{p.lse[t] * 1.4426950408889634f, ldexpf(g, s), __int_as_float(p.target ? p.target[t] : t), __int_as_float(s)};
             ++before;
         }
     }
     if (tid == 0) {
         HeadCtl c;
         c.live = all;
-        c.x_scale = sx;
-        c.w_scale = sw;
-        c.logit_scale = (float)fmin(1.0 / ((double)sx * sw), 1e38);
-        c.row_back = (float)fmin(1.0 / ((double)sg * sw), 1e38);
-        c.weight_back = (float)fmin(1.0 / ((double)sg * sx), 1e38);
+        c.w_exp = head_exponent(m[0]);
+        c.dw_exp = common;
         *p.ctl = c;
     }
 }
 
+// Chunk c (eight elements) of a row, zeros beyond d.  chunks: whole chunks at 16-byte addresses.
+template <int DT> __device__ __forceinline__ void head_load8(const char* row, int c, int d, bool chunks, u32x4 (&v)[DT == kF32 ? 2 : 1]) {
+    constexpr int kW = DT == kF32 ? 2 : 1;             // 16-byte pieces of a chunk's source
+    if (chunks) {
+#pragma unroll
+        for (int w = 0; w < kW; ++w) v[w] = reinterpret_cast<const u32x4*>(row)[c * kW + w];
+    } else if constexpr (DT == kF32) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e / 4][e & 3] = 8 * c + e < d ? reinterpret_cast<const uint32_t*>(row)[8 * c + e] : 0u;
+    } else {
+        const uint16_t* e = reinterpret_cast<const uint16_t*>(row) + 8 * c;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const uint32_t lo = 8 * c + 2 * k < d ? e[2 * k] : 0, hi = 8 * c + 2 * k + 1 < d ? e[2 * k + 1] : 0;
+            v[0][k] = lo | hi << 16;
+        }
+    }
+}
+// The chunk times 2^n as two fp16 planes.
+__device__ __forceinline__ void head_split8(const u32x4 (&v)[2], int n, char* hi_row, char* lo_row, int c) {
+    f16x8 hi, lo;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const float x = ldexpf(__uint_as_float(v[e / 4][e & 3]), n);
+        hi[e] = static_cast<_Float16>(x);
+        lo[e] = static_cast<_Float16>(x - (float)hi[e]);       // the difference is exact
+    }
+    reinterpret_cast<u32x4*>(hi_row)[c] = __builtin_bit_cast(u32x4, hi);
+    reinterpret_cast<u32x4*>(lo_row)[c] = __builtin_bit_cast(u32x4, lo);
+}
+
 // Rows into the form the products read: gathered (source != null), padded with zeros to whole 16-byte chunks, fp32 ones as two fp16 planes.
 // stacked != 0: every row a second time, `stacked` rows on, and zeros in the rows from the last one to there.
+// fp32: row_const == null: W, times 2^w_exp; otherwise the rows of x for dW, each times 2^(dw_exp - its row of G's): what is worked out here of `largest`, the
+// greatest exponents that tide_head_rows_kernel's workgroups have found.
 // A workgroup has rows_each rows, taken as one list of chunks, four a thread at a time.
 template <int DT>
 __global__ __launch_bounds__(kHeadRowThreads) void tide_head_copy_kernel(const char* rows, int64_t row_bytes, int64_t n_rows, int rows_each, int d, const int32_t* source,
-                                                                         const HeadCtl* ctl, int weights, int stacked, char* out, int64_t out_row_bytes, int64_t plane_bytes) {
+                                                                         HeadCtl* ctl, const float4* row_const, const int32_t* largest, int blocks, int stacked, char* out,
+                                                                         int64_t out_row_bytes, int64_t plane_bytes) {
     const int64_t live = source ? ctl->live : n_rows, n = stacked ? stacked : live, r0 = (int64_t)blockIdx.x * rows_each;
     if (r0 >= n) return;
-    const float scale = DT == kF32 ? (weights ? ctl->w_scale : ctl->x_scale) : 1.0f;
+    int scale = 0;
+    if constexpr (DT == kF32) {
+        scale = ctl->w_exp;
+        if (row_const) {
+            __shared__ int part[4];
+            int most = INT_MIN;
+            for (int i = threadIdx.x; i < blocks; i += kHeadRowThreads) most = max(most, largest[i]);
+#pragma unroll
+            for (int s = 1; s < kWave; s <<= 1) most = max(most, __shfl_xor(most, s, kWave));
+            if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = most;
+            __syncthreads();
+            most = max(max(part[0], part[1]), max(part[2], part[3]));
+            scale = most == INT_MIN ? 0 : 14 - most;
+            if (blockIdx.x == 0 && threadIdx.x == 0) ctl->dw_exp = scale;
+        }
+    }
     const bool chunks = ((uintptr_t)rows | (uintptr_t)row_bytes) % 16 == 0 && d % 8 == 0;
     const int per_row = (int)(out_row_bytes / 16), total = (int)min((int64_t)rows_each, n - r0) * per_row;
     constexpr int kU = 4, kW = DT == kF32 ? 2 : 1;     // 16-byte pieces of a chunk's source
@@ -158,20 +202,7 @@ __global__ __launch_bounds__(kHeadRowThreads) void tide_head_copy_kernel(const c
                 for (int w = 0; w < kW; ++w) v[u][w] = u32x4{0, 0, 0, 0};
                 continue;
             }
-            if (chunks) {
-#pragma unroll
-                for (int w = 0; w < kW; ++w) v[u][w] = reinterpret_cast<const u32x4*>(row)[c[u] * kW + w];
-            } else if constexpr (DT == kF32) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[u][e / 4][e & 3] = 8 * c[u] + e < d ? reinterpret_cast<const uint32_t*>(row)[8 * c[u] + e] : 0u;
-            } else {
-                const uint16_t* e = reinterpret_cast<const uint16_t*>(row) + 8 * c[u];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const uint32_t lo = 8 * c[u] + 2 * k < d ? e[2 * k] : 0, hi = 8 * c[u] + 2 * k + 1 < d ? e[2 * k + 1] : 0;
-                    v[u][0][k] = lo | hi << 16;
-                }
-            }
+            head_load8<DT>(row, c[u], d, chunks, v[u]);
         }
 #pragma unroll
         for (int u = 0; u < kU; ++u) {
@@ -181,18 +212,59 @@ __global__ __launch_bounds__(kHeadRowThreads) void tide_head_copy_kernel(const c
                 reinterpret_cast<u32x4*>(to)[c[u]] = v[u][0];
                 if (stacked) reinterpret_cast<u32x4*>(to + stacked * out_row_bytes)[c[u]] = v[u][0];
             } else {
-                f16x8 hi, lo;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float x = __uint_as_float(v[u][e / 4][e & 3]) * scale;
-                    hi[e] = static_cast<_Float16>(x);
-                    lo[e] = static_cast<_Float16>(x - (float)hi[e]);       // the difference is exact
-                }
-                reinterpret_cast<u32x4*>(to)[c[u]] = __builtin_bit_cast(u32x4, hi);
-                reinterpret_cast<u32x4*>(to + plane_bytes)[c[u]] = __builtin_bit_cast(u32x4, lo);
+                head_split8(v[u], row_const ? scale - __float_as_int(row_const[r[u]].w) : scale, to, to + plane_bytes, c[u]);
             }
         }
     }
+}
+
+// fp32 rows of x for the logits, as planes: gathered (source != null), padded, each times the power of two that suits its own largest finite magnitude, so that
+// a row's size is no other row's matter.  largest (with row_const): per workgroup, the greatest exponent of a row's largest magnitude less its row of G's power.
+// A row per workgroup; kWavePerRow: a wave (d up to 2048: four chunks a lane at most).  The second read of a row is a cache's.
+template <bool kWavePerRow>
+__global__ __launch_bounds__(kHeadRowThreads) void tide_head_rows_kernel(const char* rows, int64_t row_bytes, int n_rows, int d, const int32_t* source, const HeadCtl* ctl,
+                                                                         const float4* row_const, char* out, int64_t out_row_bytes, int64_t plane_bytes, int32_t* exps, int32_t* largest) {
+    constexpr int kStep = kWavePerRow ? kWave : kHeadRowThreads, kRows = kWavePerRow ? 4 : 1;
+    __shared__ uint32_t part[2][4];
+    __shared__ int most_of[4];
+    const int wave = threadIdx.x >> 6, tid = kWavePerRow ? threadIdx.x & 63 : threadIdx.x;
+    const int live = source ? ctl->live : n_rows, per_row = (int)(out_row_bytes / 16);
+    const bool chunks = ((uintptr_t)rows | (uintptr_t)row_bytes) % 16 == 0 && d % 8 == 0;
+    int most = INT_MIN, turn = 0;
+    for (int r = blockIdx.x * kRows + (kWavePerRow ? wave : 0); r < live; r += gridDim.x * kRows) {
+        const char* row = rows + (int64_t)(source ? source[r] : r) * row_bytes;
+        uint32_t m = 0;
+        for (int c = tid; c < per_row; c += kStep) {
+            u32x4 v[2];
+            head_load8<kF32>(row, c, d, chunks, v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const uint32_t b = v[e / 4][e & 3] & 0x7fffffffu;
+                m = b < 0x7f800000u && b > m ? b : m;
+            }
+        }
+#pragma unroll
+        for (int s = 1; s < kWave; s <<= 1) m = max(m, (uint32_t)__shfl_xor((int)m, s, kWave));
+        if constexpr (!kWavePerRow) {
+            if ((threadIdx.x & 63) == 0) part[turn][wave] = m;
+            __syncthreads();                           // one barrier a row: the next row's maxima go into the other half
+            m = max(max(part[turn][0], part[turn][1]), max(part[turn][2], part[turn][3]));
+            turn ^= 1;
+        }
+        const int n = head_exponent(m);
+        if (m != 0 && row_const) most = max(most, 14 - n - __float_as_int(row_const[r].w));
+        if (tid == 0) exps[r] = n;
+        char* to = out + r * out_row_bytes;
+        for (int c = tid; c < per_row; c += kStep) {
+            u32x4 v[2];
+            head_load8<kF32>(row, c, d, chunks, v);
+            head_split8(v, n, to, to + plane_bytes, c);
+        }
+    }
+    if (!largest) return;
+    if ((threadIdx.x & 63) == 0) most_of[wave] = most;
+    __syncthreads();
+    if (threadIdx.x == 0) largest[blockIdx.x] = max(max(most_of[0], most_of[1]), max(most_of[2], most_of[3]));
 }
 
 // The teacher of one row: a wave, lanes over its K entries.  An entry counts if its token is one of the vocabulary's and its value is not -inf.  Differences from
@@ -307,12 +379,12 @@ __global__ __launch_bounds__(1024) void tide_head_finish_kernel(const HeadFinish
 // dx, and dW where its k is in slices (place == null: every row is there): the slices' sums in order, scaled back, rounded once to the storage type; zeros in
 // the rows that have no gradient.
 template <int DT>
-__global__ __launch_bounds__(kHeadRowThreads) void tide_head_dx_kernel(const float* acc, int slices, int64_t slice, int acc_ld, int stacked, const int32_t* place, const HeadCtl* ctl, int T, int d,
-                                                                       char* out, int64_t out_row_bytes) {
-    const float back = place ? ctl->row_back : ctl->weight_back;
+__global__ __launch_bounds__(kHeadRowThreads) void tide_head_dx_kernel(const float* acc, int slices, int64_t slice, int acc_ld, int stacked, const int32_t* place,
+                                                                       const float4* row_const, const HeadCtl* ctl, int T, int d, char* out, int64_t out_row_bytes) {
     const bool chunks = ((uintptr_t)out | (uintptr_t)out_row_bytes) % 16 == 0 && d % 8 == 0;
     for (int t = blockIdx.x; t < T; t += gridDim.x) {
         const int i = place ? place[t] : t;
+        const int back = !place ? -ctl->dw_exp : i >= 0 ? -(ctl->w_exp + __float_as_int(row_const[i].w)) : 0;
         char* to = out + (int64_t)t * out_row_bytes;
         for (int c = threadIdx.x; c < acc_ld / 8; c += kHeadRowThreads) {
             f32x4 a = {0, 0, 0, 0}, b = a;
@@ -334,8 +406,8 @@ __global__ __launch_bounds__(kHeadRowThreads) void tide_head_dx_kernel(const flo
                 add(from);
                 if (stacked) add(from + (int64_t)stacked * acc_ld);        // the part of G's second plane
             }
-            a *= back;
-            b *= back;
+            a = head_shifted(a, back);
+            b = head_shifted(b, back);
             if (chunks) {
                 if constexpr (DT == kF32) {
                     reinterpret_cast<f32x4*>(to)[2 * c] = a;
