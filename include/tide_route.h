@@ -275,7 +275,8 @@ int tide_exit_project_grad(const void* hidden, int dtype, int64_t C, int64_t T, 
                            float* grad_gain, void* workspace, size_t workspace_bytes, void* stream);
 
 /* ---- Head operators: what the rows of tide_exit_project are scored with and trained on under the LM head W [V, d].
- * z[t,v] = x_t . W_v is never stored; products of 16-bit values are exact and summed in fp32, fp32 operands are multiplied to about 22 bits or more.
+ * z[t,v] = x_t . W_v is never stored; products of 16-bit values are exact and summed in fp32; products of fp32 operands are off by at most 2^-21 of
+ * themselves, or, where a factor is that small, by 2^-49 of the product of the largest magnitudes (of the row of x or G, of the tensor W; in dW's sums of the largest |G x| of a row).
  *
  * tide_head_loss: softmax cross entropy of every row,
  *   lse[t] = log sum_v exp(z[t,v]),   loss[t] = lse[t] - z[t, target[t]],   0 where target[t] is not one of 0 .. V-1
@@ -289,7 +290,7 @@ int tide_exit_project_grad(const void* hidden, int dtype, int64_t C, int64_t T, 
  *   G[t,v] = grad_loss[t] * tau * (exp(z[t,v] / tau - lse[t]) - sum of q[t,k] over top_ids[t,k] == v),   dx = G W,   dW = G^T x
  *
  * Rows without a target (or whose teacher has no entry) and rows with grad_loss[t] == 0 get dx = 0 and add nothing to dW, whatever
- * they hold.  G is rounded once, to `dtype` (fp16 under a common power of two; fp32, and 16-bit types up to 64 rows, to twice as many bits); dx and dW are summed in fp32 and
+ * they hold.  G is rounded once, to `dtype` (fp16 under a common power of two; 16-bit types up to 64 rows to twice as many bits, fp32 as an operand above); dx and dW are summed in fp32 and
  * rounded once.  dx or dW may be NULL: that product is left out.  T == 0: dW is filled with zeros.  The results do not depend on timing.
  *
  *   x          device [T rows] of `dtype`;  W device [V rows] of `dtype`;  strides in elements, at most 4194304

@@ -26,8 +26,10 @@
 // tell the ring's slots apart.  They have no output registers; they are ordered by explicit counts and the phases' barriers.  A stage is 128 bytes of
 // a memory row: with 64 every cache line came twice from L2, and the CU's load path was the bound (4.0 ms).
 //
-// fp32 operands are taken apart into two fp16 planes, x * 2^s = hi + lo + O(2^-23 x), and a product is three passes over k: hi hi + hi lo + lo hi
-// (what is dropped is 2^-22 of a term at most).  s is one for W; a row of x has its own in the logits, and a row of G its own, so that no row's size reaches
+// fp32 operands are taken apart into two fp16 planes, x * 2^s = hi + 2^-12 lo + O(2^-23 x), and a product is three passes over k: hi lo + lo hi, whose sums are
+// multiplied by 2^-12, then hi hi (what is dropped is 2^-22 of a term at most).  With the largest magnitude in [2^14, 2^15) lo reaches the same, and the two hold
+// every value of more than 2^-30 of the largest to 22 bits and the others to 2^-51 of it (lo as it is: 2^-17 and 2^-39, and an improbable token, p = 1e-10,
+// had two decimal digits in its row of dW).  s is one for W; a row of x has its own in the logits, and a row of G its own, so that no row's size reaches
 // another row's loss or dx.  dW adds up rows of G and x: there a row of x takes 2^c less the power that its row of G has, with one c for the call, so that the
 // largest |g x| sets the scale.  The fp32 matrix instructions have 1/16 of the 16-bit rate;
 // the forward call on few rows takes them all the same, on the rows as they are, as there reading W is the bound.
@@ -99,6 +101,7 @@ template <int WQ, int WP, int BQ, int BP, int SQ, int SP, int EB = 2> struct Hea
     static_assert(kWaves == 8 && SP >= 2 && SQ >= SP, "two groups of four waves");
     static_assert(kLdsBytes <= 160 * 1024, "LDS of a CU");
 };
+constexpr float kHeadLow = 4096.0f;                  // what the second plane of an fp32 value holds its part multiplied by
 constexpr uint32_t kHeadNowhere = 0x80000000u;       // an offset at the descriptor's bound: fetched as zeros
 
 // 64 lanes x 16 bytes from memory (offsets voff from the descriptor's base) to 1 KiB of LDS at byte `lds`.
@@ -124,7 +127,8 @@ template <int kRows, bool kAcross, int kWaves, int kEB = 2> struct HeadFeed {
         return c ^ ((kr & 3) << 1 | (kr >> 3 & 1) << 3);
     }
 
-    __device__ __forceinline__ void init(const HeadOperand& o, int row0, int rows, int first, int wave, int lane) {
+    // plane: the one that the first segment takes
+    __device__ __forceinline__ void init(const HeadOperand& o, int plane, int row0, int rows, int first, int wave, int lane) {
 #pragma unroll
         for (int i = 0; i < kN; ++i) {
             const int n = wave + kWaves * i;
@@ -140,7 +144,7 @@ template <int kRows, bool kAcross, int kWaves, int kEB = 2> struct HeadFeed {
         }
         step = kAcross ? kK * o.row_bytes : kHeadRowBytes;
         issued = kk = fill = 0;
-        seek(o, 0, row0, first);
+        seek(o, plane, row0, first);
     }
     __device__ __forceinline__ void seek(const HeadOperand& o, int plane, int row0, int stage) {
         base = o.plane[plane] + (kAcross ? (int64_t)row0 * 2 : (int64_t)row0 * o.row_bytes) + stage * step;
@@ -290,7 +294,7 @@ __global__ __launch_bounds__(Tile::kThreads) void tide_head_gemm_kernel(const He
     const int tiles_q = (q_rows + Tile::kQ - 1) / Tile::kQ;
     const uint32_t lds_q = (uint32_t)(size_t)(head_lds*)smem, lds_p = lds_q + Tile::kSQ * Tile::kQBytes;
 
-    // ---- one tile's k loop: n stages, the slice's part of every segment: (hi, hi), (hi, lo), (lo, hi)
+    // ---- one tile's k loop: n stages, the slice's part of every segment: of planes (hi, lo), (lo, hi), (hi, hi)
     int tq, tp, slice, q0, p0, p_end, first, nk, n;
     FeedQ fq;
     FeedP fp;
@@ -300,12 +304,12 @@ __global__ __launch_bounds__(Tile::kThreads) void tide_head_gemm_kernel(const He
         first = (int)((int64_t)per * slice / p.k_slices);
         nk = (int)((int64_t)per * (slice + 1) / p.k_slices) - first;
         n = nk * p.segments;
-        fq.init(p.q, q0, q_rows, first, wave, lane);
-        fp.init(p.p, p0, p_end, first, wave, lane);
+        fq.init(p.q, 0, q0, q_rows, first, wave, lane);
+        fp.init(p.p, kPlanes, p0, p_end, first, wave, lane);
     };
     // Step s issues stage s + kSP of p, then stage s + kSQ of q.
-    auto issue_p = [&] { fp.template issue<Tile::kSP>(lds_p, p.p, 1, p0, n, nk, first, k_elems, wave); };
-    auto issue_q = [&] { fq.template issue<Tile::kSQ>(lds_q, p.q, 2, q0, n, nk, first, k_elems, wave); };
+    auto issue_p = [&] { fp.template issue<Tile::kSP>(lds_p, p.p, 0, p0, n, nk, first, k_elems, wave); };
+    auto issue_q = [&] { fq.template issue<Tile::kSQ>(lds_q, p.q, 1, q0, n, nk, first, k_elems, wave); };
     auto issue_first = [&] {
 #pragma unroll
         for (int s = -Tile::kSQ; s < -1; ++s) {
@@ -344,6 +348,16 @@ __global__ __launch_bounds__(Tile::kThreads) void tide_head_gemm_kernel(const He
 #pragma unroll
             for (int j = 0; j < kBQ; ++j) acc[i][j] = head_mma<DT>(ap[i], aq[j], acc[i][j]);
     };
+    // Planes, before stage k: where the passes with a second plane end, their sums take their place.
+    auto low_done = [&](int k) {
+        if constexpr (kPlanes) {
+            if (k == 2 * nk)
+#pragma unroll
+                for (int i = 0; i < kBP; ++i)
+#pragma unroll
+                    for (int j = 0; j < kBQ; ++j) acc[i][j] *= 1.0f / kHeadLow;
+        }
+    };
     constexpr std::integral_constant<int, 0> g0;
     constexpr std::integral_constant<int, 1> g1;
     auto k_loop = [&] {
@@ -361,6 +375,7 @@ __global__ __launch_bounds__(Tile::kThreads) void tide_head_gemm_kernel(const He
                 const int next_q = slot_q + Tile::kQBytes == Tile::kSQ * Tile::kQBytes ? 0 : slot_q + Tile::kQBytes;
                 const int next_p = slot_p + Tile::kPBytes == Tile::kSP * Tile::kPBytes ? 0 : slot_p + Tile::kPBytes;
                 auto edge = [] { __builtin_amdgcn_sched_barrier(0); ring_barrier(); __builtin_amdgcn_sched_barrier(0); };
+                low_done(k);
                 read(g0, slot_q, slot_p);
                 issue_p();
                 asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -397,6 +412,7 @@ __global__ __launch_bounds__(Tile::kThreads) void tide_head_gemm_kernel(const He
                     }
             };
             for (int k = 0; k < n; ++k) {
+                low_done(k);
                 landed();
                 asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // this wave has read all of stage k - 1, whose slot is filled next
                 ring_barrier();
@@ -565,8 +581,8 @@ __global__ __launch_bounds__(Tile::kThreads) void tide_head_gemm_kernel(const He
                         f32x4 x, y;
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
-                            x[e] = a[e] - head_rounded<DT>(a[e]);
-                            y[e] = b[e] - head_rounded<DT>(b[e]);
+                            x[e] = (a[e] - head_rounded<DT>(a[e])) * (kPlanes ? kHeadLow : 1.0f);
+                            y[e] = (b[e] - head_rounded<DT>(b[e])) * (kPlanes ? kHeadLow : 1.0f);
                         }
                         *reinterpret_cast<u32x4*>(dst + p.g_plane_bytes) = u32x4{head_round2<DT>(x[0], x[1]), head_round2<DT>(x[2], x[3]), head_round2<DT>(y[0], y[1]), head_round2<DT>(y[2], y[3])};
                     }

@@ -151,7 +151,7 @@ __device__ __forceinline__ void head_split8(const u32x4 (&v)[2], int n, char* hi
     for (int e = 0; e < 8; ++e) {
         const float x = ldexpf(__uint_as_float(v[e / 4][e & 3]), n);
         hi[e] = static_cast<_Float16>(x);
-        lo[e] = static_cast<_Float16>(x - (float)hi[e]);       // the difference is exact
+        lo[e] = static_cast<_Float16>((x - (float)hi[e]) * kHeadLow);      // the difference is exact
     }
     reinterpret_cast<u32x4*>(hi_row)[c] = __builtin_bit_cast(u32x4, hi);
     reinterpret_cast<u32x4*>(lo_row)[c] = __builtin_bit_cast(u32x4, lo);

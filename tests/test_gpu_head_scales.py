@@ -105,3 +105,54 @@ def test_rows_and_gradients_of_all_sizes(tr, T, d, V, K, tau):
     near("lse", lse, want.lse, want.tol_lse)
     near("dx", dx, want.dx, want.tol_dx)
     near("dW", dW, want.dW, want.tol_dW)
+
+
+# An fp32 operand's two halves: 2^-22 of the value, 2^-51 of the largest where that is more; of a product, what is dropped included, 2^-21 of it and 2^-49 of the
+# largest magnitudes' product.
+FLOOR = 2.0 ** -49
+
+
+@pytest.mark.parametrize("T,d,V", [(150, 96, 600), (300, 520, 300)])
+def test_rows_of_a_head_of_all_sizes(tr, T, d, V):
+    """Logits of the head's rows from 1 down to 2^-26 of the largest are as exact, each for itself."""
+    import torch
+    x, W, _, _, _, _ = make(torch.float32, T, d, V, 0, V)
+    W = (W * torch.exp2(-26 * torch.arange(V, device="cuda") / V)[:, None]).contiguous()
+    K = 300
+    ids = (torch.arange(K, device="cuda") * (V // K)).to(torch.int32).repeat(T, 1).contiguous()
+    values = torch.zeros(T, K, device="cuda")
+    print(f"[gpu-case] head sizes T={T} d={d} V={V}", flush=True)
+    _, _, z = tr.head_distill(x, W, values, ids, 1.0)
+    want, size = x.double() @ W.double().T, x.double().abs() @ W.double().abs().T
+    tol = (d * E + 2.0 ** -21) * size + d * FLOOR * x.double().abs().amax(1, keepdim=True) * W.double().abs().max()
+    near("z", z, want.gather(1, ids.long()), tol.gather(1, ids.long()))
+
+
+@pytest.mark.parametrize("T,d,V", [(20, 64, 400), (150, 64, 400), (400, 160, 999)])
+def test_improbable_tokens_keep_their_digits(tr, T, d, V):
+    """Tokens down to p = e^-24 in every row: their rows of dW hold what p holds, not 2^-39 of the largest gradient."""
+    import torch
+    x, W, _, _, _, grad = make(torch.float32, T, d, V, 0, d)
+    W = 0.2 * W
+    x[:, 0] = 8.0
+    W[:, 0] = -torch.arange(V, device="cuda") * (24.0 / 8 / V)
+    target = torch.zeros(T, dtype=torch.int32, device="cuda")
+    print(f"[gpu-case] improbable T={T} d={d} V={V}", flush=True)
+    _, lse = tr.head_loss(x, W, target)
+    _, dW = tr.head_loss_grad(x, W, target, lse, grad)
+    X, H, g = x.double(), W.double(), grad.double()[:, None]
+    z = X @ H.T
+    tol_z = (d * E + 2.0 ** -21) * (X.abs() @ H.abs().T) + d * FLOOR * X.abs().max() * H.abs().max()
+    exact_lse = torch.logsumexp(z, 1)
+    p = torch.exp(z - exact_lse[:, None])
+    assert p.min() < 2.0 ** -33
+    tol_p = (tol_z + tol_z.amax(1, keepdim=True) + 2 * 2.0 ** -20 * (1 + exact_lse.abs()[:, None]))      # z's error, lse's, and the exponential's
+    G = g * p
+    G[:, 0] -= g[:, 0]
+    tol_G = 2.0 ** -22 * G.abs() + g.abs() * (p * tol_p + 16 * E * p + FLOOR)
+    tol_G[:, 0] += 16 * E * g[:, 0].abs()
+    want = G.T @ X
+    tol = tol_G.T @ X.abs() + (T * E + 2.0 ** -21) * (G.T.abs() @ X.abs()) + T * FLOOR * (g.abs()[:, 0] * X.abs().amax(1)).max() + 1.01 * E * want.abs()
+    near("dW", dW, want, tol)
+    share = ((dW.double() - want).norm(dim=1) / want.norm(dim=1)).max().item()
+    print(f"HEAD largest error of a token's row of dW: {share:.2e}", flush=True)
