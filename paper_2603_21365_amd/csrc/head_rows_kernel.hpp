@@ -83,7 +83,8 @@ __global__ __launch_bounds__(kHeadCtlThreads) void tide_head_ctl_kernel(const He
     for (int t = t0; t < t1; ++t)
         if (live(t)) {
             ++n;
-            m[1] = max(m[1], __float_as_uint(fabsf(p.grad[t] * p.tau)));
+            const uint32_t b = __float_as_uint(fabsf(p.grad[t] * p.tau));
+            m[1] = b < 0x7f800000u ? max(m[1], b) : m[1];      // (a gradient that is not finite takes no other row's bits)
         }
 #pragma unroll
     for (int j = 0; j < 2; ++j) {

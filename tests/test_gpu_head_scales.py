@@ -156,3 +156,23 @@ def test_improbable_tokens_keep_their_digits(tr, T, d, V):
     near("dW", dW, want, tol)
     share = ((dW.double() - want).norm(dim=1) / want.norm(dim=1)).max().item()
     print(f"HEAD largest error of a token's row of dW: {share:.2e}", flush=True)
+
+
+@pytest.mark.parametrize("name", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("T", [40, 200])
+@pytest.mark.parametrize("bad", ["nan", "inf"])
+def test_a_gradient_that_is_not_finite_takes_no_other_rows_bits(tr, name, T, bad):
+    """The other rows' dx is bit for bit what it is without that row."""
+    import torch
+    from test_gpu_head import types
+    x, W, target, _, _, grad = make(types()[name], T, 64, 300, 0, 17)
+    grad = grad * 2.0 ** -18
+    grad[3] = 0.0
+    print(f"[gpu-case] gradient {bad} {name} T={T}", flush=True)
+    loss, lse = tr.head_loss(x, W, target)
+    want, _ = tr.head_loss_grad(x, W, target, lse, grad)
+    grad[3] = float(bad)
+    got, _ = tr.head_loss_grad(x, W, target, lse, grad)
+    others = torch.arange(T, device="cuda") != 3
+    assert (want[others] != 0).any() and torch.equal(got[others], want[others])
+    assert not got[3].isfinite().any()
