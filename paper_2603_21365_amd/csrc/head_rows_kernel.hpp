@@ -20,12 +20,13 @@ __global__ __launch_bounds__(kHeadRowThreads) void tide_head_max_kernel(const ch
     uint32_t m = 0;
     const bool chunks = ((uintptr_t)rows | (uintptr_t)row_bytes) % 16 == 0 && d % 4 == 0;
     auto take = [&](uint32_t b) { b &= 0x7fffffffu; m = b < 0x7f800000u && b > m ? b : m; };
-    if (chunks) {                                      // contiguous rows as one, eight chunks a thread at a time
+    if (chunks) {                                      // contiguous rows as one, else each workgroup rows of its own; eight chunks a thread at a time
         const bool flat = row_bytes == (int64_t)d * 4;
-        const int64_t n = flat ? 1 : n_rows, per_row = flat ? n_rows * (d / 4) : d / 4, step = (int64_t)gridDim.x * kHeadRowThreads;
-        for (int64_t r = 0; r < n; ++r) {
+        const int64_t n = flat ? 1 : n_rows, per_row = flat ? n_rows * (d / 4) : d / 4;
+        const int64_t first = flat ? (int64_t)blockIdx.x * kHeadRowThreads : 0, step = flat ? (int64_t)gridDim.x * kHeadRowThreads : kHeadRowThreads;
+        for (int64_t r = flat ? 0 : blockIdx.x; r < n; r += gridDim.x) {
             const u32x4* row = reinterpret_cast<const u32x4*>(rows + r * row_bytes);
-            for (int64_t i = (int64_t)blockIdx.x * kHeadRowThreads + threadIdx.x; i < per_row; i += 8 * step) {
+            for (int64_t i = first + threadIdx.x; i < per_row; i += 8 * step) {
                 u32x4 v[8];
 #pragma unroll
                 for (int u = 0; u < 8; ++u) v[u] = row[min(i + u * step, per_row - 1)];
