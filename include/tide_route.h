@@ -300,7 +300,8 @@ int tide_exit_project_grad(const void* hidden, int dtype, int64_t C, int64_t T, 
  *   loss, lse, grad_loss  device [T] fp32;  z_top device [T,K] fp32
  *   dx device [T rows], dW device [V rows] of `dtype`, aligned as x and W
  *   workspace  device, 256-byte aligned, tide_head_workspace_bytes(dtype, T, d, V, K, gradient) bytes (K = 0: the loss; gradient != 0: the _grad call).  It needs no
- *              initialisation and keeps nothing: calls on different workspaces may overlap.  The size is host arithmetic; 0 with tide_last_error() set if unsupported. */
+ *              initialisation and keeps nothing: calls on different workspaces may overlap.  The size is host arithmetic and grows with T: a
+ *              workspace for the most rows serves every smaller call of the same dtype, d, V, K and kind;  0 with tide_last_error() set if unsupported. */
 size_t tide_head_workspace_bytes(int dtype, int64_t T, int64_t d, int64_t V, int64_t K, int gradient);
 int tide_head_loss(const void* x, int dtype, int64_t T, int64_t d, int64_t V, int64_t x_row_stride, const void* W,
                    int64_t w_row_stride, const int32_t* target, float* loss, float* lse, void* workspace,

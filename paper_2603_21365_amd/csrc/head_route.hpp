@@ -109,6 +109,26 @@ struct HeadShape {
         const int64_t tiles = piece() / kHeadCols * ((d + kHeadCols - 1) / kHeadCols);
         return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(cus / tiles, 32), (T + 255) / 256));
     }
+    // What a workspace has room for: bounds of the sizes above that grow with T, so that a workspace for the most rows of a program serves every smaller call
+    // (tiles, pieces and slices change with T, and what they take goes up and down).
+    int64_t part_room() const {                        // parts() * T
+        const int64_t few = ((V + HeadTile32::kP - 1) / HeadTile32::kP + cus - 1) / cus * cus, many = (V + HeadTile64::kP - 1) / HeadTile64::kP + 1;
+        return T <= 64 ? few * T : std::max(few * 64, many * T);
+    }
+    int64_t g_room() const {                           // bytes of T * g_planes() * piece() elements
+        const int64_t rows = std::max<int64_t>(T * g_planes(), T > 64 ? 128 : 0);
+        return std::min(rows * col_tiles() * kHeadCols * 2, std::max((int64_t)kHeadPieceBytes, T * g_planes() * kHeadCols * 2));
+    }
+    int64_t dx_room() const {                          // rows of dx_slices() * (T + stacked())
+        const int64_t rows = std::max<int64_t>(T + stacked(), T > 64 ? 128 : 0), tiles = (d + kHeadCols - 1) / kHeadCols;
+        return std::max(rows, std::min(std::min<int64_t>(64, col_tiles()) * rows, cus * kHeadCols / tiles));      // (as many slices as fill the chip once)
+    }
+    int64_t dw_room() const {                          // rows of dw_slices() * piece(), where any number of rows up to T takes slices
+        const int64_t tiles = (d + kHeadCols - 1) / kHeadCols, most = std::max<int64_t>(1, (int64_t)kHeadPieceBytes / (std::max<int64_t>(T, 1) * g_planes() * 2 * kHeadCols));
+        const int64_t least = (std::min(col_tiles(), most) + 1) / 2;      // tiles of a piece: equal pieces are more than half of the largest
+        if (T <= 256 || 2 * least * tiles > (int64_t)cus) return 0;
+        return std::min(std::min<int64_t>(32, (T + 255) / 256) * col_tiles() * kHeadCols, cus * kHeadCols / tiles);
+    }
 };
 
 // The workspace of a call: counted with a null base, laid out with the caller's.
@@ -149,7 +169,7 @@ size_t head_layout(const HeadShape& s, bool grads, void* base, HeadWork* out) {
     if (s.copied(grads) || grads) w.x = sp.take<char>((size_t)s.plane_bytes(std::max(s.T + (grads ? s.stacked() : 0), grads && s.T > 64 ? (int64_t)128 : 0)) * s.planes());
     w.x_dw = s.dtype == TIDE_F32 && grads ? sp.take<char>((size_t)s.plane_bytes(s.T) * 2) : w.x;
     if (!grads) {
-        w.part = sp.take<float2>((size_t)s.parts() * s.T);
+        w.part = sp.take<float2>((size_t)s.part_room());
         if (!s.K) w.z = sp.take<float>((size_t)s.T);
     } else {
         w.source = sp.take<int32_t>((size_t)s.T);
@@ -159,9 +179,9 @@ size_t head_layout(const HeadShape& s, bool grads, void* base, HeadWork* out) {
             w.wanted = sp.take<float>((size_t)s.T * s.K);
             w.taught = sp.take<uint8_t>((size_t)s.T);
         }
-        w.g = sp.take<char>((size_t)std::max<int64_t>(s.T * s.g_planes(), s.T > 64 ? 128 : 0) * s.piece() * 2);      // (no less than 64 rows of two planes take)
-        w.acc = sp.take<float>((size_t)s.dx_slices() * std::max(s.T + s.stacked(), s.T > 64 ? (int64_t)128 : 0) * s.dp());
-        if (s.dw_slices() > 1) w.dw = sp.take<float>((size_t)s.dw_slices() * s.piece() * s.dp());
+        w.g = sp.take<char>((size_t)s.g_room());
+        w.acc = sp.take<float>((size_t)s.dx_room() * s.dp());
+        w.dw = sp.take<float>((size_t)s.dw_room() * s.dp());
     }
     if (out) *out = w;
     return sp.at;
