@@ -544,11 +544,18 @@ def _dev(t, dtype, shape, name):
     return t
 
 
+def _workspace(workspace, device):
+    """A caller's workspace: its bytes are its elements, one after the other, on the call's device."""
+    if workspace.dtype != torch.uint8 or not workspace.is_contiguous() or not workspace.is_cuda or workspace.device != device:
+        raise ValueError(f"workspace must be a contiguous CUDA uint8 tensor on {device}")
+    return workspace, workspace.numel()
+
+
 def _scratch(workspace, nbytes, device):
     """The workspace of a call that needs no initialised one: the caller's (a CUDA uint8 tensor), or one of torch's allocator for this call."""
     if workspace is None:
         workspace = torch.empty(nbytes, dtype=torch.uint8, device=device)
-    return workspace, workspace.numel() * workspace.element_size()
+    return _workspace(workspace, device)
 
 
 def exit_project_grad(hidden, final_hidden, exit_layer, layer_ids, norm_gain, eps, grad_out, *, want_gain=True, workspace=None):
@@ -600,7 +607,7 @@ def _head_scratch(x, T, d, V, K, gradient, workspace):
         if need == 0:
             raise TideError(-2, last_error())
         workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
-    return workspace, workspace.numel() * workspace.element_size()
+    return _workspace(workspace, x.device)
 
 
 def _head_grads(x, W, want_dx, want_dw):

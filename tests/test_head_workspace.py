@@ -1,7 +1,9 @@
-"""A head call's workspace grows with the rows: one that is sized for a program's largest batch serves every smaller one (no GPU needed)."""
+"""A head call's workspace grows with the rows: one that is sized for a program's largest batch serves every smaller one; and what the binding refuses to take
+for one, before anything is enqueued (no GPU needed)."""
 import itertools
 
 import pytest
+import torch
 
 from paper_2603_21365_amd import tide_route as tr
 
@@ -19,3 +21,35 @@ def test_more_rows_never_need_less(dtype, d, V):
             need = tr.head_workspace_bytes(dtype, T, d, V, K, gradient=gradient)
             assert need >= most > 0 or most == 0, f"T={T} K={K} gradient={gradient}: {need} bytes, fewer rows {most}"
             most = need
+
+
+class Stand(torch.Tensor):
+    """A tensor that says it is on a GPU, for checks that come before any use of it."""
+    is_cuda = True
+    device = torch.device("cuda", 0)
+
+
+def stand(t):
+    return t.as_subclass(Stand)
+
+
+@pytest.mark.parametrize("bad", [torch.empty(1, dtype=torch.uint8).expand(1 << 20), torch.empty(1 << 21, dtype=torch.uint8)[::2], torch.empty(1 << 20, dtype=torch.float32)])
+def test_a_workspace_whose_bytes_are_not_its_elements_is_refused(bad):
+    x = stand(torch.empty(4, 64))
+    ok = stand(torch.empty(1 << 20, dtype=torch.uint8))
+    assert tr._head_scratch(x, 4, 64, 100, 0, False, ok)[1] == 1 << 20 and tr._scratch(ok, 64, x.device)[1] == 1 << 20
+    with pytest.raises(ValueError, match="workspace"):
+        tr._head_scratch(x, 4, 64, 100, 0, False, stand(bad))
+    with pytest.raises(ValueError, match="workspace"):
+        tr._scratch(stand(bad), 64, x.device)
+
+
+def test_a_workspace_of_another_device_is_refused():
+    x = stand(torch.empty(4, 64))
+    with pytest.raises(ValueError, match="workspace"):
+        tr._head_scratch(x, 4, 64, 100, 0, False, torch.empty(1 << 20, dtype=torch.uint8))
+
+    class Other(Stand):
+        device = torch.device("cuda", 1)
+    with pytest.raises(ValueError, match="workspace"):
+        tr._head_scratch(x, 4, 64, 100, 0, False, torch.empty(1 << 20, dtype=torch.uint8).as_subclass(Other))
