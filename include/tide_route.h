@@ -261,8 +261,8 @@ int tide_exit_project(const void* hidden, int dtype, int64_t C, int64_t T, int64
 /* Gradient of the exit projection: with n_t = src_t / sqrt(mean(src_t^2) + eps), u_t = grad_out_t * norm_gain and src_t as above,
  *   grad_rows[t,:] = (u_t - n_t * mean(u_t * n_t)) / sqrt(mean(src_t^2) + eps)     the gradient to the row that token t exited with
  *   grad_gain      = sum over t of grad_out_t * n_t
- * in fp32, grad_rows rounded once to `dtype`.  A token without a source (final_hidden == NULL and no exit) gets a row of zeros and
- * adds nothing to grad_gain.  The sums are taken in a fixed order.
+ * in fp32, grad_rows rounded once to `dtype`.  A token without a source (final_hidden == NULL and no exit), or whose grad_out is
+ * zero throughout, gets a row of zeros and adds nothing to grad_gain, whatever its row holds.  The sums are taken in a fixed order.
  *   grad_out     device [T rows] of `dtype`: the gradient to tide_exit_project's out
  *   grad_rows    device [T rows] of `dtype` out; bases and row strides as for tide_exit_project
  *   grad_gain    device [d] fp32 out, 16-byte aligned, or NULL

@@ -4,7 +4,8 @@
 // One pass: a workgroup takes rows in turn, every thread its chunks of the row (h and dy in registers between the two sums and the
 // write) and the same columns of dgain, which it adds up over its rows in registers; the workgroups' sums are joined by a second launch, in
 // order, so the result does not depend on timing. Bound by memory: T = 8192, d = 4096 in bf16 takes 43 us for 201 MB (4.7 TB/s, a copy of
-// 1 GiB 5.0) and 4.6 for the second launch; the first form, without the next row's request ahead, took 152.   Rows without a source (no exit and no last-layer state) have a gradient of zero.
+// 1 GiB 5.0) and 4.6 for the second launch; the first form, without the next row's request ahead, took 152.   Rows without a source (no exit and no last-layer state) have a gradient of
+// zero, and so have rows whose dy is zero throughout (tokens without a target), whatever they hold: 0 * NaN is kept out of dgain.
 #pragma once
 #include "project_kernel.hpp"
 
@@ -149,7 +150,23 @@ __global__ __launch_bounds__(kProjectThreads) void tide_project_grad_kernel(cons
             ss = (part[turn][0][0] + part[turn][0][1]) + (part[turn][0][2] + part[turn][0][3]);
             uh = (part[turn][1][0] + part[turn][1][1]) + (part[turn][1][2] + part[turn][1][3]);
         }
-        const float r = inv_rms_f32(ss, inv_d, p.eps), back = r * r * uh * inv_d;
+        float r = inv_rms_f32(ss, inv_d, p.eps), back = r * r * uh * inv_d;
+        if (uh != uh) {                                // (the same for the row) a NaN in the row or dy, or an infinity against a zero: no dy, no gradient
+            bool any = false;
+#pragma unroll
+            for (int j = 0; j < kChunks; ++j)
+#pragma unroll
+                for (int e = 0; e < E; ++e) any |= gv[j][e] != 0.0f;
+            if constexpr (kWavePerRow) any = __any(any);
+            else any = __syncthreads_or(any);
+            if (!any) {
+                r = back = 0.0f;
+#pragma unroll
+                for (int j = 0; j < kChunks; ++j)
+#pragma unroll
+                    for (int e = 0; e < E; ++e) hv[j][e] = 0.0f;
+            }
+        }
 #pragma unroll
         for (int j = 0; j < kChunks; ++j) {
             float o[E];
