@@ -104,7 +104,8 @@ template <int WQ, int WP, int BQ, int BP, int SQ, int SP, int EB = 2> struct Hea
 constexpr float kHeadLow = 4096.0f;                  // what the second plane of an fp32 value holds its part multiplied by
 constexpr uint32_t kHeadNowhere = 0x80000000u;       // an offset at the descriptor's bound: fetched as zeros
 
-// 64 lanes x 16 bytes from memory (offsets voff from the descriptor's base) to 1 KiB of LDS at byte `lds`.
+// 64 lanes x 16 bytes from memory (offsets voff from the descriptor's base) to 1 KiB of LDS at byte `lds`.  m0 is written and not named: the compiler keeps
+// nothing there between instructions (it is reserved; clang refuses it in a list of clobbers) and sets it before each use of its own, of which these kernels have none.
 __device__ __forceinline__ void head_dma(uint32_t lds, uint32_t voff, u32x4 rsrc) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(voff), "s"(rsrc) : "memory");
 }
@@ -159,6 +160,9 @@ template <int kRows, bool kAcross, int kWaves, int kEB = 2> struct HeadFeed {
         rsrc[1] = __builtin_amdgcn_readfirstlane((uint32_t)((uintptr_t)base >> 32) & 0xffffu);
         rsrc[2] = __builtin_amdgcn_readfirstlane(left > 0 ? kHeadNowhere : 0u);
         rsrc[3] = 0x00020000u;
+        // A scalar register that a vector instruction has written (v_readfirstlane) is good for a memory instruction's descriptor five wait states later; the compiler
+        // sees to that for its own instructions, not for those in inline assembly.
+        asm volatile("s_nop 4" : "+s"(rsrc));
 #pragma unroll
         for (int i = 0; i < kN; ++i) {
             if (kInstr % kWaves != 0 && wave + kWaves * i >= kInstr) break;
