@@ -291,7 +291,8 @@ int tide_exit_project_grad(const void* hidden, int dtype, int64_t C, int64_t T, 
  *
  * Rows without a target (or whose teacher has no entry) and rows with grad_loss[t] == 0 get dx = 0 and add nothing to dW, whatever
  * they hold.  G is rounded once, to `dtype` (fp16 under a common power of two; 16-bit types up to 64 rows to twice as many bits, fp32 as an operand above); dx and dW are summed in fp32 and
- * rounded once.  dx or dW may be NULL: that product is left out.  T == 0: dW is filled with zeros.  The results do not depend on timing.
+ * rounded once.  With dtype | TIDE_HEAD_WIDE the gradient calls hold G in twice as many bits for any number of rows, so that dx and dW have one rounding to 16 bits
+ * behind them and not two; their two products take up to twice as long (fp32 has those bits anyway; the workspace is asked for with the same dtype).  dx or dW may be NULL: that product is left out.  T == 0: dW is filled with zeros.  The results do not depend on timing.
  *
  *   x          device [T rows] of `dtype`;  W device [V rows] of `dtype`;  strides in elements, at most 4194304
  *              rows of whole 16-byte chunks: bases and strides multiples of 16 bytes; other hidden sizes: of an element (the call copies x and W)
@@ -302,6 +303,7 @@ int tide_exit_project_grad(const void* hidden, int dtype, int64_t C, int64_t T, 
  *   workspace  device, 256-byte aligned, tide_head_workspace_bytes(dtype, T, d, V, K, gradient) bytes (K = 0: the loss; gradient != 0: the _grad call).  It needs no
  *              initialisation and keeps nothing: calls on different workspaces may overlap.  The size is host arithmetic and grows with T: a
  *              workspace for the most rows serves every smaller call of the same dtype, d, V, K and kind;  0 with tide_last_error() set if unsupported. */
+#define TIDE_HEAD_WIDE 0x100
 size_t tide_head_workspace_bytes(int dtype, int64_t T, int64_t d, int64_t V, int64_t K, int gradient);
 int tide_head_loss(const void* x, int dtype, int64_t T, int64_t d, int64_t V, int64_t x_row_stride, const void* W,
                    int64_t w_row_stride, const int32_t* target, float* loss, float* lse, void* workspace,

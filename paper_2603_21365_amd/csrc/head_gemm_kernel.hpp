@@ -79,7 +79,7 @@ struct HeadGemmParams {
     float* acc_out;            // [k_slices][acc_rows][acc_ld]
     int64_t acc_slice;         // elements
     int acc_ld, accumulate;
-    int stacked;               // G's second plane follows its first as further rows, from this one on (0: none; 16-bit operands): rows of dx, of k in dW
+    int stacked;               // G's second plane follows its live rows as as many further ones (16-bit operands): rows of dx, of k in dW
     // dW
     char* out;
     int64_t out_row_elems;
@@ -293,8 +293,8 @@ __global__ __launch_bounds__(Tile::kThreads) void tide_head_gemm_kernel(const He
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int wq = wave % Tile::kWQ, wp = wave / Tile::kWQ;
     const int live = kMode == kHeadStats ? 0 : __builtin_amdgcn_readfirstlane(p.ctl->live);
-    const int q_rows = kMode == kHeadGrad ? live : kMode == kHeadRows ? p.stacked + live : p.q_rows;
-    const int k_elems = kMode == kHeadWeights ? (live ? p.stacked + live : 0) : p.k;
+    const int q_rows = kMode == kHeadGrad ? live : kMode == kHeadRows ? live << p.stacked : p.q_rows;
+    const int k_elems = kMode == kHeadWeights ? live << p.stacked : p.k;
     const int tiles_q = (q_rows + Tile::kQ - 1) / Tile::kQ;
     const uint32_t lds_q = (uint32_t)(size_t)(head_lds*)smem, lds_p = lds_q + Tile::kSQ * Tile::kQBytes;
 
@@ -577,18 +577,19 @@ __global__ __launch_bounds__(Tile::kThreads) void tide_head_gemm_kernel(const He
 #pragma unroll
                 for (int r0 = 0; r0 < 16; r0 += kRowsAtOnce) {
                     const int r = r0 + lane / kLanes, c = lane % kLanes * 8, tr = t - row + r;
-                    if (r >= 16 || tr >= max(q_rows, p.stacked)) continue;      // (stacked: zeros in the rows between the planes)
+                    if (r >= 16 || tr >= q_rows) continue;
                     const f32x4 a = *(lds_f32x4*)(stage + r * Tile::kLd + c), b = *(lds_f32x4*)(stage + r * Tile::kLd + c + 4);
                     char* dst = p.g_out + (int64_t)tr * p.g_row_bytes + (int64_t)(col0 + c) * 2;
                     *reinterpret_cast<u32x4*>(dst) = u32x4{head_round2<DT>(a[0], a[1]), head_round2<DT>(a[2], a[3]), head_round2<DT>(b[0], b[1]), head_round2<DT>(b[2], b[3])};
-                    if (p.g_plane_bytes) {
+                    const int64_t plane = p.stacked ? q_rows * p.g_row_bytes : p.g_plane_bytes;
+                    if (plane) {
                         f32x4 x, y;
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
                             x[e] = (a[e] - head_rounded<DT>(a[e])) * (kPlanes ? kHeadLow : 1.0f);
                             y[e] = (b[e] - head_rounded<DT>(b[e])) * (kPlanes ? kHeadLow : 1.0f);
                         }
-                        *reinterpret_cast<u32x4*>(dst + p.g_plane_bytes) = u32x4{head_round2<DT>(x[0], x[1]), head_round2<DT>(x[2], x[3]), head_round2<DT>(y[0], y[1]), head_round2<DT>(y[2], y[3])};
+                        *reinterpret_cast<u32x4*>(dst + plane) = u32x4{head_round2<DT>(x[0], x[1]), head_round2<DT>(x[2], x[3]), head_round2<DT>(y[0], y[1]), head_round2<DT>(y[2], y[3])};
                     }
                 }
                 lds_fence();

@@ -48,6 +48,7 @@ template <typename F> int by_head_rows(int rows, F&& f) {
 struct HeadShape {
     int dtype;
     int64_t T, d, V, K;
+    bool wide = false;             // G in two planes whatever T
     unsigned cus = 256;
     int64_t dp() const { return (d + 7) / 8 * 8; }                      // elements of a padded row of 16-bit values
     int planes() const { return dtype == TIDE_F32 ? 2 : 1; }
@@ -71,10 +72,11 @@ struct HeadShape {
         return 2 * ((T + rows - 1) / rows) * col_tiles() < (int64_t)cus && (T + 63) / 64 * ((V + HeadTile64::kP - 1) / HeadTile64::kP) <= 2 * (int64_t)cus ? 64 : rows;
     }
     int64_t row_tiles() const { return (T + rows_per_tile() - 1) / rows_per_tile(); }
-    // Few rows: a row of dx can hang on one element of G, whose rounding would then be all of that row's; what it leaves goes into a second plane.  Their products
-    // are bound by reading W and writing dW.
-    int g_planes() const { return dtype == TIDE_F32 || T <= 64 ? 2 : 1; }
-    // 16-bit operands: the second plane follows as further rows -- of dx, so that W is read once, and of k in dW (of x, too), where a stage has room for them
+    // G in the type of the rows, as a program has it that keeps its logits in that type.  What its rounding leaves goes into a second plane where the caller asks for it,
+    // and up to 64 rows: there a row of dx can hang on one element of G, and the products are bound by reading W and writing dW (the gradient call with one / two
+    // planes, bf16, d = 4096, V = 128000, ms: T = 1 0.66 / 0.66, 33 0.69 / 0.75, 64 0.70 / 0.79, 128 0.78 / 0.96, 322 1.29 / 1.82, 8192 20.6 / 35.4).
+    int g_planes() const { return dtype == TIDE_F32 || T <= 64 || wide ? 2 : 1; }
+    // 16-bit operands: the second plane follows as further rows -- of dx, so that W is read once, and of k in dW (of x, too)
     int64_t stacked() const { return dtype != TIDE_F32 && g_planes() == 2 ? T : 0; }
     int rows_of_dx() const { return rows_for(T + stacked()); }
     int64_t col_tiles() const { return (V + kHeadCols - 1) / kHeadCols; }
@@ -280,7 +282,7 @@ void head_max(const void* rows, int64_t stride, int64_t n, int64_t d, uint32_t* 
     if (*blocks) hipLaunchKernelGGL(tide_head_max_kernel, dim3(*blocks), dim3(kHeadRowThreads), 0, st, (const char*)rows, stride * 4, n, (int)d, out);
 }
 template <int DT> void head_copy(const HeadShape& s, const void* rows, int64_t stride, int64_t n, const int32_t* source, const HeadWork& w, const float4* row_const, int blocks, char* out, hipStream_t st,
-                                 int64_t stacked = 0) {
+                                 bool stacked = false) {
     if (n == 0) return;
     const int64_t rows_each = head_copy_rows(s.dp() / 8);
     hipLaunchKernelGGL((tide_head_copy_kernel<DT>), dim3((unsigned)((n + rows_each - 1) / rows_each)), dim3(kHeadRowThreads), 0, st, (const char*)rows, stride * Storage<DT>::kBytes, n, (int)rows_each,
@@ -402,12 +404,12 @@ int head_backward(HeadCall& c) {
             const int blocks = head_rows(s, c.x, c.x_stride, w.source, w, w.row_const, c.st);
             if (c.dW) head_copy<DT>(s, c.x, c.x_stride, s.T, w.source, w, w.row_const, blocks, w.x_dw, c.st);
         } else {
-            head_copy<DT>(s, c.x, c.x_stride, s.T, w.source, w, nullptr, 0, w.x, c.st, s.stacked());
+            head_copy<DT>(s, c.x, c.x_stride, s.T, w.source, w, nullptr, 0, w.x, c.st, s.stacked() != 0);
         }
         if (s.copied(true)) head_copy<DT>(s, c.W, c.w_stride, s.V, nullptr, w, nullptr, 0, w.w, c.st);
         const HeadOperand x = head_operand(s, nullptr, 0, w.x, s.T), x_dw = head_operand(s, nullptr, 0, w.x_dw, s.T), W = head_operand(s, c.W, c.w_stride, w.w, s.V);
         const int64_t piece = s.piece(), g_plane = s.T * piece * 2;
-        const HeadOperand g{{w.g, w.g + (s.g_planes() - 1) * g_plane}, piece * 2};     // (the second plane's rows follow the first's)
+        const HeadOperand g{{w.g, w.g + (s.stacked() ? 0 : s.g_planes() - 1) * g_plane}, piece * 2};
         const int slices = s.dx_slices(), dw_slices = s.dw_slices();
         for (int64_t v0 = 0; v0 < s.V; v0 += piece) {
             const int64_t width = std::min(piece, s.V - v0);
@@ -433,8 +435,8 @@ int head_backward(HeadCall& c) {
                 a.wanted = w.wanted;
                 a.g_out = w.g;
                 a.g_row_bytes = g.row_bytes;
-                a.g_plane_bytes = s.g_planes() == 2 ? g_plane : 0;
-                a.stacked = (int)s.stacked();
+                a.g_plane_bytes = g.plane[1] - g.plane[0];
+                a.stacked = s.stacked() != 0;
                 rc2 = by_head_tile(s.rows_per_tile(), [&](auto tile) { return launch_head<E, DT, kHeadGrad, decltype(tile)>(s.T, width, c.st, a); });
                 if (rc2) return rc2;
             }
@@ -442,7 +444,7 @@ int head_backward(HeadCall& c) {
                 HeadGemmParams a = p;
                 a.q = g;
                 a.p = Wv;
-                a.stacked = (int)s.stacked();
+                a.stacked = s.stacked() != 0;
                 a.q_rows = (int)s.T;
                 a.p_rows = (int)s.dp();
                 a.k = (int)width;
@@ -461,7 +463,7 @@ int head_backward(HeadCall& c) {
                 a.q_rows = (int)width;
                 a.p_rows = (int)s.d;
                 a.k = (int)s.T;
-                a.stacked = (int)s.stacked();
+                a.stacked = s.stacked() != 0;
                 a.out = (char*)c.dW + v0 * c.dw_stride * Storage<DT>::kBytes;
                 a.out_row_elems = c.dw_stride;
                 a.out_aligned = chunked_rows(s.dtype, s.d);
@@ -478,7 +480,7 @@ int head_backward(HeadCall& c) {
             }
         }
         if (s.T && c.dx)
-            hipLaunchKernelGGL((tide_head_dx_kernel<DT>), dim3((unsigned)std::min<int64_t>(s.T, 4096)), dim3(kHeadRowThreads), 0, c.st, w.acc, slices, (s.T + s.stacked()) * s.dp(), (int)s.dp(), (int)s.stacked(), w.place,
+            hipLaunchKernelGGL((tide_head_dx_kernel<DT>), dim3((unsigned)std::min<int64_t>(s.T, 4096)), dim3(kHeadRowThreads), 0, c.st, w.acc, slices, (s.T + s.stacked()) * s.dp(), (int)s.dp(), (int)(s.stacked() != 0), w.place,
                                w.row_const, w.ctl, (int)s.T, (int)s.d, (char*)c.dx, c.dx_stride * Storage<DT>::kBytes);
         return TIDE_OK;
     });
@@ -500,6 +502,8 @@ int project_grad_blocks(int64_t T, int64_t row_bytes, unsigned cus) {
     return (int)((turns + rounds - 1) / rounds);
 }
 
+HeadShape head_gradient_shape(int dtype, int64_t T, int64_t d, int64_t V, int64_t K) { return HeadShape{dtype & ~TIDE_HEAD_WIDE, T, d, V, K, (dtype & TIDE_HEAD_WIDE) != 0}; }
+
 }  // namespace
 
 extern "C" {
@@ -507,7 +511,7 @@ extern "C" {
 size_t tide_head_workspace_bytes(int dtype, int64_t T, int64_t d, int64_t V, int64_t K, int gradient) {
     g_err[0] = 0;
     HeadCall c{};
-    c.s = HeadShape{dtype, T, d, V, K};
+    c.s = gradient ? head_gradient_shape(dtype, T, d, V, K) : HeadShape{dtype, T, d, V, K};
     c.tau = 1.0f;
     c.x_stride = c.w_stride = (d + 7) / 8 * 8;
     alignas(256) static char some[256];                // checks of pointers that are not asked about
@@ -541,7 +545,7 @@ int tide_head_loss_grad(const void* x, int dtype, int64_t T, int64_t d, int64_t 
                         void* stream) {
     g_err[0] = 0;
     HeadCall c{};
-    c.s = HeadShape{dtype, T, d, V, 0};
+    c.s = head_gradient_shape(dtype, T, d, V, 0);
     c.x = x, c.W = W, c.x_stride = x_row_stride, c.w_stride = w_row_stride;
     c.ids = target, c.tau = 1.0f, c.lse_in = lse, c.grad = grad_loss;
     c.dx = dx, c.dx_stride = dx_row_stride, c.dW = dW, c.dw_stride = dw_row_stride;
@@ -567,7 +571,7 @@ int tide_head_distill_grad(const void* x, int dtype, int64_t T, int64_t d, int64
     g_err[0] = 0;
     if (K < 1) return fail(TIDE_ERR_INVALID_ARG, "K = %lld must be at least 1", (long long)K);
     HeadCall c{};
-    c.s = HeadShape{dtype, T, d, V, K};
+    c.s = head_gradient_shape(dtype, T, d, V, K);
     c.x = x, c.W = W, c.x_stride = x_row_stride, c.w_stride = w_row_stride;
     c.ids = top_ids, c.values = top_values, c.tau = tau, c.lse_in = lse, c.grad = grad_loss;
     c.dx = dx, c.dx_stride = dx_row_stride, c.dW = dW, c.dw_stride = dw_row_stride;

@@ -160,7 +160,7 @@ __device__ __forceinline__ void head_split8(const u32x4 (&v)[2], int n, char* hi
 }
 
 // Rows into the form the products read: gathered (source != null), padded with zeros to whole 16-byte chunks, fp32 ones as two fp16 planes.
-// stacked != 0: every row a second time, `stacked` rows on, and zeros in the rows from the last one to there.
+// stacked != 0: all of them a second time, behind the last.
 // fp32: row_const == null: W, times 2^w_exp; otherwise the rows of x for dW, each times 2^(dw_exp - its row of G's): what is worked out here of `largest`, the
 // greatest exponents that tide_head_rows_kernel's workgroups have found.
 // A workgroup has rows_each rows, taken as one list of chunks, four a thread at a time.
@@ -168,8 +168,8 @@ template <int DT>
 __global__ __launch_bounds__(kHeadRowThreads) void tide_head_copy_kernel(const char* rows, int64_t row_bytes, int64_t n_rows, int rows_each, int d, const int32_t* source,
                                                                          HeadCtl* ctl, const float4* row_const, const int32_t* largest, int blocks, int stacked, char* out,
                                                                          int64_t out_row_bytes, int64_t plane_bytes) {
-    const int64_t live = source ? ctl->live : n_rows, n = stacked ? stacked : live, r0 = (int64_t)blockIdx.x * rows_each;
-    if (r0 >= n) return;
+    const int64_t live = source ? ctl->live : n_rows, r0 = (int64_t)blockIdx.x * rows_each;
+    if (r0 >= live) return;
     int scale = 0;
     if constexpr (DT == kF32) {
         scale = ctl->w_exp;
@@ -187,7 +187,7 @@ __global__ __launch_bounds__(kHeadRowThreads) void tide_head_copy_kernel(const c
         }
     }
     const bool chunks = ((uintptr_t)rows | (uintptr_t)row_bytes) % 16 == 0 && d % 8 == 0;
-    const int per_row = (int)(out_row_bytes / 16), total = (int)min((int64_t)rows_each, n - r0) * per_row;
+    const int per_row = (int)(out_row_bytes / 16), total = (int)min((int64_t)rows_each, live - r0) * per_row;
     constexpr int kU = 4, kW = DT == kF32 ? 2 : 1;     // 16-byte pieces of a chunk's source
     for (int i0 = threadIdx.x; i0 < total; i0 += kU * kHeadRowThreads) {
         u32x4 v[kU][kW];
@@ -198,12 +198,7 @@ __global__ __launch_bounds__(kHeadRowThreads) void tide_head_copy_kernel(const c
             const int i = min(i0 + u * kHeadRowThreads, total - 1), q = i / per_row;
             r[u] = r0 + q;
             c[u] = i - q * per_row;
-            const char* row = rows + (source ? (int64_t)source[max((int64_t)0, min(r[u], live - 1))] : r[u]) * row_bytes;
-            if (r[u] >= live) {
-#pragma unroll
-                for (int w = 0; w < kW; ++w) v[u][w] = u32x4{0, 0, 0, 0};
-                continue;
-            }
+            const char* row = rows + (source ? (int64_t)source[r[u]] : r[u]) * row_bytes;
             head_load8<DT>(row, c[u], d, chunks, v[u]);
         }
 #pragma unroll
@@ -212,7 +207,7 @@ __global__ __launch_bounds__(kHeadRowThreads) void tide_head_copy_kernel(const c
             char* to = out + r[u] * out_row_bytes;
             if constexpr (DT != kF32) {
                 reinterpret_cast<u32x4*>(to)[c[u]] = v[u][0];
-                if (stacked) reinterpret_cast<u32x4*>(to + stacked * out_row_bytes)[c[u]] = v[u][0];
+                if (stacked) reinterpret_cast<u32x4*>(to + live * out_row_bytes)[c[u]] = v[u][0];
             } else {
                 head_split8(v[u], row_const ? scale - __float_as_int(row_const[r[u]].w) : scale, to, to + plane_bytes, c[u]);
             }
@@ -406,7 +401,7 @@ __global__ __launch_bounds__(kHeadRowThreads) void tide_head_dx_kernel(const flo
                     }
                 };
                 add(from);
-                if (stacked) add(from + (int64_t)stacked * acc_ld);        // the part of G's second plane
+                if (stacked) add(from + (int64_t)ctl->live * acc_ld);        // the part of G's second plane
             }
             a = head_shifted(a, back);
             b = head_shifted(b, back);

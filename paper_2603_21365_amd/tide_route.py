@@ -588,22 +588,25 @@ def exit_project_grad(hidden, final_hidden, exit_layer, layer_ids, norm_gain, ep
     return grad, gain
 
 
-def head_workspace_bytes(dtype: int, T: int, d: int, V: int, K: int = 0, *, gradient: bool = False) -> int:
-    """Bytes of workspace a head call needs (K = 0: the loss, else the distillation; 0 and last_error() if unsupported)."""
-    return int(load_library().tide_head_workspace_bytes(int(dtype), int(T), int(d), int(V), int(K), 1 if gradient else 0))
+HEAD_WIDE = 0x100
 
 
-def _head_args(x, W):
+def head_workspace_bytes(dtype: int, T: int, d: int, V: int, K: int = 0, *, gradient: bool = False, wide: bool = False) -> int:
+    """Bytes of workspace a head call needs (K = 0: the loss, else the distillation; 0 and last_error() if unsupported).  They grow with T."""
+    return int(load_library().tide_head_workspace_bytes(int(dtype) | (HEAD_WIDE if gradient and wide else 0), int(T), int(d), int(V), int(K), 1 if gradient else 0))
+
+
+def _head_args(x, W, wide=False):
     (T, d), (xs, _) = _rows(x, 2)
     (V, dw), (ws, _) = _rows(W, 2)
     if dw != d or W.dtype != x.dtype:
         raise ValueError("W must be [V, d] of x's dtype, x [T, d]")
-    return T, d, V, (_ptr(x), _dtype_code(x), T, d, V, xs if T > 1 else max(xs, d), _ptr(W), ws if V > 1 else max(ws, d))
+    return T, d, V, (_ptr(x), _dtype_code(x) | (HEAD_WIDE if wide else 0), T, d, V, xs if T > 1 else max(xs, d), _ptr(W), ws if V > 1 else max(ws, d))
 
 
-def _head_scratch(x, T, d, V, K, gradient, workspace):
+def _head_scratch(x, T, d, V, K, gradient, workspace, wide=False):
     if workspace is None:
-        need = head_workspace_bytes(_dtype_code(x), T, d, V, K, gradient=gradient)
+        need = head_workspace_bytes(_dtype_code(x), T, d, V, K, gradient=gradient, wide=wide)
         if need == 0:
             raise TideError(-2, last_error())
         workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
@@ -629,13 +632,14 @@ def head_loss(x, W, target, *, workspace=None):
     return loss, lse
 
 
-def head_loss_grad(x, W, target, lse, grad_loss, *, want_dx=True, want_dw=True, workspace=None):
-    """Gradients of head_loss for grad_loss f32 [T] and its lse -> (dx [T,d] | None, dW [V,d] | None) of x's dtype."""
-    T, d, V, rows = _head_args(x, W)
+def head_loss_grad(x, W, target, lse, grad_loss, *, want_dx=True, want_dw=True, wide=False, workspace=None):
+    """Gradients of head_loss for grad_loss f32 [T] and its lse -> (dx [T,d] | None, dW [V,d] | None) of x's dtype.
+    ``wide``: 16-bit types hold the gradient to the logits in twice as many bits for more than 64 rows, too (the header's TIDE_HEAD_WIDE)."""
+    T, d, V, rows = _head_args(x, W, wide)
     _dev(target, torch.int32, (T,), "target")
     _dev(lse, torch.float32, (T,), "lse"), _dev(grad_loss, torch.float32, (T,), "grad_loss")
     dx, dW = _head_grads(x, W, want_dx, want_dw)
-    workspace, nbytes = _head_scratch(x, T, d, V, 0, True, workspace)
+    workspace, nbytes = _head_scratch(x, T, d, V, 0, True, workspace, wide)
     _check(load_library().tide_head_loss_grad(*rows, _ptr(target), _ptr(lse), _ptr(grad_loss), _ptr(dx), d, _ptr(dW), d, _ptr(workspace), nbytes, _stream()))
     return dx, dW
 
@@ -660,13 +664,13 @@ def head_distill(x, W, top_values, top_ids, tau, *, workspace=None):
     return loss, lse, z
 
 
-def head_distill_grad(x, W, top_values, top_ids, tau, lse, grad_loss, *, want_dx=True, want_dw=True, workspace=None):
-    """Gradients of head_distill for grad_loss f32 [T] and its lse -> (dx [T,d] | None, dW [V,d] | None) of x's dtype."""
-    T, d, V, rows = _head_args(x, W)
+def head_distill_grad(x, W, top_values, top_ids, tau, lse, grad_loss, *, want_dx=True, want_dw=True, wide=False, workspace=None):
+    """Gradients of head_distill for grad_loss f32 [T] and its lse -> (dx [T,d] | None, dW [V,d] | None) of x's dtype; ``wide`` as for head_loss_grad."""
+    T, d, V, rows = _head_args(x, W, wide)
     K = _head_top(x, T, top_values, top_ids)
     _dev(lse, torch.float32, (T,), "lse"), _dev(grad_loss, torch.float32, (T,), "grad_loss")
     dx, dW = _head_grads(x, W, want_dx, want_dw)
-    workspace, nbytes = _head_scratch(x, T, d, V, K, True, workspace)
+    workspace, nbytes = _head_scratch(x, T, d, V, K, True, workspace, wide)
     _check(load_library().tide_head_distill_grad(*rows, _ptr(top_values), _ptr(top_ids), K, float(tau), _ptr(lse), _ptr(grad_loss), _ptr(dx), d, _ptr(dW), d,
                                                  _ptr(workspace), nbytes, _stream()))
     return dx, dW
