@@ -601,7 +601,7 @@ def _head_args(x, W, wide=False):
     (V, dw), (ws, _) = _rows(W, 2)
     if dw != d or W.dtype != x.dtype:
         raise ValueError("W must be [V, d] of x's dtype, x [T, d]")
-    return T, d, V, (_ptr(x), _dtype_code(x) | (HEAD_WIDE if wide else 0), T, d, V, xs if T > 1 else max(xs, d), _ptr(W), ws if V > 1 else max(ws, d))
+    return T, d, V, (_ptr(x), _dtype_code(x) | (HEAD_WIDE if wide else 0), T, d, V, xs if T > 1 else d, _ptr(W), ws if V > 1 else d)      # (one row has no stride)
 
 
 def _head_scratch(x, T, d, V, K, gradient, workspace, wide=False):

@@ -1,5 +1,5 @@
-"""A head call's workspace grows with the rows: one that is sized for a program's largest batch serves every smaller one; and what the binding refuses to take
-for one, before anything is enqueued (no GPU needed)."""
+"""A head call's workspace grows with the rows: one that is sized for a program's largest batch serves every smaller one; what the binding refuses to take
+for one, before anything is enqueued; and which strides it hands on (no GPU needed)."""
 import itertools
 
 import pytest
@@ -53,3 +53,15 @@ def test_a_workspace_of_another_device_is_refused():
         device = torch.device("cuda", 1)
     with pytest.raises(ValueError, match="workspace"):
         tr._head_scratch(x, 4, 64, 100, 0, False, torch.empty(1 << 20, dtype=torch.uint8).as_subclass(Other))
+
+
+def test_one_row_has_no_stride():
+    """The last token of a long sequence: its row's stride is the sequence's length, which no call would take between rows."""
+    last = stand(torch.empty(1, 2000, 4096, dtype=torch.bfloat16))[:, -1]
+    W = stand(torch.empty(3, 4096, dtype=torch.bfloat16))
+    assert last.stride(0) > 1 << 22
+    T, d, V, rows = tr._head_args(last, W)
+    assert (T, d, V, rows[5], rows[7]) == (1, 4096, 3, 4096, 4096)
+    assert tr._head_args(W, last)[3][7] == 4096
+    pair = stand(torch.empty(2, 70, dtype=torch.bfloat16))[:, :64]
+    assert tr._head_args(pair, pair)[3][5] == tr._head_args(pair, pair)[3][7] == 70
