@@ -189,3 +189,22 @@ def test_the_forms_for_few_and_many_fp32_rows_agree(tr):
     near("loss of many", many, ex.loss, ex.tol_loss)
     near("loss, few and many", few, many[:128].double(), 2 * ex.tol_loss[:128])
     near("lse, few and many", lse_few, lse_many[:128].double(), 2 * ex.tol_lse[:128])
+
+
+@pytest.mark.parametrize("name", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("T,d,V,K", [(1, 1, 1, 0), (2, 1, 2, 0), (3, 2, 1, 1), (2, 3, 5, 2), (7, 7, 9, 0), (70, 1, 3, 2), (129, 5, 2, 0), (300, 2, 300, 1)])
+def test_smallest_sizes(tr, name, T, d, V, K):
+    print(f"[gpu-case] smallest {name} T={T} d={d} V={V} K={K}", flush=True)
+    if K:
+        distillation_and_gradients(tr, name, T, d, V, K, 1.0)
+    else:
+        loss_and_gradients(tr, name, T, d, V)
+
+
+def test_the_last_token_of_a_long_sequence(tr):
+    import torch
+    states = torch.randn(1, 2000, 4096, device="cuda").bfloat16()
+    W, target = torch.randn(500, 4096, device="cuda").bfloat16(), torch.tensor([7], dtype=torch.int32, device="cuda")
+    print("[gpu-case] last token", flush=True)
+    for a, b in zip(tr.head_loss(states[:, -1], W, target), tr.head_loss(states[0, -1:].clone(), W, target)):
+        assert a.isfinite().all() and torch.equal(a, b)
