@@ -288,6 +288,7 @@ int tide_exit_project_grad(const void* hidden, int dtype, int64_t C, int64_t T, 
  *   loss[t] = tau^2 * sum_k q[t,k] * (log q[t,k] - z_top[t,k] / tau + lse[t]),   0 where the teacher has no entry
  * tide_head_distill_grad:
  *   G[t,v] = grad_loss[t] * tau * (exp(z[t,v] / tau - lse[t]) - sum of q[t,k] over top_ids[t,k] == v),   dx = G W,   dW = G^T x
+ * A NaN or +inf among the values that count makes a row's loss and its gradient NaN.  lse is held in fp32, so the exponential in G is off by about 2^-23 |lse|.
  *
  * Rows without a target (or whose teacher has no entry) and rows with grad_loss[t] == 0 get dx = 0 and add nothing to dW, whatever
  * they hold.  G is rounded once, to `dtype` (fp16 under a common power of two; 16-bit types up to 64 rows to twice as many bits, fp32 as an operand above); dx and dW are summed in fp32 and

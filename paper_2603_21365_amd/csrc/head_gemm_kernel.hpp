@@ -244,7 +244,7 @@ template <int DT> __device__ __forceinline__ f32x4 head_mma(u32x4 a, u32x4 b, f3
     if constexpr (DT == kBF16) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), acc, 0, 0, 0);
     else return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), acc, 0, 0, 0);
 }
-// fp32: eight steps of four k values, one from each quarter of the lanes.  (At most 64 rows are bound by reading W; three bf16 terms a value, split as the
+// fp32: eight steps of four k values, one from each quarter of the lanes, for up to 128 rows.  (A few rows are bound by reading W; three bf16 terms a value, split as the
 // fragments are read, cost as many cycles in the vector ALU as these in the matrix cores, and
 // the fragments of x in every wave: 32003 x 768 32.2 / 26.6 us at T = 17, 100000 x 4096 418 / 328 at T = 20; adding up
 // in blocks costs 3 us of that at T = 17 and none at T = 1.)
