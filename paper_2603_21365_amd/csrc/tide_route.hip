@@ -142,7 +142,9 @@ struct StaticScratch {
 };
 StaticScratch g_static[kMaxDevices];
 
-// Grow-only device buffer.  Re-allocation frees the old block, which waits for the device.
+// Grow-only device buffer.  Re-allocation frees the old block, which waits for the device.  zero: filled by the time this returns.  The fill goes through the null
+// stream and hipMemset comes back before it has run (memory on a device: asynchronous), while callers' streams are ones that do not wait for the null stream: without
+// the wait a call's first arrivals could be counted on what was there before, or be wiped out (seen once: C = 2, T = 3100, first call after tide_release).
 int reserve(Buffer& b, size_t bytes, bool zero) {
     if (b.bytes >= bytes && b.ptr) return TIDE_OK;
     if (b.ptr) {
@@ -161,7 +163,13 @@ int reserve(Buffer& b, size_t bytes, bool zero) {
     ++g_allocations;
     if (zero) {
         e = hipMemset(b.ptr, 0, want);
-        if (e != hipSuccess) return fail(TIDE_ERR_HIP, "hipMemset: %s", hipGetErrorString(e));
+        if (e == hipSuccess) e = hipStreamSynchronize(nullptr);
+        if (e != hipSuccess) {
+            (void)hipFree(b.ptr);
+            b.ptr = nullptr;
+            b.bytes = 0;
+            return fail(TIDE_ERR_HIP, "zero-fill of a workspace: %s", hipGetErrorString(e));
+        }
     }
     return TIDE_OK;
 }
