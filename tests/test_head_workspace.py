@@ -13,13 +13,13 @@ SHAPES = [(4096, 128000), (768, 1147), (64, 300), (100, 50000), (8192, 18225), (
 @pytest.mark.parametrize("d,V", SHAPES)
 @pytest.mark.parametrize("dtype", [tr.F32, tr.F16, tr.BF16])
 def test_more_rows_never_need_less(dtype, d, V):
-    for K, gradient in itertools.product((0, 32), (False, True)):
+    for K, kind in itertools.product((0, 32), ({}, {"gradient": True}, {"gradient": True, "wide": True})):
         most = 0
         for T in itertools.chain(range(0, 1400), range(1400, 9000, 37), (16384, 70000, 300000, 1 << 20)):
             if T * V > 1 << 37:
                 continue
-            need = tr.head_workspace_bytes(dtype, T, d, V, K, gradient=gradient)
-            assert need >= most > 0 or most == 0, f"T={T} K={K} gradient={gradient}: {need} bytes, fewer rows {most}"
+            need = tr.head_workspace_bytes(dtype, T, d, V, K, **kind)
+            assert need >= most > 0 or most == 0, f"T={T} K={K} {kind}: {need} bytes, fewer rows {most}"
             most = need
 
 
@@ -65,3 +65,17 @@ def test_one_row_has_no_stride():
     assert tr._head_args(W, last)[3][7] == 4096
     pair = stand(torch.empty(2, 70, dtype=torch.bfloat16))[:, :64]
     assert tr._head_args(pair, pair)[3][5] == tr._head_args(pair, pair)[3][7] == 70
+
+
+def test_two_planes_are_asked_for_with_the_type():
+    """dtype | TIDE_HEAD_WIDE: another workspace above 64 rows of a 16-bit type, the same elsewhere; no type of a forward call."""
+    size = lambda dtype, T, wide: tr.head_workspace_bytes(dtype, T, 512, 5000, gradient=True, wide=wide)
+    for dtype in (tr.F16, tr.BF16):
+        assert size(dtype, 200, True) > size(dtype, 200, False) and size(dtype, 64, True) == size(dtype, 64, False)
+    assert size(tr.F32, 200, True) == size(tr.F32, 200, False)
+    lib, fake = tr.load_library(), 0x100000
+    wide = tr.BF16 | tr.HEAD_WIDE
+    assert lib.tide_head_workspace_bytes(wide, 200, 512, 5000, 0, 1) == size(tr.BF16, 200, True)
+    assert lib.tide_head_workspace_bytes(wide, 200, 512, 5000, 0, 0) == 0 and "dtype" in tr.last_error()
+    assert lib.tide_head_workspace_bytes(3 | tr.HEAD_WIDE, 200, 512, 5000, 0, 1) == 0 and "dtype 3" in tr.last_error()
+    assert lib.tide_head_loss(fake, wide, 4, 64, 100, 64, fake, 64, fake, fake, fake, fake, 0, None) == -1 and "dtype" in tr.last_error()
