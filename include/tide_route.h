@@ -321,6 +321,64 @@ int tide_head_distill_grad(const void* x, int dtype, int64_t T, int64_t d, int64
                            const float* lse, const float* grad_loss, void* dx, int64_t dx_row_stride, void* dW,
                            int64_t dw_row_stride, void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---- Answer operators: what an exited row answers.  The LM head in four bits, and the rules that a decoding program puts on its logits.
+ *
+ * A head in four bits stands for the weights s (c - 8): c one of 0 .. 15, s a scale that `group` (32, 64 or 128) columns of a row share, fp16 or bf16.
+ *   codes   device, 16-byte aligned, ceil(V/16) * ceil(d/128) tiles of 1024 bytes, those of 16 rows one after the other.  Of a tile's row r (0 .. 15), column
+ *           32 j + 8 g + e (j, g = 0 .. 3, e = 0 .. 7) is bits 4 (e / 2) + 16 (e % 2) ..+3 of the 32-bit little-endian word 64 g + 4 r + j.  What lies beyond V and d may be anything.
+ *   scales  device, 16-byte aligned, [ceil(V/16)][ceil(d/group)][16]: the scale of row 16 i + r, group k is element [i][k][r]
+ *
+ * tide_head_quantize_q4: of a group whose largest magnitude is m,
+ *   s = m / 7 rounded once to scale_dtype,   c = 8 + round(w / s), ties to even, 1 .. 15
+ *   where m / 7 rounds to zero: s = 0, c = 8.  A group with a value that is not finite, or whose scale does not fit: s = NaN, c = 8.  Codes beyond V and d are 8.
+ * tide_head_dequantize_q4: W[v,i] = s (c - 8), rounded once to `dtype`.
+ * tide_head_logits_q4: logits[t,v] = sum_i x[t,i] W[v,i], W as it stands for, not rounded: products of 16-bit values and codes are exact (fp32 rows are taken as
+ *   three bf16 terms, which add up to them), the sums and the scales' products in fp32.  A row of x that is not finite has NaN for all of its logits, no other row does.
+ *   The results do not depend on timing.
+ *
+ *   W       device [V rows] of `dtype`, x device [T rows] of `dtype`; strides in elements.  Element alignment is enough; 16-byte bases and strides are faster.
+ *   logits  device [T rows] fp32 out, logits_row_stride >= V
+ *   1 <= d <= 16384, T <= 4194304, V <= 8388608, T * V up to about 2^34 (TIDE_ERR_UNSUPPORTED)
+ *   workspace  device, 256-byte aligned, tide_head_logits_q4_bytes(dtype, T, d) bytes, which grow with T.  No initialisation, nothing kept: calls on
+ *           different workspaces may overlap.  0 bytes with tide_last_error() set: unsupported. */
+int tide_head_quantize_q4(const void* W, int dtype, int64_t V, int64_t d, int64_t w_row_stride, int64_t group, void* codes, void* scales,
+                          int scale_dtype, void* stream);
+int tide_head_dequantize_q4(const void* codes, const void* scales, int scale_dtype, int64_t V, int64_t d, int64_t group, void* W, int dtype,
+                            int64_t w_row_stride, void* stream);
+size_t tide_head_logits_q4_bytes(int dtype, int64_t T, int64_t d);
+int tide_head_logits_q4(const void* x, int dtype, int64_t T, int64_t d, int64_t V, int64_t x_row_stride, const void* codes, const void* scales,
+                        int scale_dtype, int64_t group, float* logits, int64_t logits_row_stride, void* workspace, size_t workspace_bytes,
+                        void* stream);
+
+/* The rules of decoding.  For row t and token v, with past_t the first past_len[t] entries of past[t,:] (at most H; past_len == NULL: H), the first prompt_len[t] of
+ * them the prompt (NULL: none),
+ *   a = z[t,v]
+ *   v in past_t:                     a = a > 0 ? a / repetition[t] : a * repetition[t]
+ *   n > 0 times beyond the prompt:   a = a - (frequency[t] * n + presence[t])
+ *   entries bias_ids[t,k] == v:      a = a + the sum of their bias_values[t,k], added up in their order
+ *   bit v % 32 of allowed[t, v / 32] is 0:  a = -inf, whatever z[t,v] is
+ * in fp32, each operation rounded by itself.  Tokens outside 0 .. V-1 (negative: none) do not count.  A NULL array's rule is left out (past: H = 0; biases: B = 0).
+ *
+ * tide_logit_rules: out[t,v] = a, rounded once to `dtype`; what no rule touches keeps its bits.  out may be the logits themselves (same base and stride), else
+ *   it must not overlap them.
+ * tide_logit_pick: token[t] = the v with the largest a, the lowest of equal ones, log_prob[t] = a[token] - log sum_v exp(a[v]).  Where no token is allowed or all are -inf:
+ *   token -1, log_prob -inf.  A NaN, or +inf at two tokens, among a row's allowed ones: token -1, log_prob NaN.
+ *   The results of both do not depend on timing.
+ *
+ *   logits  device [T rows] of `dtype`, row_stride >= V elements; element alignment.  past device [T,H] int32;  past_len, prompt_len device [T] int32
+ *   repetition, presence, frequency device [T] fp32;  bias_ids int32, bias_values fp32 device [T,B], B <= 1024;  allowed device [T, ceil(V/32)] u32
+ *   out     device [T rows] of `dtype`;  token device [T] int32, log_prob device [T] fp32
+ *   T <= 4194304, V <= 8388608, T * V up to about 2^34 (TIDE_ERR_UNSUPPORTED)
+ *   workspace  device, 16-byte aligned, tide_logit_pick_bytes(T, V) bytes, which grow with T; no initialisation, nothing kept.                  */
+int tide_logit_rules(const void* logits, int dtype, int64_t T, int64_t V, int64_t row_stride, const int32_t* past, int64_t H, const int32_t* past_len,
+                     const int32_t* prompt_len, const float* repetition, const float* presence, const float* frequency, const int32_t* bias_ids,
+                     const float* bias_values, int64_t B, const uint32_t* allowed, void* out, int64_t out_row_stride, void* stream);
+size_t tide_logit_pick_bytes(int64_t T, int64_t V);
+int tide_logit_pick(const void* logits, int dtype, int64_t T, int64_t V, int64_t row_stride, const int32_t* past, int64_t H, const int32_t* past_len,
+                    const int32_t* prompt_len, const float* repetition, const float* presence, const float* frequency, const int32_t* bias_ids,
+                    const float* bias_values, int64_t B, const uint32_t* allowed, int32_t* token, float* log_prob, void* workspace,
+                    size_t workspace_bytes, void* stream);
+
 /* Batch compaction (Sec. 3.4 kernel 2): the tokens that have exited at or before `layer`
  * (exit_layer[t] <= layer) and those that continue, as two index lists in ascending token order --
  * what a layer-skipping runtime needs to gather the continuing tokens after a checkpoint.

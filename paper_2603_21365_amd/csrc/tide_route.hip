@@ -21,7 +21,9 @@
 #include "decode_kernel.hpp"
 #include "few_rows_kernel.hpp"
 #include "head_gemm_kernel.hpp"
+#include "head_q4_kernel.hpp"
 #include "head_rows_kernel.hpp"
+#include "logit_rules_kernel.hpp"
 #include "pack_kernel.hpp"
 #include "prefill_dma_kernel.hpp"
 #include "prefill_kernel.hpp"
@@ -1483,7 +1485,7 @@ int run(const void* hidden, int dtype, int64_t C, int64_t T, int64_t d, int64_t 
 
 extern "C" {
 
-int tide_version(void) { return 112; }
+int tide_version(void) { return 113; }
 
 const char* tide_last_error(void) { return g_err; }
 
@@ -2146,3 +2148,4 @@ int tide_release(void) {
 }  // extern "C"
 
 #include "head_route.hpp"
+#include "answer_route.hpp"

@@ -31,6 +31,8 @@ EXPORTS = (
     "tide_select_exit_packed_noalloc", "tide_noalloc_scratch_bytes", "tide_workspace_allocations", "tide_mfma_probe",
     "tide_exit_project_grad_bytes", "tide_exit_project_grad", "tide_head_workspace_bytes", "tide_head_loss", "tide_head_loss_grad",
     "tide_head_distill", "tide_head_distill_grad",
+    "tide_head_quantize_q4", "tide_head_dequantize_q4", "tide_head_logits_q4_bytes", "tide_head_logits_q4", "tide_logit_rules", "tide_logit_pick_bytes",
+    "tide_logit_pick",
 )
 
 _lib = None
@@ -97,7 +99,18 @@ def load_library() -> ctypes.CDLL:
     lib.tide_head_loss_grad.argtypes = [*head, vp, vp, vp, vp, i64, vp, i64, vp, sz, vp]
     lib.tide_head_distill.argtypes = [*head, vp, vp, i64, f32, vp, vp, vp, vp, sz, vp]
     lib.tide_head_distill_grad.argtypes = [*head, vp, vp, i64, f32, vp, vp, vp, i64, vp, i64, vp, sz, vp]
-    for name in ("tide_exit_project_grad", "tide_head_loss", "tide_head_loss_grad", "tide_head_distill", "tide_head_distill_grad"):
+    lib.tide_head_quantize_q4.argtypes = [vp, ci, i64, i64, i64, i64, vp, vp, ci, vp]
+    lib.tide_head_dequantize_q4.argtypes = [vp, vp, ci, i64, i64, i64, vp, ci, i64, vp]
+    lib.tide_head_logits_q4_bytes.argtypes = [ci, i64, i64]
+    lib.tide_head_logits_q4_bytes.restype = sz
+    lib.tide_head_logits_q4.argtypes = [vp, ci, i64, i64, i64, i64, vp, vp, ci, i64, vp, i64, vp, sz, vp]
+    rules = [vp, ci, i64, i64, i64, vp, i64, vp, vp, vp, vp, vp, vp, vp, i64, vp]
+    lib.tide_logit_rules.argtypes = [*rules, vp, i64, vp]
+    lib.tide_logit_pick.argtypes = [*rules, vp, vp, vp, sz, vp]
+    lib.tide_logit_pick_bytes.argtypes = [i64, i64]
+    lib.tide_logit_pick_bytes.restype = sz
+    for name in ("tide_exit_project_grad", "tide_head_loss", "tide_head_loss_grad", "tide_head_distill", "tide_head_distill_grad",
+                 "tide_head_quantize_q4", "tide_head_dequantize_q4", "tide_head_logits_q4", "tide_logit_rules", "tide_logit_pick"):
         getattr(lib, name).restype = ci
     for name in ("tide_router_eval", "tide_router_eval_packed", "tide_select_exit", "tide_select_exit_packed",
                  "tide_router_pack", "tide_exit_project", "tide_batch_exit", "tide_cosine_labels", "tide_batch_compact", "tide_set_variant", "tide_set_prefill_form", "tide_release",
@@ -674,6 +687,140 @@ def head_distill_grad(x, W, top_values, top_ids, tau, lse, grad_loss, *, want_dx
     _check(load_library().tide_head_distill_grad(*rows, _ptr(top_values), _ptr(top_ids), K, float(tau), _ptr(lse), _ptr(grad_loss), _ptr(dx), d, _ptr(dW), d,
                                                  _ptr(workspace), nbytes, _stream()))
     return dx, dW
+
+
+def _stream_on(device) -> int:
+    """The current stream, for a call whose tensors are on ``device``: that has to be the current device."""
+    if _raw_device is not None and torch.cuda.is_initialized() and device.index != _raw_device():
+        raise ValueError(f"the tensors are on {device}, the current device is another")
+    return _stream()
+
+
+def _scale_code(dtype) -> int:
+    if dtype == torch.float16:
+        return F16
+    if dtype == torch.bfloat16:
+        return BF16
+    raise TypeError(f"scales are float16 or bfloat16, not {dtype}")
+
+
+def _q4(codes, scales, V, d, group):
+    """Codes and scales of a head of V rows and d columns: their sizes."""
+    V, d, group = int(V), int(d), int(group)
+    if group not in (32, 64, 128):
+        raise TideError(-2, f"group = {group}: 32, 64 or 128 columns")
+    rows = (V + 15) // 16
+    if codes.dtype != torch.uint8 or not codes.is_cuda or not codes.is_contiguous() or tuple(codes.shape) != (rows, (d + 127) // 128, 1024):
+        raise ValueError(f"codes must be a contiguous CUDA uint8 tensor of shape {(rows, (d + 127) // 128, 1024)}")
+    code = _scale_code(scales.dtype)
+    if not scales.is_cuda or not scales.is_contiguous() or tuple(scales.shape) != (rows, (d + group - 1) // group, 16) or scales.device != codes.device:
+        raise ValueError(f"scales must be a contiguous CUDA tensor of shape {(rows, (d + group - 1) // group, 16)} on {codes.device}")
+    return V, d, group, code
+
+
+def head_quantize_q4(W, group=128, *, scale_dtype=torch.bfloat16):
+    """An LM head W [V,d] in four bits with a scale per ``group`` (32, 64, 128) columns -> (codes uint8 [ceil(V/16), ceil(d/128), 1024], scales
+    [ceil(V/16), ceil(d/group), 16] of scale_dtype), as the header lays them out."""
+    (V, d), (ws, _) = _rows(W, 2)
+    group, code = int(group), _scale_code(scale_dtype)
+    if group not in (32, 64, 128):
+        raise TideError(-2, f"group = {group}: 32, 64 or 128 columns")
+    rows = (V + 15) // 16
+    codes = torch.empty((rows, (d + 127) // 128, 1024), dtype=torch.uint8, device=W.device)
+    scales = torch.empty((rows, (d + group - 1) // group, 16), dtype=scale_dtype, device=W.device)
+    _check(load_library().tide_head_quantize_q4(_ptr(W), _dtype_code(W), V, d, ws if V > 1 else d, group, _ptr(codes), _ptr(scales), code, _stream_on(W.device)))
+    return codes, scales
+
+
+def head_dequantize_q4(codes, scales, V, d, dtype, group=128):
+    """The weights [V,d] of ``dtype`` that codes and scales stand for."""
+    V, d, group, code = _q4(codes, scales, V, d, group)
+    W = torch.empty((V, d), dtype=dtype, device=codes.device)
+    _check(load_library().tide_head_dequantize_q4(_ptr(codes), _ptr(scales), code, V, d, group, _ptr(W), _dtype_code(W), d, _stream_on(W.device)))
+    return W
+
+
+def head_logits_q4_bytes(dtype: int, T: int, d: int) -> int:
+    """Bytes of workspace a head_logits_q4 call needs (0 and last_error() if unsupported).  They grow with T."""
+    return int(load_library().tide_head_logits_q4_bytes(int(dtype), int(T), int(d)))
+
+
+def head_logits_q4(x, codes, scales, V, group=128, *, out=None, workspace=None):
+    """Rows under an LM head in four bits: x [T,d], codes and scales as head_quantize_q4 gives them, V rows of the head -> logits f32 [T,V]."""
+    (T, d), (xs, _) = _rows(x, 2)
+    V, d, group, code = _q4(codes, scales, V, d, group)
+    if out is None:
+        out = torch.empty((T, V), dtype=torch.float32, device=x.device)
+    (To, Vo), (os_, _) = _rows(out, 2)
+    if To != T or Vo != V or out.dtype != torch.float32 or out.device != x.device or codes.device != x.device:
+        raise ValueError(f"x, codes and out must be on one device, out float32 of shape {(T, V)}")
+    if T == 0:
+        return out
+    dtype = _dtype_code(x)
+    workspace, nbytes = _scratch(workspace, head_logits_q4_bytes(dtype, T, d), x.device)
+    _check(load_library().tide_head_logits_q4(_ptr(x), dtype, T, d, V, xs if T > 1 else d, _ptr(codes), _ptr(scales), code, group, _ptr(out), os_ if T > 1 else V,
+                                              _ptr(workspace), nbytes, _stream_on(x.device)))
+    return out
+
+
+def _rule_args(logits, past, past_len, prompt_len, repetition, presence, frequency, bias_ids, bias_values, allowed):
+    (T, V), (rs, _) = _rows(logits, 2)
+    dev, H, B = logits.device, 0, 0
+    if past is None:
+        if past_len is not None or prompt_len is not None or repetition is not None or presence is not None or frequency is not None:
+            raise ValueError("lengths and penalties need a past")
+    else:
+        H = int(past.shape[-1])
+        _dev(past, torch.int32, (T, H), "past")
+        for t, name in ((past_len, "past_len"), (prompt_len, "prompt_len")):
+            if t is not None:
+                _dev(t, torch.int32, (T,), name)
+        for t, name in ((repetition, "repetition"), (presence, "presence"), (frequency, "frequency")):
+            if t is not None:
+                _dev(t, torch.float32, (T,), name)
+    if (bias_ids is None) != (bias_values is None):
+        raise ValueError("bias_ids and bias_values come together")
+    if bias_ids is not None:
+        B = int(bias_ids.shape[-1])
+        _dev(bias_ids, torch.int32, (T, B), "bias_ids"), _dev(bias_values, torch.float32, (T, B), "bias_values")
+    if allowed is not None:
+        _dev(allowed, torch.int32, (T, (V + 31) // 32), "allowed")
+    for t in (past, past_len, prompt_len, repetition, presence, frequency, bias_ids, bias_values, allowed):
+        if t is not None and t.device != dev:
+            raise ValueError(f"every array must be on {dev}")
+    return T, V, (_ptr(logits), _dtype_code(logits), T, V, rs if T > 1 else V, _ptr(past), H, _ptr(past_len), _ptr(prompt_len), _ptr(repetition), _ptr(presence),
+                  _ptr(frequency), _ptr(bias_ids), _ptr(bias_values), B, _ptr(allowed))
+
+
+def logit_rules(logits, *, past=None, past_len=None, prompt_len=None, repetition=None, presence=None, frequency=None, bias_ids=None, bias_values=None,
+                allowed=None, out=None):
+    """The rules of decoding on logits [T,V]: past int32 [T,H] (negative: none), its length past_len and its prompt's prompt_len int32 [T]; repetition, presence,
+    frequency f32 [T]; bias_ids int32, bias_values f32 [T,B]; allowed int32 [T, ceil(V/32)], a bit per token -> out [T,V] of the logits' dtype
+    (``out`` may be the logits)."""
+    T, V, args = _rule_args(logits, past, past_len, prompt_len, repetition, presence, frequency, bias_ids, bias_values, allowed)
+    if out is None:
+        out = torch.empty((T, V), dtype=logits.dtype, device=logits.device)
+    (To, Vo), (os_, _) = _rows(out, 2)
+    if To != T or Vo != V or out.dtype != logits.dtype or out.device != logits.device:
+        raise ValueError(f"out must be of the logits' dtype, device and shape {(T, V)}")
+    _check(load_library().tide_logit_rules(*args, _ptr(out), os_ if T > 1 else V, _stream_on(logits.device)))
+    return out
+
+
+def logit_pick_bytes(T: int, V: int) -> int:
+    """Bytes of workspace a logit_pick call needs (0 and last_error() if unsupported).  They grow with T."""
+    return int(load_library().tide_logit_pick_bytes(int(T), int(V)))
+
+
+def logit_pick(logits, *, past=None, past_len=None, prompt_len=None, repetition=None, presence=None, frequency=None, bias_ids=None, bias_values=None,
+               allowed=None, workspace=None):
+    """The token with the largest logit under logit_rules' rules -> (token int32 [T], -1 where none is left; log_prob f32 [T])."""
+    T, V, args = _rule_args(logits, past, past_len, prompt_len, repetition, presence, frequency, bias_ids, bias_values, allowed)
+    token = torch.empty(T, dtype=torch.int32, device=logits.device)
+    log_prob = torch.empty(T, dtype=torch.float32, device=logits.device)
+    workspace, nbytes = _scratch(workspace, logit_pick_bytes(T, V), logits.device)
+    _check(load_library().tide_logit_pick(*args, _ptr(token), _ptr(log_prob), _ptr(workspace), nbytes, _stream_on(logits.device)))
+    return token, log_prob
 
 
 class PreparedCall:

@@ -1,0 +1,140 @@
+"""What the answer operators -- the LM head in four bits, the rules of decoding -- refuse before anything is enqueued (no GPU needed), and the size of their workspaces."""
+import pytest
+import torch
+
+from paper_2603_21365_amd import tide_route as tr
+
+FAKE, OTHER = 0x100000, 0x90000000     # never dereferenced: every call below fails its checks first
+OK, INVALID, UNSUPPORTED, ALIGNMENT, WORKSPACE = 0, -1, -2, -3, -4
+
+
+def quantize(W=FAKE, dtype=2, V=100, d=64, ws=64, group=32, codes=FAKE, scales=FAKE, sdtype=2):
+    return tr.load_library().tide_head_quantize_q4(W, dtype, V, d, ws, group, codes, scales, sdtype, None)
+
+
+def dequantize(W=FAKE, dtype=2, V=100, d=64, ws=64, group=32, codes=FAKE, scales=FAKE, sdtype=2):
+    return tr.load_library().tide_head_dequantize_q4(codes, scales, sdtype, V, d, group, W, dtype, ws, None)
+
+
+def logits(x=FAKE, dtype=2, T=4, d=64, V=100, xs=64, codes=FAKE, scales=FAKE, sdtype=2, group=32, out=FAKE, os=100, space=FAKE, nbytes=1 << 30):
+    return tr.load_library().tide_head_logits_q4(x, dtype, T, d, V, xs, codes, scales, sdtype, group, out, os, space, nbytes, None)
+
+
+@pytest.mark.parametrize("call", [quantize, dequantize, logits])
+@pytest.mark.parametrize("bad,status,word", [
+    (dict(dtype=3), INVALID, "dtype"), (dict(sdtype=0), INVALID, "scale_dtype"), (dict(d=0), INVALID, "positive"), (dict(d=16385), UNSUPPORTED, "16384"), (dict(V=0), INVALID, "V = 0"),
+    (dict(V=1 << 24), UNSUPPORTED, "V ="), (dict(group=16), UNSUPPORTED, "group"), (dict(group=256), UNSUPPORTED, "group"), (dict(codes=None), INVALID, "NULL"),
+    (dict(scales=None), INVALID, "NULL"), (dict(codes=FAKE + 8), ALIGNMENT, "codes"), (dict(scales=FAKE + 2), ALIGNMENT, "codes")])
+def test_refusals_of_a_head_in_four_bits(call, bad, status, word):
+    assert call(**bad) == status and word in tr.last_error()
+
+
+@pytest.mark.parametrize("call", [quantize, dequantize])
+@pytest.mark.parametrize("bad,status,word", [(dict(W=None), INVALID, "NULL"), (dict(ws=63), INVALID, "stride"), (dict(W=FAKE + 1), ALIGNMENT, "elements"),
+                                             (dict(V=1 << 23, d=16384, ws=16384), UNSUPPORTED, "too many")])
+def test_refusals_of_weights(call, bad, status, word):
+    assert call(**bad) == status and word in tr.last_error()
+
+
+@pytest.mark.parametrize("bad,status,word", [
+    (dict(T=-1), INVALID, "negative"), (dict(T=1 << 23), UNSUPPORTED, "exceeds"), (dict(T=1 << 22, V=1 << 20, os=1 << 20), UNSUPPORTED, "too many"), (dict(x=None), INVALID, "x must"),
+    (dict(xs=63), INVALID, "x: the row stride"), (dict(x=FAKE + 1), ALIGNMENT, "x must"), (dict(out=None), INVALID, "logits"), (dict(os=99), INVALID, "logits_row_stride"),
+    (dict(out=FAKE + 2), ALIGNMENT, "logits"), (dict(space=None), WORKSPACE, "workspace"), (dict(nbytes=100), WORKSPACE, "workspace"), (dict(space=FAKE + 16), ALIGNMENT, "workspace")])
+def test_refusals_of_rows_under_a_head_in_four_bits(bad, status, word):
+    assert logits(**bad) == status and word in tr.last_error()
+
+
+def rules(z=FAKE, dtype=0, T=4, V=100, rs=100, past=FAKE, H=5, past_len=None, prompt=None, rep=None, pres=None, freq=None, ids=FAKE, values=FAKE, B=3, allowed=None, out=OTHER, os=100):
+    return tr.load_library().tide_logit_rules(z, dtype, T, V, rs, past, H, past_len, prompt, rep, pres, freq, ids, values, B, allowed, out, os, None)
+
+
+def pick(z=FAKE, dtype=0, T=4, V=100, rs=100, past=FAKE, H=5, past_len=None, prompt=None, rep=None, pres=None, freq=None, ids=FAKE, values=FAKE, B=3, allowed=None, token=FAKE,
+         log_prob=FAKE, space=FAKE, nbytes=1 << 20):
+    return tr.load_library().tide_logit_pick(z, dtype, T, V, rs, past, H, past_len, prompt, rep, pres, freq, ids, values, B, allowed, token, log_prob, space, nbytes, None)
+
+
+@pytest.mark.parametrize("call", [rules, pick])
+@pytest.mark.parametrize("bad,status,word", [
+    (dict(dtype=3), INVALID, "dtype"), (dict(T=-1), INVALID, "negative"), (dict(T=1 << 23), UNSUPPORTED, "exceeds"), (dict(V=0), INVALID, "V = 0"), (dict(V=1 << 24), UNSUPPORTED, "V ="),
+    (dict(H=-1), INVALID, "negative"), (dict(B=-1), INVALID, "negative"), (dict(H=1 << 31), UNSUPPORTED, "H ="), (dict(B=1025), UNSUPPORTED, "B ="), (dict(rs=99), INVALID, "row_stride"),
+    (dict(z=None), INVALID, "logits"), (dict(past=None), INVALID, "past"), (dict(ids=None), INVALID, "bias_ids"), (dict(values=None), INVALID, "bias_values"),
+    (dict(z=FAKE + 2), ALIGNMENT, "elements"), (dict(past=FAKE + 2), ALIGNMENT, "4-byte"), (dict(rep=FAKE + 1), ALIGNMENT, "4-byte"), (dict(allowed=FAKE + 2), ALIGNMENT, "4-byte")])
+def test_refusals_of_the_rules(call, bad, status, word):
+    assert call(**bad) == status and word in tr.last_error()
+
+
+@pytest.mark.parametrize("bad,status,word", [(dict(out=None), INVALID, "out"), (dict(os=99), INVALID, "out_row_stride"), (dict(out=OTHER + 2), ALIGNMENT, "out")])
+def test_refusals_of_their_output(bad, status, word):
+    assert rules(**bad) == status and word in tr.last_error()
+
+
+def test_overlapping_outputs_are_refused():
+    """Rows of 100 floats every 300: into the columns beside them, or nowhere near them -- not across them."""
+    for at, stride in ((4, 300), (396, 300), (-4, 300), (804, 300), (0, 301), (1200, 299), (4 * 300 * 3, 300), (4 * 3, 100)):
+        assert rules(rs=300, out=FAKE + at, os=stride) == INVALID and "overlap" in tr.last_error(), (at, stride)
+    assert rules(T=1, out=FAKE + 396) == INVALID and rules(T=1, out=FAKE - 396) == INVALID
+
+
+@pytest.mark.parametrize("bad,status,word", [(dict(token=None), INVALID, "token"), (dict(log_prob=None), INVALID, "log_prob"), (dict(token=FAKE + 2), ALIGNMENT, "4-byte")])
+def test_refusals_of_the_pick(bad, status, word):
+    assert pick(**bad) == status and word in tr.last_error()
+
+
+def test_no_rows_is_no_work():
+    assert logits(T=0, x=None, out=None, space=None) == OK
+    assert rules(T=0, z=None, out=None, past=None, ids=None, values=None) == OK
+    assert pick(T=0, z=None, token=None, log_prob=None, past=None, ids=None, values=None, space=None) == OK
+
+
+def test_workspaces_grow_with_the_rows():
+    for dtype in (tr.F32, tr.F16, tr.BF16):
+        for d in (1, 768, 1600, 16384):
+            sizes = [tr.head_logits_q4_bytes(dtype, T, d) for T in range(0, 700)]
+            assert min(sizes) > 0 and sizes == sorted(sizes)
+    assert tr.head_logits_q4_bytes(3, 4, 64) == 0 and tr.head_logits_q4_bytes(tr.F32, 4, 20000) == 0 and "unsupported" in tr.last_error()
+    for V in (1, 1024, 1025, 128000):
+        sizes = [tr.logit_pick_bytes(T, V) for T in range(0, 700)]
+        assert min(sizes) > 0 and sizes == sorted(sizes)
+    assert tr.logit_pick_bytes(4, 0) == 0 and tr.logit_pick_bytes(-1, 10) == 0
+
+
+class Stand(torch.Tensor):
+    """A tensor that says it is on a GPU, for checks that come before any use of it."""
+    is_cuda = True
+    device = torch.device("cuda", 0)
+
+
+def stand(*shape, dtype=torch.float32):
+    return torch.empty(*shape, dtype=dtype).as_subclass(Stand)
+
+
+def test_the_binding_refuses_other_shapes_and_types():
+    i32 = torch.int32
+    z = stand(3, 70)
+    with pytest.raises(ValueError, match="past"):
+        tr.logit_pick(z, past=stand(3, 5))
+    with pytest.raises(ValueError, match="past"):
+        tr.logit_pick(z, past=stand(2, 5, dtype=i32))
+    with pytest.raises(ValueError, match="need a past"):
+        tr.logit_rules(z, repetition=stand(3))
+    with pytest.raises(ValueError, match="come together"):
+        tr.logit_rules(z, bias_ids=stand(3, 5, dtype=i32))
+    with pytest.raises(ValueError, match="allowed"):
+        tr.logit_rules(z, allowed=stand(3, 2, dtype=i32))
+    with pytest.raises(ValueError, match="out"):
+        tr.logit_rules(z, out=stand(3, 70, dtype=torch.float16))
+    with pytest.raises(ValueError, match="every array"):
+        other = stand(3, 5, dtype=i32)
+        other.device = torch.device("cuda", 1)
+        tr.logit_rules(z, past=other)
+    x, codes, scales = stand(3, 64), stand(5, 1, 1024, dtype=torch.uint8), stand(5, 2, 16, dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="codes"):
+        tr.head_logits_q4(x, codes, scales, 81, 32)
+    with pytest.raises(ValueError, match="scales"):
+        tr.head_logits_q4(x, codes, scales, 80, 64)
+    with pytest.raises(TypeError, match="scales"):
+        tr.head_logits_q4(x, codes, stand(5, 2, 16), 80, 32)
+    with pytest.raises(tr.TideError, match="group"):
+        tr.head_quantize_q4(stand(5, 64), 48)
+    with pytest.raises(ValueError, match="out"):
+        tr.head_logits_q4(x, codes, scales, 80, 32, out=stand(3, 81))
