@@ -4,6 +4,7 @@
 
 namespace {
 
+constexpr int kMostLds = 158 * 1024;                   // dynamic LDS of a workgroup: some is left for what a kernel has beside it
 constexpr int64_t kMostBlocks = ((int64_t)1 << 24) - 1;      // a launch has fewer than 2^32 threads, a workgroup 256
 
 struct Q4Shape {
@@ -73,8 +74,73 @@ int q4_weights(const void* W, void* W_out, int dtype, const Q4Shape& s, int64_t 
     return TIDE_OK;
 }
 
-size_t q4_rows_bytes(int dtype, int64_t T, const Q4Shape& s) {
-    return (size_t)((T + 15) / 16) * s.blocks() * 4 * kQ4TileBytes * (dtype == TIDE_F32 ? kQ4Planes<kF32> : 1);
+// A kernel's dynamic LDS beyond the default, once per device.
+template <auto kKernel> int raise_lds() {
+    static std::atomic<bool> raised[kMaxDevices];
+    int dev = 0;
+    int rc = current_device(&dev);
+    if (rc) return rc;
+    if (!raised[dev].load(std::memory_order_relaxed)) {
+        TIDE_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(kKernel), hipFuncAttributeMaxDynamicSharedMemorySize, kMostLds));
+        raised[dev].store(true, std::memory_order_relaxed);
+    }
+    return TIDE_OK;
+}
+
+// How the rows under a head in four bits are divided.
+struct Q4Plan {
+    int planes;                // bf16 terms of a row's value
+    int64_t T, tiles, blocks;
+    int per;                   // groups of a block of 128 columns
+    unsigned cus;
+    // few rows
+    int rows_log, nt, waves, split, lds;
+    // many rows: tiles of 16 rows of a row block, row blocks, LDS; waves as above
+    int mt;
+    int64_t row_blocks;
+    bool few;
+
+    int few_lds(int log, int nt_, int waves_, int split_) const {
+        return (int)(blocks * (4 * planes * (64 << log) + per * (4 << std::max(log, 2)))) + waves_ * 1024 + (split_ > 1 ? waves_ * nt_ * 1024 : 0);
+    }
+    int region(int mt_) const { return 4 * planes * mt_ * 1024 + (per * mt_ * 64 + 1023) / 1024 * 1024; }
+    int many_lds(int mt_) const { return kQ4Stages * region(mt_) + kQ4ManyThreads / kWave * 1024; }
+    int64_t workspace() const { return few ? 0 : row_blocks * blocks * region(mt); }
+};
+Q4Plan q4_plan(int dtype, int64_t T, const Q4Shape& s, unsigned cus) {
+    Q4Plan p{};
+    p.planes = dtype == TIDE_F32 ? kQ4Planes<kF32> : 1;
+    p.T = T, p.tiles = s.tiles(), p.blocks = s.blocks(), p.per = (int)(128 / s.group), p.cus = cus;
+    while ((1 << p.rows_log) < T && p.rows_log < 4) ++p.rows_log;
+    p.few = T <= 16 && p.few_lds(p.rows_log, 2, 16, 1) <= kMostLds;
+    if (p.few) {
+        // Rows that leave room for several workgroups a CU: small ones, which start and end apart from each other; else one of as many waves as share its CU's tokens
+        // evenly, two tiles a wave where there are enough (bf16, d = 4096, V = 128000, us, 4 waves of one tile / 16 of two: T = 1 49.5 / 53.8, 8 63 / 55, 16 66 / 58).
+        const bool small = p.few_lds(p.rows_log, 1, 4, 1) <= 32 * 1024;
+        p.nt = !small && p.tiles >= 24 * (int64_t)cus ? 2 : 1;
+        p.waves = small ? 4 : (int)std::min<int64_t>(16, std::max<int64_t>(4, (p.tiles + p.nt * (int64_t)cus - 1) / (p.nt * (int64_t)cus)));
+        p.split = 1;
+        // few tokens: waves share tiles until the chip is filled
+        while (p.split < 4 && p.tiles * p.split * 2 <= 8 * (int64_t)cus && p.split * 4 <= p.blocks) p.split *= 2;
+        if (p.split > 1) p.waves = 4;
+        p.lds = p.few_lds(p.rows_log, p.nt, p.waves, p.split);
+        return p;
+    }
+    // Many rows: the least of rounds of workgroups times the matrix steps of a round, for as few waves as fill the chip (a CU's four SIMDs take eight of them)
+    p.nt = 4;
+    double least = 0;
+    for (int mt : {8, 4, 2}) {
+        if (mt == 8 && p.planes > 1) continue;         // (three stages of it are more than the LDS)
+        for (int waves : {8, 4, 2}) {
+            const int64_t row_blocks = (T + 16 * mt - 1) / (16 * mt), sets = (p.tiles + waves * p.nt - 1) / (waves * p.nt);
+            const int64_t together = std::max<int64_t>(1, std::min<int64_t>(kMostLds / p.many_lds(mt), 8 / waves));
+            const int64_t rounds = (sets * row_blocks + cus * together - 1) / (cus * together);
+            const double work = (double)rounds * std::max<double>(mt * 256 * p.planes * ((waves * together + 3) / 4) + 600, 1500);
+            if (least == 0 || work < least) least = work, p.mt = mt, p.waves = waves, p.row_blocks = row_blocks;
+        }
+    }
+    p.lds = p.many_lds(p.mt);
+    return p;
 }
 
 constexpr int64_t kMostPast = (int64_t)1 << 30;
@@ -185,10 +251,11 @@ int run_rules(const RuleCall& c, bool pick) {
     rc = by_dtype(c.dtype, [&](auto dt) -> int {
         constexpr int DT = decltype(dt)::value;
         auto go = [&](auto kernel) -> int {
-            if (lds > 48 * 1024) TIDE_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds));
             hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(kRuleThreads), lds, c.st, p);
             return TIDE_OK;
         };
+        const int rc2 = pick ? raise_lds<&tide_logit_rules_kernel<DT, true>>() : raise_lds<&tide_logit_rules_kernel<DT, false>>();
+        if (rc2) return rc2;
         return pick ? go(&tide_logit_rules_kernel<DT, true>) : go(&tide_logit_rules_kernel<DT, false>);
     });
     if (rc) return rc;
@@ -218,7 +285,9 @@ size_t tide_head_logits_q4_bytes(int dtype, int64_t T, int64_t d) {
         fail(TIDE_ERR_UNSUPPORTED, "unsupported dtype %d, T = %lld or d = %lld", dtype, (long long)T, (long long)d);
         return 0;
     }
-    return std::max<size_t>(256, q4_rows_bytes(dtype, T, Q4Shape{1, d, 128, TIDE_BF16}));
+    // Row blocks of 16 mt rows for the mt that leaves most of them over, groups of 32 columns, no matter how many tokens: more than any call of these rows takes
+    const int64_t planes = dtype == TIDE_F32 ? kQ4Planes<kF32> : 1, blocks = (d + kQ4Cols - 1) / kQ4Cols, most = planes > 1 ? 4 : 8;
+    return (size_t)((T + 16 * most - 1) / (16 * most) * most * blocks * (4 * planes * 1024 + 512) + 256 + 255) & ~size_t(255);
 }
 
 int tide_head_logits_q4(const void* x, int dtype, int64_t T, int64_t d, int64_t V, int64_t x_row_stride, const void* codes, const void* scales, int scale_dtype, int64_t group,
@@ -234,42 +303,52 @@ int tide_head_logits_q4(const void* x, int dtype, int64_t T, int64_t d, int64_t 
     if (!logits) return fail(TIDE_ERR_INVALID_ARG, "logits must not be NULL");
     if (logits_row_stride < V) return fail(TIDE_ERR_INVALID_ARG, "logits_row_stride must be at least V");
     if ((uintptr_t)logits & 3) return fail(TIDE_ERR_ALIGNMENT, "logits must be aligned to a float");
-    const int64_t row_tiles = (T + 15) / 16, waves = row_tiles * s.tiles(), blocks = (waves + 3) / 4;
-    if (blocks > kMostBlocks) return fail(TIDE_ERR_UNSUPPORTED, "T = %lld rows of V = %lld logits are too many for one call", (long long)T, (long long)V);
-    const size_t need = q4_rows_bytes(dtype, T, s);
+    if ((T + 15) / 16 * s.tiles() > 4 * kMostBlocks) return fail(TIDE_ERR_UNSUPPORTED, "T = %lld rows of V = %lld logits are too many for one call", (long long)T, (long long)V);
+    const size_t need = tide_head_logits_q4_bytes(dtype, T, d);
     if (!workspace || workspace_bytes < need) return fail(TIDE_ERR_WORKSPACE, "this call needs %zu bytes of workspace, %zu given", need, workspace ? workspace_bytes : 0);
     if ((uintptr_t)workspace & 255) return fail(TIDE_ERR_ALIGNMENT, "the workspace must be 256-byte aligned");
+    unsigned cus = 0;
+    if ((rc = resident_cus(&cus))) return rc;
+    const Q4Plan plan = q4_plan(dtype, T, s, cus);
     hipStream_t st = (hipStream_t)stream;
-    Q4RowParams r{};
-    r.x = (const char*)x;
-    r.row_bytes = x_row_stride * (int64_t)elem_bytes(dtype);
-    r.out = (char*)workspace;
-    r.T = (int)T;
-    r.d = (int)d;
-    r.steps = (int)s.blocks() * 4;
-    r.chunks = q4_chunks(x, x_row_stride, dtype);
-    r.fragments = row_tiles * r.steps;
-    Q4LogitParams p{};
-    p.rows = (const char*)workspace;
-    p.codes = (const char*)codes;
-    p.scales = (const uint16_t*)scales;
-    p.out = logits;
-    p.out_stride = logits_row_stride;
-    p.T = (int)T;
-    p.V = (int)V;
-    p.blocks = (int)s.blocks();
-    p.groups = (int)s.groups();
-    p.row_tiles = (int)row_tiles;
-    p.half = scale_dtype == TIDE_F16;
-    p.waves = waves;
-    by_dtype(dtype, [&](auto dt) {
-        constexpr int DT = decltype(dt)::value;
-        hipLaunchKernelGGL((tide_head_q4_rows_kernel<DT>), dim3((unsigned)((r.fragments + 3) / 4)), dim3(kQ4Threads), 0, st, r);
-        return by_runs(group, [&](auto runs) {
-            hipLaunchKernelGGL((tide_head_q4_kernel<DT, decltype(runs)::value>), dim3((unsigned)blocks), dim3(kQ4Threads), 0, st, p);
-            return 0;
+    const Q4Rows rows{(const char*)x, x_row_stride * (int64_t)elem_bytes(dtype), (int)T, (int)d, q4_chunks(x, x_row_stride, dtype)};
+    const Q4Head head{(const char*)codes, (const uint16_t*)scales, (int)V, (int)s.tiles(), (int)s.blocks(), (int)s.groups(), scale_dtype == TIDE_F16};
+    using std::integral_constant;
+    rc = by_dtype(dtype, [&](auto dt) -> int {
+        return by_runs(group, [&](auto runs) -> int {
+            constexpr int DT = decltype(dt)::value, kRuns = decltype(runs)::value;
+            auto few = [&](auto tiles) -> int {
+                constexpr int NT = decltype(tiles)::value;
+                int rc2 = raise_lds<&tide_head_q4_few_kernel<DT, kRuns, NT>>();
+                if (rc2) return rc2;
+                const int per_set = plan.waves / plan.split * NT, sets = (int)((plan.tiles + per_set - 1) / per_set);
+                const int together = std::max(1, std::min(kMostLds / plan.lds, plan.waves > 4 ? 1 : dtype == TIDE_F32 ? 5 : 7));
+                const Q4FewParams p{rows, head, logits, logits_row_stride, sets, plan.rows_log, plan.split};
+                hipLaunchKernelGGL((tide_head_q4_few_kernel<DT, kRuns, NT>), dim3((unsigned)std::min<int64_t>(sets, (int64_t)cus * together)), dim3(plan.waves * kWave), plan.lds, st, p);
+                return TIDE_OK;
+            };
+            auto many = [&](auto row_tiles) -> int {
+                constexpr int MT = decltype(row_tiles)::value, NT = 4;
+                int rc2 = raise_lds<&tide_head_q4_many_kernel<DT, kRuns, MT, NT>>();
+                if (rc2) return rc2;
+                const Q4LayParams lay{rows, (char*)workspace, head.blocks, plan.row_blocks * MT * head.blocks};
+                hipLaunchKernelGGL((tide_head_q4_lay_kernel<DT, kRuns, MT>), dim3((unsigned)((lay.waves + 3) / 4)), dim3(kQ4Threads), 0, st, lay);
+                const int per_set = plan.waves * NT, sets = (int)((plan.tiles + per_set - 1) / per_set);
+                const int64_t together = std::max<int64_t>(1, std::min<int64_t>(kMostLds / plan.lds, 8 / plan.waves));
+                const int64_t set_grid = (std::min<int64_t>(sets, std::max<int64_t>(cus * together / plan.row_blocks, 1)) + 7) / 8 * 8;
+                const Q4ManyParams p{(const char*)workspace, head, logits, logits_row_stride, (int)T, (int)plan.row_blocks, sets, (int)set_grid};
+                hipLaunchKernelGGL((tide_head_q4_many_kernel<DT, kRuns, MT, NT>), dim3((unsigned)(set_grid * plan.row_blocks)), dim3(plan.waves * kWave), plan.lds, st, p);
+                return TIDE_OK;
+            };
+            if (plan.few) return plan.nt == 2 ? few(integral_constant<int, 2>{}) : few(integral_constant<int, 1>{});
+            if (plan.mt == 2) return many(integral_constant<int, 2>{});
+            if constexpr (DT != kF32) {
+                if (plan.mt == 8) return many(integral_constant<int, 8>{});
+            }
+            return many(integral_constant<int, 4>{});
         });
     });
+    if (rc) return rc;
     TIDE_HIP(hipGetLastError());
     return TIDE_OK;
 }

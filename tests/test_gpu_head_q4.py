@@ -165,6 +165,29 @@ def test_logits_where_nothing_is_rounded(d, V, dtype, group):
         assert bool((off <= bound).all()), f"T={T}: {off.max()}"
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V,d,group", [(200003, 40, 32), (100, 2100, 128), (3000, 1300, 64)])
+def test_logits_of_many_and_of_few_tokens(V, d, group, dtype):
+    """More tiles of tokens than the chip takes at a time, and so few that waves share the columns of one; sums as above, of integers of one bit fewer."""
+    g = generator(d)
+    codes, scales = torch.randint(0, 16, (V, d), generator=g, device="cpu").to(torch.uint8), torch.pow(2.0, torch.randint(-2, 3, (V, -(-d // group)), generator=g).float())
+    rows, blocks = -(-V // 16), -(-d // 128)
+    full = torch.full((rows * 16, blocks * 128), 8, dtype=torch.uint8)
+    full[:V, :d] = codes
+    n = full.view(rows, 16, blocks, 4, 4, 4, 2).permute(0, 2, 4, 1, 3, 6, 5).reshape(rows, blocks, 1024, 2)
+    s = torch.zeros((rows * 16, scales.shape[1]))
+    s[:V] = scales
+    s = s.view(rows, 16, -1).transpose(1, 2).contiguous().to(torch.bfloat16).cuda()
+    packed_codes = (n[..., 0] | n[..., 1] << 4).contiguous().cuda()
+    w = scales.double().repeat_interleave(group, dim=1)[:, :d] * (codes.double() - 8)
+    for T in (1, 3, 9, 16, 20, 40, 100, 300):
+        if T > 40 and V > 100000:
+            continue
+        x = torch.randint(-2, 3, (T, d), generator=generator(T)).double()
+        got = tr.head_logits_q4(x.to(DTYPES[dtype]).cuda(), packed_codes, s, V, group)
+        assert torch.equal(got.cpu().double(), x @ w.T), f"T={T}"
+
+
 @pytest.mark.parametrize("scale", ["bf16", "f16"])
 @pytest.mark.parametrize("group", [32, 64, 128])
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
