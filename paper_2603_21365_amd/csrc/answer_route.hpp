@@ -5,7 +5,7 @@
 namespace {
 
 constexpr int kMostLds = 158 * 1024;                   // dynamic LDS of a workgroup: some is left for what a kernel has beside it
-constexpr int64_t kMostBlocks = ((int64_t)1 << 24) - 1;      // a launch has fewer than 2^32 threads, a workgroup 256
+constexpr int64_t kMostBlocks = ((int64_t)1 << 24) - 1;      // a launch has fewer than 2^32 threads, a workgroup 256 (of the rules: 1024)
 
 struct Q4Shape {
     int64_t V, d, group;
@@ -144,16 +144,19 @@ Q4Plan q4_plan(int dtype, int64_t T, const Q4Shape& s, unsigned cus) {
 }
 
 constexpr int64_t kMostPast = (int64_t)1 << 30;
-constexpr int64_t kMostBias = 1024;                    // entries of one token are joined by a search through them
-constexpr int kRuleMostSlice = 8192;
+constexpr int64_t kMostBias = kRuleThreads;            // a thread each
+constexpr int kRuleMostSlice = 32768;                 // 64 KiB of counts: two workgroups a CU
 
-// Slices of a row: as few as leave every CU four workgroups.
+// Slices of a row: as few as leave every CU two workgroups, of whole rounds of the workgroup's threads.
 struct RuleShape {
-    int64_t T, V;
+    int dtype;
+    int64_t T, V, H;
     unsigned cus = 256;
+    bool wide() const { return H >= 32768; }           // counts beyond 16 bits
     int slice() const {
-        const int64_t want = (T * V + 4 * (int64_t)cus - 1) / (4 * (int64_t)cus);
-        return (int)std::min<int64_t>(kRuleMostSlice, std::max<int64_t>(1024, (want + 1023) / 1024 * 1024));
+        const int64_t round = 16 / (int64_t)elem_bytes(dtype) * kRuleThreads, most = wide() ? kRuleMostSlice / 2 : kRuleMostSlice;
+        const int64_t slices = std::max<int64_t>((V + most - 1) / most, std::min<int64_t>((2 * (int64_t)cus + T - 1) / T, (V + round - 1) / round));
+        return (int)(((V + slices - 1) / slices + 127) / 128 * 128);
     }
     int64_t slices() const { return (V + slice() - 1) / slice(); }
 };
@@ -218,10 +221,10 @@ int check_rules(const RuleCall& c, bool pick) {
 int run_rules(const RuleCall& c, bool pick) {
     int rc = check_rules(c, pick);
     if (rc || c.T == 0) return rc;
-    RuleShape s{c.T, c.V};
+    RuleShape s{c.dtype, c.T, c.V, c.H};
     if ((rc = resident_cus(&s.cus))) return rc;
     const int64_t slices = s.slices(), blocks = c.T * slices;
-    if (blocks > kMostBlocks) return fail(TIDE_ERR_UNSUPPORTED, "T = %lld rows of V = %lld logits are too many for one call", (long long)c.T, (long long)c.V);
+    if (blocks > kMostBlocks / 4) return fail(TIDE_ERR_UNSUPPORTED, "T = %lld rows of V = %lld logits are too many for one call", (long long)c.T, (long long)c.V);
     if (pick && slices > 1) {
         const size_t need = (size_t)blocks * sizeof(uint4);
         if (!c.workspace || c.workspace_bytes < need) return fail(TIDE_ERR_WORKSPACE, "this call needs %zu bytes of workspace, %zu given", need, c.workspace ? c.workspace_bytes : 0);
@@ -246,20 +249,21 @@ int run_rules(const RuleCall& c, bool pick) {
     p.words = (int)((c.V + 31) / 32);
     p.token = c.token, p.log_prob = c.log_prob;
     p.part = (uint4*)c.workspace;
-    RuleTables none;
-    const int lds = rule_tables(nullptr, p.slice, p.H != 0, p.B != 0, &none);
+    const int lds = rule_tables(p.slice, p.H ? (s.wide() ? 4 : 2) : 0, p.B).bytes;
     rc = by_dtype(c.dtype, [&](auto dt) -> int {
         constexpr int DT = decltype(dt)::value;
-        auto go = [&](auto kernel) -> int {
-            hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(kRuleThreads), lds, c.st, p);
+        auto go = [&](auto picks, auto wide) -> int {
+            constexpr bool kPick = decltype(picks)::value, kWide = decltype(wide)::value;
+            const int rc2 = raise_lds<&tide_logit_rules_kernel<DT, kPick, kWide>>();
+            if (rc2) return rc2;
+            hipLaunchKernelGGL((tide_logit_rules_kernel<DT, kPick, kWide>), dim3((unsigned)blocks), dim3(kRuleThreads), lds, c.st, p);
             return TIDE_OK;
         };
-        const int rc2 = pick ? raise_lds<&tide_logit_rules_kernel<DT, true>>() : raise_lds<&tide_logit_rules_kernel<DT, false>>();
-        if (rc2) return rc2;
-        return pick ? go(&tide_logit_rules_kernel<DT, true>) : go(&tide_logit_rules_kernel<DT, false>);
+        if (s.wide()) return pick ? go(std::true_type{}, std::true_type{}) : go(std::false_type{}, std::true_type{});
+        return pick ? go(std::true_type{}, std::false_type{}) : go(std::false_type{}, std::false_type{});
     });
     if (rc) return rc;
-    if (pick && slices > 1) hipLaunchKernelGGL(tide_logit_join_kernel, dim3((unsigned)((c.T + 3) / 4)), dim3(kRuleThreads), 0, c.st, p.part, p.T, p.slices, c.token, c.log_prob);
+    if (pick && slices > 1) hipLaunchKernelGGL(tide_logit_join_kernel, dim3((unsigned)((c.T + 3) / 4)), dim3(kRuleJoinThreads), 0, c.st, p.part, p.T, p.slices, c.token, c.log_prob);
     TIDE_HIP(hipGetLastError());
     return TIDE_OK;
 }

@@ -1,21 +1,22 @@
 // The rules of decoding on rows of logits: penalties for tokens of the past, biases, a grammar's mask; and the token with the largest of the logits so ruled.
 //
-// A workgroup has a slice of a row's tokens.  It counts the row's past in a table of its slice in LDS (one word per token), lays the biases beside it, then
-// passes over the slice's logits once.  Integer counts do not depend on the order of their atomics, and the entries of one token's bias are added by one thread, in their
-// order: the results do not depend on timing.
+// A workgroup has a slice of a row's tokens, up to 32768.  It counts the row's past in a table of its slice in LDS, 16 bits a token (32 for pasts that could
+// overflow them), then passes over the slice's logits once, the first of which are requested before the counting.  A bias is the business of the thread that
+// has its first entry: it fetched the logit before anything was written, adds up the token's entries in their order and deals with the token in place of the
+// pass.  Integer counts do not depend on the order of their atomics and every sum has a fixed order: the results do not depend on timing.
 #pragma once
 #include "device_utils.hpp"
 
 namespace tide {
 
-constexpr int kRuleThreads = 256;
+constexpr int kRuleThreads = 1024, kRuleJoinThreads = 256;
 
 struct RuleParams {
     const char* z;
     char* out;
     int64_t row_bytes, out_row_bytes;
     int T, V, H, B;
-    int slice, slices;         // tokens of a slice (a multiple of 32), slices of a row
+    int slice, slices;         // tokens of a slice (a multiple of 128), slices of a row
     const int32_t *past, *past_len, *prompt_len;
     const float *repetition, *presence, *frequency;
     const int32_t* bias_ids;
@@ -56,51 +57,42 @@ __device__ __forceinline__ void best_write(const Best& a, int32_t* token, float*
     *log_prob = wrong ? __uint_as_float(0x7fc00000u) : none ? -INFINITY : -log1pf(a.rest);
 }
 
-template <int DT> __device__ __forceinline__ void rule_load(const char* p, float (&x)[16 / Storage<DT>::kBytes]) {
-    uint32_t c[4];
-    __builtin_memcpy(c, p, 16);                        // rows of odd sizes: aligned to their elements only
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        if constexpr (DT == kF32) {
-            x[e] = __uint_as_float(c[e]);
-        } else if constexpr (DT == kBF16) {
-            x[2 * e] = __uint_as_float(c[e] << 16);
-            x[2 * e + 1] = __uint_as_float(c[e] & 0xffff0000u);
-        } else {
-            const f16x2 h = __builtin_bit_cast(f16x2, c[e]);
-            x[2 * e] = (float)h[0];
-            x[2 * e + 1] = (float)h[1];
-        }
-    }
+// 16 bytes of logits, as they lie in memory (rows of odd sizes: aligned to their elements only), and single ones.
+template <int DT> __device__ __forceinline__ float rule_value(const u32x4& raw, int e) {
+    if constexpr (DT == kF32) return __uint_as_float(raw[e]);
+    else if constexpr (DT == kBF16) return __uint_as_float(e % 2 ? raw[e / 2] & 0xffff0000u : raw[e / 2] << 16);
+    else return (float)__builtin_bit_cast(_Float16, (uint16_t)(e % 2 ? raw[e / 2] >> 16 : raw[e / 2]));
 }
-template <int DT> __device__ __forceinline__ float rule_load1(const char* p) {
-    if constexpr (DT == kF32) return *reinterpret_cast<const float*>(p);
-    else if constexpr (DT == kBF16) return bf16_bits_to_f32(*reinterpret_cast<const uint16_t*>(p));
-    else return (float)*reinterpret_cast<const _Float16*>(p);
+template <int DT> __device__ __forceinline__ uint32_t rule_bits(float a) {
+    if constexpr (DT == kF32) return __float_as_uint(a);
+    else if constexpr (DT == kBF16) return __builtin_bit_cast(uint16_t, (__bf16)a);
+    else return __builtin_bit_cast(uint16_t, (_Float16)a);
 }
-template <int DT> __device__ __forceinline__ void rule_store1(char* p, float x) {
-    if constexpr (DT == kF32) *reinterpret_cast<float*>(p) = x;
-    else if constexpr (DT == kBF16) *reinterpret_cast<__bf16*>(p) = (__bf16)x;
-    else *reinterpret_cast<_Float16*>(p) = (_Float16)x;
+template <int DT> constexpr uint32_t kRuleLow = DT == kF32 ? 0xff800000u : DT == kBF16 ? 0xff80u : 0xfc00u;      // -inf
+template <int DT> __device__ __forceinline__ void rule_insert(u32x4& raw, int e, uint32_t bits) {
+    if constexpr (DT == kF32) raw[e] = bits;
+    else raw[e / 2] = e % 2 ? (raw[e / 2] & 0xffffu) | bits << 16 : (raw[e / 2] & 0xffff0000u) | bits;
 }
-template <int DT> __device__ __forceinline__ void rule_store(char* p, const float (&x)[16 / Storage<DT>::kBytes]) {
-    uint32_t c[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        if constexpr (DT == kF32) c[e] = __float_as_uint(x[e]);
-        else if constexpr (DT == kBF16) c[e] = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)x[2 * e], (__bf16)x[2 * e + 1]});
-        else c[e] = __builtin_bit_cast(uint32_t, f16x2{(_Float16)x[2 * e], (_Float16)x[2 * e + 1]});
-    }
-    __builtin_memcpy(p, c, 16);
+template <int DT> __device__ __forceinline__ uint32_t rule_load1(const char* p) {
+    if constexpr (DT == kF32) return *reinterpret_cast<const uint32_t*>(p);
+    else return *reinterpret_cast<const uint16_t*>(p);
+}
+template <int DT> __device__ __forceinline__ void rule_store1(char* p, uint32_t bits) {
+    if constexpr (DT == kF32) *reinterpret_cast<uint32_t*>(p) = bits;
+    else *reinterpret_cast<uint16_t*>(p) = (uint16_t)bits;
 }
 
-// One logit's rules; every operation rounded by itself, in the order of the formula.
+// The past's rules for one logit; every operation rounded by itself, in the order of the formula.  Division by the row's penalty: times its reciprocal in 64 bits, which
+// is off by 2^-52 of the quotient, and a quotient of two 24-bit numbers is never that near to a midpoint of two 24-bit ones (2^-49): rounded to 32 bits it is the quotient
+// rounded once.
 struct RuleRow {
     float repetition, presence, frequency;
+    double inverse;
 };
 __device__ __forceinline__ float rule_past(float a, uint32_t count, const RuleRow& r) {
 #pragma clang fp contract(off)
-    if (count) a = a > 0.0f ? a / r.repetition : a * r.repetition;
+    const float less = (float)((double)a * r.inverse), more = a * r.repetition;
+    a = a > 0.0f ? less : more;
     if (count > 1) {
         const float often = r.frequency * (float)(count >> 1);
         a = a - (often + r.presence);
@@ -108,150 +100,237 @@ __device__ __forceinline__ float rule_past(float a, uint32_t count, const RuleRo
     return a;
 }
 
-// The tables of a slice, in LDS.
+// A slice's tables in LDS.  A token's count: twice the times that it was generated, and bit 0 where the prompt has it.
 struct RuleTables {
-    uint32_t* counts;          // of a token: twice the times that it was generated, and bit 0 where the prompt has it
-    float* bias;               // the sum of a token's entries, where it has any
-    uint32_t *biased, *twice;  // a bit for each token with an entry, with several
+    int counts, ids, values, biased, twice, bytes;     // biased, twice: a bit for each token that has an entry, several
 };
-// The layout; returns its bytes.
-__host__ __device__ inline int rule_tables(char* base, int slice, bool past, bool bias, RuleTables* t) {
-    int at = 0;
-    t->counts = (uint32_t*)base;
-    if (past) at += slice * 4;
-    t->bias = (float*)(base + at);
-    if (bias) at += slice * 4;
-    t->biased = (uint32_t*)(base + at);
-    if (bias) at += slice / 8;
-    t->twice = (uint32_t*)(base + at);
-    if (bias) at += slice / 8;
-    return at;
-}
-__device__ __forceinline__ void rule_fill(const RuleParams& p, int t, int v0, int width, const RuleTables& tab) {
-    const int tid = threadIdx.x;
-    if (p.H)
-        for (int i = tid; i < p.slice; i += kRuleThreads) tab.counts[i] = 0;
-    if (p.B)
-        for (int i = tid; i < p.slice / 32; i += kRuleThreads) tab.biased[i] = tab.twice[i] = 0;
-    __syncthreads();
-    if (p.H) {
-        const int32_t* past = p.past + (int64_t)t * p.H;
-        const int n = p.past_len ? min(p.past_len[t], p.H) : p.H, prompt = p.prompt_len ? p.prompt_len[t] : 0;
-        for (int i = tid; i < n; i += kRuleThreads) {
-            const uint32_t at = (uint32_t)past[i] - (uint32_t)v0;      // (a negative token is beyond any slice)
-            if (at >= (uint32_t)width) continue;
-            if (i >= prompt) atomicAdd(&tab.counts[at], 2u);
-            else atomicOr(&tab.counts[at], 1u);
-        }
-    }
-    if (p.B) {
-        const int32_t* ids = p.bias_ids + (int64_t)t * p.B;
-        const float* values = p.bias_values + (int64_t)t * p.B;
-        for (int k = tid; k < p.B; k += kRuleThreads) {
-            const uint32_t at = (uint32_t)ids[k] - (uint32_t)v0, bit = 1u << (at & 31);
-            if (at < (uint32_t)width && (atomicOr(&tab.biased[at / 32], bit) & bit)) atomicOr(&tab.twice[at / 32], bit);
-        }
-        __syncthreads();
-        for (int k = tid; k < p.B; k += kRuleThreads) {
-            const int32_t id = ids[k];
-            const uint32_t at = (uint32_t)id - (uint32_t)v0;
-            if (at >= (uint32_t)width) continue;
-            float sum = values[k];
-            if (tab.twice[at / 32] >> (at & 31) & 1) { // the first entry of a token adds up the others, in their order
-                bool first = true;
-                for (int m = 0; m < k && first; ++m) first = ids[m] != id;
-                if (!first) continue;
-                for (int m = k + 1; m < p.B; ++m)
-                    if (ids[m] == id) sum += values[m];
-            }
-            tab.bias[at] = sum;
-        }
-    }
-    __syncthreads();
+__host__ __device__ inline RuleTables rule_tables(int slice, int count_bytes, int B) {
+    RuleTables t{};
+    const int entries = (B + 3) / 4 * 4;
+    t.ids = t.counts + slice * count_bytes;
+    t.values = t.ids + entries * 4;
+    t.biased = t.values + entries * 4;
+    t.twice = t.biased + (B ? slice / 8 : 0);
+    t.bytes = t.twice + (B ? slice / 8 : 0);
+    return t;
 }
 
-template <int DT, bool kPick> __global__ __launch_bounds__(kRuleThreads) void tide_logit_rules_kernel(RuleParams p) {
-    constexpr int kB = Storage<DT>::kBytes, N = 16 / kB;
+// kWide: counts of 32 bits.
+template <int DT, bool kPick, bool kWide> __global__ __launch_bounds__(kRuleThreads) void tide_logit_rules_kernel(RuleParams p) {
+    constexpr int kB = Storage<DT>::kBytes, N = 16 / kB, kAhead = 4, kStep = kRuleThreads * N;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     __shared__ Best of_wave[kRuleThreads / kWave];
-    const int t = blockIdx.x / p.slices, part = blockIdx.x - t * p.slices, v0 = part * p.slice, width = min(p.slice, p.V - v0);
-    RuleTables tab;
-    rule_tables(lds, p.slice, p.H != 0, p.B != 0, &tab);
-    if (p.H || p.B) rule_fill(p, t, v0, width, tab);
-    const RuleRow row = {p.repetition ? p.repetition[t] : 1.0f, p.presence ? p.presence[t] : 0.0f, p.frequency ? p.frequency[t] : 0.0f};
-    const char* z = p.z + (int64_t)t * p.row_bytes;
-    char* out = kPick ? nullptr : p.out + (int64_t)t * p.out_row_bytes;
-    const uint32_t* allowed = p.allowed ? p.allowed + (int64_t)t * p.words : nullptr;
-    Best best = best_none();
-    for (int i = threadIdx.x * N; i < width; i += kRuleThreads * N) {
-        const int v = v0 + i, n = min(N, width - i);
-        float a[N];
-        if (n == N) {
-            rule_load<DT>(z + (int64_t)v * kB, a);
+    const int tid = threadIdx.x, t = blockIdx.x / p.slices, part = blockIdx.x - t * p.slices, v0 = part * p.slice, width = min(p.slice, p.V - v0);
+    const char* const z = p.z + (int64_t)t * p.row_bytes + (int64_t)v0 * kB;
+    char* const out = kPick ? nullptr : p.out + (int64_t)t * p.out_row_bytes + (int64_t)v0 * kB;
+    const uint32_t* const allowed = p.allowed ? p.allowed + (int64_t)t * p.words + v0 / 32 : nullptr;
+
+    u32x4 raw[kAhead];
+    uint32_t may[kAhead];
+    auto request = [&](int slot, int i) {
+        raw[slot] = u32x4{0, 0, 0, 0};
+        may[slot] = 0xffffffffu;
+        if (i >= width) return;
+        if (allowed) may[slot] = allowed[i / 32] >> (i & 31);
+        if (i + N <= width) {
+            __builtin_memcpy(&raw[slot], z + (int64_t)i * kB, 16);
         } else {
-#pragma unroll
-            for (int e = 0; e < N; ++e) a[e] = e < n ? rule_load1<DT>(z + (int64_t)(v + e) * kB) : -INFINITY;
-        }
-        if (p.H) {
-#pragma unroll
-            for (int e = 0; e < N; ++e) a[e] = rule_past(a[e], tab.counts[i + e], row);
-        }
-        if (p.B) {
-            const uint32_t bits = tab.biased[i / 32] >> (i & 31);
-            if (bits & ((1u << N) - 1)) {
-#pragma unroll
-                for (int e = 0; e < N; ++e)
-                    if (bits >> e & 1) a[e] += tab.bias[i + e];
-            }
-        }
-        if (allowed) {
-            const uint32_t bits = allowed[v / 32] >> (v & 31);
 #pragma unroll
             for (int e = 0; e < N; ++e)
-                if (!(bits >> e & 1)) a[e] = -INFINITY;
+                if (i + e < width) rule_insert<DT>(raw[slot], e, rule_load1<DT>(z + (int64_t)(i + e) * kB));
         }
-        if constexpr (!kPick) {
-            if (n == N) {
-                rule_store<DT>(out + (int64_t)v * kB, a);
-            } else {
+    };
+#pragma unroll
+    for (int slot = 0; slot < kAhead; ++slot) request(slot, tid * N + slot * kStep);
+
+    const RuleTables at = rule_tables(p.slice, p.H ? (kWide ? 4 : 2) : 0, p.B);
+    uint32_t* const counts = reinterpret_cast<uint32_t*>(lds + at.counts);
+    RuleRow row = {1.0f, 0.0f, 0.0f, 1.0};
+    int32_t bias_id = -1;      // this thread's entry: its token, where that is in the slice and the entry its first; the logit; the sum of the token's entries
+    uint32_t bias_bits = 0;
+    float bias = 0.0f;
+    if (p.H || p.B) {
+        const int32_t* const past = p.past + (int64_t)t * p.H;
+        // up to 16 tokens a thread at a time; the first are requested before the tables are cleared
+        constexpr int kTokens = 4 * kRuleThreads;
+        int32_t some[4][4];
+        auto bring = [&](int i0, int n) {
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int i = i0 + u * kTokens + tid * 4;
+                if (i + 4 <= n) {
+                    __builtin_memcpy(some[u], past + i, 16);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) some[u][e] = i + e < n ? past[i + e] : -1;
+                }
+            }
+        };
+        if (p.H) bring(0, p.H);
+        const int n = p.past_len ? min(p.past_len[t], p.H) : p.H, prompt = p.prompt_len ? p.prompt_len[t] : 0;
+        if (p.repetition) row.repetition = p.repetition[t];
+        if (p.presence) row.presence = p.presence[t];
+        if (p.frequency) row.frequency = p.frequency[t];
+        if (tid < p.B) {
+            bias_id = p.bias_ids[(int64_t)t * p.B + tid];
+            bias = p.bias_values[(int64_t)t * p.B + tid];
+            if ((uint32_t)bias_id - (uint32_t)v0 < (uint32_t)width) bias_bits = rule_load1<DT>(z + (int64_t)(bias_id - v0) * kB);
+        }
+        for (int i = tid * 16; i < at.bytes; i += kRuleThreads * 16)
+            if (i < at.ids || i >= at.biased) *reinterpret_cast<u32x4*>(lds + i) = u32x4{0, 0, 0, 0};
+        if (tid < (p.B + 3) / 4 * 4) {
+            reinterpret_cast<int32_t*>(lds + at.ids)[tid] = bias_id;
+            reinterpret_cast<float*>(lds + at.values)[tid] = bias;
+        }
+        __syncthreads();
+        for (int i0 = 0; i0 < n;) {
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int i = i0 + u * kTokens + tid * 4 + e;
+                    const uint32_t v = (uint32_t)some[u][e] - (uint32_t)v0;        // (a negative token is beyond any slice)
+                    if (i >= n || v >= (uint32_t)width) continue;
+                    uint32_t* const word = kWide ? counts + v : counts + v / 2;
+                    const int shift = kWide ? 0 : 16 * (v & 1);
+                    if (i >= prompt) atomicAdd(word, 2u << shift);
+                    else atomicOr(word, 1u << shift);
+                }
+            i0 += 4 * kTokens;
+            if (i0 < n) bring(i0, n);
+        }
+        if (p.B) {
+            uint32_t *const biased = reinterpret_cast<uint32_t*>(lds + at.biased), *const twice = reinterpret_cast<uint32_t*>(lds + at.twice);
+            const uint32_t v = (uint32_t)bias_id - (uint32_t)v0, bit = 1u << (v & 31);
+            const bool here = tid < p.B && v < (uint32_t)width;
+            if (here && (atomicOr(&biased[v / 32], bit) & bit)) atomicOr(&twice[v / 32], bit);
+            __syncthreads();
+            if (!here) bias_id = -1;
+            if (here && (twice[v / 32] & bit)) {       // the first entry of a token adds up the others, in their order
+                const int32_t id = bias_id;
+                for (int m = 0; m < p.B; m += 4) {
+                    const int4 ids = *reinterpret_cast<const int4*>(lds + at.ids + m * 4);
+                    const float4 values = *reinterpret_cast<const float4*>(lds + at.values + m * 4);
+                    auto one = [&](int k, int32_t other, float value) {
+                        if (other != id) return;
+                        if (k < tid) bias_id = -1;
+                        else if (k > tid) bias += value;
+                    };
+                    one(m, ids.x, values.x), one(m + 1, ids.y, values.y), one(m + 2, ids.z, values.z), one(m + 3, ids.w, values.w);
+                }
+            }
+        }
+        __syncthreads();
+        row.inverse = 1.0 / (double)row.repetition;
+    }
+    auto count_of = [&](uint32_t v) { return kWide ? counts[v] : counts[v / 2] >> (16 * (v & 1)) & 0xffffu; };
+
+    Best best = best_none();
+    for (int i0 = 0; i0 < width; i0 += kAhead * kStep) {
+#pragma unroll
+        for (int slot = 0; slot < kAhead; ++slot) {
+            const int i = i0 + slot * kStep + tid * N;
+            u32x4 now = raw[slot];
+            const uint32_t bits = may[slot];
+            request(slot, i + kAhead * kStep);
+            if (i >= width) continue;
+            const int n = width - i;
+            float a[N];
+            if constexpr (kPick) {
+#pragma unroll
+                for (int e = 0; e < N; ++e) a[e] = rule_value<DT>(now, e);
+            }
+            if (p.H) {
+                uint32_t c[kWide ? N : N / 2];
+#pragma unroll
+                for (int w = 0; w < (kWide ? N : N / 2); ++w) c[w] = counts[(kWide ? i : i / 2) + w];
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    const uint32_t count = kWide ? c[e] : c[e / 2] >> (16 * (e % 2)) & 0xffffu;
+                    if (count) {
+                        if constexpr (kPick) a[e] = rule_past(a[e], count, row);
+                        else rule_insert<DT>(now, e, rule_bits<DT>(rule_past(rule_value<DT>(now, e), count, row)));
+                    }
+                }
+            }
+            if constexpr (!kPick) {
 #pragma unroll
                 for (int e = 0; e < N; ++e)
-                    if (e < n) rule_store1<DT>(out + (int64_t)(v + e) * kB, a[e]);
-            }
-        } else {
-            float most = a[0];
+                    if (!(bits >> e & 1)) rule_insert<DT>(now, e, kRuleLow<DT>);
+                if (n >= N) {
+                    __builtin_memcpy(out + (int64_t)i * kB, &now, 16);
+                } else {
 #pragma unroll
-            for (int e = 1; e < N; ++e) most = fmaxf(most, a[e]);
-            int own = -1;
-            if (most > best.most) {
+                    for (int e = 0; e < N; ++e)
+                        if (e < n) rule_store1<DT>(out + (int64_t)(i + e) * kB, kB == 4 ? now[e % 4] : now[e / 2 % 4] >> (16 * (e % 2)) & 0xffffu);
+                }
+            } else {
+                uint32_t out_of_it = ~bits;            // masked, beyond the row, or a bias's thread's
+                if (n < N) out_of_it |= ~0u << n;
+                if (p.B) out_of_it |= reinterpret_cast<const uint32_t*>(lds + at.biased)[i / 32] >> (i & 31);
 #pragma unroll
-                for (int e = N - 1; e >= 0; --e) own = a[e] == most ? e : own;
-                if (best.token >= 0) best.rest = (1.0f + best.rest) * __expf(best.most - most);
-                best.most = most;
-                best.token = v + own;
-            }
+                for (int e = 0; e < N; ++e)
+                    if (out_of_it >> e & 1) a[e] = -INFINITY;
+                float most = a[0];
 #pragma unroll
-            for (int e = 0; e < N; ++e) {
-                if (best.token >= 0 ? e != own : a[e] != a[e]) best.rest += __expf(a[e] - best.most);
+                for (int e = 1; e < N; ++e) most = fmaxf(most, a[e]);
+                int own = -1;
+                if (most > best.most) {
+#pragma unroll
+                    for (int e = N - 1; e >= 0; --e) own = a[e] == most ? e : own;
+                    if (best.token >= 0) best.rest = (1.0f + best.rest) * __expf(best.most - most);
+                    best.most = most;
+                    best.token = v0 + i + own;
+                }
+#pragma unroll
+                for (int e = 0; e < N; ++e)
+                    if (best.token >= 0 ? e != own : a[e] != a[e]) best.rest += __expf(a[e] - best.most);
             }
         }
     }
-    if constexpr (kPick) {
+    if constexpr (!kPick) {
+        if (p.B) {
+            __syncthreads();                           // (the pass wrote these tokens without their biases)
+            if (bias_id >= 0) {
+                const uint32_t v = (uint32_t)(bias_id - v0);
+                float a = rule_value<DT>(u32x4{bias_bits, 0, 0, 0}, 0);
+                if (p.H) {
+                    const uint32_t count = count_of(v);
+                    if (count) a = rule_past(a, count, row);
+                }
+                const bool is_allowed = !allowed || (allowed[v / 32] >> (v & 31) & 1);
+                rule_store1<DT>(out + (int64_t)v * kB, is_allowed ? rule_bits<DT>(a + bias) : kRuleLow<DT>);
+            }
+        }
+    } else {
+        if (bias_id >= 0) {
+            const uint32_t v = (uint32_t)(bias_id - v0);
+            float a = rule_value<DT>(u32x4{bias_bits, 0, 0, 0}, 0);
+            if (p.H) {
+                const uint32_t count = count_of(v);
+                if (count) a = rule_past(a, count, row);
+            }
+            a += bias;
+            if (allowed && !(allowed[v / 32] >> (v & 31) & 1)) a = -INFINITY;
+            if (a != a) best.rest = a;
+            else if (a > -INFINITY) best = best_of(best, Best{a, bias_id, 0.0f});
+        }
         best = best_of_wave(best);
-        if (threadIdx.x % kWave == 0) of_wave[threadIdx.x / kWave] = best;
+        if (tid % kWave == 0) of_wave[tid / kWave] = best;
         __syncthreads();
-        if (threadIdx.x == 0) {
-#pragma unroll
-            for (int w = 1; w < kRuleThreads / kWave; ++w) best = best_of(best, of_wave[w]);
-            if (p.slices == 1) best_write(best, p.token + t, p.log_prob + t);
-            else p.part[(int64_t)t * p.slices + part] = make_uint4(__float_as_uint(best.most), (uint32_t)best.token, __float_as_uint(best.rest), 0u);
+        if (tid < kWave) {
+            best = best_of_wave(tid < kRuleThreads / kWave ? of_wave[tid] : best_none());
+            if (tid == 0) {
+                if (p.slices == 1) best_write(best, p.token + t, p.log_prob + t);
+                else p.part[(int64_t)t * p.slices + part] = make_uint4(__float_as_uint(best.most), (uint32_t)best.token, __float_as_uint(best.rest), 0u);
+            }
         }
     }
 }
 
 // The slices of a row joined: a wave per row.
-__global__ __launch_bounds__(kRuleThreads) void tide_logit_join_kernel(const uint4* part, int T, int slices, int32_t* token, float* log_prob) {
-    const int t = blockIdx.x * (kRuleThreads / kWave) + threadIdx.x / kWave;
+__global__ __launch_bounds__(kRuleJoinThreads) void tide_logit_join_kernel(const uint4* part, int T, int slices, int32_t* token, float* log_prob) {
+    const int t = blockIdx.x * (kRuleJoinThreads / kWave) + threadIdx.x / kWave;
     if (t >= T) return;
     Best best = best_none();
     for (int i = threadIdx.x % kWave; i < slices; i += kWave) {
