@@ -43,13 +43,23 @@ __device__ __forceinline__ Best best_of(const Best& a, const Best& b) {
     // (equal infinities: the difference is no number and the sum becomes none, as the log-probability of one of two infinities is)
     return Best{hi.most, hi.token, hi.rest + (1.0f + lo.rest) * __expf(lo.most - hi.most)};
 }
-__device__ __forceinline__ Best best_exchange(const Best& a, int x) {
-    return Best{__shfl_xor(a.most, x, kWave), __shfl_xor(a.token, x, kWave), __shfl_xor(a.rest, x, kWave)};
+// The same over a wave: the largest, the lowest of its tokens, then every lane's sum relative to it, added up in a fixed order.
+template <int kCtrl> __device__ __forceinline__ uint32_t dpp_u32(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, kCtrl, 0xF, 0xF, false); }
+template <typename F> __device__ __forceinline__ uint32_t wave_fold(uint32_t v, F&& f) {
+    v = f(v, dpp_u32<kDppXor1>(v));
+    v = f(v, dpp_u32<kDppXor2>(v));
+    v = f(v, dpp_u32<kDppHalfMirror>(v));
+    v = f(v, dpp_u32<kDppRor8>(v));
+    v = f(v, (uint32_t)__shfl_xor((int)v, 16, kWave));
+    return f(v, (uint32_t)__shfl_xor((int)v, 32, kWave));
 }
-__device__ __forceinline__ Best best_of_wave(Best a) {
-#pragma unroll
-    for (int x = 1; x < kWave; x <<= 1) a = best_of(a, best_exchange(a, x));
-    return a;
+__device__ __forceinline__ Best best_of_wave(const Best& a) {
+    const float most = __uint_as_float(wave_fold(__float_as_uint(a.most), [](uint32_t x, uint32_t y) { return __float_as_uint(fmaxf(__uint_as_float(x), __uint_as_float(y))); }));
+    // (no token: the largest unsigned number)
+    const int32_t token = (int32_t)wave_fold(a.most == most ? (uint32_t)a.token : ~0u, [](uint32_t x, uint32_t y) { return min(x, y); });
+    float rest = a.rest;
+    if (a.token >= 0) rest = a.token == token ? rest : (1.0f + rest) * __expf(a.most - most);
+    return Best{most, token, wave_sum(rest)};
 }
 __device__ __forceinline__ void best_write(const Best& a, int32_t* token, float* log_prob) {
     const bool none = a.token < 0, wrong = a.rest != a.rest;
@@ -120,7 +130,7 @@ template <int DT, bool kPick, bool kWide> __global__ __launch_bounds__(kRuleThre
     constexpr int kB = Storage<DT>::kBytes, N = 16 / kB, kAhead = 4, kStep = kRuleThreads * N;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     __shared__ Best of_wave[kRuleThreads / kWave];
-    const int tid = threadIdx.x, t = blockIdx.x / p.slices, part = blockIdx.x - t * p.slices, v0 = part * p.slice, width = min(p.slice, p.V - v0);
+    const int tid = threadIdx.x, t = blockIdx.x / p.slices, part = blockIdx.x - t * p.slices, v0 = part * p.slice, width = min(p.slice, p.V - v0), whole = width & -N;
     const char* const z = p.z + (int64_t)t * p.row_bytes + (int64_t)v0 * kB;
     char* const out = kPick ? nullptr : p.out + (int64_t)t * p.out_row_bytes + (int64_t)v0 * kB;
     const uint32_t* const allowed = p.allowed ? p.allowed + (int64_t)t * p.words + v0 / 32 : nullptr;
@@ -128,53 +138,47 @@ template <int DT, bool kPick, bool kWide> __global__ __launch_bounds__(kRuleThre
     u32x4 raw[kAhead];
     uint32_t may[kAhead];
     auto request = [&](int slot, int i) {
-        raw[slot] = u32x4{0, 0, 0, 0};
         may[slot] = 0xffffffffu;
-        if (i >= width) return;
+        if (i >= whole) return;
         if (allowed) may[slot] = allowed[i / 32] >> (i & 31);
-        if (i + N <= width) {
-            __builtin_memcpy(&raw[slot], z + (int64_t)i * kB, 16);
-        } else {
-#pragma unroll
-            for (int e = 0; e < N; ++e)
-                if (i + e < width) rule_insert<DT>(raw[slot], e, rule_load1<DT>(z + (int64_t)(i + e) * kB));
-        }
+        __builtin_memcpy(&raw[slot], z + (int64_t)i * kB, 16);
     };
 #pragma unroll
     for (int slot = 0; slot < kAhead; ++slot) request(slot, tid * N + slot * kStep);
 
     const RuleTables at = rule_tables(p.slice, p.H ? (kWide ? 4 : 2) : 0, p.B);
     uint32_t* const counts = reinterpret_cast<uint32_t*>(lds + at.counts);
+    uint32_t *const biased = reinterpret_cast<uint32_t*>(lds + at.biased), *const twice = reinterpret_cast<uint32_t*>(lds + at.twice);
     RuleRow row = {1.0f, 0.0f, 0.0f, 1.0};
-    int32_t bias_id = -1;      // this thread's entry: its token, where that is in the slice and the entry its first; the logit; the sum of the token's entries
-    uint32_t bias_bits = 0;
+    // this thread's single tokens of the slice, or -1: its bias's, where that is the first entry of its token, and one of those behind the last whole 16 bytes
+    int bias_at = -1, tail_at = tid < width - whole ? whole + tid : -1;
     float bias = 0.0f;
+    uint32_t bias_bits = 0, tail_bits = tail_at >= 0 ? rule_load1<DT>(z + (int64_t)tail_at * kB) : 0;
     if (p.H || p.B) {
         const int32_t* const past = p.past + (int64_t)t * p.H;
-        // up to 16 tokens a thread at a time; the first are requested before the tables are cleared
+        // 16 tokens a thread at a time; the first are requested before the tables are cleared
         constexpr int kTokens = 4 * kRuleThreads;
-        int32_t some[4][4];
-        auto bring = [&](int i0, int n) {
+        const int whole_past = p.H & ~3;
+        int32_t some[4][4], last = -1;
+        auto bring = [&](int i0) {
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
                 const int i = i0 + u * kTokens + tid * 4;
-                if (i + 4 <= n) {
-                    __builtin_memcpy(some[u], past + i, 16);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) some[u][e] = i + e < n ? past[i + e] : -1;
-                }
+                if (i < whole_past) __builtin_memcpy(some[u], past + i, 16);
             }
         };
-        if (p.H) bring(0, p.H);
-        const int n = p.past_len ? min(p.past_len[t], p.H) : p.H, prompt = p.prompt_len ? p.prompt_len[t] : 0;
+        bring(0);
+        if (tid < p.H - whole_past) last = past[whole_past + tid];
+        const int n = p.H && p.past_len ? min(p.past_len[t], p.H) : p.H, prompt = p.prompt_len ? p.prompt_len[t] : 0;
         if (p.repetition) row.repetition = p.repetition[t];
         if (p.presence) row.presence = p.presence[t];
         if (p.frequency) row.frequency = p.frequency[t];
+        int32_t bias_id = -1;
         if (tid < p.B) {
             bias_id = p.bias_ids[(int64_t)t * p.B + tid];
             bias = p.bias_values[(int64_t)t * p.B + tid];
-            if ((uint32_t)bias_id - (uint32_t)v0 < (uint32_t)width) bias_bits = rule_load1<DT>(z + (int64_t)(bias_id - v0) * kB);
+            if ((uint32_t)bias_id - (uint32_t)v0 < (uint32_t)width) bias_at = bias_id - v0;
+            if (bias_at >= 0) bias_bits = rule_load1<DT>(z + (int64_t)bias_at * kB);
         }
         for (int i = tid * 16; i < at.bytes; i += kRuleThreads * 16)
             if (i < at.ids || i >= at.biased) *reinterpret_cast<u32x4*>(lds + i) = u32x4{0, 0, 0, 0};
@@ -183,58 +187,65 @@ template <int DT, bool kPick, bool kWide> __global__ __launch_bounds__(kRuleThre
             reinterpret_cast<float*>(lds + at.values)[tid] = bias;
         }
         __syncthreads();
-        for (int i0 = 0; i0 < n;) {
+        auto count = [&](int32_t token, int i) {
+            const uint32_t v = (uint32_t)token - (uint32_t)v0;         // (a negative token is beyond any slice)
+            if (i >= n || v >= (uint32_t)width) return;
+            uint32_t* const word = kWide ? counts + v : counts + v / 2;
+            const int shift = kWide ? 0 : 16 * (v & 1);
+            if (i >= prompt) atomicAdd(word, 2u << shift);
+            else atomicOr(word, 1u << shift);
+        };
+        for (int i0 = 0; i0 < n; i0 += 4 * kTokens) {
+            if (i0) bring(i0);
 #pragma unroll
-            for (int u = 0; u < 4; ++u)
+            for (int u = 0; u < 4; ++u) {
+                const int i = i0 + u * kTokens + tid * 4;
+                if (i >= min(n, whole_past)) break;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int i = i0 + u * kTokens + tid * 4 + e;
-                    const uint32_t v = (uint32_t)some[u][e] - (uint32_t)v0;        // (a negative token is beyond any slice)
-                    if (i >= n || v >= (uint32_t)width) continue;
-                    uint32_t* const word = kWide ? counts + v : counts + v / 2;
-                    const int shift = kWide ? 0 : 16 * (v & 1);
-                    if (i >= prompt) atomicAdd(word, 2u << shift);
-                    else atomicOr(word, 1u << shift);
-                }
-            i0 += 4 * kTokens;
-            if (i0 < n) bring(i0, n);
+                for (int e = 0; e < 4; ++e) count(some[u][e], i + e);
+            }
         }
+        if (tid < p.H - whole_past) count(last, whole_past + tid);
         if (p.B) {
-            uint32_t *const biased = reinterpret_cast<uint32_t*>(lds + at.biased), *const twice = reinterpret_cast<uint32_t*>(lds + at.twice);
-            const uint32_t v = (uint32_t)bias_id - (uint32_t)v0, bit = 1u << (v & 31);
-            const bool here = tid < p.B && v < (uint32_t)width;
-            if (here && (atomicOr(&biased[v / 32], bit) & bit)) atomicOr(&twice[v / 32], bit);
+            const uint32_t bit = 1u << (bias_at & 31);
+            if (bias_at >= 0 && (atomicOr(&biased[bias_at / 32], bit) & bit)) atomicOr(&twice[bias_at / 32], bit);
             __syncthreads();
-            if (!here) bias_id = -1;
-            if (here && (twice[v / 32] & bit)) {       // the first entry of a token adds up the others, in their order
-                const int32_t id = bias_id;
-                for (int m = 0; m < p.B; m += 4) {
-                    const int4 ids = *reinterpret_cast<const int4*>(lds + at.ids + m * 4);
-                    const float4 values = *reinterpret_cast<const float4*>(lds + at.values + m * 4);
-                    auto one = [&](int k, int32_t other, float value) {
-                        if (other != id) return;
-                        if (k < tid) bias_id = -1;
-                        else if (k > tid) bias += value;
-                    };
-                    one(m, ids.x, values.x), one(m + 1, ids.y, values.y), one(m + 2, ids.z, values.z), one(m + 3, ids.w, values.w);
+            // Tokens with several entries, one after the other in the wave that has one: its lanes look through all entries, 64 at a time.  The first entry of a token adds up
+            // the others, in their order.
+            for (uint64_t todo = __ballot(bias_at >= 0 && (twice[bias_at / 32] & bit)); todo; todo &= todo - 1) {
+                const int lane = __ffsll((unsigned long long)todo) - 1, k = (tid & ~(kWave - 1)) + lane;
+                const int32_t id = __builtin_amdgcn_readlane(bias_id, lane);
+                float sum = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(bias), lane));
+                bool first = true;
+                for (int m = 0; m < p.B && first; m += kWave) {
+                    const int at_m = m + tid % kWave;
+                    const int32_t other = at_m < p.B ? reinterpret_cast<const int32_t*>(lds + at.ids)[at_m] : -1;
+                    for (uint64_t same = __ballot(other == id); same; same &= same - 1) {
+                        const int which = m + __ffsll((unsigned long long)same) - 1;
+                        if (which < k) first = false;
+                        else if (which > k) sum += reinterpret_cast<const float*>(lds + at.values)[which];
+                    }
+                }
+                if (tid % kWave == lane) {
+                    bias = sum;
+                    if (!first) bias_at = -1;
                 }
             }
+            if (tail_at >= 0 && (biased[tail_at / 32] >> (tail_at & 31) & 1)) tail_at = -1;
         }
         __syncthreads();
         row.inverse = 1.0 / (double)row.repetition;
     }
-    auto count_of = [&](uint32_t v) { return kWide ? counts[v] : counts[v / 2] >> (16 * (v & 1)) & 0xffffu; };
 
     Best best = best_none();
-    for (int i0 = 0; i0 < width; i0 += kAhead * kStep) {
+    for (int i0 = 0; i0 < whole; i0 += kAhead * kStep) {
 #pragma unroll
         for (int slot = 0; slot < kAhead; ++slot) {
             const int i = i0 + slot * kStep + tid * N;
             u32x4 now = raw[slot];
             const uint32_t bits = may[slot];
             request(slot, i + kAhead * kStep);
-            if (i >= width) continue;
-            const int n = width - i;
+            if (i >= whole) continue;
             float a[N];
             if constexpr (kPick) {
 #pragma unroll
@@ -257,17 +268,10 @@ template <int DT, bool kPick, bool kWide> __global__ __launch_bounds__(kRuleThre
 #pragma unroll
                 for (int e = 0; e < N; ++e)
                     if (!(bits >> e & 1)) rule_insert<DT>(now, e, kRuleLow<DT>);
-                if (n >= N) {
-                    __builtin_memcpy(out + (int64_t)i * kB, &now, 16);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < N; ++e)
-                        if (e < n) rule_store1<DT>(out + (int64_t)(i + e) * kB, kB == 4 ? now[e % 4] : now[e / 2 % 4] >> (16 * (e % 2)) & 0xffffu);
-                }
+                __builtin_memcpy(out + (int64_t)i * kB, &now, 16);
             } else {
-                uint32_t out_of_it = ~bits;            // masked, beyond the row, or a bias's thread's
-                if (n < N) out_of_it |= ~0u << n;
-                if (p.B) out_of_it |= reinterpret_cast<const uint32_t*>(lds + at.biased)[i / 32] >> (i & 31);
+                uint32_t out_of_it = ~bits;            // masked, or a bias's thread's
+                if (p.B) out_of_it |= biased[i / 32] >> (i & 31);
 #pragma unroll
                 for (int e = 0; e < N; ++e)
                     if (out_of_it >> e & 1) a[e] = -INFINITY;
@@ -282,39 +286,33 @@ template <int DT, bool kPick, bool kWide> __global__ __launch_bounds__(kRuleThre
                     best.most = most;
                     best.token = v0 + i + own;
                 }
+                const float base = fmaxf(best.most, -3.4028235e38f);   // (nothing but -inf yet: zeros, and a NaN is one)
 #pragma unroll
-                for (int e = 0; e < N; ++e)
-                    if (best.token >= 0 ? e != own : a[e] != a[e]) best.rest += __expf(a[e] - best.most);
+                for (int e = 0; e < N; ++e) best.rest += __expf((e == own ? -INFINITY : a[e]) - base);
             }
         }
     }
+    // the single tokens
     if constexpr (!kPick) {
-        if (p.B) {
-            __syncthreads();                           // (the pass wrote these tokens without their biases)
-            if (bias_id >= 0) {
-                const uint32_t v = (uint32_t)(bias_id - v0);
-                float a = rule_value<DT>(u32x4{bias_bits, 0, 0, 0}, 0);
-                if (p.H) {
-                    const uint32_t count = count_of(v);
-                    if (count) a = rule_past(a, count, row);
-                }
-                const bool is_allowed = !allowed || (allowed[v / 32] >> (v & 31) & 1);
-                rule_store1<DT>(out + (int64_t)v * kB, is_allowed ? rule_bits<DT>(a + bias) : kRuleLow<DT>);
-            }
-        }
-    } else {
-        if (bias_id >= 0) {
-            const uint32_t v = (uint32_t)(bias_id - v0);
-            float a = rule_value<DT>(u32x4{bias_bits, 0, 0, 0}, 0);
-            if (p.H) {
-                const uint32_t count = count_of(v);
-                if (count) a = rule_past(a, count, row);
-            }
-            a += bias;
-            if (allowed && !(allowed[v / 32] >> (v & 31) & 1)) a = -INFINITY;
+        if (p.B) __syncthreads();                      // (the pass wrote the biases' tokens without them)
+    }
+    auto single = [&](int v, uint32_t bits, float more) {
+        uint32_t count = 0;
+        if (p.H) count = kWide ? counts[v] : counts[v / 2] >> (16 * (v & 1)) & 0xffffu;
+        const bool in = !allowed || (allowed[v / 32] >> (v & 31) & 1), touched = count || bias_at == v;
+        float a = rule_value<DT>(u32x4{bits, 0, 0, 0}, 0);
+        if (count) a = rule_past(a, count, row);
+        if (bias_at == v) a += more;
+        if constexpr (!kPick) {
+            rule_store1<DT>(out + (int64_t)v * kB, !in ? kRuleLow<DT> : touched ? rule_bits<DT>(a) : bits);
+        } else if (in) {
             if (a != a) best.rest = a;
-            else if (a > -INFINITY) best = best_of(best, Best{a, bias_id, 0.0f});
+            else if (a > -INFINITY) best = best_of(best, Best{a, v0 + v, 0.0f});
         }
+    };
+    if (bias_at >= 0) single(bias_at, bias_bits, bias);
+    if (tail_at >= 0) single(tail_at, tail_bits, 0.0f);
+    if constexpr (kPick) {
         best = best_of_wave(best);
         if (tid % kWave == 0) of_wave[tid / kWave] = best;
         __syncthreads();
