@@ -103,10 +103,9 @@ struct Q4Plan {
     int few_lds(int log, int nt_, int waves_, int split_) const {
         return (int)(blocks * (4 * planes * (64 << log) + per * (4 << std::max(log, 2)))) + waves_ * 1024 + (split_ > 1 ? waves_ * nt_ * 1024 : 0);
     }
-    int region(int mt_) const { return 4 * planes * mt_ * 1024 + (per * mt_ * 64 + 1023) / 1024 * 1024; }
-    int many_lds(int mt_) const { return kQ4Stages * region(mt_) + kQ4ManyThreads / kWave * 1024; }
-    int64_t workspace() const { return few ? 0 : row_blocks * blocks * region(mt); }
+    int64_t sets() const { return (tiles + waves * nt - 1) / (waves * nt); }
 };
+constexpr int kQ4ManyTiles[] = {8, 6, 4, 3, 2};        // of 16 rows, of a row block; fp32 rows: 2
 Q4Plan q4_plan(int dtype, int64_t T, const Q4Shape& s, unsigned cus) {
     Q4Plan p{};
     p.planes = dtype == TIDE_F32 ? kQ4Planes<kF32> : 1;
@@ -115,7 +114,7 @@ Q4Plan q4_plan(int dtype, int64_t T, const Q4Shape& s, unsigned cus) {
     p.few = T <= 16 && p.few_lds(p.rows_log, 2, 16, 1) <= kMostLds;
     if (p.few) {
         // Rows that leave room for several workgroups a CU: small ones, which start and end apart from each other; else one of as many waves as share its CU's tokens
-        // evenly, two tiles a wave where there are enough (bf16, d = 4096, V = 128000, us, 4 waves of one tile / 16 of two: T = 1 49.5 / 53.8, 8 63 / 55, 16 66 / 58).
+        // evenly, two tiles a wave where there are enough (bf16, d = 4096, V = 128000, us, 4 waves of one tile / 16 of two: T = 1 50 / 53, 8 63 / 55, 16 66 / 57).
         const bool small = p.few_lds(p.rows_log, 1, 4, 1) <= 32 * 1024;
         p.nt = !small && p.tiles >= 24 * (int64_t)cus ? 2 : 1;
         p.waves = small ? 4 : (int)std::min<int64_t>(16, std::max<int64_t>(4, (p.tiles + p.nt * (int64_t)cus - 1) / (p.nt * (int64_t)cus)));
@@ -126,20 +125,18 @@ Q4Plan q4_plan(int dtype, int64_t T, const Q4Shape& s, unsigned cus) {
         p.lds = p.few_lds(p.rows_log, p.nt, p.waves, p.split);
         return p;
     }
-    // Many rows: the least of rounds of workgroups times the matrix steps of a round, for as few waves as fill the chip (a CU's four SIMDs take eight of them)
-    p.nt = 4;
+    // Many rows: the fewest rounds of workgroups times what a block of 128 columns takes, which is some 1.5 us and 0.3 for each tile of 16 rows where the workgroup has 512
+    // tokens (bf16, d = 4096, V = 128000, us: T = 32 65, 48 74, 64 82, 96 104, 128 135), and about 1 of it with few
     double least = 0;
-    for (int mt : {8, 4, 2}) {
-        if (mt == 8 && p.planes > 1) continue;         // (three stages of it are more than the LDS)
-        for (int waves : {8, 4, 2}) {
-            const int64_t row_blocks = (T + 16 * mt - 1) / (16 * mt), sets = (p.tiles + waves * p.nt - 1) / (waves * p.nt);
-            const int64_t together = std::max<int64_t>(1, std::min<int64_t>(kMostLds / p.many_lds(mt), 8 / waves));
-            const int64_t rounds = (sets * row_blocks + cus * together - 1) / (cus * together);
-            const double work = (double)rounds * std::max<double>(mt * 256 * p.planes * ((waves * together + 3) / 4) + 600, 1500);
-            if (least == 0 || work < least) least = work, p.mt = mt, p.waves = waves, p.row_blocks = row_blocks;
+    for (int mt : kQ4ManyTiles) {
+        if (p.planes > 1 && mt != 2) continue;
+        const int nt = mt == 8 ? 4 : 2, most = 32 / nt;
+        for (int waves = most; waves >= most / 4; waves /= 2) {
+            const int64_t row_blocks = (T + 16 * mt - 1) / (16 * mt), items = (p.tiles + waves * nt - 1) / (waves * nt) * row_blocks;
+            const double work = (double)((items + cus - 1) / cus) * (1.0 + (0.5 + 0.3 * mt) * waves / most);
+            if (least == 0 || work < least) least = work, p.mt = mt, p.nt = nt, p.waves = waves, p.row_blocks = row_blocks;
         }
     }
-    p.lds = p.many_lds(p.mt);
     return p;
 }
 
@@ -289,9 +286,13 @@ size_t tide_head_logits_q4_bytes(int dtype, int64_t T, int64_t d) {
         fail(TIDE_ERR_UNSUPPORTED, "unsupported dtype %d, T = %lld or d = %lld", dtype, (long long)T, (long long)d);
         return 0;
     }
-    // Row blocks of 16 mt rows for the mt that leaves most of them over, groups of 32 columns, no matter how many tokens: more than any call of these rows takes
-    const int64_t planes = dtype == TIDE_F32 ? kQ4Planes<kF32> : 1, blocks = (d + kQ4Cols - 1) / kQ4Cols, most = planes > 1 ? 4 : 8;
-    return (size_t)((T + 16 * most - 1) / (16 * most) * most * blocks * (4 * planes * 1024 + 512) + 256 + 255) & ~size_t(255);
+    // Row blocks of 16 mt rows for any mt, and groups of 32 columns: no matter how many tokens, and more than any call of fewer rows takes.  (A region's sums are at most 512
+    // bytes a tile, its padding included.)
+    const int64_t planes = dtype == TIDE_F32 ? kQ4Planes<kF32> : 1, blocks = (d + kQ4Cols - 1) / kQ4Cols;
+    int64_t tiles = 0;
+    for (int mt : kQ4ManyTiles)
+        if (planes == 1 || mt == 2) tiles = std::max(tiles, (T + 16 * mt - 1) / (16 * mt) * mt);
+    return (size_t)(tiles * blocks * (4 * planes * 1024 + 512) + 256 + 255) & ~size_t(255);
 }
 
 int tide_head_logits_q4(const void* x, int dtype, int64_t T, int64_t d, int64_t V, int64_t x_row_stride, const void* codes, const void* scales, int scale_dtype, int64_t group,
@@ -322,34 +323,37 @@ int tide_head_logits_q4(const void* x, int dtype, int64_t T, int64_t d, int64_t 
         return by_runs(group, [&](auto runs) -> int {
             constexpr int DT = decltype(dt)::value, kRuns = decltype(runs)::value;
             auto few = [&](auto tiles) -> int {
-                constexpr int NT = decltype(tiles)::value;
-                int rc2 = raise_lds<&tide_head_q4_few_kernel<DT, kRuns, NT>>();
+                constexpr int NT = decltype(tiles)::value, kDepth = NT == 1 ? 4 : 2;
+                int rc2 = raise_lds<&tide_head_q4_few_kernel<DT, kRuns, NT, kDepth>>();
                 if (rc2) return rc2;
                 const int per_set = plan.waves / plan.split * NT, sets = (int)((plan.tiles + per_set - 1) / per_set);
                 const int together = std::max(1, std::min(kMostLds / plan.lds, plan.waves > 4 ? 1 : dtype == TIDE_F32 ? 5 : 7));
                 const Q4FewParams p{rows, head, logits, logits_row_stride, sets, plan.rows_log, plan.split};
-                hipLaunchKernelGGL((tide_head_q4_few_kernel<DT, kRuns, NT>), dim3((unsigned)std::min<int64_t>(sets, (int64_t)cus * together)), dim3(plan.waves * kWave), plan.lds, st, p);
+                hipLaunchKernelGGL((tide_head_q4_few_kernel<DT, kRuns, NT, kDepth>), dim3((unsigned)std::min<int64_t>(sets, (int64_t)cus * together)), dim3(plan.waves * kWave), plan.lds, st, p);
                 return TIDE_OK;
             };
             auto many = [&](auto row_tiles) -> int {
-                constexpr int MT = decltype(row_tiles)::value, NT = 4;
+                constexpr int MT = decltype(row_tiles)::value, NT = MT == 8 ? 4 : 2;
                 int rc2 = raise_lds<&tide_head_q4_many_kernel<DT, kRuns, MT, NT>>();
                 if (rc2) return rc2;
                 const Q4LayParams lay{rows, (char*)workspace, head.blocks, plan.row_blocks * MT * head.blocks};
                 hipLaunchKernelGGL((tide_head_q4_lay_kernel<DT, kRuns, MT>), dim3((unsigned)((lay.waves + 3) / 4)), dim3(kQ4Threads), 0, st, lay);
-                const int per_set = plan.waves * NT, sets = (int)((plan.tiles + per_set - 1) / per_set);
-                const int64_t together = std::max<int64_t>(1, std::min<int64_t>(kMostLds / plan.lds, 8 / plan.waves));
-                const int64_t set_grid = (std::min<int64_t>(sets, std::max<int64_t>(cus * together / plan.row_blocks, 1)) + 7) / 8 * 8;
-                const Q4ManyParams p{(const char*)workspace, head, logits, logits_row_stride, (int)T, (int)plan.row_blocks, sets, (int)set_grid};
-                hipLaunchKernelGGL((tide_head_q4_many_kernel<DT, kRuns, MT, NT>), dim3((unsigned)(set_grid * plan.row_blocks)), dim3(plan.waves * kWave), plan.lds, st, p);
+                const int64_t sets = plan.sets();
+                const Q4ManyParams p{(const char*)workspace, head, logits, logits_row_stride, (int)T, (int)plan.row_blocks, (int)sets, sets >= 64};
+                const int lds = q4_many_lds<NT>(Q4Region<DT, kRuns, MT>::kBytes, kQ4CodeStages<DT, kRuns, MT, NT>, plan.waves);
+                const int64_t together = std::min<int64_t>(kMostLds / lds, kQ4ManyThreads<NT> / kWave / plan.waves);
+                const int64_t grid = std::min<int64_t>((sets * plan.row_blocks + 7) / 8 * 8, std::max<int64_t>(8, cus * together / 8 * 8));
+                hipLaunchKernelGGL((tide_head_q4_many_kernel<DT, kRuns, MT, NT>), dim3((unsigned)grid), dim3(plan.waves * kWave), lds, st, p);
                 return TIDE_OK;
             };
             if (plan.few) return plan.nt == 2 ? few(integral_constant<int, 2>{}) : few(integral_constant<int, 1>{});
-            if (plan.mt == 2) return many(integral_constant<int, 2>{});
             if constexpr (DT != kF32) {
                 if (plan.mt == 8) return many(integral_constant<int, 8>{});
+                if (plan.mt == 6) return many(integral_constant<int, 6>{});
+                if (plan.mt == 4) return many(integral_constant<int, 4>{});
+                if (plan.mt == 3) return many(integral_constant<int, 3>{});
             }
-            return many(integral_constant<int, 4>{});
+            return many(integral_constant<int, 2>{});
         });
     });
     if (rc) return rc;

@@ -7,6 +7,8 @@
 //     sum x (c - 8) = 16 (sum x (1 + c / 16) - 1.5 sum x),
 // the products exact, the sums in fp32, and the scale is applied to it in fp32.  No weight is rounded.
 #pragma once
+#include <type_traits>
+
 #include "device_utils.hpp"
 
 namespace tide {
@@ -337,8 +339,8 @@ template <int DT, int kRuns, int NT> __host__ __device__ inline Q4FewLds q4_few_
     return l;
 }
 
-template <int DT, int kRuns, int NT> __global__ __launch_bounds__(kQ4FewThreads) void tide_head_q4_few_kernel(Q4FewParams p) {
-    constexpr int E = kQ4Elem<DT>, P = kQ4Planes<DT>, kPer = 4 / kRuns, kDepth = NT == 1 ? 4 : 2;
+template <int DT, int kRuns, int NT, int kDepth> __global__ __launch_bounds__(kQ4FewThreads) void tide_head_q4_few_kernel(Q4FewParams p) {
+    constexpr int E = kQ4Elem<DT>, P = kQ4Planes<DT>, kPer = 4 / kRuns;
     constexpr int kScaleBlocks = 32 / NT / kPer;       // blocks of 128 columns whose scales a kilobyte holds
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), waves = blockDim.x / kWave;
@@ -351,10 +353,10 @@ template <int DT, int kRuns, int NT> __global__ __launch_bounds__(kQ4FewThreads)
     const int passes = (p.sets - blockIdx.x + gridDim.x - 1) / gridDim.x;
     auto tile_of = [&](int pass) { return ((int)(blockIdx.x + pass * gridDim.x) * units + unit) * NT; };
     u32x4 c[kDepth][NT];
-    int f_pass = 0, f_at = 0;                          // what is fetched next; beyond the last tile: the last again, for nothing
+    int f_pass = 0, f_at = 0;                          // what is fetched next
     const char* f_codes[NT];
     auto point = [&](int pass) {
-        const int tile0 = tile_of(min(pass, passes - 1));
+        const int tile0 = tile_of(pass);
 #pragma unroll
         for (int n = 0; n < NT; ++n) f_codes[n] = p.head.codes + ((int64_t)min(tile0 + n, p.head.tiles - 1) * blocks + begin) * kQ4TileBytes;
     };
@@ -369,9 +371,11 @@ template <int DT, int kRuns, int NT> __global__ __launch_bounds__(kQ4FewThreads)
     };
     u32x4 s_next;
     auto fetch_scales = [&](int pass, int i) { s_next = q4_scales<NT>(p.head, tile_of(min(pass, passes - 1)), (begin + i) * kPer, lane); };
-#pragma unroll
-    for (int slot = 0; slot < kDepth; ++slot) fetch(slot);
+    const int steps = passes * own;
     fetch_scales(0, 0);
+#pragma unroll
+    for (int slot = 0; slot < kDepth; ++slot)
+        if (slot < steps) fetch(slot);
 
     for (int item = threadIdx.x; item < blocks * 4 << log; item += blockDim.x) {
         const int row = item & (rows - 1), g = item >> log & 3, kb = item >> (log + 2);
@@ -390,78 +394,92 @@ template <int DT, int kRuns, int NT> __global__ __launch_bounds__(kQ4FewThreads)
 #pragma unroll
     for (int n = 0; n < NT; ++n) total[n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     int pass = 0, i = 0, s_at = 0;
-    for (int left = passes * own; left > 0; left -= kDepth) {
+    auto step = [&](const u32x4 (&now)[NT]) {
+        if (s_at == 0) {
+            *reinterpret_cast<u32x4*>(my_scales + lane * 16) = s_next;
+            if (i + kScaleBlocks < own) fetch_scales(pass, i + kScaleBlocks);
+            else fetch_scales(pass + 1, 0);
+        }
+        const char* x = my_x + ((begin + i) * 4 * P << (log + 6));
+        const float* offs = my_offs + ((begin + i) * kPer << offs_log);
 #pragma unroll
-        for (int slot = 0; slot < kDepth; ++slot) {    // (beyond the last block: what was fetched again, into sums that nothing takes)
-            if (s_at == 0) {
-                *reinterpret_cast<u32x4*>(my_scales + lane * 16) = s_next;
-                if (i + kScaleBlocks < own) fetch_scales(pass, i + kScaleBlocks);
-                else fetch_scales(pass + 1, 0);
+        for (int gr = 0; gr < kPer; ++gr) {
+            f32x4 sum[NT];
+            const f32x4 start = *reinterpret_cast<const f32x4*>(offs + (gr << offs_log));
+#pragma unroll
+            for (int n = 0; n < NT; ++n) sum[n] = start;
+#pragma unroll
+            for (int j = gr * kRuns; j < (gr + 1) * kRuns; ++j) {
+                u32x4 w[NT];
+#pragma unroll
+                for (int n = 0; n < NT; ++n) w[n] = ones.expand(now[n][j]);
+#pragma unroll
+                for (int plane = 0; plane < P; ++plane) {
+                    const u32x4 a = *reinterpret_cast<const u32x4*>(x + ((j * P + plane) << (log + 6)));
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) sum[n] = q4_mma<E>(a, w[n], sum[n]);
+                }
             }
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                const float s = q4_scale_at(my_scales, NT, n, s_at * kPer + gr, lane, half);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) total[n][e] = fmaf(s, sum[n][e], total[n][e]);
+            }
+        }
+        if (++s_at == kScaleBlocks) s_at = 0;
+        if (++i < own) return;
+        if (p.split > 1) {
+            f32x4* const sums = reinterpret_cast<f32x4*>(lds + at.sums);
+            __syncthreads();                       // (the last pass's sums have been read)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) sums[(wave * NT + n) * kWave + lane] = total[n];
+            __syncthreads();
+            if (part == 0)
+                for (int m = 1; m < p.split; ++m)
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        const f32x4 more = sums[((wave + m) * NT + n) * kWave + lane];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) total[n][e] += more[e];
+                    }
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const int v = (tile_of(pass) + n) * kQ4Rows + (lane & 15);
+            const bool writes = part == 0 && v < p.head.V;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int t = 4 * (lane >> 4) + e;
+                if (writes && t < p.x.T) p.out[(int64_t)t * p.out_stride + v] = 16.0f * total[n][e];
+                total[n][e] = 0.0f;
+            }
+        }
+        ++pass;
+        i = 0;
+        s_at = 0;
+    };
+    // whole rounds of the ring while there is something left to fetch, then what is in it
+    int left = steps;
+    for (; left >= 2 * kDepth; left -= kDepth)
+#pragma unroll
+        for (int slot = 0; slot < kDepth; ++slot) {
             u32x4 now[NT];
 #pragma unroll
             for (int n = 0; n < NT; ++n) now[n] = c[slot][n];
             fetch(slot);
-            const char* x = my_x + ((begin + i) * 4 * P << (log + 6));
-            const float* offs = my_offs + ((begin + i) * kPer << offs_log);
-#pragma unroll
-            for (int gr = 0; gr < kPer; ++gr) {
-                f32x4 sum[NT];
-                const f32x4 start = *reinterpret_cast<const f32x4*>(offs + (gr << offs_log));
-#pragma unroll
-                for (int n = 0; n < NT; ++n) sum[n] = start;
-#pragma unroll
-                for (int j = gr * kRuns; j < (gr + 1) * kRuns; ++j) {
-                    u32x4 w[NT];
-#pragma unroll
-                    for (int n = 0; n < NT; ++n) w[n] = ones.expand(now[n][j]);
-#pragma unroll
-                    for (int plane = 0; plane < P; ++plane) {
-                        const u32x4 a = *reinterpret_cast<const u32x4*>(x + ((j * P + plane) << (log + 6)));
-#pragma unroll
-                        for (int n = 0; n < NT; ++n) sum[n] = q4_mma<E>(a, w[n], sum[n]);
-                    }
-                }
-#pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    const float s = q4_scale_at(my_scales, NT, n, s_at * kPer + gr, lane, half);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) total[n][e] = fmaf(s, sum[n][e], total[n][e]);
-                }
-            }
-            if (++s_at == kScaleBlocks) s_at = 0;
-            if (++i < own) continue;
-            if (p.split > 1 && pass < passes) {
-                f32x4* const sums = reinterpret_cast<f32x4*>(lds + at.sums);
-                __syncthreads();                       // (the last pass's sums have been read)
-#pragma unroll
-                for (int n = 0; n < NT; ++n) sums[(wave * NT + n) * kWave + lane] = total[n];
-                __syncthreads();
-                if (part == 0)
-                    for (int m = 1; m < p.split; ++m)
-#pragma unroll
-                        for (int n = 0; n < NT; ++n) {
-                            const f32x4 more = sums[((wave + m) * NT + n) * kWave + lane];
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) total[n][e] += more[e];
-                        }
-            }
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                const int v = (tile_of(pass) + n) * kQ4Rows + (lane & 15);
-                const bool writes = pass < passes && part == 0 && v < p.head.V;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int t = 4 * (lane >> 4) + e;
-                    if (writes && t < p.x.T) p.out[(int64_t)t * p.out_stride + v] = 16.0f * total[n][e];
-                    total[n][e] = 0.0f;
-                }
-            }
-            ++pass;
-            i = 0;
-            s_at = 0;
+            step(now);
         }
-    }
+    for (; left > 0; left -= kDepth)
+#pragma unroll
+        for (int slot = 0; slot < kDepth; ++slot) {
+            if (slot >= left) break;
+            u32x4 now[NT];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) now[n] = c[slot][n];
+            if (slot + kDepth < left) fetch(slot);
+            step(now);
+        }
 }
 
 // ---- Many rows.
@@ -487,150 +505,164 @@ template <int DT, int kRuns, int MT> __global__ __launch_bounds__(kQ4Threads) vo
     q4_put<DT, kRuns>(raw, lane >> 4, 16, region + rt * 1024 + lane * 16, MT * 1024, reinterpret_cast<float*>(region + R::kX) + rt * 16 + (lane & 15), MT * 16);
 }
 
-// A workgroup has 16 MT rows and its waves NT tiles of 16 tokens each.  The regions of the rows go through a ring of three stages in LDS by transfers that no register waits
-// for; the codes through registers, a block or two ahead; a barrier for each block of 128 columns.  The transfers are inline assembly, which the compiler does not
-// count, so the waits for them are written out: at a block's start all but the transfers and loads of the two blocks after the one that requested its
-// region may be under way.
+// A workgroup has 16 MT rows and its waves NT tiles of 16 tokens each.  Everything comes to LDS by transfers that no register waits for: the rows' regions in two
+// stages, for all waves, behind a barrier for each block of 128 columns; each wave's codes in two or three stages and its scales, a kilobyte at a time, in two.  The
+// transfers are inline assembly, which the compiler does not count, and the waits for them are written out; there are no other loads from memory in the loop.
 struct Q4ManyParams {
     const char* regions;
     Q4Head head;
     float* out;
     int64_t out_stride;
     int T, row_blocks;
-    int sets, set_grid;        // sets of tokens, each a workgroup's at a time; workgroups that share them (a multiple of 8)
+    int sets;                  // of tokens: a workgroup has a set and a row block at a time
+    bool by_xcd;               // the row blocks of a set run on one XCD (workgroups whose numbers are equal modulo 8), for its codes to be in that L2
 };
-constexpr int kQ4ManyThreads = 512;
-constexpr int kQ4Stages = 3;
-template <int DT, int kRuns, int MT> constexpr int kQ4ManyLds = kQ4Stages * Q4Region<DT, kRuns, MT>::kBytes + kQ4ManyThreads / kWave * 1024;
+// Four tiles a wave, eight waves; or two tiles and sixteen waves
+template <int NT> constexpr int kQ4ManyThreads = 2048 / NT;
+template <int NT> __host__ __device__ constexpr int q4_many_lds(int region, int stages, int waves) { return 2 * region + waves * (stages * NT + 2) * 1024; }
+template <int DT, int kRuns, int MT, int NT> constexpr int kQ4CodeStages = q4_many_lds<NT>(Q4Region<DT, kRuns, MT>::kBytes, 3, kQ4ManyThreads<NT> / kWave) <= 158 * 1024 ? 3 : 2;
 
 // 64 lanes x 16 bytes from memory to a kilobyte of LDS (m0 as in the head products).  The wait states: five between a vector instruction that wrote the base and this one.
-__device__ __forceinline__ void q4_transfer(uint32_t lds, const char* base, uint32_t lane16) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(lane16), "s"(base) : "memory");
+__device__ __forceinline__ void q4_transfer(uint32_t lds, const char* base, uint32_t lane_bytes) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(lane_bytes), "s"(base) : "memory");
 }
 
-template <int DT, int kRuns, int MT, int NT> __global__ __launch_bounds__(kQ4ManyThreads) void tide_head_q4_many_kernel(Q4ManyParams p) {
+template <int DT, int kRuns, int MT, int NT> __global__ __launch_bounds__(kQ4ManyThreads<NT>) void tide_head_q4_many_kernel(Q4ManyParams p) {
     using R = Q4Region<DT, kRuns, MT>;
-    constexpr int E = kQ4Elem<DT>, P = kQ4Planes<DT>, kPer = 4 / kRuns, kDepth = MT * NT >= 32 ? 1 : 2;
-    constexpr int kScaleBlocks = 32 / NT / kPer;
+    constexpr int E = kQ4Elem<DT>, P = kQ4Planes<DT>, kPer = 4 / kRuns, kStages = kQ4CodeStages<DT, kRuns, MT, NT>, kSteps = kRuns * P, kAhead = 2;
+    constexpr int kScaleBlocks = 32 / NT / kPer;       // blocks of 128 columns whose scales a kilobyte holds
+    static_assert(kScaleBlocks >= 2, "a kilobyte is requested two blocks before it is read");
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), waves = blockDim.x / kWave;
-    // workgroups of the same tokens run on one XCD (numbers that are equal modulo 8), for their codes to be in its L2
-    const int eighth = blockIdx.x & 7, rest = blockIdx.x >> 3, row_block = rest % p.row_blocks, set0 = rest / p.row_blocks * 8 + eighth, blocks = p.head.blocks;
-    if (set0 >= p.sets) return;
-    const int passes = (p.sets - set0 + p.set_grid - 1) / p.set_grid;
-    auto tile_of = [&](int pass) { return ((set0 + pass * p.set_grid) * waves + wave) * NT; };
+    const int blocks = p.head.blocks, xcd = p.by_xcd ? blockIdx.x & 7 : 0, xcds = p.by_xcd ? 8 : 1, first_item = blockIdx.x / xcds, stride = gridDim.x / xcds;
+    const int items = (p.sets - xcd + xcds - 1) / xcds * p.row_blocks, passes = (items - first_item + stride - 1) / stride;
+    if (first_item >= items) return;
+    auto item_of = [&](int pass) { return first_item + min(pass, passes - 1) * stride; };
+    auto tile_of = [&](int pass) { return ((item_of(pass) / p.row_blocks * xcds + xcd) * waves + wave) * NT; };
 
-    const char* const regions = p.regions + (int64_t)row_block * blocks * R::kBytes;
+    char* const my_codes = lds + 2 * R::kBytes + wave * (kStages * NT + 2) * 1024;
+    char* const my_scales = my_codes + kStages * NT * 1024;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds, lane16 = lane * 16;
-    int x_kb = 0, x_stage = 0;
-    auto request = [&] {
+    const uint32_t codes0 = lds0 + (uint32_t)(my_codes - lds), scales0 = codes0 + kStages * NT * 1024;
+    // the regions of the rows: every wave a part of each
+    const char* regions = p.regions + (int64_t)(item_of(0) % p.row_blocks) * blocks * R::kBytes;
+    int x_pass = 0, x_kb = 0, x_stage = 0;
+    auto request_region = [&] {
         const char* from = regions + (int64_t)x_kb * R::kBytes;
         for (int i = wave * 1024; i < R::kBytes; i += waves * 1024) q4_transfer(lds0 + x_stage * R::kBytes + i, from + i, lane16);
-        if (++x_kb == blocks) x_kb = 0;
-        if (++x_stage == kQ4Stages) x_stage = 0;
+        if (++x_kb == blocks) x_kb = 0, regions = p.regions + (int64_t)(item_of(++x_pass) % p.row_blocks) * blocks * R::kBytes;
+        x_stage ^= 1;
     };
-    u32x4 c[kDepth][NT];
-    int f_pass = 0, f_at = 0;
-    const char* f_codes[NT];
-    auto point = [&](int pass) {
-        const int tile0 = tile_of(min(pass, passes - 1));
+    // the wave's codes; beyond its last block: the last tiles again, into a stage that nothing reads
+    int f_pass = 0, f_kb = 0, f_stage = 0, f_tile = tile_of(0);
+    auto request_codes = [&] {
 #pragma unroll
-        for (int n = 0; n < NT; ++n) f_codes[n] = p.head.codes + (int64_t)min(tile0 + n, p.head.tiles - 1) * blocks * kQ4TileBytes;
+        for (int n = 0; n < NT; ++n)
+            q4_transfer(codes0 + (f_stage * NT + n) * 1024, p.head.codes + ((int64_t)min(f_tile + n, p.head.tiles - 1) * blocks + f_kb) * kQ4TileBytes, lane16);
+        if (++f_kb == blocks) f_kb = 0, f_tile = tile_of(++f_pass);
+        if (++f_stage == kStages) f_stage = 0;
     };
-    point(0);
-    auto fetch = [&](int slot) {
-#pragma unroll
-        for (int n = 0; n < NT; ++n) c[slot][n] = *reinterpret_cast<const u32x4*>(f_codes[n] + (uint32_t)(f_at * kQ4TileBytes) + lane * 16);
-        if (++f_at == blocks) {
-            f_at = 0;
-            point(++f_pass);
-        }
+    // and its scales: lane l brings eight rows of a group, 64 / NT lanes those of a tile
+    int s_stage = 0;
+    auto request_scales = [&](int pass, int kb) {
+        constexpr int kLanes = kWave / NT;
+        const int tile0 = tile_of(pass), l = lane % kLanes, tile = min(tile0 + lane / kLanes, p.head.tiles - 1) - min(tile0, p.head.tiles - 1);
+        const int group = min(kb * kPer + l / 2, p.head.groups - 1);       // (a group of padding: its sums are zero)
+        q4_transfer(scales0 + s_stage * 1024, (const char*)(p.head.scales + (int64_t)min(tile0, p.head.tiles - 1) * p.head.groups * kQ4Rows),
+                    ((uint32_t)(tile * p.head.groups + group) * kQ4Rows + (l & 1) * 8) * 2);
+        s_stage ^= 1;
     };
-    u32x4 s_next;
-    auto fetch_scales = [&](int pass, int i) { s_next = q4_scales<NT>(p.head, tile_of(min(pass, passes - 1)), i * kPer, lane); };
-    fetch_scales(0, 0);
-    request();
-    request();
+    request_scales(0, 0);
+    request_region();
 #pragma unroll
-    for (int slot = 0; slot < kDepth; ++slot) fetch(slot);
+    for (int i = 1; i < kStages; ++i) request_codes();
 
     const Q4Ones<E> ones;
     const uint32_t half = p.head.half ? 0xffffffffu : 0u;
-    char* const my_scales = lds + kQ4Stages * R::kBytes + wave * 1024;
     f32x4 total[NT][MT];
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int rt = 0; rt < MT; ++rt) total[n][rt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    int pass = 0, i = 0, s_at = 0, stage = 0;
-    // requested after a block's region: the rest of the region's block (a fetch), the next block (transfers, a fetch)
-    constexpr int kUnderWay = R::kBytes / 1024 / (kQ4ManyThreads / kWave) + (kDepth == 1 ? 1 : 2) * NT;
-    for (int left = passes * blocks; left > 0; left -= kDepth) {
-#pragma unroll
-        for (int slot = 0; slot < kDepth; ++slot) {    // (beyond the last block: into sums that nothing takes)
-            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"i"(kUnderWay) : "memory");
-            request();
+    int stage = 0, c_stage = 0, s_at = 0, s_read = 0;
+    for (int pass = 0; pass < passes; ++pass) {
+        for (int kb = 0; kb < blocks; ++kb) {
+            // What this block reads has arrived: with three stages all but the last request for codes; the wave has read what the next requests overwrite, and behind the
+            // barrier so have all
+            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"i"(kStages == 3 ? NT : 0) : "memory");
             if (s_at == 0) {
-                *reinterpret_cast<u32x4*>(my_scales + lane * 16) = s_next;
-                if (i + kScaleBlocks < blocks) fetch_scales(pass, i + kScaleBlocks);
-                else fetch_scales(pass + 1, 0);
+                if (kb + kScaleBlocks < blocks) request_scales(pass, kb + kScaleBlocks);
+                else request_scales(pass + 1, 0);
             }
-            u32x4 now[NT];
+            request_region();
+            request_codes();
+            const char* const x = lds + stage * R::kBytes + lane * 16;
+            const float* const offs = reinterpret_cast<const float*>(lds + stage * R::kBytes + R::kX) + 4 * (lane >> 4);
+            u32x4 c[NT];
 #pragma unroll
-            for (int n = 0; n < NT; ++n) now[n] = c[slot][n];
-            fetch(slot);
-            const char* x = lds + stage * R::kBytes + lane * 16;
-            const float* offs = reinterpret_cast<const float*>(lds + stage * R::kBytes + R::kX) + 4 * (lane >> 4);
+            for (int n = 0; n < NT; ++n) c[n] = *reinterpret_cast<const u32x4*>(my_codes + (c_stage * NT + n) * 1024 + lane * 16);
 #pragma unroll
             for (int gr = 0; gr < kPer; ++gr) {
-                u32x4 w[kRuns][NT];
+                // fragments are read kAhead steps of NT matrix steps ahead of their use, a row tile's start one; the codes of a step are expanded beside the matrix steps of the
+                // one before
+                auto fragment = [&](int step) { return *reinterpret_cast<const u32x4*>(x + ((gr * kSteps + step % kSteps) * MT + step / kSteps) * 1024); };
+                auto first = [&](int rt) { return *reinterpret_cast<const f32x4*>(offs + (gr * MT + rt) * 16); };
+                u32x4 a[kAhead], w[kRuns][NT];
+                f32x4 start = first(0);
+#pragma unroll
+                for (int step = 0; step < kAhead; ++step) a[step] = fragment(step);
                 float s[NT];
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
-#pragma unroll
-                    for (int j = 0; j < kRuns; ++j) w[j][n] = ones.expand(now[n][gr * kRuns + j]);
-                    s[n] = q4_scale_at(my_scales, NT, n, s_at * kPer + gr, lane, half);
+                    s[n] = q4_scale_at(my_scales + s_read * 1024, NT, n, s_at * kPer + gr, lane, half);
+                    w[0][n] = ones.expand(c[n][gr * kRuns]);
                 }
 #pragma unroll
                 for (int rt = 0; rt < MT; ++rt) {
                     f32x4 sum[NT];
-                    const f32x4 start = *reinterpret_cast<const f32x4*>(offs + (gr * MT + rt) * 16);
 #pragma unroll
                     for (int n = 0; n < NT; ++n) sum[n] = start;
 #pragma unroll
-                    for (int j = 0; j < kRuns; ++j)
+                    for (int step = 0; step < kSteps; ++step) {
+                        const int at = rt * kSteps + step;
+                        const u32x4 now = a[at % kAhead];
+                        if (step + 1 == kSteps && rt + 1 < MT) start = first(rt + 1);
+                        if (at + kAhead < MT * kSteps) a[at % kAhead] = fragment(at + kAhead);
+                        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                        for (int plane = 0; plane < P; ++plane) {
-                            const u32x4 a = *reinterpret_cast<const u32x4*>(x + (((gr * kRuns + j) * P + plane) * MT + rt) * 1024);
+                        for (int n = 0; n < NT; ++n) sum[n] = q4_mma<E>(now, w[step / P][n], sum[n]);
+                        if (rt == 0 && step % P == 0 && step / P + 1 < kRuns) {
 #pragma unroll
-                            for (int n = 0; n < NT; ++n) sum[n] = q4_mma<E>(a, w[j][n], sum[n]);
+                            for (int n = 0; n < NT; ++n) w[step / P + 1][n] = ones.expand(c[n][gr * kRuns + step / P + 1]);
                         }
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
 #pragma unroll
-                    for (int n = 0; n < NT; ++n)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) total[n][rt][e] = fmaf(s[n], sum[n][e], total[n][rt][e]);
+                    for (int n = 0; n < NT; ++n) {
+                        total[n][rt] = __builtin_elementwise_fma(f32x4{s[n], s[n], s[n], s[n]}, sum[n], total[n][rt]);
+                        asm volatile("" : "+v"(total[n][rt]));     // here: not behind the next branch, with all sums kept until then
+                    }
                 }
             }
-            if (++stage == kQ4Stages) stage = 0;
-            if (++s_at == kScaleBlocks) s_at = 0;
-            if (++i < blocks) continue;
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                const int v = (tile_of(pass) + n) * kQ4Rows + (lane & 15);
-                const bool writes = pass < passes && v < p.head.V;
-#pragma unroll
-                for (int rt = 0; rt < MT; ++rt)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int t = (row_block * MT + rt) * 16 + 4 * (lane >> 4) + e;
-                        if (writes && t < p.T) p.out[(int64_t)t * p.out_stride + v] = 16.0f * total[n][rt][e];
-                        total[n][rt][e] = 0.0f;
-                    }
-            }
-            ++pass;
-            i = 0;
-            s_at = 0;
+            stage ^= 1;
+            if (++c_stage == kStages) c_stage = 0;
+            if (++s_at == kScaleBlocks || kb + 1 == blocks) s_at = 0, s_read ^= 1;
         }
+        int quad = 4 * (lane >> 4);
+        asm volatile("" : "+v"(quad));                 // (the rows' addresses are made here, not kept over the loop)
+#pragma unroll
+        for (int rt = 0; rt < MT; ++rt)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int t = (item_of(pass) % p.row_blocks * MT + rt) * 16 + quad + e;
+                float* const out = p.out + (int64_t)t * p.out_stride + (lane & 15);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    const int v0 = (tile_of(pass) + n) * kQ4Rows;
+                    if (t < p.T && v0 + (lane & 15) < p.head.V) out[v0] = 16.0f * total[n][rt][e];
+                    total[n][rt][e] = 0.0f;
+                }
+            }
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // the last transfers: the LDS is another workgroup's afterwards
 }

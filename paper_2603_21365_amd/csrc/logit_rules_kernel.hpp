@@ -213,18 +213,19 @@ template <int DT, bool kPick, bool kWide> __global__ __launch_bounds__(kRuleThre
             // Tokens with several entries, one after the other in the wave that has one: its lanes look through all entries, 64 at a time.  The first entry of a token adds up
             // the others, in their order.
             for (uint64_t todo = __ballot(bias_at >= 0 && (twice[bias_at / 32] & bit)); todo; todo &= todo - 1) {
-                const int lane = __ffsll((unsigned long long)todo) - 1, k = (tid & ~(kWave - 1)) + lane;
+                const int lane = __ffsll((unsigned long long)todo) - 1, k = __builtin_amdgcn_readfirstlane(tid & ~(kWave - 1)) + lane;
                 const int32_t id = __builtin_amdgcn_readlane(bias_id, lane);
                 float sum = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(bias), lane));
                 bool first = true;
                 for (int m = 0; m < p.B && first; m += kWave) {
                     const int at_m = m + tid % kWave;
                     const int32_t other = at_m < p.B ? reinterpret_cast<const int32_t*>(lds + at.ids)[at_m] : -1;
-                    for (uint64_t same = __ballot(other == id); same; same &= same - 1) {
-                        const int which = m + __ffsll((unsigned long long)same) - 1;
-                        if (which < k) first = false;
-                        else if (which > k) sum += reinterpret_cast<const float*>(lds + at.values)[which];
-                    }
+                    const float value = at_m < p.B ? reinterpret_cast<const float*>(lds + at.values)[at_m] : 0.0f;
+                    uint64_t same = __ballot(other == id);
+                    first = !same || m + __ffsll((unsigned long long)same) - 1 >= k;
+                    if (first && m + kWave > k && m <= k) same &= ~(1ull << (k - m));      // (itself)
+                    for (; first && same; same &= same - 1)
+                        sum += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(value), __ffsll((unsigned long long)same) - 1));
                 }
                 if (tid % kWave == lane) {
                     bias = sum;

@@ -763,33 +763,32 @@ def head_logits_q4(x, codes, scales, V, group=128, *, out=None, workspace=None):
     return out
 
 
+def _row_array(t, dtype, shape, device, name) -> int | None:
+    """The address of an array that goes with a call's rows: contiguous, of this type and shape, on their device; None for none."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous() or not t.is_cuda:
+        raise ValueError(f"{name} must be a contiguous CUDA {dtype} tensor of shape {tuple(shape)}")
+    if t.device != device:
+        raise ValueError(f"every array must be on {device}: {name} is on {t.device}")
+    return t.data_ptr()
+
+
 def _rule_args(logits, past, past_len, prompt_len, repetition, presence, frequency, bias_ids, bias_values, allowed):
     (T, V), (rs, _) = _rows(logits, 2)
-    dev, H, B = logits.device, 0, 0
-    if past is None:
-        if past_len is not None or prompt_len is not None or repetition is not None or presence is not None or frequency is not None:
-            raise ValueError("lengths and penalties need a past")
-    else:
-        H = int(past.shape[-1])
-        _dev(past, torch.int32, (T, H), "past")
-        for t, name in ((past_len, "past_len"), (prompt_len, "prompt_len")):
-            if t is not None:
-                _dev(t, torch.int32, (T,), name)
-        for t, name in ((repetition, "repetition"), (presence, "presence"), (frequency, "frequency")):
-            if t is not None:
-                _dev(t, torch.float32, (T,), name)
+    dev, H, B, i32, f32, rows = logits.device, 0, 0, torch.int32, torch.float32, (T,)
+    if past is not None:
+        H = past.shape[-1]
+    elif past_len is not None or prompt_len is not None or repetition is not None or presence is not None or frequency is not None:
+        raise ValueError("lengths and penalties need a past")
     if (bias_ids is None) != (bias_values is None):
         raise ValueError("bias_ids and bias_values come together")
     if bias_ids is not None:
-        B = int(bias_ids.shape[-1])
-        _dev(bias_ids, torch.int32, (T, B), "bias_ids"), _dev(bias_values, torch.float32, (T, B), "bias_values")
-    if allowed is not None:
-        _dev(allowed, torch.int32, (T, (V + 31) // 32), "allowed")
-    for t in (past, past_len, prompt_len, repetition, presence, frequency, bias_ids, bias_values, allowed):
-        if t is not None and t.device != dev:
-            raise ValueError(f"every array must be on {dev}")
-    return T, V, (_ptr(logits), _dtype_code(logits), T, V, rs if T > 1 else V, _ptr(past), H, _ptr(past_len), _ptr(prompt_len), _ptr(repetition), _ptr(presence),
-                  _ptr(frequency), _ptr(bias_ids), _ptr(bias_values), B, _ptr(allowed))
+        B = bias_ids.shape[-1]
+    return T, V, (_ptr(logits), _dtype_code(logits), T, V, rs if T > 1 else V, _row_array(past, i32, (T, H), dev, "past"), H, _row_array(past_len, i32, rows, dev, "past_len"),
+                  _row_array(prompt_len, i32, rows, dev, "prompt_len"), _row_array(repetition, f32, rows, dev, "repetition"), _row_array(presence, f32, rows, dev, "presence"),
+                  _row_array(frequency, f32, rows, dev, "frequency"), _row_array(bias_ids, i32, (T, B), dev, "bias_ids"),
+                  _row_array(bias_values, f32, (T, B), dev, "bias_values"), B, _row_array(allowed, i32, (T, (V + 31) // 32), dev, "allowed"))
 
 
 def logit_rules(logits, *, past=None, past_len=None, prompt_len=None, repetition=None, presence=None, frequency=None, bias_ids=None, bias_values=None,
