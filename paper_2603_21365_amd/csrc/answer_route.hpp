@@ -50,7 +50,6 @@ int q4_weights(const void* W, void* W_out, int dtype, const Q4Shape& s, int64_t 
     const int64_t tiles = s.tiles() * s.blocks(), blocks = (tiles + 3) / 4;
     if (blocks > kMostBlocks) return fail(TIDE_ERR_UNSUPPORTED, "V = %lld rows of d = %lld are too many for one call", (long long)s.V, (long long)s.d);
     Q4WeightParams p{};
-    p.W = (const char*)W;
     p.W_out = (char*)W_out;
     p.row_bytes = w_row_stride * (int64_t)elem_bytes(dtype);
     p.codes = (char*)codes;
@@ -62,6 +61,7 @@ int q4_weights(const void* W, void* W_out, int dtype, const Q4Shape& s, int64_t 
     p.half = s.scale_dtype == TIDE_F16;
     p.chunks = q4_chunks(W ? W : W_out, w_row_stride, dtype);
     p.tiles = tiles;
+    p.x = Q4Rows{(const char*)W, p.row_bytes, p.V, p.d, p.chunks};
     by_dtype(dtype, [&](auto dt) {
         return by_runs(s.group, [&](auto runs) {
             constexpr int DT = decltype(dt)::value, kRuns = decltype(runs)::value;

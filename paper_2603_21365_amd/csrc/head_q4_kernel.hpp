@@ -26,188 +26,11 @@ __device__ __forceinline__ float q4_scale_select(uint32_t bits, uint32_t half) {
     return __uint_as_float((a & half) | (b & ~half));
 }
 
-// Elements col .. col+7 of a row, zeros from d on.
-template <int DT> __device__ __forceinline__ void q4_load8(const char* row, int col, int d, bool chunks, float (&x)[8]) {
-    constexpr int kB = Storage<DT>::kBytes;
-    if (chunks && col + 8 <= d) {
-#pragma unroll
-        for (int h = 0; h < kB / 2; ++h) {
-            const u32x4 c = *reinterpret_cast<const u32x4*>(row + (int64_t)col * kB + 16 * h);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                if constexpr (DT == kF32) {
-                    x[4 * h + e] = __uint_as_float(c[e]);
-                } else if constexpr (DT == kBF16) {
-                    x[2 * e] = __uint_as_float(c[e] << 16);
-                    x[2 * e + 1] = __uint_as_float(c[e] & 0xffff0000u);
-                } else {
-                    const f16x2 p = __builtin_bit_cast(f16x2, (uint32_t)c[e]);
-                    x[2 * e] = (float)p[0];
-                    x[2 * e + 1] = (float)p[1];
-                }
-            }
-        }
-        return;
-    }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        x[e] = 0.0f;
-        if (col + e < d) {
-            const char* p = row + (int64_t)(col + e) * kB;
-            if constexpr (DT == kF32) x[e] = *reinterpret_cast<const float*>(p);
-            else if constexpr (DT == kBF16) x[e] = bf16_bits_to_f32(*reinterpret_cast<const uint16_t*>(p));
-            else x[e] = (float)*reinterpret_cast<const _Float16*>(p);
-        }
-    }
-}
 // Two values rounded to 16 bits.
 template <int DT> __device__ __forceinline__ uint32_t q4_pair(float a, float b) {
     if constexpr (DT == kBF16) return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)a, (__bf16)b});
     else return __builtin_bit_cast(uint32_t, f16x2{(_Float16)a, (_Float16)b});
 }
-
-struct Q4WeightParams {
-    const char* W;             // quantise: in; read back: unused
-    char* W_out;
-    int64_t row_bytes;
-    char* codes;
-    uint16_t* scales;
-    int V, d, blocks, groups;  // tiles of 128 columns; groups of a row
-    int per_block;             // waves' tiles in a row of tiles: blocks, for the index arithmetic
-    bool half, chunks;         // scales in fp16; rows in 16-byte chunks
-    int64_t tiles;
-};
-
-// The largest magnitude (its bits: infinities and NaN above all else) of the lane's values in each of the tile's groups.
-template <int kRuns> __device__ __forceinline__ void q4_group_max(uint32_t (&most)[4]) {
-#pragma unroll
-    for (int j = 0; j < 4; j += kRuns) {
-        uint32_t m = most[j];
-#pragma unroll
-        for (int i = 1; i < kRuns; ++i) m = max(m, most[j + i]);
-        m = max(m, (uint32_t)__shfl_xor((int)m, 16, kWave));
-        m = max(m, (uint32_t)__shfl_xor((int)m, 32, kWave));
-#pragma unroll
-        for (int i = 0; i < kRuns; ++i) most[j + i] = m;
-    }
-}
-
-// The scale of a group whose largest magnitude is `most`: most / 7, rounded once.  The quotient is first rounded to odd (its last bit set where it is not exact, by the
-// sign of the exact remainder), so that the rounding to the scale's type sees on which side of a midpoint it lies.
-__device__ __forceinline__ uint32_t q4_scale_bits(uint32_t most, bool half) {
-    const float a = __uint_as_float(most), q = a / 7.0f, rest = fmaf(-7.0f, q, a);
-    uint32_t bits = __float_as_uint(q);
-    if (rest != 0.0f) bits = (rest < 0.0f ? bits - 1 : bits) | 1;
-    const float odd = __uint_as_float(bits);
-    uint32_t s = half ? __builtin_bit_cast(uint16_t, (_Float16)odd) : __builtin_bit_cast(uint16_t, (__bf16)odd);
-    const bool lost = most >= 0x7f800000u || s == (half ? 0x7c00u : 0x7f80u);
-    return lost ? (half ? 0x7e00u : 0x7fc0u) : s;
-}
-// The code of a weight: |w| / s to the nearest integer, ties to even, at most 7.  The quotient only proposes the integer below; on which side of the half
-// the weight lies is the sign of one fused multiply-add, which no rounding changes.
-__device__ __forceinline__ uint32_t q4_code(float w, float s, float inv) {
-    const float a = fabsf(w), k = fminf(floorf(a * inv), 7.0f), r = fmaf(-(k + 0.5f), s, a);
-    int q = (int)k;
-    if (r > 0.0f || (r == 0.0f && (q & 1))) ++q;
-    q = min(q, 7);
-    return (uint32_t)(8 + (w < 0.0f ? -q : q));
-}
-
-// A wave per tile: read once, quantised in registers.
-template <int DT, int kRuns> __global__ __launch_bounds__(kQ4Threads) void tide_head_quantize_kernel(Q4WeightParams p) {
-    const int64_t at = (int64_t)blockIdx.x * (kQ4Threads / kWave) + threadIdx.x / kWave;
-    if (at >= p.tiles) return;
-    const int lane = threadIdx.x % kWave, g = lane >> 4, tile = (int)(at / p.blocks), kb = (int)(at - (int64_t)tile * p.blocks), v = tile * kQ4Rows + (lane & 15);
-    float x[4][8];
-    uint32_t most[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[j][e] = 0.0f;
-        if (v < p.V) q4_load8<DT>(p.W + (int64_t)v * p.row_bytes, kb * kQ4Cols + 32 * j + 8 * g, p.d, p.chunks, x[j]);
-    }
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        most[j] = 0;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) most[j] = max(most[j], __float_as_uint(x[j][e]) & 0x7fffffffu);
-    }
-    q4_group_max<kRuns>(most);
-    u32x4 out;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const uint32_t sb = q4_scale_bits(most[j], p.half);
-        const int group = (kb * 4 + j) / kRuns;
-        if (j % kRuns == 0 && g == 0 && group < p.groups) p.scales[((int64_t)tile * p.groups + group) * kQ4Rows + lane] = (uint16_t)sb;
-        float s = q4_scale(sb, p.half);
-        const bool some = s > 0.0f;                    // neither zero nor NaN
-        const float up = s < 0x1p-100f ? 0x1p64f : 1.0f;      // both a power of two larger, so that the reciprocal is finite
-        s *= up;
-        const float inv = some ? 1.0f / s : 0.0f;
-        uint32_t word = 0;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) word |= (some ? q4_code(x[j][e] * up, s, inv) : 8u) << (4 * (e >> 1) + 16 * (e & 1));
-        out[j] = word;
-    }
-    *reinterpret_cast<u32x4*>(p.codes + at * kQ4TileBytes + lane * 16) = out;
-}
-
-// A wave per tile: the values that codes and scales stand for, each rounded once.
-template <int DT, int kRuns> __global__ __launch_bounds__(kQ4Threads) void tide_head_dequantize_kernel(Q4WeightParams p) {
-    const int64_t at = (int64_t)blockIdx.x * (kQ4Threads / kWave) + threadIdx.x / kWave;
-    if (at >= p.tiles) return;
-    const int lane = threadIdx.x % kWave, g = lane >> 4, tile = (int)(at / p.blocks), kb = (int)(at - (int64_t)tile * p.blocks), v = tile * kQ4Rows + (lane & 15);
-    if (v >= p.V) return;
-    const u32x4 codes = *reinterpret_cast<const u32x4*>(p.codes + at * kQ4TileBytes + lane * 16);
-    constexpr int kB = Storage<DT>::kBytes;
-    char* row = p.W_out + (int64_t)v * p.row_bytes;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const int col = kb * kQ4Cols + 32 * j + 8 * g, group = (kb * 4 + j) / kRuns;
-        if (col >= p.d) continue;
-        const float s = q4_scale(p.scales[((int64_t)tile * p.groups + group) * kQ4Rows + (lane & 15)], p.half);
-        float x[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = s * (float)((int)(codes[j] >> (4 * (e >> 1) + 16 * (e & 1)) & 15u) - 8);
-        if (p.chunks && col + 8 <= p.d) {
-#pragma unroll
-            for (int h = 0; h < kB / 2; ++h) {
-                u32x4 c;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    if constexpr (DT == kF32) c[e] = __float_as_uint(x[4 * h + e]);
-                    else c[e] = q4_pair<DT>(x[2 * e], x[2 * e + 1]);
-                }
-                *reinterpret_cast<u32x4*>(row + (int64_t)col * kB + 16 * h) = c;
-            }
-        } else {
-            for (int e = 0; e < 8 && col + e < p.d; ++e) {
-                if constexpr (DT == kF32) *reinterpret_cast<float*>(row + (int64_t)(col + e) * 4) = x[e];
-                else *reinterpret_cast<uint16_t*>(row + (int64_t)(col + e) * 2) = (uint16_t)q4_pair<DT>(x[e], 0.0f);
-            }
-        }
-    }
-}
-
-template <int E> __device__ __forceinline__ f32x4 q4_mma(u32x4 a, u32x4 b, f32x4 acc) {
-    if constexpr (E == kBF16) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), acc, 0, 0, 0);
-    else return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), acc, 0, 0, 0);
-}
-// Eight codes as numbers 1 + c / 16: a shift and an and-or for two (the constants from registers, as that instruction takes no literals).
-template <int E> struct Q4Ones {
-    uint32_t mask = E == kBF16 ? 0x00780078u : 0x03c003c0u, one = E == kBF16 ? 0x3f803f80u : 0x3c003c00u;
-    __device__ __forceinline__ Q4Ones() { asm("" : "+s"(mask), "+v"(one)); }
-    __device__ __forceinline__ u32x4 expand(uint32_t w) const {
-        if constexpr (E == kBF16) return u32x4{(w << 3 & mask) | one, (w >> 1 & mask) | one, (w >> 5 & mask) | one, (w >> 9 & mask) | one};
-        else return u32x4{(w << 6 & mask) | one, (w << 2 & mask) | one, (w >> 2 & mask) | one, (w >> 6 & mask) | one};
-    }
-};
-// fp32 rows are three bf16 planes that add up to them exactly: the first eight significant bits, the next eight, the last eight, cut off and not rounded, so that none is
-// larger than the value.
-template <int DT> constexpr int kQ4Planes = DT == kF32 ? 3 : 1;
-template <int DT> constexpr int kQ4Elem = DT == kF32 ? (int)kBF16 : DT;
-
-// ---- Rows under a head in four bits: what the two kernels share.
 
 // The columns col + 32 j ..+7, j = 0 .. 3, of row t, as they lie in memory; zeros beyond the row and the rows.
 struct Q4Rows {
@@ -241,8 +64,8 @@ template <int DT> __device__ __forceinline__ void q4_raw(const Q4Rows& p, int t,
         }
     }
 }
-template <int DT> __device__ __forceinline__ float q4_sum8(const u32x4 (&c)[Storage<DT>::kBytes / 2]) {
-    float x[8];
+// Eight of them in 32 bits, their sum, and the bits of the largest magnitude (infinities and NaN above all else).
+template <int DT> __device__ __forceinline__ void q4_values(const u32x4 (&c)[Storage<DT>::kBytes / 2], float (&x)[8]) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         if constexpr (DT == kF32) {
@@ -257,8 +80,203 @@ template <int DT> __device__ __forceinline__ float q4_sum8(const u32x4 (&c)[Stor
             x[2 * e + 1] = (float)h[1];
         }
     }
+}
+template <int DT> __device__ __forceinline__ float q4_sum8(const u32x4 (&c)[Storage<DT>::kBytes / 2]) {
+    float x[8];
+    q4_values<DT>(c, x);
     return ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
 }
+template <int DT> __device__ __forceinline__ uint32_t q4_most8(const u32x4 (&c)[Storage<DT>::kBytes / 2]) {
+    typedef __attribute__((ext_vector_type(2))) uint16_t u16x2;
+    if constexpr (DT == kF32) {
+        uint32_t m = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) m = max(m, max(c[0][e] & 0x7fffffffu, c[1][e] & 0x7fffffffu));
+        return m;
+    } else {
+        u16x2 m = {0, 0};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, c[0][e] & 0x7fff7fffu));
+        const uint32_t bits = max((uint32_t)m[0], (uint32_t)m[1]);
+        return DT == kBF16 ? bits << 16 : __float_as_uint((float)__builtin_bit_cast(_Float16, (uint16_t)bits));
+    }
+}
+
+struct Q4WeightParams {
+    Q4Rows x;                  // quantise: the weights, V rows
+    char* W_out;               // read back
+    int64_t row_bytes;
+    char* codes;
+    uint16_t* scales;
+    int V, d, blocks, groups;  // tiles of 128 columns; groups of a row
+    bool half, chunks;         // scales in fp16; rows in 16-byte chunks
+    int64_t tiles;
+};
+
+// The largest magnitude (its bits: infinities and NaN above all else) of the lane's values in each of the tile's groups.
+template <int kRuns> __device__ __forceinline__ void q4_group_max(uint32_t (&most)[4]) {
+#pragma unroll
+    for (int j = 0; j < 4; j += kRuns) {
+        uint32_t m = most[j];
+#pragma unroll
+        for (int i = 1; i < kRuns; ++i) m = max(m, most[j + i]);
+        m = max(m, (uint32_t)__shfl_xor((int)m, 16, kWave));
+        m = max(m, (uint32_t)__shfl_xor((int)m, 32, kWave));
+#pragma unroll
+        for (int i = 0; i < kRuns; ++i) most[j + i] = m;
+    }
+}
+
+// The scale of a group whose largest magnitude is `most`: most / 7, rounded once.  The quotient is first rounded to odd (its last bit set where it is not exact, by the
+// sign of the exact remainder), so that the rounding to the scale's type sees on which side of a midpoint it lies.
+__device__ __forceinline__ uint32_t q4_scale_bits(uint32_t most, bool half) {
+    const float a = __uint_as_float(most), q = a / 7.0f, rest = fmaf(-7.0f, q, a);
+    uint32_t bits = __float_as_uint(q);
+    if (rest != 0.0f) bits = (rest < 0.0f ? bits - 1 : bits) | 1;
+    const float odd = __uint_as_float(bits);
+    uint32_t s = half ? __builtin_bit_cast(uint16_t, (_Float16)odd) : __builtin_bit_cast(uint16_t, (__bf16)odd);
+    const bool lost = most >= 0x7f800000u || s == (half ? 0x7c00u : 0x7f80u);
+    return lost ? (half ? 0x7e00u : 0x7fc0u) : s;
+}
+// Eight weights' codes in a word: w / s to the nearest integer, ties to even, within +-7.  The product with the reciprocal, improved by its exact remainder, is the quotient rounded
+// once.  Weights of 16 bits: their quotients by a scale are halves of integers or further than 2^-20 from one, so rounding it again is exact.  fp32: the remainder after
+// the nearest integer, exact as well, says whether it was; a quotient so near to a tie is rare enough for a branch.  `s` and `inv`: zero where the codes are to be 8.
+template <int DT> __device__ __forceinline__ uint32_t q4_codes(const float (&w)[8], float s, float inv) {
+    float q[8];
+    bool ties = false;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        float t = w[e] * inv;
+        if constexpr (DT != kF32) t = fmaf(fmaf(-t, s, w[e]), inv, t);
+        q[e] = __builtin_amdgcn_fmed3f(rintf(t), -7.0f, 7.0f);
+        if constexpr (DT == kF32) ties |= fabsf(fmaf(-q[e], s, w[e])) >= 0.5f * s;
+    }
+    if constexpr (DT == kF32) {
+        if (ties) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float rest = fmaf(-q[e], s, w[e]), off = fabsf(rest) - 0.5f * s;
+                const bool odd = (int)q[e] & 1;
+                if (off > 0.0f || (off == 0.0f && odd)) q[e] = __builtin_amdgcn_fmed3f(q[e] + copysignf(1.0f, rest), -7.0f, 7.0f);
+            }
+        }
+    }
+    uint32_t word = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) word |= (uint32_t)(q[e] + 8.0f) << (4 * (e >> 1) + 16 * (e & 1));
+    return word;
+}
+
+// A wave per tile: read once, quantised in registers (bf16, 128000 x 4096, groups of 128 / 32: 245 / 232 us, 5.4 / 5.8 TB/s).
+template <int DT, int kRuns> __global__ __launch_bounds__(kQ4Threads) void tide_head_quantize_kernel(Q4WeightParams p) {
+    const int64_t at = (int64_t)blockIdx.x * (kQ4Threads / kWave) + threadIdx.x / kWave;
+    if (at >= p.tiles) return;
+    const int lane = threadIdx.x % kWave, g = lane >> 4, tile = (int)(at / p.blocks), kb = (int)(at - (int64_t)tile * p.blocks), v = tile * kQ4Rows + (lane & 15);
+    Q4Raw<DT> raw;
+    q4_raw<DT>(p.x, v, kb * kQ4Cols + 8 * g, raw);
+    uint32_t most[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) most[j] = q4_most8<DT>(raw.c[j]);
+    q4_group_max<kRuns>(most);
+    // a scale for each group: of the 16 lanes of four that have a group's largest magnitudes, those of number g make that of group g (mod the number of groups)
+    constexpr int kPer = 4 / kRuns;
+    uint32_t mine = most[0];
+#pragma unroll
+    for (int gr = 1; gr < kPer; ++gr) mine = g % kPer == gr ? most[gr * kRuns] : mine;
+    const uint32_t sb = q4_scale_bits(mine, p.half);
+    if (g < kPer && kb * kPer + g < p.groups) p.scales[((int64_t)tile * p.groups + kb * kPer + g) * kQ4Rows + (lane & 15)] = (uint16_t)sb;
+    float s = q4_scale(sb, p.half);
+    const bool some = s > 0.0f;                        // neither zero nor NaN
+    // tiny ones: scale and weights a power of two larger, so that the reciprocal is finite and the remainders exact
+    const float up = !some ? 0.0f : s < 0x1p-100f ? 0x1p64f : 1.0f;
+    s = some ? s * up : 0.0f;
+    const float inv = some ? 1.0f / s : 0.0f;
+    u32x4 out;
+#pragma unroll
+    for (int gr = 0; gr < kPer; ++gr) {
+        const int from = gr * 16 + (lane & 15);
+        const float s_gr = kPer == 1 ? s : __shfl(s, from, kWave), inv_gr = kPer == 1 ? inv : __shfl(inv, from, kWave), up_gr = kPer == 1 ? up : __shfl(up, from, kWave);
+#pragma unroll
+        for (int j = gr * kRuns; j < (gr + 1) * kRuns; ++j) {
+            float x[8];
+            q4_values<DT>(raw.c[j], x);
+            if (up_gr != 1.0f) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] = up_gr != 0.0f ? x[e] * up_gr : 0.0f;
+            }
+            out[j] = q4_codes<DT>(x, s_gr, inv_gr);
+        }
+    }
+    *reinterpret_cast<u32x4*>(p.codes + at * kQ4TileBytes + lane * 16) = out;
+}
+
+// A wave per tile: the values that codes and scales stand for, each rounded once.  A lane makes 16 bytes at a time, and the lanes whole rows of the tile, one after the other (bf16,
+// 128000 x 4096: 198 us, 6.6 TB/s; in the codes' order, stores of 64 bytes of a row, 317; with stores that stay in L2 239).
+template <int DT, int kRuns> __global__ __launch_bounds__(kQ4Threads) void tide_head_dequantize_kernel(Q4WeightParams p) {
+    constexpr int kB = Storage<DT>::kBytes, N = 16 / kB, kLanes = kQ4Cols / N, kStores = kQ4Rows * kLanes / kWave;
+    const int64_t at = (int64_t)blockIdx.x * (kQ4Threads / kWave) + threadIdx.x / kWave;
+    if (at >= p.tiles) return;
+    const int lane = threadIdx.x % kWave, tile = (int)(at / p.blocks), kb = (int)(at - (int64_t)tile * p.blocks);
+    const int octet = lane % kLanes * N / 8, half = DT == kF32 ? lane & 1 : 0, j = octet >> 2, g = octet & 3, col = kb * kQ4Cols + lane % kLanes * N, row0 = lane / kLanes;
+    const int group = min((kb * 4 + j) / kRuns, p.groups - 1);
+    uint32_t codes[kStores], scales[kStores];
+#pragma unroll
+    for (int i = 0; i < kStores; ++i) {
+        const int row = row0 + i * (kQ4Rows / kStores);
+        codes[i] = *reinterpret_cast<const uint32_t*>(p.codes + at * kQ4TileBytes + (g * 16 + row) * 16 + j * 4);
+        scales[i] = p.scales[((int64_t)tile * p.groups + group) * kQ4Rows + row];
+    }
+#pragma unroll
+    for (int i = 0; i < kStores; ++i) {
+        const int v = tile * kQ4Rows + row0 + i * (kQ4Rows / kStores);
+        const float s = q4_scale(scales[i], p.half);
+        float x[N];
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            const int k = e + half * 4;
+            x[e] = s * (float)((int)(codes[i] >> (4 * (k >> 1) + 16 * (k & 1)) & 15u) - 8);
+        }
+        if (v >= p.V || col >= p.d) continue;
+        char* out = p.W_out + (int64_t)v * p.row_bytes + (int64_t)col * kB;
+        if (p.chunks && col + N <= p.d) {
+            u32x4 c;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if constexpr (DT == kF32) c[e] = __float_as_uint(x[e]);
+                else c[e] = q4_pair<DT>(x[2 * e], x[2 * e + 1]);
+            }
+            __builtin_nontemporal_store(c, reinterpret_cast<u32x4*>(out));
+        } else {
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                if (col + e >= p.d) continue;
+                if constexpr (DT == kF32) *reinterpret_cast<float*>(out + e * 4) = x[e];
+                else *reinterpret_cast<uint16_t*>(out + e * 2) = (uint16_t)q4_pair<DT>(x[e], 0.0f);
+            }
+        }
+    }
+}
+
+template <int E> __device__ __forceinline__ f32x4 q4_mma(u32x4 a, u32x4 b, f32x4 acc) {
+    if constexpr (E == kBF16) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), acc, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), acc, 0, 0, 0);
+}
+// Eight codes as numbers 1 + c / 16: a shift and an and-or for two (the constants from registers, as that instruction takes no literals).
+template <int E> struct Q4Ones {
+    uint32_t mask = E == kBF16 ? 0x00780078u : 0x03c003c0u, one = E == kBF16 ? 0x3f803f80u : 0x3c003c00u;
+    __device__ __forceinline__ Q4Ones() { asm("" : "+s"(mask), "+v"(one)); }
+    __device__ __forceinline__ u32x4 expand(uint32_t w) const {
+        if constexpr (E == kBF16) return u32x4{(w << 3 & mask) | one, (w >> 1 & mask) | one, (w >> 5 & mask) | one, (w >> 9 & mask) | one};
+        else return u32x4{(w << 6 & mask) | one, (w << 2 & mask) | one, (w >> 2 & mask) | one, (w >> 6 & mask) | one};
+    }
+};
+// fp32 rows are three bf16 planes that add up to them exactly: the first eight significant bits, the next eight, the last eight, cut off and not rounded, so that none is
+// larger than the value.
+template <int DT> constexpr int kQ4Planes = DT == kF32 ? 3 : 1;
+template <int DT> constexpr int kQ4Elem = DT == kF32 ? (int)kBF16 : DT;
+
+// ---- Rows under a head in four bits: what the two kernels share.
+
 // The operands of a block of 128 columns from what four groups of lanes, `apart` lanes each, have of its rows: fragment j, plane to x + (j planes + plane) * step, and the
 // sum of each group of columns times -1.5 to offs[group * offs_step].
 template <int DT, int kRuns> __device__ __forceinline__ void q4_put(const Q4Raw<DT>& raw, int g, int apart, char* x, int step, float* offs, int offs_step) {
