@@ -101,17 +101,27 @@ struct Q4Plan {
     bool few;
 
     int few_lds(int log, int nt_, int waves_, int split_) const {
-        return (int)(blocks * (4 * planes * (64 << log) + per * (4 << std::max(log, 2)))) + waves_ * 1024 + (split_ > 1 ? waves_ * nt_ * 1024 : 0);
+        return (int)(blocks * (4 * planes * (64 << log) + per * (planes > 1 ? kQ4Sums<kF32> : 1) * (4 << std::max(log, 2)))) + waves_ * 1024 + (split_ > 1 ? waves_ * nt_ * 1024 : 0);
     }
     int64_t sets() const { return (tiles + waves * nt - 1) / (waves * nt); }
 };
+// Whether the rows fit in LDS, with groups of 32 columns and sixteen waves' scales.
+bool q4_few(int dtype, int64_t T, int64_t d) {
+    const Q4Shape s{1, d, 32, TIDE_BF16};
+    Q4Plan p{};
+    p.planes = dtype == TIDE_F32 ? kQ4Planes<kF32> : 1;
+    p.blocks = s.blocks(), p.per = 4;
+    int log = 0;
+    while ((1 << log) < T && log < 4) ++log;
+    return T <= 16 && p.few_lds(log, 2, 16, 1) <= kMostLds;
+}
 constexpr int kQ4ManyTiles[] = {8, 6, 4, 3, 2};        // of 16 rows, of a row block; fp32 rows: 2
 Q4Plan q4_plan(int dtype, int64_t T, const Q4Shape& s, unsigned cus) {
     Q4Plan p{};
     p.planes = dtype == TIDE_F32 ? kQ4Planes<kF32> : 1;
     p.T = T, p.tiles = s.tiles(), p.blocks = s.blocks(), p.per = (int)(128 / s.group), p.cus = cus;
     while ((1 << p.rows_log) < T && p.rows_log < 4) ++p.rows_log;
-    p.few = T <= 16 && p.few_lds(p.rows_log, 2, 16, 1) <= kMostLds;
+    p.few = q4_few(dtype, T, s.d);
     if (p.few) {
         // Rows that leave room for several workgroups a CU: small ones, which start and end apart from each other; else one of as many waves as share its CU's tokens
         // evenly, two tiles a wave where there are enough (bf16, d = 4096, V = 128000, us, 4 waves of one tile / 16 of two: T = 1 50 / 53, 8 63 / 55, 16 66 / 57).
@@ -286,13 +296,14 @@ size_t tide_head_logits_q4_bytes(int dtype, int64_t T, int64_t d) {
         fail(TIDE_ERR_UNSUPPORTED, "unsupported dtype %d, T = %lld or d = %lld", dtype, (long long)T, (long long)d);
         return 0;
     }
+    if (q4_few(dtype, T, d)) return 0;
     // Row blocks of 16 mt rows for any mt, and groups of 32 columns: no matter how many tokens, and more than any call of fewer rows takes.  (A region's sums are at most 512
     // bytes a tile, its padding included.)
     const int64_t planes = dtype == TIDE_F32 ? kQ4Planes<kF32> : 1, blocks = (d + kQ4Cols - 1) / kQ4Cols;
     int64_t tiles = 0;
     for (int mt : kQ4ManyTiles)
         if (planes == 1 || mt == 2) tiles = std::max(tiles, (T + 16 * mt - 1) / (16 * mt) * mt);
-    return (size_t)(tiles * blocks * (4 * planes * 1024 + 512) + 256 + 255) & ~size_t(255);
+    return (size_t)(tiles * blocks * (4 * planes * 1024 + 512) + 255) & ~size_t(255);
 }
 
 int tide_head_logits_q4(const void* x, int dtype, int64_t T, int64_t d, int64_t V, int64_t x_row_stride, const void* codes, const void* scales, int scale_dtype, int64_t group,
@@ -310,8 +321,9 @@ int tide_head_logits_q4(const void* x, int dtype, int64_t T, int64_t d, int64_t 
     if ((uintptr_t)logits & 3) return fail(TIDE_ERR_ALIGNMENT, "logits must be aligned to a float");
     if ((T + 15) / 16 * s.tiles() > 4 * kMostBlocks) return fail(TIDE_ERR_UNSUPPORTED, "T = %lld rows of V = %lld logits are too many for one call", (long long)T, (long long)V);
     const size_t need = tide_head_logits_q4_bytes(dtype, T, d);
-    if (!workspace || workspace_bytes < need) return fail(TIDE_ERR_WORKSPACE, "this call needs %zu bytes of workspace, %zu given", need, workspace ? workspace_bytes : 0);
-    if ((uintptr_t)workspace & 255) return fail(TIDE_ERR_ALIGNMENT, "the workspace must be 256-byte aligned");
+    if (need && (!workspace || workspace_bytes < need))
+        return fail(TIDE_ERR_WORKSPACE, "this call needs %zu bytes of workspace, %zu given", need, workspace ? workspace_bytes : 0);
+    if (need && ((uintptr_t)workspace & 255)) return fail(TIDE_ERR_ALIGNMENT, "the workspace must be 256-byte aligned");
     unsigned cus = 0;
     if ((rc = resident_cus(&cus))) return rc;
     const Q4Plan plan = q4_plan(dtype, T, s, cus);

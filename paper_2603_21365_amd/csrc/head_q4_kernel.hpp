@@ -274,18 +274,21 @@ template <int E> struct Q4Ones {
 // larger than the value.
 template <int DT> constexpr int kQ4Planes = DT == kF32 ? 3 : 1;
 template <int DT> constexpr int kQ4Elem = DT == kF32 ? (int)kBF16 : DT;
+// A group has a sum of its first plane's products and another of the rest's, with a start each.  The first's terms have few bits, so that it is all but exact although the
+// offset cancels most of it; the other is 2^-8 of it, and so are its roundings.  (One sum, from a start of all 24 bits, rounds at the size from before it cancels: errors of
+// up to 1.3e-6 of the logits' size, and 2e-7 like this, which is what rows in bf16 have.)
+template <int DT> constexpr int kQ4Sums = DT == kF32 ? 2 : 1;
 
 // ---- Rows under a head in four bits: what the two kernels share.
 
 // The operands of a block of 128 columns from what four groups of lanes, `apart` lanes each, have of its rows: fragment j, plane to x + (j planes + plane) * step, and the
-// sum of each group of columns times -1.5 to offs[group * offs_step].
+// sums of each group of columns times -1.5 to offs[(group sums + sum) * offs_step].
 template <int DT, int kRuns> __device__ __forceinline__ void q4_put(const Q4Raw<DT>& raw, int g, int apart, char* x, int step, float* offs, int offs_step) {
 #pragma unroll
     for (int j0 = 0; j0 < 4; j0 += kRuns) {
-        float sum = 0.0f;
+        float sum[kQ4Sums<DT>] = {};
 #pragma unroll
         for (int j = j0; j < j0 + kRuns; ++j) {
-            sum += q4_sum8<DT>(raw.c[j]);
             if constexpr (DT == kF32) {
                 float y[8];
 #pragma unroll
@@ -299,16 +302,24 @@ template <int DT, int kRuns> __device__ __forceinline__ void q4_put(const Q4Raw<
                         v[e] = a >> 16 | b;
                         y[2 * e] -= __uint_as_float(a);
                         y[2 * e + 1] -= __uint_as_float(b);
+                        if (plane == 0) sum[0] += __uint_as_float(a) + __uint_as_float(b);
                     }
+                    if (plane == 0)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) sum[1] += y[e];
                     *reinterpret_cast<u32x4*>(x + (j * 3 + plane) * step) = v;
                 }
             } else {
+                sum[0] += q4_sum8<DT>(raw.c[j]);
                 *reinterpret_cast<u32x4*>(x + j * step) = raw.c[j][0];
             }
         }
-        sum += __shfl_xor(sum, apart, kWave);
-        sum += __shfl_xor(sum, 2 * apart, kWave);
-        if (g == 0) offs[j0 / kRuns * offs_step] = -1.5f * sum;
+#pragma unroll
+        for (int h = 0; h < kQ4Sums<DT>; ++h) {
+            sum[h] += __shfl_xor(sum[h], apart, kWave);
+            sum[h] += __shfl_xor(sum[h], 2 * apart, kWave);
+            if (g == 0) offs[(j0 / kRuns * kQ4Sums<DT> + h) * offs_step] = -1.5f * sum[h];
+        }
     }
 }
 
@@ -351,14 +362,14 @@ struct Q4FewLds {
 template <int DT, int kRuns, int NT> __host__ __device__ inline Q4FewLds q4_few_lds(int rows_log, int blocks, int waves, int split) {
     Q4FewLds l{};
     l.offs = blocks * 4 * kQ4Planes<DT> * (64 << rows_log);
-    l.scales = l.offs + blocks * (4 / kRuns) * (4 << (rows_log < 2 ? 2 : rows_log));
+    l.scales = l.offs + blocks * (4 / kRuns) * kQ4Sums<DT> * (4 << (rows_log < 2 ? 2 : rows_log));
     l.sums = l.scales + waves * 1024;
     l.bytes = l.sums + (split > 1 ? waves * NT * 1024 : 0);
     return l;
 }
 
 template <int DT, int kRuns, int NT, int kDepth> __global__ __launch_bounds__(kQ4FewThreads) void tide_head_q4_few_kernel(Q4FewParams p) {
-    constexpr int E = kQ4Elem<DT>, P = kQ4Planes<DT>, kPer = 4 / kRuns;
+    constexpr int E = kQ4Elem<DT>, P = kQ4Planes<DT>, kSums = kQ4Sums<DT>, kPer = 4 / kRuns;
     constexpr int kScaleBlocks = 32 / NT / kPer;       // blocks of 128 columns whose scales a kilobyte holds
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), waves = blockDim.x / kWave;
@@ -399,7 +410,7 @@ template <int DT, int kRuns, int NT, int kDepth> __global__ __launch_bounds__(kQ
         const int row = item & (rows - 1), g = item >> log & 3, kb = item >> (log + 2);
         Q4Raw<DT> raw;
         q4_raw<DT>(p.x, row, kb * kQ4Cols + 8 * g, raw);
-        q4_put<DT, kRuns>(raw, g, rows, lds + ((kb * 16 * P + g) << (log + 4)) + row * 16, 64 << log, reinterpret_cast<float*>(lds + at.offs) + (kb * kPer << offs_log) + row, 1 << offs_log);
+        q4_put<DT, kRuns>(raw, g, rows, lds + ((kb * 16 * P + g) << (log + 4)) + row * 16, 64 << log, reinterpret_cast<float*>(lds + at.offs) + (kb * kPer * kSums << offs_log) + row, 1 << offs_log);
     }
     __syncthreads();
 
@@ -419,13 +430,16 @@ template <int DT, int kRuns, int NT, int kDepth> __global__ __launch_bounds__(kQ
             else fetch_scales(pass + 1, 0);
         }
         const char* x = my_x + ((begin + i) * 4 * P << (log + 6));
-        const float* offs = my_offs + ((begin + i) * kPer << offs_log);
+        const float* offs = my_offs + ((begin + i) * kPer * kSums << offs_log);
 #pragma unroll
         for (int gr = 0; gr < kPer; ++gr) {
-            f32x4 sum[NT];
-            const f32x4 start = *reinterpret_cast<const f32x4*>(offs + (gr << offs_log));
+            f32x4 sum[kSums][NT];
 #pragma unroll
-            for (int n = 0; n < NT; ++n) sum[n] = start;
+            for (int h = 0; h < kSums; ++h) {
+                const f32x4 start = *reinterpret_cast<const f32x4*>(offs + (gr * kSums + h << offs_log));
+#pragma unroll
+                for (int n = 0; n < NT; ++n) sum[h][n] = start;
+            }
 #pragma unroll
             for (int j = gr * kRuns; j < (gr + 1) * kRuns; ++j) {
                 u32x4 w[NT];
@@ -435,14 +449,15 @@ template <int DT, int kRuns, int NT, int kDepth> __global__ __launch_bounds__(kQ
                 for (int plane = 0; plane < P; ++plane) {
                     const u32x4 a = *reinterpret_cast<const u32x4*>(x + ((j * P + plane) << (log + 6)));
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) sum[n] = q4_mma<E>(a, w[n], sum[n]);
+                    for (int n = 0; n < NT; ++n) sum[plane > 0][n] = q4_mma<E>(a, w[n], sum[plane > 0][n]);
                 }
             }
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
                 const float s = q4_scale_at(my_scales, NT, n, s_at * kPer + gr, lane, half);
+                if constexpr (kSums > 1) sum[0][n] += sum[1][n];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) total[n][e] = fmaf(s, sum[n][e], total[n][e]);
+                for (int e = 0; e < 4; ++e) total[n][e] = fmaf(s, sum[0][n][e], total[n][e]);
             }
         }
         if (++s_at == kScaleBlocks) s_at = 0;
@@ -504,7 +519,7 @@ template <int DT, int kRuns, int NT, int kDepth> __global__ __launch_bounds__(kQ
 //
 // The rows are first laid out in memory: for 16 MT rows and 128 columns one region, the fragments and behind them the groups' sums times -1.5, whole kilobytes.
 template <int DT, int kRuns, int MT> struct Q4Region {
-    static constexpr int kX = 4 * kQ4Planes<DT> * MT * 1024, kOffs = (4 / kRuns * MT * 64 + 1023) / 1024 * 1024, kBytes = kX + kOffs;
+    static constexpr int kX = 4 * kQ4Planes<DT> * MT * 1024, kOffs = (4 / kRuns * kQ4Sums<DT> * MT * 64 + 1023) / 1024 * 1024, kBytes = kX + kOffs;
 };
 struct Q4LayParams {
     Q4Rows x;
@@ -547,7 +562,7 @@ __device__ __forceinline__ void q4_transfer(uint32_t lds, const char* base, uint
 
 template <int DT, int kRuns, int MT, int NT> __global__ __launch_bounds__(kQ4ManyThreads<NT>) void tide_head_q4_many_kernel(Q4ManyParams p) {
     using R = Q4Region<DT, kRuns, MT>;
-    constexpr int E = kQ4Elem<DT>, P = kQ4Planes<DT>, kPer = 4 / kRuns, kStages = kQ4CodeStages<DT, kRuns, MT, NT>, kSteps = kRuns * P, kAhead = 2;
+    constexpr int E = kQ4Elem<DT>, P = kQ4Planes<DT>, kSums = kQ4Sums<DT>, kPer = 4 / kRuns, kStages = kQ4CodeStages<DT, kRuns, MT, NT>, kSteps = kRuns * P, kAhead = 2;
     constexpr int kScaleBlocks = 32 / NT / kPer;       // blocks of 128 columns whose scales a kilobyte holds
     static_assert(kScaleBlocks >= 2, "a kilobyte is requested two blocks before it is read");
     extern __shared__ __attribute__((aligned(16))) char lds[];
@@ -624,9 +639,11 @@ template <int DT, int kRuns, int MT, int NT> __global__ __launch_bounds__(kQ4Man
                 // fragments are read kAhead steps of NT matrix steps ahead of their use, a row tile's start one; the codes of a step are expanded beside the matrix steps of the
                 // one before
                 auto fragment = [&](int step) { return *reinterpret_cast<const u32x4*>(x + ((gr * kSteps + step % kSteps) * MT + step / kSteps) * 1024); };
-                auto first = [&](int rt) { return *reinterpret_cast<const f32x4*>(offs + (gr * MT + rt) * 16); };
+                auto first = [&](int rt, int h) { return *reinterpret_cast<const f32x4*>(offs + ((gr * kSums + h) * MT + rt) * 16); };
                 u32x4 a[kAhead], w[kRuns][NT];
-                f32x4 start = first(0);
+                f32x4 start[kSums];
+#pragma unroll
+                for (int h = 0; h < kSums; ++h) start[h] = first(0, h);
 #pragma unroll
                 for (int step = 0; step < kAhead; ++step) a[step] = fragment(step);
                 float s[NT];
@@ -637,18 +654,22 @@ template <int DT, int kRuns, int MT, int NT> __global__ __launch_bounds__(kQ4Man
                 }
 #pragma unroll
                 for (int rt = 0; rt < MT; ++rt) {
-                    f32x4 sum[NT];
+                    f32x4 sum[kSums][NT];
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) sum[n] = start;
+                    for (int h = 0; h < kSums; ++h)
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) sum[h][n] = start[h];
 #pragma unroll
                     for (int step = 0; step < kSteps; ++step) {
                         const int at = rt * kSteps + step;
                         const u32x4 now = a[at % kAhead];
-                        if (step + 1 == kSteps && rt + 1 < MT) start = first(rt + 1);
+                        if (step + 1 == kSteps && rt + 1 < MT)
+#pragma unroll
+                            for (int h = 0; h < kSums; ++h) start[h] = first(rt + 1, h);
                         if (at + kAhead < MT * kSteps) a[at % kAhead] = fragment(at + kAhead);
                         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                        for (int n = 0; n < NT; ++n) sum[n] = q4_mma<E>(now, w[step / P][n], sum[n]);
+                        for (int n = 0; n < NT; ++n) sum[step % P > 0][n] = q4_mma<E>(now, w[step / P][n], sum[step % P > 0][n]);
                         if (rt == 0 && step % P == 0 && step / P + 1 < kRuns) {
 #pragma unroll
                             for (int n = 0; n < NT; ++n) w[step / P + 1][n] = ones.expand(c[n][gr * kRuns + step / P + 1]);
@@ -657,7 +678,8 @@ template <int DT, int kRuns, int MT, int NT> __global__ __launch_bounds__(kQ4Man
                     }
 #pragma unroll
                     for (int n = 0; n < NT; ++n) {
-                        total[n][rt] = __builtin_elementwise_fma(f32x4{s[n], s[n], s[n], s[n]}, sum[n], total[n][rt]);
+                        if constexpr (kSums > 1) sum[0][n] += sum[1][n];
+                        total[n][rt] = __builtin_elementwise_fma(f32x4{s[n], s[n], s[n], s[n]}, sum[0][n], total[n][rt]);
                         asm volatile("" : "+v"(total[n][rt]));     // here: not behind the next branch, with all sums kept until then
                     }
                 }

@@ -707,13 +707,12 @@ def _scale_code(dtype) -> int:
 def _q4(codes, scales, V, d, group):
     """Codes and scales of a head of V rows and d columns: their sizes."""
     V, d, group = int(V), int(d), int(group)
-    if group not in (32, 64, 128):
+    if group != 128 and group != 64 and group != 32:
         raise TideError(-2, f"group = {group}: 32, 64 or 128 columns")
-    rows = (V + 15) // 16
-    if codes.dtype != torch.uint8 or not codes.is_cuda or not codes.is_contiguous() or tuple(codes.shape) != (rows, (d + 127) // 128, 1024):
+    rows, code = (V + 15) // 16, _scale_code(scales.dtype)
+    if codes.dtype is not torch.uint8 or codes.shape != (rows, (d + 127) // 128, 1024) or not codes.is_contiguous() or not codes.is_cuda:
         raise ValueError(f"codes must be a contiguous CUDA uint8 tensor of shape {(rows, (d + 127) // 128, 1024)}")
-    code = _scale_code(scales.dtype)
-    if not scales.is_cuda or not scales.is_contiguous() or tuple(scales.shape) != (rows, (d + group - 1) // group, 16) or scales.device != codes.device:
+    if scales.shape != (rows, (d + group - 1) // group, 16) or not scales.is_contiguous() or scales.device != codes.device:
         raise ValueError(f"scales must be a contiguous CUDA tensor of shape {(rows, (d + group - 1) // group, 16)} on {codes.device}")
     return V, d, group, code
 
@@ -741,7 +740,7 @@ def head_dequantize_q4(codes, scales, V, d, dtype, group=128):
 
 
 def head_logits_q4_bytes(dtype: int, T: int, d: int) -> int:
-    """Bytes of workspace a head_logits_q4 call needs (0 and last_error() if unsupported).  They grow with T."""
+    """Bytes of workspace a head_logits_q4 call needs: 0 for few rows (and with last_error() if unsupported).  They grow with T."""
     return int(load_library().tide_head_logits_q4_bytes(int(dtype), int(T), int(d)))
 
 
@@ -757,9 +756,12 @@ def head_logits_q4(x, codes, scales, V, group=128, *, out=None, workspace=None):
     if T == 0:
         return out
     dtype = _dtype_code(x)
-    workspace, nbytes = _scratch(workspace, head_logits_q4_bytes(dtype, T, d), x.device)
-    _check(load_library().tide_head_logits_q4(_ptr(x), dtype, T, d, V, xs if T > 1 else d, _ptr(codes), _ptr(scales), code, group, _ptr(out), os_ if T > 1 else V,
-                                              _ptr(workspace), nbytes, _stream_on(x.device)))
+    lib = load_library()
+    nbytes = lib.tide_head_logits_q4_bytes(dtype, T, d)
+    if nbytes:
+        workspace, nbytes = _scratch(workspace, nbytes, x.device)
+    _check(lib.tide_head_logits_q4(_ptr(x), dtype, T, d, V, xs if T > 1 else d, codes.data_ptr(), scales.data_ptr(), code, group, out.data_ptr(), os_ if T > 1 else V,
+                                   _ptr(workspace) if nbytes else None, nbytes, _stream_on(x.device)))
     return out
 
 

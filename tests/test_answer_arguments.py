@@ -16,7 +16,7 @@ def dequantize(W=FAKE, dtype=2, V=100, d=64, ws=64, group=32, codes=FAKE, scales
     return tr.load_library().tide_head_dequantize_q4(codes, scales, sdtype, V, d, group, W, dtype, ws, None)
 
 
-def logits(x=FAKE, dtype=2, T=4, d=64, V=100, xs=64, codes=FAKE, scales=FAKE, sdtype=2, group=32, out=FAKE, os=100, space=FAKE, nbytes=1 << 30):
+def logits(x=FAKE, dtype=2, T=20, d=64, V=100, xs=64, codes=FAKE, scales=FAKE, sdtype=2, group=32, out=FAKE, os=100, space=FAKE, nbytes=1 << 30):
     return tr.load_library().tide_head_logits_q4(x, dtype, T, d, V, xs, codes, scales, sdtype, group, out, os, space, nbytes, None)
 
 
@@ -90,7 +90,7 @@ def test_workspaces_grow_with_the_rows():
     for dtype in (tr.F32, tr.F16, tr.BF16):
         for d in (1, 768, 1600, 16384):
             sizes = [tr.head_logits_q4_bytes(dtype, T, d) for T in range(0, 700)]
-            assert min(sizes) > 0 and sizes == sorted(sizes)
+            assert sizes[0] == sizes[1] == 0 and min(sizes[17:]) > 0 and sizes == sorted(sizes) and tr.last_error() == ""
     assert tr.head_logits_q4_bytes(3, 4, 64) == 0 and tr.head_logits_q4_bytes(tr.F32, 4, 20000) == 0 and "unsupported" in tr.last_error()
     for V in (1, 1024, 1025, 128000):
         sizes = [tr.logit_pick_bytes(T, V) for T in range(0, 700)]

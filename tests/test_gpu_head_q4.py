@@ -206,6 +206,19 @@ def test_logits_of_random_rows(dtype, group, scale):
         assert ((got - x.double() @ w.T).abs() <= bound).all()
 
 
+@pytest.mark.parametrize("d", [32, 64, 128])
+def test_fp32_rows_round_a_group_once(d):
+    """x = 1024 m + r with m of 8 bits and r of 10: the first term of a row's value is 1024 m, whose sums with up to 128 codes and the offset are multiples of 2^6 below 2^27, and
+    the rest's are multiples of 2^-4 below 2^18.  Both are exact in 32 bits, so one rounding is left, of their sum, which is the logit divided by a power of two."""
+    V = 50
+    (codes, scales), w = head(V, d, d, exact=True, seed=d)
+    for T in (1, 3, 9, 16, 20, 70):
+        g = generator(T + d)
+        x = 1024.0 * torch.randint(128, 256, (T, d), generator=g) + torch.randint(0, 1024, (T, d), generator=g)
+        got = tr.head_logits_q4(x.cuda(), codes, scales, V, d)
+        assert torch.equal(got.cpu(), (x.double() @ w.T).float()), f"T={T}"
+
+
 def test_a_row_or_a_token_that_is_not_finite_stays_alone():
     V, d = 70, 160
     (codes, scales), w = head(V, d, 32, exact=True)
