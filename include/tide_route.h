@@ -333,11 +333,12 @@ int tide_head_distill_grad(const void* x, int dtype, int64_t T, int64_t d, int64
  *   where m / 7 rounds to zero: s = 0, c = 8.  A group with a value that is not finite, or whose scale does not fit: s = NaN, c = 8.  Codes beyond V and d are 8.
  * tide_head_dequantize_q4: W[v,i] = s (c - 8), rounded once to `dtype`.
  * tide_head_logits_q4: logits[t,v] = sum_i x[t,i] W[v,i], W as it stands for, not rounded: products of 16-bit values and codes are exact (fp32 rows are taken as
- *   three bf16 terms, which add up to them), the sums and the scales' products in fp32.  A row of x that is not finite has NaN for all of its logits, no other row does.
+ *   three bf16 terms, which add up to them), the sums and the scales' products in fp32.  A row of x that is not finite has NaN for all of its logits, as has one whose
+ *   magnitudes in a group of columns add up to 2^126 or more; no other row does.  bf16 terms below 2^-126 may be taken as zero.
  *   The results do not depend on timing.
  *
  *   W       device [V rows] of `dtype`, x device [T rows] of `dtype`; strides in elements.  Element alignment is enough; 16-byte bases and strides are faster.
- *   logits  device [T rows] fp32 out, logits_row_stride >= V
+ *   logits  device [T rows] fp32 out, logits_row_stride >= V.  Outputs must not overlap what a call reads.
  *   1 <= d <= 16384, T <= 4194304, V <= 8388608, T * V up to about 2^34 (TIDE_ERR_UNSUPPORTED)
  *   workspace  device, 256-byte aligned, tide_head_logits_q4_bytes(dtype, T, d) bytes, which grow with T; 0 (up to 16 rows, as long as they fit in a CU's memory): none,
  *           and NULL will do.  No initialisation, nothing kept: calls on different workspaces may overlap.  0 bytes with tide_last_error() set: unsupported. */

@@ -94,7 +94,7 @@ template <int DT> __device__ __forceinline__ void rule_store1(char* p, uint32_t 
 
 // The past's rules for one logit; every operation rounded by itself, in the order of the formula.  Division by the row's penalty: times its reciprocal in 64 bits, which
 // is off by 2^-52 of the quotient, and a quotient of two 24-bit numbers is never that near to a midpoint of two 24-bit ones (2^-49): rounded to 32 bits it is the quotient
-// rounded once.
+// rounded once.  (Quotients below 2^-126, which have fewer bits, may be off by one of their steps where they lie at a midpoint.)
 struct RuleRow {
     float repetition, presence, frequency;
     double inverse;

@@ -780,13 +780,13 @@ def _rule_args(logits, past, past_len, prompt_len, repetition, presence, frequen
     (T, V), (rs, _) = _rows(logits, 2)
     dev, H, B, i32, f32, rows = logits.device, 0, 0, torch.int32, torch.float32, (T,)
     if past is not None:
-        H = past.shape[-1]
+        H = past.shape[-1] if past.dim() else 0
     elif past_len is not None or prompt_len is not None or repetition is not None or presence is not None or frequency is not None:
         raise ValueError("lengths and penalties need a past")
     if (bias_ids is None) != (bias_values is None):
         raise ValueError("bias_ids and bias_values come together")
     if bias_ids is not None:
-        B = bias_ids.shape[-1]
+        B = bias_ids.shape[-1] if bias_ids.dim() else 0
     return T, V, (_ptr(logits), _dtype_code(logits), T, V, rs if T > 1 else V, _row_array(past, i32, (T, H), dev, "past"), H, _row_array(past_len, i32, rows, dev, "past_len"),
                   _row_array(prompt_len, i32, rows, dev, "prompt_len"), _row_array(repetition, f32, rows, dev, "repetition"), _row_array(presence, f32, rows, dev, "presence"),
                   _row_array(frequency, f32, rows, dev, "frequency"), _row_array(bias_ids, i32, (T, B), dev, "bias_ids"),
