@@ -345,6 +345,7 @@ __device__ __forceinline__ float q4_scale_at(const char* mine, int NT, int n, in
 // group start from: no instruction is spent on the offset -- and its waves then stream tiles of codes, each wave NT tiles at a time, kDepth blocks of 128
 // columns ahead.  The scales come a kilobyte at a time through LDS (a load of each step's scales, 32 bytes of use, cost 4 of 50 us at one row, 128000 x 4096).
 // Where there are few tokens, `split` waves share the columns of a wave's tiles and add up their sums, in order, through LDS.
+// Bound by reading the codes (bf16, 128000 x 4096, groups of 128: 47 us at one row, 5.7 TB/s with the scales, 55 at 8, 57 at 16; a pure read of as much 41).
 struct Q4FewParams {
     Q4Rows x;
     Q4Head head;
@@ -541,6 +542,8 @@ template <int DT, int kRuns, int MT> __global__ __launch_bounds__(kQ4Threads) vo
 // A workgroup has 16 MT rows and its waves NT tiles of 16 tokens each.  Everything comes to LDS by transfers that no register waits for: the rows' regions in two
 // stages, for all waves, behind a barrier for each block of 128 columns; each wave's codes in two or three stages and its scales, a kilobyte at a time, in two.  The
 // transfers are inline assembly, which the compiler does not count, and the waits for them are written out; there are no other loads from memory in the loop.
+// Some dozen rows are bound by making operands of the codes (half of the vector instructions at 48 rows) beside the matrix steps, many by the matrix steps under the power
+// limit (bf16, 128000 x 4096, groups of 128: 48 rows 69 us, 512 rows 465, 1.16 PFLOP/s; with codes and scales through registers 84 and 512).
 struct Q4ManyParams {
     const char* regions;
     Q4Head head;
