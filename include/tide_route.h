@@ -340,13 +340,13 @@ int tide_head_distill_grad(const void* x, int dtype, int64_t T, int64_t d, int64
  *   W       device [V rows] of `dtype`, x device [T rows] of `dtype`; strides in elements.  Element alignment is enough; 16-byte bases and strides are faster.
  *   logits  device [T rows] fp32 out, logits_row_stride >= V.  Outputs must not overlap what a call reads.
  *   1 <= d <= 16384, T <= 4194304, V <= 8388608, T * V up to about 2^34 (TIDE_ERR_UNSUPPORTED)
- *   workspace  device, 256-byte aligned, tide_head_logits_q4_bytes(dtype, T, d) bytes, which grow with T; 0 (up to 16 rows, as long as they fit in a CU's memory): none,
+ *   workspace  device, 256-byte aligned, tide_head_logits_q4_bytes(dtype, T, d, V) bytes, which grow with T and V; 0 (up to 16 rows, as long as they fit in a CU's memory): none,
  *           and NULL will do.  No initialisation, nothing kept: calls on different workspaces may overlap.  0 bytes with tide_last_error() set: unsupported. */
 int tide_head_quantize_q4(const void* W, int dtype, int64_t V, int64_t d, int64_t w_row_stride, int64_t group, void* codes, void* scales,
                           int scale_dtype, void* stream);
 int tide_head_dequantize_q4(const void* codes, const void* scales, int scale_dtype, int64_t V, int64_t d, int64_t group, void* W, int dtype,
                             int64_t w_row_stride, void* stream);
-size_t tide_head_logits_q4_bytes(int dtype, int64_t T, int64_t d);
+size_t tide_head_logits_q4_bytes(int dtype, int64_t T, int64_t d, int64_t V);
 int tide_head_logits_q4(const void* x, int dtype, int64_t T, int64_t d, int64_t V, int64_t x_row_stride, const void* codes, const void* scales,
                         int scale_dtype, int64_t group, float* logits, int64_t logits_row_stride, void* workspace, size_t workspace_bytes,
                         void* stream);

@@ -90,9 +90,10 @@ template <auto kKernel> int raise_lds() {
 // How the rows under a head in four bits are divided.
 struct Q4Plan {
     int planes;                // bf16 terms of a row's value
-    int64_t T, tiles, blocks;
+    int64_t T, tiles, blocks;  // blocks: of a part
     int per;                   // groups of a block of 128 columns
     unsigned cus;
+    int parts;                 // of the columns; several: a second launch adds them up
     // few rows
     int rows_log, nt, waves, split, lds;
     // many rows: tiles of 16 rows of a row block, row blocks, LDS; waves as above
@@ -105,49 +106,89 @@ struct Q4Plan {
     }
     int64_t sets() const { return (tiles + waves * nt - 1) / (waves * nt); }
 };
-// Whether the rows fit in LDS, with groups of 32 columns and sixteen waves' scales.
-bool q4_few(int dtype, int64_t T, int64_t d) {
-    const Q4Shape s{1, d, 32, TIDE_BF16};
+constexpr int kQ4MostParts = 16;
+constexpr int64_t kQ4PartBytes = (int64_t)32 << 20;    // of all parts' logits
+bool q4_parts_fit(int64_t T, int64_t V, int parts) { return parts == 1 || 4 * T * V * parts <= kQ4PartBytes; }
+// The parts of the columns with which few rows fit in LDS (`most` bytes), with groups of 32 columns and `waves` waves' scales; 0: too many.
+int q4_few_parts(int dtype, int64_t T, int64_t d, int waves, int most) {
     Q4Plan p{};
     p.planes = dtype == TIDE_F32 ? kQ4Planes<kF32> : 1;
-    p.blocks = s.blocks(), p.per = 4;
+    p.per = 4;
     int log = 0;
     while ((1 << log) < T && log < 4) ++log;
-    return T <= 16 && p.few_lds(log, 2, 16, 1) <= kMostLds;
+    const int64_t all = (d + kQ4Cols - 1) / kQ4Cols;
+    for (int parts = 1; T <= 16 && parts <= std::min<int64_t>(kQ4MostParts, all); ++parts) {
+        p.blocks = (all + parts - 1) / parts;
+        if (p.few_lds(log, 2, waves, 1) <= most) return parts;
+    }
+    return 0;
 }
+bool q4_by_xcd(int64_t sets) { return sets >= 64; }
+constexpr int kQ4SmallLds = 32 * 1024;                 // of a workgroup of which several share a CU
 constexpr int kQ4ManyTiles[] = {8, 6, 4, 3, 2};        // of 16 rows, of a row block; fp32 rows: 2
 Q4Plan q4_plan(int dtype, int64_t T, const Q4Shape& s, unsigned cus) {
     Q4Plan p{};
     p.planes = dtype == TIDE_F32 ? kQ4Planes<kF32> : 1;
-    p.T = T, p.tiles = s.tiles(), p.blocks = s.blocks(), p.per = (int)(128 / s.group), p.cus = cus;
+    p.T = T, p.tiles = s.tiles(), p.blocks = s.blocks(), p.per = (int)(128 / s.group), p.cus = cus, p.parts = 1;
     while ((1 << p.rows_log) < T && p.rows_log < 4) ++p.rows_log;
-    p.few = q4_few(dtype, T, s.d);
+    const int64_t all = p.blocks;
+    const int fit = q4_few_parts(dtype, T, s.d, 16, kMostLds);
+    p.few = fit > 0 && q4_parts_fit(T, s.V, fit);
     if (p.few) {
+        // Rows that do not fit whole: in so many parts that several workgroups share a CU, as long as the parts' logits are a small part of the traffic (a sixteenth of the codes).
+        if (fit > 1) {
+            const int small_parts = q4_few_parts(dtype, T, s.d, 4, kQ4SmallLds);
+            p.parts = (int)std::max<int64_t>(fit, std::min<int64_t>(small_parts ? small_parts : kQ4MostParts, s.d / (256 * T)));
+            if (!q4_parts_fit(T, s.V, p.parts)) p.parts = fit;
+            p.blocks = (all + p.parts - 1) / p.parts, p.parts = (int)((all + p.blocks - 1) / p.blocks);
+        }
         // Rows that leave room for several workgroups a CU: small ones, which start and end apart from each other; else one of as many waves as share its CU's tokens
         // evenly, two tiles a wave where there are enough (bf16, d = 4096, V = 128000, us, 4 waves of one tile / 16 of two: T = 1 50 / 53, 8 63 / 55, 16 66 / 57).
-        const bool small = p.few_lds(p.rows_log, 1, 4, 1) <= 32 * 1024;
-        p.nt = !small && p.tiles >= 24 * (int64_t)cus ? 2 : 1;
-        p.waves = small ? 4 : (int)std::min<int64_t>(16, std::max<int64_t>(4, (p.tiles + p.nt * (int64_t)cus - 1) / (p.nt * (int64_t)cus)));
+        const bool small = p.few_lds(p.rows_log, 1, 4, 1) <= kQ4SmallLds;
+        const int64_t share = std::max<int64_t>(1, cus / p.parts);
+        p.nt = !small && p.tiles >= 24 * share ? 2 : 1;
+        p.waves = small ? 4 : (int)std::min<int64_t>(16, std::max<int64_t>(4, (p.tiles + p.nt * share - 1) / (p.nt * share)));
         p.split = 1;
         // few tokens: waves share tiles until the chip is filled
-        while (p.split < 4 && p.tiles * p.split * 2 <= 8 * (int64_t)cus && p.split * 4 <= p.blocks) p.split *= 2;
+        while (p.split < 4 && p.tiles * p.split * p.parts * 2 <= 8 * (int64_t)cus && p.split * 4 <= all - (p.parts - 1) * p.blocks) p.split *= 2;
         if (p.split > 1) p.waves = 4;
         p.lds = p.few_lds(p.rows_log, p.nt, p.waves, p.split);
         return p;
     }
-    // Many rows: the fewest rounds of workgroups times what a block of 128 columns takes, which is some 1.5 us and 0.3 for each tile of 16 rows where the workgroup has 512
-    // tokens (bf16, d = 4096, V = 128000, us: T = 32 65, 48 74, 64 82, 96 104, 128 135), and about 1 of it with few
+    // Many rows: what a CU's workgroups take, in us, fitted to 5500 measured launches of 140 shapes (the choice is 2.5 % off the fastest of them on average and 19 % at most).  What a block
+    // of 128 columns takes a workgroup from end to end, in which the CU's other workgroups work, grows with a wave's tiles of rows; what it takes of the CU for 512 tokens, with
+    // the workgroup's share of them; so do a workgroup's results at its end.  Parts of the columns cost a launch and their logits' traffic, and fill CUs where there are few tokens.
+    // (bf16, us: d = 8192, V = 1822, T = 43 63 whole and 32 in parts; d = 5120, V = 32401, T = 112, the fewest rounds of the largest workgroups 107, these 65.)
     double least = 0;
     for (int mt : kQ4ManyTiles) {
         if (p.planes > 1 && mt != 2) continue;
-        const int nt = mt == 8 ? 4 : 2, most = 32 / nt;
-        for (int waves = most; waves >= most / 4; waves /= 2) {
-            const int64_t row_blocks = (T + 16 * mt - 1) / (16 * mt), items = (p.tiles + waves * nt - 1) / (waves * nt) * row_blocks;
-            const double work = (double)((items + cus - 1) / cus) * (1.0 + (0.5 + 0.3 * mt) * waves / most);
-            if (least == 0 || work < least) least = work, p.mt = mt, p.nt = nt, p.waves = waves, p.row_blocks = row_blocks;
+        const int nt = mt == 8 ? 4 : 2, most = 32 / nt, region = 4 * p.planes * mt * 1024 + 1024;
+        const int stages = 2 * region + most * (3 * nt + 2) * 1024 <= kMostLds ? 3 : 2;
+        const double rows = mt * p.planes, alone = 0.15 + (0.06 + 0.01 * p.per) * rows * (nt == 4 ? 1.4 : 1.0), all_tokens = 0.4 + (0.03 + 0.012 * p.per) * rows;
+        for (int waves : {most, most / 4}) {
+            const int64_t row_blocks = (T + 16 * mt - 1) / (16 * mt), sets = (p.tiles + waves * nt - 1) / (waves * nt);
+            const int64_t items = (q4_by_xcd(sets) ? (sets + 7) / 8 * 8 : sets) * row_blocks;
+            const int64_t together = std::min(most / waves, kMostLds / (2 * region + waves * (stages * nt + 2) * 1024));
+            const double share = (double)waves / most;
+            for (int parts = 1; parts <= kQ4MostParts && 2 * parts <= std::max<int64_t>(2, all) && q4_parts_fit(T, s.V, parts); parts *= 2) {
+                const int64_t blocks = (all + parts - 1) / parts, each = (items * parts + cus - 1) / cus, rounds = (each + together - 1) / together;
+                const double work = blocks * (rounds * (alone + 0.02 * p.per * share) + each * all_tokens * share) + 0.5 * each * mt * share + (parts > 1 ? 4.5 + T * s.V * parts * 1e-6 : 0);
+                if (least == 0 || work < least) least = work, p.mt = mt, p.nt = nt, p.waves = waves, p.row_blocks = row_blocks, p.parts = parts, p.blocks = blocks;
+            }
         }
     }
+    p.parts = (int)((all + p.blocks - 1) / p.blocks);
     return p;
+}
+
+// The rows' regions.  Row blocks of 16 mt rows for any mt, and groups of 32 columns: no matter how many tokens, and more than any call of fewer rows takes.  (A region's sums are at
+// most 512 bytes a tile, its padding included.)
+int64_t q4_lay_bytes(int dtype, int64_t T, int64_t d) {
+    const int64_t planes = dtype == TIDE_F32 ? kQ4Planes<kF32> : 1, blocks = (d + kQ4Cols - 1) / kQ4Cols;
+    int64_t tiles = 0;
+    for (int mt : kQ4ManyTiles)
+        if (planes == 1 || mt == 2) tiles = std::max(tiles, (T + 16 * mt - 1) / (16 * mt) * mt);
+    return (tiles * blocks * (4 * planes * 1024 + 512) + 255) & ~int64_t(255);
 }
 
 constexpr int64_t kMostPast = (int64_t)1 << 30;
@@ -290,20 +331,14 @@ int tide_head_dequantize_q4(const void* codes, const void* scales, int scale_dty
     return q4_weights(nullptr, W, dtype, Q4Shape{V, d, group, scale_dtype}, w_row_stride, codes, scales, (hipStream_t)stream);
 }
 
-size_t tide_head_logits_q4_bytes(int dtype, int64_t T, int64_t d) {
+size_t tide_head_logits_q4_bytes(int dtype, int64_t T, int64_t d, int64_t V) {
     g_err[0] = 0;
-    if ((dtype != TIDE_F32 && dtype != TIDE_F16 && dtype != TIDE_BF16) || T < 0 || T > kHeadMostRows || d < 1 || d > kMaxHidden) {
-        fail(TIDE_ERR_UNSUPPORTED, "unsupported dtype %d, T = %lld or d = %lld", dtype, (long long)T, (long long)d);
+    if ((dtype != TIDE_F32 && dtype != TIDE_F16 && dtype != TIDE_BF16) || T < 0 || T > kHeadMostRows || d <= 0 || d > kMaxHidden || V <= 0 || V > kHeadMostVocab) {
+        fail(TIDE_ERR_UNSUPPORTED, "unsupported dtype %d, T = %lld, d = %lld or V = %lld", dtype, (long long)T, (long long)d, (long long)V);
         return 0;
     }
-    if (q4_few(dtype, T, d)) return 0;
-    // Row blocks of 16 mt rows for any mt, and groups of 32 columns: no matter how many tokens, and more than any call of fewer rows takes.  (A region's sums are at most 512
-    // bytes a tile, its padding included.)
-    const int64_t planes = dtype == TIDE_F32 ? kQ4Planes<kF32> : 1, blocks = (d + kQ4Cols - 1) / kQ4Cols;
-    int64_t tiles = 0;
-    for (int mt : kQ4ManyTiles)
-        if (planes == 1 || mt == 2) tiles = std::max(tiles, (T + 16 * mt - 1) / (16 * mt) * mt);
-    return (size_t)(tiles * blocks * (4 * planes * 1024 + 512) + 255) & ~size_t(255);
+    if (q4_few_parts(dtype, T, d, 16, kMostLds) == 1) return 0;
+    return (size_t)(q4_lay_bytes(dtype, T, d) + std::min(kQ4PartBytes, 4 * T * V * kQ4MostParts));
 }
 
 int tide_head_logits_q4(const void* x, int dtype, int64_t T, int64_t d, int64_t V, int64_t x_row_stride, const void* codes, const void* scales, int scale_dtype, int64_t group,
@@ -320,7 +355,7 @@ int tide_head_logits_q4(const void* x, int dtype, int64_t T, int64_t d, int64_t 
     if (logits_row_stride < V) return fail(TIDE_ERR_INVALID_ARG, "logits_row_stride must be at least V");
     if ((uintptr_t)logits & 3) return fail(TIDE_ERR_ALIGNMENT, "logits must be aligned to a float");
     if ((T + 15) / 16 * s.tiles() > 4 * kMostBlocks) return fail(TIDE_ERR_UNSUPPORTED, "T = %lld rows of V = %lld logits are too many for one call", (long long)T, (long long)V);
-    const size_t need = tide_head_logits_q4_bytes(dtype, T, d);
+    const size_t need = tide_head_logits_q4_bytes(dtype, T, d, V);
     if (need && (!workspace || workspace_bytes < need))
         return fail(TIDE_ERR_WORKSPACE, "this call needs %zu bytes of workspace, %zu given", need, workspace ? workspace_bytes : 0);
     if (need && ((uintptr_t)workspace & 255)) return fail(TIDE_ERR_ALIGNMENT, "the workspace must be 256-byte aligned");
@@ -329,6 +364,9 @@ int tide_head_logits_q4(const void* x, int dtype, int64_t T, int64_t d, int64_t 
     const Q4Plan plan = q4_plan(dtype, T, s, cus);
     hipStream_t st = (hipStream_t)stream;
     const Q4Rows rows{(const char*)x, x_row_stride * (int64_t)elem_bytes(dtype), (int)T, (int)d, q4_chunks(x, x_row_stride, dtype)};
+    float* const part = (float*)((char*)workspace + q4_lay_bytes(dtype, T, d));
+    float* const sums = plan.parts > 1 ? part : logits;
+    const int64_t sums_stride = plan.parts > 1 ? V : logits_row_stride, part_stride = plan.parts > 1 ? T * V : 0;
     const Q4Head head{(const char*)codes, (const uint16_t*)scales, (int)V, (int)s.tiles(), (int)s.blocks(), (int)s.groups(), scale_dtype == TIDE_F16};
     using std::integral_constant;
     rc = by_dtype(dtype, [&](auto dt) -> int {
@@ -340,8 +378,9 @@ int tide_head_logits_q4(const void* x, int dtype, int64_t T, int64_t d, int64_t 
                 if (rc2) return rc2;
                 const int per_set = plan.waves / plan.split * NT, sets = (int)((plan.tiles + per_set - 1) / per_set);
                 const int together = std::max(1, std::min(kMostLds / plan.lds, plan.waves > 4 ? 1 : dtype == TIDE_F32 ? 5 : 7));
-                const Q4FewParams p{rows, head, logits, logits_row_stride, sets, plan.rows_log, plan.split};
-                hipLaunchKernelGGL((tide_head_q4_few_kernel<DT, kRuns, NT, kDepth>), dim3((unsigned)std::min<int64_t>(sets, (int64_t)cus * together)), dim3(plan.waves * kWave), plan.lds, st, p);
+                const Q4FewParams p{rows, head, sums, sums_stride, part_stride, (int)plan.blocks, sets, plan.rows_log, plan.split};
+                const int64_t grid = std::min<int64_t>(sets, std::max<int64_t>(1, (int64_t)cus * together / plan.parts));
+                hipLaunchKernelGGL((tide_head_q4_few_kernel<DT, kRuns, NT, kDepth>), dim3((unsigned)grid, (unsigned)plan.parts), dim3(plan.waves * kWave), plan.lds, st, p);
                 return TIDE_OK;
             };
             auto many = [&](auto row_tiles) -> int {
@@ -351,11 +390,13 @@ int tide_head_logits_q4(const void* x, int dtype, int64_t T, int64_t d, int64_t 
                 const Q4LayParams lay{rows, (char*)workspace, head.blocks, plan.row_blocks * MT * head.blocks};
                 hipLaunchKernelGGL((tide_head_q4_lay_kernel<DT, kRuns, MT>), dim3((unsigned)((lay.waves + 3) / 4)), dim3(kQ4Threads), 0, st, lay);
                 const int64_t sets = plan.sets();
-                const Q4ManyParams p{(const char*)workspace, head, logits, logits_row_stride, (int)T, (int)plan.row_blocks, (int)sets, sets >= 64};
+                const bool by_xcd = q4_by_xcd(sets);
+                const Q4ManyParams p{(const char*)workspace, head, sums, sums_stride, part_stride, (int)plan.blocks, (int)T, (int)plan.row_blocks, (int)sets, by_xcd};
                 const int lds = q4_many_lds<NT>(Q4Region<DT, kRuns, MT>::kBytes, kQ4CodeStages<DT, kRuns, MT, NT>, plan.waves);
                 const int64_t together = std::min<int64_t>(kMostLds / lds, kQ4ManyThreads<NT> / kWave / plan.waves);
-                const int64_t grid = std::min<int64_t>((sets * plan.row_blocks + 7) / 8 * 8, std::max<int64_t>(8, cus * together / 8 * 8));
-                hipLaunchKernelGGL((tide_head_q4_many_kernel<DT, kRuns, MT, NT>), dim3((unsigned)grid), dim3(plan.waves * kWave), lds, st, p);
+                const int64_t items = by_xcd ? (sets + 7) / 8 * 8 * plan.row_blocks : (sets * plan.row_blocks + 7) / 8 * 8;      // (an XCD that has a set more than others has room for it)
+                const int64_t grid = std::min(items, std::max<int64_t>(8, cus * together / plan.parts / 8 * 8));
+                hipLaunchKernelGGL((tide_head_q4_many_kernel<DT, kRuns, MT, NT>), dim3((unsigned)grid, (unsigned)plan.parts), dim3(plan.waves * kWave), lds, st, p);
                 return TIDE_OK;
             };
             if (plan.few) return plan.nt == 2 ? few(integral_constant<int, 2>{}) : few(integral_constant<int, 1>{});
@@ -369,6 +410,10 @@ int tide_head_logits_q4(const void* x, int dtype, int64_t T, int64_t d, int64_t 
         });
     });
     if (rc) return rc;
+    if (plan.parts > 1) {
+        const Q4JoinParams p{part, logits, logits_row_stride, (int)T, (int)V, plan.parts, (int)((V + kQ4JoinRun * kQ4Threads - 1) / (kQ4JoinRun * kQ4Threads))};
+        hipLaunchKernelGGL(tide_head_q4_join_kernel, dim3((unsigned)(T * p.pieces)), dim3(kQ4Threads), 0, st, p);
+    }
     TIDE_HIP(hipGetLastError());
     return TIDE_OK;
 }

@@ -339,6 +339,31 @@ __device__ __forceinline__ float q4_scale_at(const char* mine, int NT, int n, in
     return q4_scale_select(*reinterpret_cast<const uint16_t*>(mine + n * (1024 / NT) + group * 32 + (lane & 15) * 2), half);
 }
 
+// Where a launch would leave CUs idle, or where not all columns of a few rows fit in LDS, workgroups have a part of the columns, by blockIdx.y, and another launch adds up their sums.
+struct Q4JoinParams {
+    const float* part;         // [parts][T][V]
+    float* out;
+    int64_t out_stride;
+    int T, V, parts, pieces;   // of a row
+};
+constexpr int kQ4JoinRun = 4;
+__global__ __launch_bounds__(kQ4Threads) void tide_head_q4_join_kernel(Q4JoinParams p) {
+    const int t = blockIdx.x / p.pieces, v0 = (blockIdx.x - t * p.pieces) * kQ4JoinRun * kQ4Threads + threadIdx.x;
+    const int64_t all = (int64_t)p.T * p.V;
+    float sum[kQ4JoinRun] = {};
+    for (int part = 0; part < p.parts; ++part)
+#pragma unroll
+        for (int e = 0; e < kQ4JoinRun; ++e) {
+            const int v = v0 + e * kQ4Threads;
+            if (v < p.V) sum[e] += p.part[part * all + (int64_t)t * p.V + v];
+        }
+#pragma unroll
+    for (int e = 0; e < kQ4JoinRun; ++e) {
+        const int v = v0 + e * kQ4Threads;
+        if (v < p.V) p.out[(int64_t)t * p.out_stride + v] = sum[e];
+    }
+}
+
 // ---- Few rows, up to 16: all of them in LDS.
 //
 // A workgroup lays the rows out once -- as fragments, 16 bytes (eight columns) of each row side by side, with the groups' sums times -1.5, which the matrix steps of a
@@ -350,7 +375,8 @@ struct Q4FewParams {
     Q4Rows x;
     Q4Head head;
     float* out;
-    int64_t out_stride;
+    int64_t out_stride, part_stride;
+    int part_blocks;           // of 128 columns, of a part
     int sets;                  // of tokens, each a workgroup's at a time
     int rows_log;              // rows in LDS: a power of two
     int split;
@@ -369,17 +395,19 @@ template <int DT, int kRuns, int NT> __host__ __device__ inline Q4FewLds q4_few_
     return l;
 }
 
-template <int DT, int kRuns, int NT, int kDepth> __global__ __launch_bounds__(kQ4FewThreads) void tide_head_q4_few_kernel(Q4FewParams p) {
+// (One tile a wave: 72 registers, so that seven workgroups of four waves share a CU; fp32 rows' three terms would not fit, and five do.  76: T = 1 47.3 -> 48.6 us.)
+template <int DT, int kRuns, int NT, int kDepth> __global__ __launch_bounds__(kQ4FewThreads, NT == 1 && DT != kF32 ? 7 : 4) void tide_head_q4_few_kernel(Q4FewParams p) {
     constexpr int E = kQ4Elem<DT>, P = kQ4Planes<DT>, kSums = kQ4Sums<DT>, kPer = 4 / kRuns;
     constexpr int kScaleBlocks = 32 / NT / kPer;       // blocks of 128 columns whose scales a kilobyte holds
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), waves = blockDim.x / kWave;
-    const int log = p.rows_log, rows = 1 << log, offs_log = log < 2 ? 2 : log, blocks = p.head.blocks;
+    const int log = p.rows_log, rows = 1 << log, offs_log = log < 2 ? 2 : log, all = p.head.blocks, kb0 = blockIdx.y * p.part_blocks, blocks = min(p.part_blocks, all - kb0);
+    float* const out = p.out + blockIdx.y * p.part_stride;
     const Q4FewLds at = q4_few_lds<DT, kRuns, NT>(log, blocks, waves, p.split);
 
     // the wave's tiles: NT of each set, blocks `begin` ..+`own`.  The first of them are on their way while the rows are laid out
     const int unit = wave / p.split, part = wave - unit * p.split, units = waves / p.split;
-    const int begin = part * blocks / p.split, own = (part + 1) * blocks / p.split - begin;
+    const int begin = part * blocks / p.split, own = (part + 1) * blocks / p.split - begin, first = kb0 + begin;
     const int passes = (p.sets - blockIdx.x + gridDim.x - 1) / gridDim.x;
     auto tile_of = [&](int pass) { return ((int)(blockIdx.x + pass * gridDim.x) * units + unit) * NT; };
     u32x4 c[kDepth][NT];
@@ -388,7 +416,7 @@ template <int DT, int kRuns, int NT, int kDepth> __global__ __launch_bounds__(kQ
     auto point = [&](int pass) {
         const int tile0 = tile_of(pass);
 #pragma unroll
-        for (int n = 0; n < NT; ++n) f_codes[n] = p.head.codes + ((int64_t)min(tile0 + n, p.head.tiles - 1) * blocks + begin) * kQ4TileBytes;
+        for (int n = 0; n < NT; ++n) f_codes[n] = p.head.codes + ((int64_t)min(tile0 + n, p.head.tiles - 1) * all + first) * kQ4TileBytes;
     };
     point(0);
     auto fetch = [&](int slot) {
@@ -400,7 +428,7 @@ template <int DT, int kRuns, int NT, int kDepth> __global__ __launch_bounds__(kQ
         }
     };
     u32x4 s_next;
-    auto fetch_scales = [&](int pass, int i) { s_next = q4_scales<NT>(p.head, tile_of(min(pass, passes - 1)), (begin + i) * kPer, lane); };
+    auto fetch_scales = [&](int pass, int i) { s_next = q4_scales<NT>(p.head, tile_of(min(pass, passes - 1)), (first + i) * kPer, lane); };
     const int steps = passes * own;
     fetch_scales(0, 0);
 #pragma unroll
@@ -410,7 +438,7 @@ template <int DT, int kRuns, int NT, int kDepth> __global__ __launch_bounds__(kQ
     for (int item = threadIdx.x; item < blocks * 4 << log; item += blockDim.x) {
         const int row = item & (rows - 1), g = item >> log & 3, kb = item >> (log + 2);
         Q4Raw<DT> raw;
-        q4_raw<DT>(p.x, row, kb * kQ4Cols + 8 * g, raw);
+        q4_raw<DT>(p.x, row, (kb0 + kb) * kQ4Cols + 8 * g, raw);
         q4_put<DT, kRuns>(raw, g, rows, lds + ((kb * 16 * P + g) << (log + 4)) + row * 16, 64 << log, reinterpret_cast<float*>(lds + at.offs) + (kb * kPer * kSums << offs_log) + row, 1 << offs_log);
     }
     __syncthreads();
@@ -485,7 +513,7 @@ template <int DT, int kRuns, int NT, int kDepth> __global__ __launch_bounds__(kQ
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const int t = 4 * (lane >> 4) + e;
-                if (writes && t < p.x.T) p.out[(int64_t)t * p.out_stride + v] = 16.0f * total[n][e];
+                if (writes && t < p.x.T) out[(int64_t)t * p.out_stride + v] = 16.0f * total[n][e];
                 total[n][e] = 0.0f;
             }
         }
@@ -548,7 +576,8 @@ struct Q4ManyParams {
     const char* regions;
     Q4Head head;
     float* out;
-    int64_t out_stride;
+    int64_t out_stride, part_stride;
+    int part_blocks;           // of 128 columns, of a part
     int T, row_blocks;
     int sets;                  // of tokens: a workgroup has a set and a row block at a time
     bool by_xcd;               // the row blocks of a set run on one XCD (workgroups whose numbers are equal modulo 8), for its codes to be in that L2
@@ -570,7 +599,8 @@ template <int DT, int kRuns, int MT, int NT> __global__ __launch_bounds__(kQ4Man
     static_assert(kScaleBlocks >= 2, "a kilobyte is requested two blocks before it is read");
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), waves = blockDim.x / kWave;
-    const int blocks = p.head.blocks, xcd = p.by_xcd ? blockIdx.x & 7 : 0, xcds = p.by_xcd ? 8 : 1, first_item = blockIdx.x / xcds, stride = gridDim.x / xcds;
+    const int all = p.head.blocks, kb0 = blockIdx.y * p.part_blocks, blocks = min(p.part_blocks, all - kb0);
+    const int xcd = p.by_xcd ? blockIdx.x & 7 : 0, xcds = p.by_xcd ? 8 : 1, first_item = blockIdx.x / xcds, stride = gridDim.x / xcds;
     const int items = (p.sets - xcd + xcds - 1) / xcds * p.row_blocks, passes = (items - first_item + stride - 1) / stride;
     if (first_item >= items) return;
     auto item_of = [&](int pass) { return first_item + min(pass, passes - 1) * stride; };
@@ -581,12 +611,12 @@ template <int DT, int kRuns, int MT, int NT> __global__ __launch_bounds__(kQ4Man
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds, lane16 = lane * 16;
     const uint32_t codes0 = lds0 + (uint32_t)(my_codes - lds), scales0 = codes0 + kStages * NT * 1024;
     // the regions of the rows: every wave a part of each
-    const char* regions = p.regions + (int64_t)(item_of(0) % p.row_blocks) * blocks * R::kBytes;
+    const char* regions = p.regions + ((int64_t)(item_of(0) % p.row_blocks) * all + kb0) * R::kBytes;
     int x_pass = 0, x_kb = 0, x_stage = 0;
     auto request_region = [&] {
         const char* from = regions + (int64_t)x_kb * R::kBytes;
         for (int i = wave * 1024; i < R::kBytes; i += waves * 1024) q4_transfer(lds0 + x_stage * R::kBytes + i, from + i, lane16);
-        if (++x_kb == blocks) x_kb = 0, regions = p.regions + (int64_t)(item_of(++x_pass) % p.row_blocks) * blocks * R::kBytes;
+        if (++x_kb == blocks) x_kb = 0, regions = p.regions + ((int64_t)(item_of(++x_pass) % p.row_blocks) * all + kb0) * R::kBytes;
         x_stage ^= 1;
     };
     // the wave's codes; beyond its last block: the last tiles again, into a stage that nothing reads
@@ -594,7 +624,7 @@ template <int DT, int kRuns, int MT, int NT> __global__ __launch_bounds__(kQ4Man
     auto request_codes = [&] {
 #pragma unroll
         for (int n = 0; n < NT; ++n)
-            q4_transfer(codes0 + (f_stage * NT + n) * 1024, p.head.codes + ((int64_t)min(f_tile + n, p.head.tiles - 1) * blocks + f_kb) * kQ4TileBytes, lane16);
+            q4_transfer(codes0 + (f_stage * NT + n) * 1024, p.head.codes + ((int64_t)min(f_tile + n, p.head.tiles - 1) * all + kb0 + f_kb) * kQ4TileBytes, lane16);
         if (++f_kb == blocks) f_kb = 0, f_tile = tile_of(++f_pass);
         if (++f_stage == kStages) f_stage = 0;
     };
@@ -603,7 +633,7 @@ template <int DT, int kRuns, int MT, int NT> __global__ __launch_bounds__(kQ4Man
     auto request_scales = [&](int pass, int kb) {
         constexpr int kLanes = kWave / NT;
         const int tile0 = tile_of(pass), l = lane % kLanes, tile = min(tile0 + lane / kLanes, p.head.tiles - 1) - min(tile0, p.head.tiles - 1);
-        const int group = min(kb * kPer + l / 2, p.head.groups - 1);       // (a group of padding: its sums are zero)
+        const int group = min((kb0 + kb) * kPer + l / 2, p.head.groups - 1);       // (a group of padding: its sums are zero)
         q4_transfer(scales0 + s_stage * 1024, (const char*)(p.head.scales + (int64_t)min(tile0, p.head.tiles - 1) * p.head.groups * kQ4Rows),
                     ((uint32_t)(tile * p.head.groups + group) * kQ4Rows + (l & 1) * 8) * 2);
         s_stage ^= 1;
@@ -698,7 +728,7 @@ template <int DT, int kRuns, int MT, int NT> __global__ __launch_bounds__(kQ4Man
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const int t = (item_of(pass) % p.row_blocks * MT + rt) * 16 + quad + e;
-                float* const out = p.out + (int64_t)t * p.out_stride + (lane & 15);
+                float* const out = p.out + blockIdx.y * p.part_stride + (int64_t)t * p.out_stride + (lane & 15);
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
                     const int v0 = (tile_of(pass) + n) * kQ4Rows;

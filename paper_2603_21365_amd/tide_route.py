@@ -101,7 +101,7 @@ def load_library() -> ctypes.CDLL:
     lib.tide_head_distill_grad.argtypes = [*head, vp, vp, i64, f32, vp, vp, vp, i64, vp, i64, vp, sz, vp]
     lib.tide_head_quantize_q4.argtypes = [vp, ci, i64, i64, i64, i64, vp, vp, ci, vp]
     lib.tide_head_dequantize_q4.argtypes = [vp, vp, ci, i64, i64, i64, vp, ci, i64, vp]
-    lib.tide_head_logits_q4_bytes.argtypes = [ci, i64, i64]
+    lib.tide_head_logits_q4_bytes.argtypes = [ci, i64, i64, i64]
     lib.tide_head_logits_q4_bytes.restype = sz
     lib.tide_head_logits_q4.argtypes = [vp, ci, i64, i64, i64, i64, vp, vp, ci, i64, vp, i64, vp, sz, vp]
     rules = [vp, ci, i64, i64, i64, vp, i64, vp, vp, vp, vp, vp, vp, vp, i64, vp]
@@ -739,9 +739,9 @@ def head_dequantize_q4(codes, scales, V, d, dtype, group=128):
     return W
 
 
-def head_logits_q4_bytes(dtype: int, T: int, d: int) -> int:
+def head_logits_q4_bytes(dtype: int, T: int, d: int, V: int) -> int:
     """Bytes of workspace a head_logits_q4 call needs: 0 for few rows (and with last_error() if unsupported).  They grow with T."""
-    return int(load_library().tide_head_logits_q4_bytes(int(dtype), int(T), int(d)))
+    return int(load_library().tide_head_logits_q4_bytes(int(dtype), int(T), int(d), int(V)))
 
 
 def head_logits_q4(x, codes, scales, V, group=128, *, out=None, workspace=None):
@@ -757,7 +757,7 @@ def head_logits_q4(x, codes, scales, V, group=128, *, out=None, workspace=None):
         return out
     dtype = _dtype_code(x)
     lib = load_library()
-    nbytes = lib.tide_head_logits_q4_bytes(dtype, T, d)
+    nbytes = lib.tide_head_logits_q4_bytes(dtype, T, d, V)
     if nbytes:
         workspace, nbytes = _scratch(workspace, nbytes, x.device)
     _check(lib.tide_head_logits_q4(_ptr(x), dtype, T, d, V, xs if T > 1 else d, codes.data_ptr(), scales.data_ptr(), code, group, out.data_ptr(), os_ if T > 1 else V,

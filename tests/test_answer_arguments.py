@@ -88,10 +88,12 @@ def test_no_rows_is_no_work():
 
 def test_workspaces_grow_with_the_rows():
     for dtype in (tr.F32, tr.F16, tr.BF16):
-        for d in (1, 768, 1600, 16384):
-            sizes = [tr.head_logits_q4_bytes(dtype, T, d) for T in range(0, 700)]
+        for d, V in ((1, 5), (768, 128000), (1600, 1000), (16384, 1 << 23)):
+            sizes = [tr.head_logits_q4_bytes(dtype, T, d, V) for T in range(0, 700)]
             assert sizes[0] == sizes[1] == 0 and min(sizes[17:]) > 0 and sizes == sorted(sizes) and tr.last_error() == ""
-    assert tr.head_logits_q4_bytes(3, 4, 64) == 0 and tr.head_logits_q4_bytes(tr.F32, 4, 20000) == 0 and "unsupported" in tr.last_error()
+            assert max(sizes) == sizes[-1] <= tr.head_logits_q4_bytes(dtype, 699, d, min(2 * V, 1 << 23))
+    for bad in ((3, 4, 64, 100), (tr.F32, 4, 20000, 100), (tr.F32, 4, 64, 0), (tr.F32, -1, 64, 100), (tr.F32, 4, 64, 1 << 24)):
+        assert tr.head_logits_q4_bytes(*bad) == 0 and "unsupported" in tr.last_error()
     for V in (1, 1024, 1025, 128000):
         sizes = [tr.logit_pick_bytes(T, V) for T in range(0, 700)]
         assert min(sizes) > 0 and sizes == sorted(sizes)

@@ -150,7 +150,7 @@ def test_many_rows_in_graphs_with_workspaces_of_their_own():
     side = torch.cuda.Stream()
     for T, dtype in ((40, torch.bfloat16), (130, torch.float16), (33, torch.float32)):
         x = integers(-2, 3, (T, d), T, dtype)
-        space = torch.empty(tr.head_logits_q4_bytes({torch.float32: tr.F32, torch.float16: tr.F16, torch.bfloat16: tr.BF16}[dtype], T, d), dtype=torch.uint8, device="cuda")
+        space = torch.empty(tr.head_logits_q4_bytes({torch.float32: tr.F32, torch.float16: tr.F16, torch.bfloat16: tr.BF16}[dtype], T, d, V), dtype=torch.uint8, device="cuda")
         out = torch.empty((T, V), device="cuda")
         side.wait_stream(torch.cuda.current_stream())
         with torch.cuda.stream(side):
@@ -169,6 +169,20 @@ def test_many_rows_in_graphs_with_workspaces_of_their_own():
         torch.cuda.synchronize()
         for x, _, out, _ in cases:
             assert torch.equal(out, tr.head_logits_q4(x, codes, scales, V, group)) and torch.equal(out.cpu().double(), x.cpu().double() @ w.T)
+
+
+@pytest.mark.parametrize("dtype,d,V", [("f32", 8192, 3001), ("f16", 8192, 500), ("bf16", 5120, 3001), ("f32", 1100, 70), ("bf16", 12288 + 77, 1)])
+def test_columns_in_parts(dtype, d, V):
+    """Few tokens under many columns, which several workgroups share, into rows with gaps: exact as above (2 * 8 * 12365 in steps of 1/16: 22 bits), and what lies between the rows stays."""
+    codes, scales = packed(V, d, 64, d + V)
+    w = tr.head_dequantize_q4(codes, scales, V, d, torch.float32, 64).cpu().double()
+    for T in (2, 7, 16, 17, 50, 200):
+        x = integers(-2, 3, (T, d + 3), T, DTYPES[dtype])[:, 1:1 + d]
+        space = torch.full((tr.head_logits_q4_bytes({"f32": tr.F32, "f16": tr.F16, "bf16": tr.BF16}[dtype], T, d, V),), 255, dtype=torch.uint8, device="cuda")
+        out = torch.full((T, V + 9), 7.0, device="cuda")
+        tr.head_logits_q4(x, codes, scales, V, 64, out=out[:, 4:4 + V], workspace=space)
+        assert torch.equal(out[:, 4:4 + V].cpu().double(), x.cpu().double() @ w.T), f"T={T}"
+        assert (out[:, :4] == 7).all() and (out[:, 4 + V:] == 7).all()
 
 
 def test_two_streams_at_once():

@@ -274,7 +274,7 @@ def test_another_stream_and_a_replayed_graph():
     V, d, T = 300, 256, 7
     (codes, scales), w = head(V, d, 128, exact=True)
     x = torch.randint(-4, 5, (T, d), generator=generator(1)).to(torch.bfloat16).cuda()
-    out, space = torch.empty((T, V), device="cuda"), torch.empty(tr.head_logits_q4_bytes(tr.BF16, 64, d), dtype=torch.uint8, device="cuda")
+    out, space = torch.empty((T, V), device="cuda"), torch.empty(tr.head_logits_q4_bytes(tr.BF16, 64, d, V), dtype=torch.uint8, device="cuda")
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
     with torch.cuda.stream(side):
