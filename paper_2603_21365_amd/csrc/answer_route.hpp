@@ -193,16 +193,20 @@ int64_t q4_lay_bytes(int dtype, int64_t T, int64_t d) {
 
 constexpr int64_t kMostPast = (int64_t)1 << 30;
 constexpr int64_t kMostBias = kRuleThreads;            // a thread each
+constexpr int kRuleOneSlice = 24576;
 constexpr int kRuleMostSlice = 32768;                 // 64 KiB of counts: two workgroups a CU
 
-// Slices of a row: as few as leave every CU two workgroups, of whole rounds of the workgroup's threads.
+// Slices of a row: as few as leave every CU two workgroups, of whole rounds of the workgroup's threads.  One where it spares the pick its second launch and is not the longer for it (us,
+// 44 rows in fp32: 16000 tokens, pasts of 500 14.3 -> 12.1; 24000, pasts of 8000, 300 biases 15.1 -> 14.5; 32000 of these 15.1 -> 16.1).
 struct RuleShape {
     int dtype;
     int64_t T, V, H;
+    bool pick;
     unsigned cus = 256;
     bool wide() const { return H >= 32768; }           // counts beyond 16 bits
     int slice() const {
         const int64_t round = 16 / (int64_t)elem_bytes(dtype) * kRuleThreads, most = wide() ? kRuleMostSlice / 2 : kRuleMostSlice;
+        if (pick && V <= std::min<int64_t>(kRuleOneSlice, most)) return (int)((V + 127) / 128 * 128);
         const int64_t slices = std::max<int64_t>((V + most - 1) / most, std::min<int64_t>((2 * (int64_t)cus + T - 1) / T, (V + round - 1) / round));
         return (int)(((V + slices - 1) / slices + 127) / 128 * 128);
     }
@@ -269,7 +273,7 @@ int check_rules(const RuleCall& c, bool pick) {
 int run_rules(const RuleCall& c, bool pick) {
     int rc = check_rules(c, pick);
     if (rc || c.T == 0) return rc;
-    RuleShape s{c.dtype, c.T, c.V, c.H};
+    RuleShape s{c.dtype, c.T, c.V, c.H, pick};
     if ((rc = resident_cus(&s.cus))) return rc;
     const int64_t slices = s.slices(), blocks = c.T * slices;
     if (blocks > kMostBlocks / 4) return fail(TIDE_ERR_UNSUPPORTED, "T = %lld rows of V = %lld logits are too many for one call", (long long)c.T, (long long)c.V);
@@ -364,8 +368,7 @@ int tide_head_logits_q4(const void* x, int dtype, int64_t T, int64_t d, int64_t 
     const Q4Plan plan = q4_plan(dtype, T, s, cus);
     hipStream_t st = (hipStream_t)stream;
     const Q4Rows rows{(const char*)x, x_row_stride * (int64_t)elem_bytes(dtype), (int)T, (int)d, q4_chunks(x, x_row_stride, dtype)};
-    float* const part = (float*)((char*)workspace + q4_lay_bytes(dtype, T, d));
-    float* const sums = plan.parts > 1 ? part : logits;
+    float* const sums = plan.parts > 1 ? (float*)((char*)workspace + q4_lay_bytes(dtype, T, d)) : logits;
     const int64_t sums_stride = plan.parts > 1 ? V : logits_row_stride, part_stride = plan.parts > 1 ? T * V : 0;
     const Q4Head head{(const char*)codes, (const uint16_t*)scales, (int)V, (int)s.tiles(), (int)s.blocks(), (int)s.groups(), scale_dtype == TIDE_F16};
     using std::integral_constant;
@@ -377,6 +380,7 @@ int tide_head_logits_q4(const void* x, int dtype, int64_t T, int64_t d, int64_t 
                 int rc2 = raise_lds<&tide_head_q4_few_kernel<DT, kRuns, NT, kDepth>>();
                 if (rc2) return rc2;
                 const int per_set = plan.waves / plan.split * NT, sets = (int)((plan.tiles + per_set - 1) / per_set);
+                // (as many as LDS and registers have room for)
                 const int together = std::max(1, std::min(kMostLds / plan.lds, plan.waves > 4 ? 1 : dtype == TIDE_F32 ? 5 : 7));
                 const Q4FewParams p{rows, head, sums, sums_stride, part_stride, (int)plan.blocks, sets, plan.rows_log, plan.split};
                 const int64_t grid = std::min<int64_t>(sets, std::max<int64_t>(1, (int64_t)cus * together / plan.parts));
@@ -411,7 +415,7 @@ int tide_head_logits_q4(const void* x, int dtype, int64_t T, int64_t d, int64_t 
     });
     if (rc) return rc;
     if (plan.parts > 1) {
-        const Q4JoinParams p{part, logits, logits_row_stride, (int)T, (int)V, plan.parts, (int)((V + kQ4JoinRun * kQ4Threads - 1) / (kQ4JoinRun * kQ4Threads))};
+        const Q4JoinParams p{sums, logits, logits_row_stride, (int)T, (int)V, plan.parts, (int)((V + kQ4JoinRun * kQ4Threads - 1) / (kQ4JoinRun * kQ4Threads))};
         hipLaunchKernelGGL(tide_head_q4_join_kernel, dim3((unsigned)(T * p.pieces)), dim3(kQ4Threads), 0, st, p);
     }
     TIDE_HIP(hipGetLastError());
