@@ -441,6 +441,7 @@ size_t tide_logit_pick_bytes(int64_t T, int64_t V) {
         fail(TIDE_ERR_UNSUPPORTED, "unsupported T = %lld or V = %lld", (long long)T, (long long)V);
         return 0;
     }
+    if (V <= kRuleMostSlice / 2) return 0;             // one slice, however long the past
     return (size_t)std::max<int64_t>(T, 1) * ((V + 1023) / 1024) * sizeof(uint4);
 }
 

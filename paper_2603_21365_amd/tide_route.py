@@ -809,7 +809,7 @@ def logit_rules(logits, *, past=None, past_len=None, prompt_len=None, repetition
 
 
 def logit_pick_bytes(T: int, V: int) -> int:
-    """Bytes of workspace a logit_pick call needs (0 and last_error() if unsupported).  They grow with T."""
+    """Bytes of workspace a logit_pick call needs: 0 for up to 16384 tokens (and with last_error() if unsupported).  They grow with T."""
     return int(load_library().tide_logit_pick_bytes(int(T), int(V)))
 
 
@@ -819,8 +819,11 @@ def logit_pick(logits, *, past=None, past_len=None, prompt_len=None, repetition=
     T, V, args = _rule_args(logits, past, past_len, prompt_len, repetition, presence, frequency, bias_ids, bias_values, allowed)
     token = torch.empty(T, dtype=torch.int32, device=logits.device)
     log_prob = torch.empty(T, dtype=torch.float32, device=logits.device)
-    workspace, nbytes = _scratch(workspace, logit_pick_bytes(T, V), logits.device)
-    _check(load_library().tide_logit_pick(*args, _ptr(token), _ptr(log_prob), _ptr(workspace), nbytes, _stream_on(logits.device)))
+    lib = load_library()
+    nbytes = lib.tide_logit_pick_bytes(T, V)
+    if nbytes:
+        workspace, nbytes = _scratch(workspace, nbytes, logits.device)
+    _check(lib.tide_logit_pick(*args, token.data_ptr(), log_prob.data_ptr(), _ptr(workspace) if nbytes else None, nbytes, _stream_on(logits.device)))
     return token, log_prob
 
 

@@ -94,10 +94,12 @@ def test_workspaces_grow_with_the_rows():
             assert max(sizes) == sizes[-1] <= tr.head_logits_q4_bytes(dtype, 699, d, min(2 * V, 1 << 23))
     for bad in ((3, 4, 64, 100), (tr.F32, 4, 20000, 100), (tr.F32, 4, 64, 0), (tr.F32, -1, 64, 100), (tr.F32, 4, 64, 1 << 24)):
         assert tr.head_logits_q4_bytes(*bad) == 0 and "unsupported" in tr.last_error()
-    for V in (1, 1024, 1025, 128000):
+    for V in (16385, 20000, 128000):
         sizes = [tr.logit_pick_bytes(T, V) for T in range(0, 700)]
         assert min(sizes) > 0 and sizes == sorted(sizes)
-    assert tr.logit_pick_bytes(4, 0) == 0 and tr.logit_pick_bytes(-1, 10) == 0
+    assert tr.logit_pick_bytes(700, 1) == tr.logit_pick_bytes(700, 16384) == 0 and tr.last_error() == ""
+    for bad in ((4, 0), (-1, 10), (4, 1 << 24)):
+        assert tr.logit_pick_bytes(*bad) == 0 and "unsupported" in tr.last_error()
 
 
 class Stand(torch.Tensor):
