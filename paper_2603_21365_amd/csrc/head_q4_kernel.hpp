@@ -86,6 +86,12 @@ template <int DT> __device__ __forceinline__ float q4_sum8(const u32x4 (&c)[Stor
     q4_values<DT>(c, x);
     return ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
 }
+// The sum of their magnitudes.
+template <int DT> __device__ __forceinline__ float q4_size8(const u32x4 (&c)[Storage<DT>::kBytes / 2]) {
+    float x[8];
+    q4_values<DT>(c, x);
+    return ((fabsf(x[0]) + fabsf(x[1])) + (fabsf(x[2]) + fabsf(x[3]))) + ((fabsf(x[4]) + fabsf(x[5])) + (fabsf(x[6]) + fabsf(x[7])));
+}
 template <int DT> __device__ __forceinline__ uint32_t q4_most8(const u32x4 (&c)[Storage<DT>::kBytes / 2]) {
     typedef __attribute__((ext_vector_type(2))) uint16_t u16x2;
     if constexpr (DT == kF32) {
@@ -282,13 +288,15 @@ template <int DT> constexpr int kQ4Sums = DT == kF32 ? 2 : 1;
 // ---- Rows under a head in four bits: what the two kernels share.
 
 // The operands of a block of 128 columns from what four groups of lanes, `apart` lanes each, have of its rows: fragment j, plane to x + (j planes + plane) * step, and the
-// sums of each group of columns times -1.5 to offs[(group sums + sum) * offs_step].
+// sums of each group of columns times -1.5 to offs[(group sums + sum) * offs_step]: NaN where the magnitudes add up to 2^126 or more (infinities, NaN), so that no logit of such a
+// row is a number.  Below that no sum of a group's products leaves the range.
 template <int DT, int kRuns> __device__ __forceinline__ void q4_put(const Q4Raw<DT>& raw, int g, int apart, char* x, int step, float* offs, int offs_step) {
 #pragma unroll
     for (int j0 = 0; j0 < 4; j0 += kRuns) {
-        float sum[kQ4Sums<DT>] = {};
+        float sum[kQ4Sums<DT>] = {}, size = 0.0f;
 #pragma unroll
         for (int j = j0; j < j0 + kRuns; ++j) {
+            size += q4_size8<DT>(raw.c[j]);
             if constexpr (DT == kF32) {
                 float y[8];
 #pragma unroll
@@ -314,11 +322,13 @@ template <int DT, int kRuns> __device__ __forceinline__ void q4_put(const Q4Raw<
                 *reinterpret_cast<u32x4*>(x + j * step) = raw.c[j][0];
             }
         }
+        size += __shfl_xor(size, apart, kWave);
+        size += __shfl_xor(size, 2 * apart, kWave);
 #pragma unroll
         for (int h = 0; h < kQ4Sums<DT>; ++h) {
             sum[h] += __shfl_xor(sum[h], apart, kWave);
             sum[h] += __shfl_xor(sum[h], 2 * apart, kWave);
-            if (g == 0) offs[(j0 / kRuns * kQ4Sums<DT> + h) * offs_step] = -1.5f * sum[h];
+            if (g == 0) offs[(j0 / kRuns * kQ4Sums<DT> + h) * offs_step] = size < 0x1p126f ? -1.5f * sum[h] : __uint_as_float(0x7fc00000u);
         }
     }
 }
