@@ -332,9 +332,10 @@ int tide_head_distill_grad(const void* x, int dtype, int64_t T, int64_t d, int64
  *   s = m / 7 rounded once to scale_dtype,   c = 8 + round(w / s), ties to even, 1 .. 15
  *   where m / 7 rounds to zero: s = 0, c = 8.  A group with a value that is not finite, or whose scale does not fit: s = NaN, c = 8.  Codes beyond V and d are 8.
  * tide_head_dequantize_q4: W[v,i] = s (c - 8), rounded once to `dtype`.
- * tide_head_logits_q4: logits[t,v] = sum_i x[t,i] W[v,i], W as it stands for, not rounded: products of 16-bit values and codes are exact (fp32 rows are taken as
- *   three bf16 terms, which add up to them), the sums and the scales' products in fp32.  A row of x that is not finite has NaN for all of its logits, as has one whose
- *   magnitudes in a group of columns add up to 2^126 or more; no other row does.  bf16 terms below 2^-126 may be taken as zero.
+ * tide_head_logits_q4: logits[t,v] = sum_i x[t,i] W[v,i], W as it stands for, not rounded: products x (c - 8) of 16-bit values and codes are exact (fp32 rows are taken as
+ *   three bf16 terms, which add up to them), a group's sum of them, its product with the scale and the groups' sum are in fp32.  A column whose weight is zero adds nothing to a
+ *   logit or its roundings, however large x is there.  A row of x that is not finite has NaN for all of its logits, as has one whose magnitudes in a group of
+ *   columns add up to 2^126 or more; no other row does, unless a scale is infinite or what a group adds is beyond fp32.  bf16 terms below 2^-122 may be taken as zero.
  *   The results do not depend on timing.
  *
  *   W       device [V rows] of `dtype`, x device [T rows] of `dtype`; strides in elements.  Element alignment is enough; 16-byte bases and strides are faster.

@@ -102,18 +102,17 @@ struct Q4Plan {
     bool few;
 
     int few_lds(int log, int nt_, int waves_, int split_) const {
-        return (int)(blocks * (4 * planes * (64 << log) + per * (planes > 1 ? kQ4Sums<kF32> : 1) * (4 << std::max(log, 2)))) + waves_ * 1024 + (split_ > 1 ? waves_ * nt_ * 1024 : 0);
+        return (int)(blocks * 4 * planes * (64 << log)) + waves_ * 1024 + (split_ > 1 ? waves_ * nt_ * 1024 : 0);
     }
     int64_t sets() const { return (tiles + waves * nt - 1) / (waves * nt); }
 };
 constexpr int kQ4MostParts = 16;
 constexpr int64_t kQ4PartBytes = (int64_t)32 << 20;    // of all parts' logits
 bool q4_parts_fit(int64_t T, int64_t V, int parts) { return parts == 1 || 4 * T * V * parts <= kQ4PartBytes; }
-// The parts of the columns with which few rows fit in LDS (`most` bytes), with groups of 32 columns and `waves` waves' scales; 0: too many.
+// The parts of the columns with which few rows fit in LDS (`most` bytes), with `waves` waves' scales; 0: too many.
 int q4_few_parts(int dtype, int64_t T, int64_t d, int waves, int most) {
     Q4Plan p{};
     p.planes = dtype == TIDE_F32 ? kQ4Planes<kF32> : 1;
-    p.per = 4;
     int log = 0;
     while ((1 << log) < T && log < 4) ++log;
     const int64_t all = (d + kQ4Cols - 1) / kQ4Cols;
@@ -162,7 +161,7 @@ Q4Plan q4_plan(int dtype, int64_t T, const Q4Shape& s, unsigned cus) {
     double least = 0;
     for (int mt : kQ4ManyTiles) {
         if (p.planes > 1 && mt != 2) continue;
-        const int nt = mt == 8 ? 4 : 2, most = 32 / nt, region = 4 * p.planes * mt * 1024 + 1024;
+        const int nt = mt == 8 ? 4 : 2, most = 32 / nt, region = 4 * p.planes * mt * 1024;
         const int stages = 2 * region + most * (3 * nt + 2) * 1024 <= kMostLds ? 3 : 2;
         const double rows = mt * p.planes, alone = 0.15 + (0.06 + 0.01 * p.per) * rows * (nt == 4 ? 1.4 : 1.0), all_tokens = 0.4 + (0.03 + 0.012 * p.per) * rows;
         for (int waves : {most, most / 4}) {
@@ -181,14 +180,13 @@ Q4Plan q4_plan(int dtype, int64_t T, const Q4Shape& s, unsigned cus) {
     return p;
 }
 
-// The rows' regions.  Row blocks of 16 mt rows for any mt, and groups of 32 columns: no matter how many tokens, and more than any call of fewer rows takes.  (A region's sums are at
-// most 512 bytes a tile, its padding included.)
+// The rows' regions.  Row blocks of 16 mt rows for any mt: no matter how many tokens, and more than any call of fewer rows takes.
 int64_t q4_lay_bytes(int dtype, int64_t T, int64_t d) {
     const int64_t planes = dtype == TIDE_F32 ? kQ4Planes<kF32> : 1, blocks = (d + kQ4Cols - 1) / kQ4Cols;
     int64_t tiles = 0;
     for (int mt : kQ4ManyTiles)
         if (planes == 1 || mt == 2) tiles = std::max(tiles, (T + 16 * mt - 1) / (16 * mt) * mt);
-    return (tiles * blocks * (4 * planes * 1024 + 512) + 255) & ~int64_t(255);
+    return (tiles * blocks * 4 * planes * 1024 + 255) & ~int64_t(255);
 }
 
 constexpr int64_t kMostPast = (int64_t)1 << 30;
@@ -396,7 +394,7 @@ int tide_head_logits_q4(const void* x, int dtype, int64_t T, int64_t d, int64_t 
                 const int64_t sets = plan.sets();
                 const bool by_xcd = q4_by_xcd(sets);
                 const Q4ManyParams p{(const char*)workspace, head, sums, sums_stride, part_stride, (int)plan.blocks, (int)T, (int)plan.row_blocks, (int)sets, by_xcd};
-                const int lds = q4_many_lds<NT>(Q4Region<DT, kRuns, MT>::kBytes, kQ4CodeStages<DT, kRuns, MT, NT>, plan.waves);
+                const int lds = q4_many_lds<NT>(kQ4Region<DT, MT>, kQ4CodeStages<DT, MT, NT>, plan.waves);
                 const int64_t together = std::min<int64_t>(kMostLds / lds, kQ4ManyThreads<NT> / kWave / plan.waves);
                 const int64_t items = by_xcd ? (sets + 7) / 8 * 8 * plan.row_blocks : (sets * plan.row_blocks + 7) / 8 * 8;      // (an XCD that has a set more than others has room for it)
                 const int64_t grid = std::min(items, std::max<int64_t>(8, cus * together / plan.parts / 8 * 8));

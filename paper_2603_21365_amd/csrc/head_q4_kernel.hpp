@@ -2,10 +2,13 @@
 //
 // The codes' layout is the matrix cores'.  A tile is 16 rows of the head and 128 columns, 1024 bytes, 16 for each lane of a wave; lane l has row l % 16, and in its
 // dword j the eight columns 32 j + 8 (l / 16) ..+7: what it supplies to the 16 x 16 x 32 matrix step on the tile's columns 32 j ..+31.  Within a dword column 2i has bits
-// 4i ..+3 and column 2i + 1 bits 16 + 4i ..+3, so that one shift and one and-or make a pair of adjacent 16-bit values:
-// the code in the top mantissa bits of a number in [1, 2), 1 + c / 16.  A group's sum is then
-//     sum x (c - 8) = 16 (sum x (1 + c / 16) - 1.5 sum x),
-// the products exact, the sums in fp32, and the scale is applied to it in fp32.  No weight is rounded.
+// 4i ..+3 and column 2i + 1 bits 16 + 4i ..+3, and one mask takes the same nibble of both.
+// A group's sum is
+//     sum x (c - 8) = 16 sum x ((c - 8) / 16),
+// the operands (c - 8) / 16 and the products exact, the sums in fp32, and the scale is applied to it in fp32.  No weight is rounded, and a column whose weight is zero adds
+// nothing, neither to a sum nor to its roundings.  (Operands 1 + c / 16, a shift and an and-or for two, with sums that start from -1.5 sum x, save six instructions of
+// fourteen for eight codes in bf16, but round every sum at the size of 24 |x| whatever the weights are: twelve columns of no weight, 5000 times as large as the others, made
+// errors of 2e-4 to 4e-4 of the logits in the mean square, where these are 5e-8 to 9e-8 with and without such columns.)
 #pragma once
 #include <type_traits>
 
@@ -64,7 +67,7 @@ template <int DT> __device__ __forceinline__ void q4_raw(const Q4Rows& p, int t,
         }
     }
 }
-// Eight of them in 32 bits, their sum, and the bits of the largest magnitude (infinities and NaN above all else).
+// Eight of them in 32 bits, the sum of their magnitudes, and the bits of the largest magnitude (infinities and NaN above all else).
 template <int DT> __device__ __forceinline__ void q4_values(const u32x4 (&c)[Storage<DT>::kBytes / 2], float (&x)[8]) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
@@ -81,12 +84,6 @@ template <int DT> __device__ __forceinline__ void q4_values(const u32x4 (&c)[Sto
         }
     }
 }
-template <int DT> __device__ __forceinline__ float q4_sum8(const u32x4 (&c)[Storage<DT>::kBytes / 2]) {
-    float x[8];
-    q4_values<DT>(c, x);
-    return ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
-}
-// The sum of their magnitudes.
 template <int DT> __device__ __forceinline__ float q4_size8(const u32x4 (&c)[Storage<DT>::kBytes / 2]) {
     float x[8];
     q4_values<DT>(c, x);
@@ -267,36 +264,61 @@ template <int E> __device__ __forceinline__ f32x4 q4_mma(u32x4 a, u32x4 b, f32x4
     if constexpr (E == kBF16) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), acc, 0, 0, 0);
     else return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), acc, 0, 0, 0);
 }
-// Eight codes as numbers 1 + c / 16: a shift and an and-or for two (the constants from registers, as that instruction takes no literals).
-template <int E> struct Q4Ones {
-    uint32_t mask = E == kBF16 ? 0x00780078u : 0x03c003c0u, one = E == kBF16 ? 0x3f803f80u : 0x3c003c00u;
-    __device__ __forceinline__ Q4Ones() { asm("" : "+s"(mask), "+v"(one)); }
+// Eight codes as numbers (c - 8) / 16, in pairs.
+//   fp16  a nibble in the lowest mantissa bits of 64, whose steps are 1/16, or in the next four of 4, and a packed subtraction of 64.5 or 4.5: a shift, four and-or and four
+//         subtractions.  (The constants from registers, as the and-or takes no literals.)
+//   bf16  there is no packed arithmetic of that type: with its top bit turned a code is a signed number of four bits, which one instruction makes a float of a 16th of (of a byte's
+//         lower nibble); the upper halves of two are a pair.  Fourteen instructions.
+template <int B> __device__ __forceinline__ float q4_sixteenths(uint32_t w) {
+    float f;
+    if constexpr (B == 0) asm("v_cvt_off_f32_i4_sdwa %0, %1 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_0" : "=v"(f) : "v"(w));
+    else if constexpr (B == 1) asm("v_cvt_off_f32_i4_sdwa %0, %1 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_1" : "=v"(f) : "v"(w));
+    else if constexpr (B == 2) asm("v_cvt_off_f32_i4_sdwa %0, %1 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_2" : "=v"(f) : "v"(w));
+    else asm("v_cvt_off_f32_i4_sdwa %0, %1 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_3" : "=v"(f) : "v"(w));
+    return f;
+}
+template <int E> struct Q4Centred {
     __device__ __forceinline__ u32x4 expand(uint32_t w) const {
-        if constexpr (E == kBF16) return u32x4{(w << 3 & mask) | one, (w >> 1 & mask) | one, (w >> 5 & mask) | one, (w >> 9 & mask) | one};
-        else return u32x4{(w << 6 & mask) | one, (w << 2 & mask) | one, (w >> 2 & mask) | one, (w >> 6 & mask) | one};
+        const uint32_t u = w ^ 0x88888888u, v = u >> 4;
+        auto pair = [](float a, float b) { return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u); };
+        return u32x4{pair(q4_sixteenths<0>(u), q4_sixteenths<2>(u)), pair(q4_sixteenths<0>(v), q4_sixteenths<2>(v)), pair(q4_sixteenths<1>(u), q4_sixteenths<3>(u)),
+                     pair(q4_sixteenths<1>(v), q4_sixteenths<3>(v))};
+    }
+};
+template <> struct Q4Centred<kF16> {
+    uint32_t low = 0x000f000fu, next = 0x00f000f0u, sixty_four = 0x54005400u, four = 0x44004400u;
+    __device__ __forceinline__ Q4Centred() { asm("" : "+s"(low), "+s"(next), "+v"(sixty_four), "+v"(four)); }
+    __device__ __forceinline__ u32x4 expand(uint32_t w) const {
+        const uint32_t v = w >> 8;
+        const f16x2 a = {(_Float16)64.5f, (_Float16)64.5f}, b = {(_Float16)4.5f, (_Float16)4.5f};
+        auto less = [](uint32_t bits, f16x2 by) { return __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, bits) - by); };
+        return u32x4{less((w & low) | sixty_four, a), less((w & next) | four, b), less((v & low) | sixty_four, a), less((v & next) | four, b)};
     }
 };
 // fp32 rows are three bf16 planes that add up to them exactly: the first eight significant bits, the next eight, the last eight, cut off and not rounded, so that none is
 // larger than the value.
 template <int DT> constexpr int kQ4Planes = DT == kF32 ? 3 : 1;
 template <int DT> constexpr int kQ4Elem = DT == kF32 ? (int)kBF16 : DT;
-// A group has a sum of its first plane's products and another of the rest's, with a start each.  The first's terms have few bits, so that it is all but exact although the
-// offset cancels most of it; the other is 2^-8 of it, and so are its roundings.  (One sum, from a start of all 24 bits, rounds at the size from before it cancels: errors of
-// up to 1.3e-6 of the logits' size, and 2e-7 like this, which is what rows in bf16 have.)
+// A group has a sum of its first plane's products and another of the rest's: the first's terms have few bits, so that it is all but exact, and the other is 2^-8 of it, and so are
+// its roundings.
 template <int DT> constexpr int kQ4Sums = DT == kF32 ? 2 : 1;
 
 // ---- Rows under a head in four bits: what the two kernels share.
 
-// The operands of a block of 128 columns from what four groups of lanes, `apart` lanes each, have of its rows: fragment j, plane to x + (j planes + plane) * step, and the
-// sums of each group of columns times -1.5 to offs[(group sums + sum) * offs_step]: NaN where the magnitudes add up to 2^126 or more (infinities, NaN), so that no logit of such a
-// row is a number.  Below that no sum of a group's products leaves the range.
-template <int DT, int kRuns> __device__ __forceinline__ void q4_put(const Q4Raw<DT>& raw, int g, int apart, char* x, int step, float* offs, int offs_step) {
+// The operands of a block of 128 columns from what four groups of lanes, `apart` lanes each, have of its rows: fragment j, plane to x + (j planes + plane) * step.  Where a row's
+// magnitudes in a group of columns add up to 2^126 or more (infinities, NaN) its values there are NaN, so that no logit of the row is a number; below that no sum of a group's
+// products leaves the range.
+template <int DT, int kRuns> __device__ __forceinline__ void q4_put(const Q4Raw<DT>& raw, int apart, char* x, int step) {
 #pragma unroll
     for (int j0 = 0; j0 < 4; j0 += kRuns) {
-        float sum[kQ4Sums<DT>] = {}, size = 0.0f;
+        float size = 0.0f;
+#pragma unroll
+        for (int j = j0; j < j0 + kRuns; ++j) size += q4_size8<DT>(raw.c[j]);
+        size += __shfl_xor(size, apart, kWave);
+        size += __shfl_xor(size, 2 * apart, kWave);
+        const uint32_t nan = size < 0x1p126f ? 0u : 0x7fff7fffu;
 #pragma unroll
         for (int j = j0; j < j0 + kRuns; ++j) {
-            size += q4_size8<DT>(raw.c[j]);
             if constexpr (DT == kF32) {
                 float y[8];
 #pragma unroll
@@ -307,28 +329,15 @@ template <int DT, int kRuns> __device__ __forceinline__ void q4_put(const Q4Raw<
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const uint32_t a = __float_as_uint(y[2 * e]) & 0xffff0000u, b = __float_as_uint(y[2 * e + 1]) & 0xffff0000u;
-                        v[e] = a >> 16 | b;
+                        v[e] = a >> 16 | b | nan;
                         y[2 * e] -= __uint_as_float(a);
                         y[2 * e + 1] -= __uint_as_float(b);
-                        if (plane == 0) sum[0] += __uint_as_float(a) + __uint_as_float(b);
                     }
-                    if (plane == 0)
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) sum[1] += y[e];
                     *reinterpret_cast<u32x4*>(x + (j * 3 + plane) * step) = v;
                 }
             } else {
-                sum[0] += q4_sum8<DT>(raw.c[j]);
-                *reinterpret_cast<u32x4*>(x + j * step) = raw.c[j][0];
+                *reinterpret_cast<u32x4*>(x + j * step) = raw.c[j][0] | u32x4{nan, nan, nan, nan};
             }
-        }
-        size += __shfl_xor(size, apart, kWave);
-        size += __shfl_xor(size, 2 * apart, kWave);
-#pragma unroll
-        for (int h = 0; h < kQ4Sums<DT>; ++h) {
-            sum[h] += __shfl_xor(sum[h], apart, kWave);
-            sum[h] += __shfl_xor(sum[h], 2 * apart, kWave);
-            if (g == 0) offs[(j0 / kRuns * kQ4Sums<DT> + h) * offs_step] = size < 0x1p126f ? -1.5f * sum[h] : __uint_as_float(0x7fc00000u);
         }
     }
 }
@@ -376,9 +385,8 @@ __global__ __launch_bounds__(kQ4Threads) void tide_head_q4_join_kernel(Q4JoinPar
 
 // ---- Few rows, up to 16: all of them in LDS.
 //
-// A workgroup lays the rows out once -- as fragments, 16 bytes (eight columns) of each row side by side, with the groups' sums times -1.5, which the matrix steps of a
-// group start from: no instruction is spent on the offset -- and its waves then stream tiles of codes, each wave NT tiles at a time, kDepth blocks of 128
-// columns ahead.  The scales come a kilobyte at a time through LDS (a load of each step's scales, 32 bytes of use, cost 4 of 50 us at one row, 128000 x 4096).
+// A workgroup lays the rows out once -- as fragments, 16 bytes (eight columns) of each row side by side -- and its waves then stream tiles of codes, each wave NT tiles at a
+// time, kDepth blocks of 128 columns ahead.  The scales come a kilobyte at a time through LDS (a load of each step's scales, 32 bytes of use, cost 4 of 50 us at one row, 128000 x 4096).
 // Where there are few tokens, `split` waves share the columns of a wave's tiles and add up their sums, in order, through LDS.
 // Bound by reading the codes (bf16, 128000 x 4096, groups of 128: 47 us at one row, 5.7 TB/s with the scales, 55 at 8, 57 at 16; a pure read of as much 41).
 struct Q4FewParams {
@@ -394,12 +402,11 @@ struct Q4FewParams {
 constexpr int kQ4FewThreads = 1024;
 
 struct Q4FewLds {
-    int offs, scales, sums, bytes;
+    int scales, sums, bytes;
 };
-template <int DT, int kRuns, int NT> __host__ __device__ inline Q4FewLds q4_few_lds(int rows_log, int blocks, int waves, int split) {
+template <int DT, int NT> __host__ __device__ inline Q4FewLds q4_few_lds(int rows_log, int blocks, int waves, int split) {
     Q4FewLds l{};
-    l.offs = blocks * 4 * kQ4Planes<DT> * (64 << rows_log);
-    l.scales = l.offs + blocks * (4 / kRuns) * kQ4Sums<DT> * (4 << (rows_log < 2 ? 2 : rows_log));
+    l.scales = blocks * 4 * kQ4Planes<DT> * (64 << rows_log);
     l.sums = l.scales + waves * 1024;
     l.bytes = l.sums + (split > 1 ? waves * NT * 1024 : 0);
     return l;
@@ -411,9 +418,9 @@ template <int DT, int kRuns, int NT, int kDepth> __global__ __launch_bounds__(kQ
     constexpr int kScaleBlocks = 32 / NT / kPer;       // blocks of 128 columns whose scales a kilobyte holds
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), waves = blockDim.x / kWave;
-    const int log = p.rows_log, rows = 1 << log, offs_log = log < 2 ? 2 : log, all = p.head.blocks, kb0 = blockIdx.y * p.part_blocks, blocks = min(p.part_blocks, all - kb0);
+    const int log = p.rows_log, rows = 1 << log, all = p.head.blocks, kb0 = blockIdx.y * p.part_blocks, blocks = min(p.part_blocks, all - kb0);
     float* const out = p.out + blockIdx.y * p.part_stride;
-    const Q4FewLds at = q4_few_lds<DT, kRuns, NT>(log, blocks, waves, p.split);
+    const Q4FewLds at = q4_few_lds<DT, NT>(log, blocks, waves, p.split);
 
     // the wave's tiles: NT of each set, blocks `begin` ..+`own`.  The first of them are on their way while the rows are laid out
     const int unit = wave / p.split, part = wave - unit * p.split, units = waves / p.split;
@@ -449,14 +456,13 @@ template <int DT, int kRuns, int NT, int kDepth> __global__ __launch_bounds__(kQ
         const int row = item & (rows - 1), g = item >> log & 3, kb = item >> (log + 2);
         Q4Raw<DT> raw;
         q4_raw<DT>(p.x, row, (kb0 + kb) * kQ4Cols + 8 * g, raw);
-        q4_put<DT, kRuns>(raw, g, rows, lds + ((kb * 16 * P + g) << (log + 4)) + row * 16, 64 << log, reinterpret_cast<float*>(lds + at.offs) + (kb * kPer * kSums << offs_log) + row, 1 << offs_log);
+        q4_put<DT, kRuns>(raw, rows, lds + ((kb * 16 * P + g) << (log + 4)) + row * 16, 64 << log);
     }
     __syncthreads();
 
-    const Q4Ones<E> ones;
+    const Q4Centred<E> centred;
     const uint32_t half = p.head.half ? 0xffffffffu : 0u;
     const char* const my_x = lds + ((lane >> 4) << (log + 4)) + (lane & (rows - 1)) * 16;
-    const float* const my_offs = reinterpret_cast<const float*>(lds + at.offs) + (4 * (lane >> 4) & ((1 << offs_log) - 1));
     char* const my_scales = lds + at.scales + wave * 1024;
     f32x4 total[NT];
 #pragma unroll
@@ -469,21 +475,14 @@ template <int DT, int kRuns, int NT, int kDepth> __global__ __launch_bounds__(kQ
             else fetch_scales(pass + 1, 0);
         }
         const char* x = my_x + ((begin + i) * 4 * P << (log + 6));
-        const float* offs = my_offs + ((begin + i) * kPer * kSums << offs_log);
 #pragma unroll
         for (int gr = 0; gr < kPer; ++gr) {
-            f32x4 sum[kSums][NT];
-#pragma unroll
-            for (int h = 0; h < kSums; ++h) {
-                const f32x4 start = *reinterpret_cast<const f32x4*>(offs + (gr * kSums + h << offs_log));
-#pragma unroll
-                for (int n = 0; n < NT; ++n) sum[h][n] = start;
-            }
+            f32x4 sum[kSums][NT] = {};
 #pragma unroll
             for (int j = gr * kRuns; j < (gr + 1) * kRuns; ++j) {
                 u32x4 w[NT];
 #pragma unroll
-                for (int n = 0; n < NT; ++n) w[n] = ones.expand(now[n][j]);
+                for (int n = 0; n < NT; ++n) w[n] = centred.expand(now[n][j]);
 #pragma unroll
                 for (int plane = 0; plane < P; ++plane) {
                     const u32x4 a = *reinterpret_cast<const u32x4*>(x + ((j * P + plane) << (log + 6)));
@@ -556,10 +555,8 @@ template <int DT, int kRuns, int NT, int kDepth> __global__ __launch_bounds__(kQ
 
 // ---- Many rows.
 //
-// The rows are first laid out in memory: for 16 MT rows and 128 columns one region, the fragments and behind them the groups' sums times -1.5, whole kilobytes.
-template <int DT, int kRuns, int MT> struct Q4Region {
-    static constexpr int kX = 4 * kQ4Planes<DT> * MT * 1024, kOffs = (4 / kRuns * kQ4Sums<DT> * MT * 64 + 1023) / 1024 * 1024, kBytes = kX + kOffs;
-};
+// The rows are first laid out in memory: for 16 MT rows and 128 columns one region, the fragments.
+template <int DT, int MT> constexpr int kQ4Region = 4 * kQ4Planes<DT> * MT * 1024;
 struct Q4LayParams {
     Q4Rows x;
     char* out;
@@ -567,14 +564,12 @@ struct Q4LayParams {
     int64_t waves;             // row tiles of all row blocks, times blocks
 };
 template <int DT, int kRuns, int MT> __global__ __launch_bounds__(kQ4Threads) void tide_head_q4_lay_kernel(Q4LayParams p) {
-    using R = Q4Region<DT, kRuns, MT>;
     const int64_t at = (int64_t)blockIdx.x * (kQ4Threads / kWave) + threadIdx.x / kWave;
     if (at >= p.waves) return;
     const int lane = threadIdx.x % kWave, tile = (int)(at / p.blocks), kb = (int)(at - (int64_t)tile * p.blocks), rb = tile / MT, rt = tile - rb * MT;
     Q4Raw<DT> raw;
     q4_raw<DT>(p.x, tile * 16 + (lane & 15), kb * kQ4Cols + 8 * (lane >> 4), raw);
-    char* region = p.out + ((int64_t)rb * p.blocks + kb) * R::kBytes;
-    q4_put<DT, kRuns>(raw, lane >> 4, 16, region + rt * 1024 + lane * 16, MT * 1024, reinterpret_cast<float*>(region + R::kX) + rt * 16 + (lane & 15), MT * 16);
+    q4_put<DT, kRuns>(raw, 16, p.out + ((int64_t)rb * p.blocks + kb) * kQ4Region<DT, MT> + rt * 1024 + lane * 16, MT * 1024);
 }
 
 // A workgroup has 16 MT rows and its waves NT tiles of 16 tokens each.  Everything comes to LDS by transfers that no register waits for: the rows' regions in two
@@ -595,7 +590,7 @@ struct Q4ManyParams {
 // Four tiles a wave, eight waves; or two tiles and sixteen waves
 template <int NT> constexpr int kQ4ManyThreads = 2048 / NT;
 template <int NT> __host__ __device__ constexpr int q4_many_lds(int region, int stages, int waves) { return 2 * region + waves * (stages * NT + 2) * 1024; }
-template <int DT, int kRuns, int MT, int NT> constexpr int kQ4CodeStages = q4_many_lds<NT>(Q4Region<DT, kRuns, MT>::kBytes, 3, kQ4ManyThreads<NT> / kWave) <= 158 * 1024 ? 3 : 2;
+template <int DT, int MT, int NT> constexpr int kQ4CodeStages = q4_many_lds<NT>(kQ4Region<DT, MT>, 3, kQ4ManyThreads<NT> / kWave) <= 158 * 1024 ? 3 : 2;
 
 // 64 lanes x 16 bytes from memory to a kilobyte of LDS (m0 as in the head products).  The wait states: five between a vector instruction that wrote the base and this one.
 __device__ __forceinline__ void q4_transfer(uint32_t lds, const char* base, uint32_t lane_bytes) {
@@ -603,8 +598,7 @@ __device__ __forceinline__ void q4_transfer(uint32_t lds, const char* base, uint
 }
 
 template <int DT, int kRuns, int MT, int NT> __global__ __launch_bounds__(kQ4ManyThreads<NT>) void tide_head_q4_many_kernel(Q4ManyParams p) {
-    using R = Q4Region<DT, kRuns, MT>;
-    constexpr int E = kQ4Elem<DT>, P = kQ4Planes<DT>, kSums = kQ4Sums<DT>, kPer = 4 / kRuns, kStages = kQ4CodeStages<DT, kRuns, MT, NT>, kSteps = kRuns * P, kAhead = 2;
+    constexpr int E = kQ4Elem<DT>, P = kQ4Planes<DT>, kSums = kQ4Sums<DT>, kPer = 4 / kRuns, kRegion = kQ4Region<DT, MT>, kStages = kQ4CodeStages<DT, MT, NT>, kSteps = kRuns * P, kAhead = 2;
     constexpr int kScaleBlocks = 32 / NT / kPer;       // blocks of 128 columns whose scales a kilobyte holds
     static_assert(kScaleBlocks >= 2, "a kilobyte is requested two blocks before it is read");
     extern __shared__ __attribute__((aligned(16))) char lds[];
@@ -616,17 +610,17 @@ template <int DT, int kRuns, int MT, int NT> __global__ __launch_bounds__(kQ4Man
     auto item_of = [&](int pass) { return first_item + min(pass, passes - 1) * stride; };
     auto tile_of = [&](int pass) { return ((item_of(pass) / p.row_blocks * xcds + xcd) * waves + wave) * NT; };
 
-    char* const my_codes = lds + 2 * R::kBytes + wave * (kStages * NT + 2) * 1024;
+    char* const my_codes = lds + 2 * kRegion + wave * (kStages * NT + 2) * 1024;
     char* const my_scales = my_codes + kStages * NT * 1024;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds, lane16 = lane * 16;
     const uint32_t codes0 = lds0 + (uint32_t)(my_codes - lds), scales0 = codes0 + kStages * NT * 1024;
     // the regions of the rows: every wave a part of each
-    const char* regions = p.regions + ((int64_t)(item_of(0) % p.row_blocks) * all + kb0) * R::kBytes;
+    const char* regions = p.regions + ((int64_t)(item_of(0) % p.row_blocks) * all + kb0) * kRegion;
     int x_pass = 0, x_kb = 0, x_stage = 0;
     auto request_region = [&] {
-        const char* from = regions + (int64_t)x_kb * R::kBytes;
-        for (int i = wave * 1024; i < R::kBytes; i += waves * 1024) q4_transfer(lds0 + x_stage * R::kBytes + i, from + i, lane16);
-        if (++x_kb == blocks) x_kb = 0, regions = p.regions + ((int64_t)(item_of(++x_pass) % p.row_blocks) * all + kb0) * R::kBytes;
+        const char* from = regions + (int64_t)x_kb * kRegion;
+        for (int i = wave * 1024; i < kRegion; i += waves * 1024) q4_transfer(lds0 + x_stage * kRegion + i, from + i, lane16);
+        if (++x_kb == blocks) x_kb = 0, regions = p.regions + ((int64_t)(item_of(++x_pass) % p.row_blocks) * all + kb0) * kRegion;
         x_stage ^= 1;
     };
     // the wave's codes; beyond its last block: the last tiles again, into a stage that nothing reads
@@ -653,7 +647,7 @@ template <int DT, int kRuns, int MT, int NT> __global__ __launch_bounds__(kQ4Man
 #pragma unroll
     for (int i = 1; i < kStages; ++i) request_codes();
 
-    const Q4Ones<E> ones;
+    const Q4Centred<E> centred;
     const uint32_t half = p.head.half ? 0xffffffffu : 0u;
     f32x4 total[NT][MT];
 #pragma unroll
@@ -672,50 +666,38 @@ template <int DT, int kRuns, int MT, int NT> __global__ __launch_bounds__(kQ4Man
             }
             request_region();
             request_codes();
-            const char* const x = lds + stage * R::kBytes + lane * 16;
-            const float* const offs = reinterpret_cast<const float*>(lds + stage * R::kBytes + R::kX) + 4 * (lane >> 4);
+            const char* const x = lds + stage * kRegion + lane * 16;
             u32x4 c[NT];
 #pragma unroll
             for (int n = 0; n < NT; ++n) c[n] = *reinterpret_cast<const u32x4*>(my_codes + (c_stage * NT + n) * 1024 + lane * 16);
 #pragma unroll
             for (int gr = 0; gr < kPer; ++gr) {
-                // fragments are read kAhead steps of NT matrix steps ahead of their use, a row tile's start one; the codes of a step are expanded beside the matrix steps of the
+                // fragments are read kAhead steps of NT matrix steps ahead of their use; the codes of a step are expanded beside the matrix steps of the
                 // one before
                 auto fragment = [&](int step) { return *reinterpret_cast<const u32x4*>(x + ((gr * kSteps + step % kSteps) * MT + step / kSteps) * 1024); };
-                auto first = [&](int rt, int h) { return *reinterpret_cast<const f32x4*>(offs + ((gr * kSums + h) * MT + rt) * 16); };
                 u32x4 a[kAhead], w[kRuns][NT];
-                f32x4 start[kSums];
-#pragma unroll
-                for (int h = 0; h < kSums; ++h) start[h] = first(0, h);
 #pragma unroll
                 for (int step = 0; step < kAhead; ++step) a[step] = fragment(step);
                 float s[NT];
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
                     s[n] = q4_scale_at(my_scales + s_read * 1024, NT, n, s_at * kPer + gr, lane, half);
-                    w[0][n] = ones.expand(c[n][gr * kRuns]);
+                    w[0][n] = centred.expand(c[n][gr * kRuns]);
                 }
 #pragma unroll
                 for (int rt = 0; rt < MT; ++rt) {
-                    f32x4 sum[kSums][NT];
-#pragma unroll
-                    for (int h = 0; h < kSums; ++h)
-#pragma unroll
-                        for (int n = 0; n < NT; ++n) sum[h][n] = start[h];
+                    f32x4 sum[kSums][NT] = {};
 #pragma unroll
                     for (int step = 0; step < kSteps; ++step) {
                         const int at = rt * kSteps + step;
                         const u32x4 now = a[at % kAhead];
-                        if (step + 1 == kSteps && rt + 1 < MT)
-#pragma unroll
-                            for (int h = 0; h < kSums; ++h) start[h] = first(rt + 1, h);
                         if (at + kAhead < MT * kSteps) a[at % kAhead] = fragment(at + kAhead);
                         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                         for (int n = 0; n < NT; ++n) sum[step % P > 0][n] = q4_mma<E>(now, w[step / P][n], sum[step % P > 0][n]);
                         if (rt == 0 && step % P == 0 && step / P + 1 < kRuns) {
 #pragma unroll
-                            for (int n = 0; n < NT; ++n) w[step / P + 1][n] = ones.expand(c[n][gr * kRuns + step / P + 1]);
+                            for (int n = 0; n < NT; ++n) w[step / P + 1][n] = centred.expand(c[n][gr * kRuns + step / P + 1]);
                         }
                         __builtin_amdgcn_sched_barrier(0);
                     }
