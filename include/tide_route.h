@@ -370,7 +370,7 @@ int tide_head_logits_q4(const void* x, int dtype, int64_t T, int64_t d, int64_t 
  *   logits  device [T rows] of `dtype`, row_stride >= V elements; element alignment.  past device [T,H] int32;  past_len, prompt_len device [T] int32
  *   repetition, presence, frequency device [T] fp32;  bias_ids int32, bias_values fp32 device [T,B], B <= 1024;  allowed device [T, ceil(V/32)] u32
  *   out     device [T rows] of `dtype`;  token device [T] int32, log_prob device [T] fp32
- *   T <= 4194304, V <= 8388608, T * V up to about 2^34 (TIDE_ERR_UNSUPPORTED)
+ *   T <= 4194303, V <= 8388608, T * V up to about 2^34 (TIDE_ERR_UNSUPPORTED)
  *   workspace  device, 16-byte aligned, tide_logit_pick_bytes(T, V) bytes, which grow with T and V; 0 (V up to 16384): none, and NULL will do.  No initialisation, nothing kept.
  *           0 bytes with tide_last_error() set: unsupported. */
 int tide_logit_rules(const void* logits, int dtype, int64_t T, int64_t V, int64_t row_stride, const int32_t* past, int64_t H, const int32_t* past_len,

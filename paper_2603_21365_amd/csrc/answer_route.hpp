@@ -189,6 +189,7 @@ int64_t q4_lay_bytes(int dtype, int64_t T, int64_t d) {
     return (tiles * blocks * 4 * planes * 1024 + 255) & ~int64_t(255);
 }
 
+constexpr int64_t kMostRuleRows = kMostBlocks / 4;     // a workgroup of 1024 threads each, at least
 constexpr int64_t kMostPast = (int64_t)1 << 30;
 constexpr int64_t kMostBias = kRuleThreads;            // a thread each
 constexpr int kRuleOneSlice = 24576;
@@ -235,7 +236,7 @@ struct RuleCall {
 int check_rules(const RuleCall& c, bool pick) {
     if (c.dtype != TIDE_F32 && c.dtype != TIDE_F16 && c.dtype != TIDE_BF16) return fail(TIDE_ERR_INVALID_ARG, "dtype %d is not a tide_dtype_t", c.dtype);
     if (c.T < 0) return fail(TIDE_ERR_INVALID_ARG, "T = %lld is negative", (long long)c.T);
-    if (c.T > kHeadMostRows) return fail(TIDE_ERR_UNSUPPORTED, "T = %lld exceeds %lld", (long long)c.T, (long long)kHeadMostRows);
+    if (c.T > kMostRuleRows) return fail(TIDE_ERR_UNSUPPORTED, "T = %lld exceeds %lld", (long long)c.T, (long long)kMostRuleRows);
     if (c.V <= 0) return fail(TIDE_ERR_INVALID_ARG, "V = %lld must be positive", (long long)c.V);
     if (c.V > kHeadMostVocab) return fail(TIDE_ERR_UNSUPPORTED, "V = %lld exceeds %lld", (long long)c.V, (long long)kHeadMostVocab);
     if (c.H < 0 || c.B < 0) return fail(TIDE_ERR_INVALID_ARG, "H = %lld and B = %lld must not be negative", (long long)c.H, (long long)c.B);
@@ -274,7 +275,7 @@ int run_rules(const RuleCall& c, bool pick) {
     RuleShape s{c.dtype, c.T, c.V, c.H, pick};
     if ((rc = resident_cus(&s.cus))) return rc;
     const int64_t slices = s.slices(), blocks = c.T * slices;
-    if (blocks > kMostBlocks / 4) return fail(TIDE_ERR_UNSUPPORTED, "T = %lld rows of V = %lld logits are too many for one call", (long long)c.T, (long long)c.V);
+    if (blocks > kMostRuleRows) return fail(TIDE_ERR_UNSUPPORTED, "T = %lld rows of V = %lld logits are too many for one call", (long long)c.T, (long long)c.V);
     if (pick && slices > 1) {
         const size_t need = (size_t)blocks * sizeof(uint4);
         if (!c.workspace || c.workspace_bytes < need) return fail(TIDE_ERR_WORKSPACE, "this call needs %zu bytes of workspace, %zu given", need, c.workspace ? c.workspace_bytes : 0);
@@ -435,7 +436,7 @@ int tide_logit_rules(const void* logits, int dtype, int64_t T, int64_t V, int64_
 
 size_t tide_logit_pick_bytes(int64_t T, int64_t V) {
     g_err[0] = 0;
-    if (T < 0 || T > kHeadMostRows || V < 1 || V > kHeadMostVocab) {
+    if (T < 0 || T > kMostRuleRows || V < 1 || V > kHeadMostVocab) {
         fail(TIDE_ERR_UNSUPPORTED, "unsupported T = %lld or V = %lld", (long long)T, (long long)V);
         return 0;
     }
