@@ -193,7 +193,7 @@ constexpr int64_t kMostRuleRows = kMostBlocks / 4;     // a workgroup of 1024 th
 constexpr int64_t kMostPast = (int64_t)1 << 30;
 constexpr int64_t kMostBias = kRuleThreads;            // a thread each
 constexpr int kRuleOneSlice = 24576;
-constexpr int kRuleMostSlice = 32768;                 // 64 KiB of counts: two workgroups a CU
+constexpr int kRuleMostSlice = 32768;                 // 64 KiB of counts: two workgroups a CU with up to 992 biases a row (8 bytes each, two bits a token), one with more
 
 // Slices of a row: as few as leave every CU two workgroups, of whole rounds of the workgroup's threads.  One where it spares the pick its second launch and is not the longer for it (us,
 // 44 rows in fp32: 16000 tokens, pasts of 500 14.3 -> 12.1; 24000, pasts of 8000, 300 biases 15.1 -> 14.5; 32000 of these 15.1 -> 16.1).

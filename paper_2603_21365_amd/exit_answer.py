@@ -53,7 +53,7 @@ class ExitAnswer:
 
 def answer_step(hidden, final_hidden, routers: Routers, norm_gain, eps, head: Head, **rules) -> ExitAnswer:
     """hidden [C,T,d], final_hidden [T,d] (the last layer's states, for tokens that no router lets exit), norm_gain f32 [d] | None and eps of the final norm;
-    ``rules``: logit_pick's past, penalties, biases and mask."""
+    ``rules``: logit_pick's past, penalties, biases and mask.  Inference only: no gradients."""
     r = routers
     exit_layer, _, _ = tr.select_exit_packed(hidden, r.packed, r.eps, r.b1, r.w2, r.b2, r.threshold, r.layer_ids, r.min_layer, r.n_layers, d=hidden.shape[-1],
                                              want_logits=False, want_mask=False)

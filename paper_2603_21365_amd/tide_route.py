@@ -719,7 +719,8 @@ def _q4(codes, scales, V, d, group):
 
 def head_quantize_q4(W, group=128, *, scale_dtype=torch.bfloat16):
     """An LM head W [V,d] in four bits with a scale per ``group`` (32, 64, 128) columns -> (codes uint8 [ceil(V/16), ceil(d/128), 1024], scales
-    [ceil(V/16), ceil(d/group), 16] of scale_dtype), as the header lays them out."""
+    [ceil(V/16), ceil(d/group), 16] of scale_dtype), as the header lays them out.  For inference, as all five answer operators: whatever requires a gradient gets none, and
+    what is returned is outside any graph."""
     (V, d), (ws, _) = _rows(W, 2)
     group, code = int(group), _scale_code(scale_dtype)
     if group not in (32, 64, 128):
@@ -732,7 +733,7 @@ def head_quantize_q4(W, group=128, *, scale_dtype=torch.bfloat16):
 
 
 def head_dequantize_q4(codes, scales, V, d, dtype, group=128):
-    """The weights [V,d] of ``dtype`` that codes and scales stand for."""
+    """The weights [V,d] of ``dtype`` that codes and scales stand for.  No gradient."""
     V, d, group, code = _q4(codes, scales, V, d, group)
     W = torch.empty((V, d), dtype=dtype, device=codes.device)
     _check(load_library().tide_head_dequantize_q4(_ptr(codes), _ptr(scales), code, V, d, group, _ptr(W), _dtype_code(W), d, _stream_on(W.device)))
@@ -745,7 +746,7 @@ def head_logits_q4_bytes(dtype: int, T: int, d: int, V: int) -> int:
 
 
 def head_logits_q4(x, codes, scales, V, group=128, *, out=None, workspace=None):
-    """Rows under an LM head in four bits: x [T,d], codes and scales as head_quantize_q4 gives them, V rows of the head -> logits f32 [T,V]."""
+    """Rows under an LM head in four bits: x [T,d], codes and scales as head_quantize_q4 gives them, V rows of the head -> logits f32 [T,V].  No gradient goes back to x."""
     (T, d), (xs, _) = _rows(x, 2)
     V, d, group, code = _q4(codes, scales, V, d, group)
     if out is None:
@@ -797,7 +798,7 @@ def logit_rules(logits, *, past=None, past_len=None, prompt_len=None, repetition
                 allowed=None, out=None):
     """The rules of decoding on logits [T,V]: past int32 [T,H] (negative: none), its length past_len and its prompt's prompt_len int32 [T]; repetition, presence,
     frequency f32 [T]; bias_ids int32, bias_values f32 [T,B]; allowed int32 [T, ceil(V/32)], a bit per token -> out [T,V] of the logits' dtype
-    (``out`` may be the logits)."""
+    (``out`` may be the logits).  No gradient goes back to any of them."""
     T, V, args = _rule_args(logits, past, past_len, prompt_len, repetition, presence, frequency, bias_ids, bias_values, allowed)
     if out is None:
         out = torch.empty((T, V), dtype=logits.dtype, device=logits.device)
@@ -809,13 +810,13 @@ def logit_rules(logits, *, past=None, past_len=None, prompt_len=None, repetition
 
 
 def logit_pick_bytes(T: int, V: int) -> int:
-    """Bytes of workspace a logit_pick call needs: 0 for up to 16384 tokens (and with last_error() if unsupported).  They grow with T."""
+    """Bytes of workspace a logit_pick call needs: 0 for up to 16384 tokens (and with last_error() if unsupported: more than 4194303 rows, 8388608 tokens).  They grow with T."""
     return int(load_library().tide_logit_pick_bytes(int(T), int(V)))
 
 
 def logit_pick(logits, *, past=None, past_len=None, prompt_len=None, repetition=None, presence=None, frequency=None, bias_ids=None, bias_values=None,
                allowed=None, workspace=None):
-    """The token with the largest logit under logit_rules' rules -> (token int32 [T], -1 where none is left; log_prob f32 [T])."""
+    """The token with the largest logit under logit_rules' rules -> (token int32 [T], -1 where none is left; log_prob f32 [T]).  No gradient: log_prob is outside any graph."""
     T, V, args = _rule_args(logits, past, past_len, prompt_len, repetition, presence, frequency, bias_ids, bias_values, allowed)
     token = torch.empty(T, dtype=torch.int32, device=logits.device)
     log_prob = torch.empty(T, dtype=torch.float32, device=logits.device)
