@@ -269,17 +269,12 @@ template <int E> __device__ __forceinline__ f32x4 q4_mma(u32x4 a, u32x4 b, f32x4
 //         subtractions.  (The constants from registers, as the and-or takes no literals.)
 //   bf16  there is no packed arithmetic of that type: with its top bit turned a code is a signed number of four bits, which one instruction makes a float of a 16th of (of a byte's
 //         lower nibble); the upper halves of two are a pair.  Fourteen instructions.
-template <int B> __device__ __forceinline__ float q4_sixteenths(uint32_t w) {
-    float f;
-    if constexpr (B == 0) asm("v_cvt_off_f32_i4_sdwa %0, %1 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_0" : "=v"(f) : "v"(w));
-    else if constexpr (B == 1) asm("v_cvt_off_f32_i4_sdwa %0, %1 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_1" : "=v"(f) : "v"(w));
-    else if constexpr (B == 2) asm("v_cvt_off_f32_i4_sdwa %0, %1 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_2" : "=v"(f) : "v"(w));
-    else asm("v_cvt_off_f32_i4_sdwa %0, %1 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_3" : "=v"(f) : "v"(w));
-    return f;
-}
+template <int B> __device__ __forceinline__ float q4_sixteenths(uint32_t w) { return __builtin_amdgcn_cvt_off_f32_i4(B == 0 ? w : B == 3 ? w >> 24 : w >> 8 * B & 0xffu); }
 template <int E> struct Q4Centred {
     __device__ __forceinline__ u32x4 expand(uint32_t w) const {
-        const uint32_t u = w ^ 0x88888888u, v = u >> 4;
+        const uint32_t u = w ^ 0x88888888u;
+        uint32_t v = u >> 4;
+        asm("" : "+v"(v));                             // (so that its bytes stay bytes, which the conversion can select, and do not become fields of u, which it cannot)
         auto pair = [](float a, float b) { return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u); };
         return u32x4{pair(q4_sixteenths<0>(u), q4_sixteenths<2>(u)), pair(q4_sixteenths<0>(v), q4_sixteenths<2>(v)), pair(q4_sixteenths<1>(u), q4_sixteenths<3>(u)),
                      pair(q4_sixteenths<1>(v), q4_sixteenths<3>(v))};
