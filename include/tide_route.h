@@ -359,7 +359,7 @@ int tide_head_logits_q4(const void* x, int dtype, int64_t T, int64_t d, int64_t 
  *   n > 0 times beyond the prompt:   a = a - (frequency[t] * n + presence[t])
  *   entries bias_ids[t,k] == v:      a = a + the sum of their bias_values[t,k], added up in their order
  *   bit v % 32 of allowed[t, v / 32] is 0:  a = -inf, whatever z[t,v] is
- * in fp32, each operation rounded by itself.  Tokens outside 0 .. V-1 (negative: none) do not count.  A NULL array's rule is left out (past: H = 0; biases: B = 0).
+ * in fp32, each operation rounded by itself (a quotient below 2^-126 may be off by one of its steps).  Tokens outside 0 .. V-1 (negative: none) do not count.  A NULL array's rule is left out (past: H = 0; biases: B = 0).
  *
  * tide_logit_rules: out[t,v] = a, rounded once to `dtype`; what no rule touches keeps its bits.  out may be the logits themselves (same base and stride), else
  *   it must not overlap them.

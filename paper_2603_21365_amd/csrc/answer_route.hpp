@@ -142,22 +142,24 @@ Q4Plan q4_plan(int dtype, int64_t T, const Q4Shape& s, unsigned cus) {
             p.blocks = (all + p.parts - 1) / p.parts, p.parts = (int)((all + p.blocks - 1) / p.blocks);
         }
         // Rows that leave room for several workgroups a CU: small ones, which start and end apart from each other; else one of as many waves as share its CU's tokens
-        // evenly, two tiles a wave where there are enough (bf16, d = 4096, V = 128000, us, 4 waves of one tile / 16 of two: T = 1 50 / 53, 8 63 / 55, 16 66 / 57).
+        // evenly, two tiles a wave where there are enough (bf16, d = 4096, V = 128000, us, 4 waves of one tile / 16 of two: T = 1 51 / 51, 8 61 / 52, 16 93 / 55; V = 32000, T = 1 17 / 42).
         const bool small = p.few_lds(p.rows_log, 1, 4, 1) <= kQ4SmallLds;
         const int64_t share = std::max<int64_t>(1, cus / p.parts);
         p.nt = !small && p.tiles >= 24 * share ? 2 : 1;
         p.waves = small ? 4 : (int)std::min<int64_t>(16, std::max<int64_t>(4, (p.tiles + p.nt * share - 1) / (p.nt * share)));
         p.split = 1;
-        // few tokens: waves share tiles until the chip is filled
+        // few tokens: waves share tiles while there are no more than eight a CU (us, a tile's columns on 1 / 2 / 4 waves; bf16, T = 1, d = 4096: V = 8000 15.7 / 10.1 / 8.3, 16000 16.2 / 12.0 / 11.4,
+        // 32003 19.9 / 17.8 / 18.0, 64000 31.5 / 31.2 / 30.6; T = 8, V = 16000 19.0 / 15.3 / 15.9, 64000 38.4 / 40.0 / 44.1; fp32, T = 4, d = 1600, V = 32003 13.2 / 13.0 / 13.6.  At four of 237
+        // shapes, of one or two rows, the rule is more than a tenth behind the best of the three: 8192 columns, V = 32003, T = 1 38 / 32 / 31)
         while (p.split < 4 && p.tiles * p.split * p.parts * 2 <= 8 * (int64_t)cus && p.split * 4 <= all - (p.parts - 1) * p.blocks) p.split *= 2;
         if (p.split > 1) p.waves = 4;
         p.lds = p.few_lds(p.rows_log, p.nt, p.waves, p.split);
         return p;
     }
-    // Many rows: what a CU's workgroups take, in us, fitted to 5500 measured launches of 140 shapes (the choice is 2.5 % off the fastest of them on average and 19 % at most).  What a block
+    // Many rows: what a CU's workgroups take, in us, fitted to measured launches of 140 shapes in all their divisions (the choice is 2.1 % off the fastest of them on average and 22 % at most).  What a block
     // of 128 columns takes a workgroup from end to end, in which the CU's other workgroups work, grows with a wave's tiles of rows; what it takes of the CU for 512 tokens, with
     // the workgroup's share of them; so do a workgroup's results at its end.  Parts of the columns cost a launch and their logits' traffic, and fill CUs where there are few tokens.
-    // (bf16, us: d = 8192, V = 1822, T = 43 63 whole and 32 in parts; d = 5120, V = 32401, T = 112, the fewest rounds of the largest workgroups 107, these 65.)
+    // (bf16, us, one part of the largest workgroups / these: d = 8192, V = 1822, T = 43 275 / 33; d = 5120, V = 32401, T = 112 144 / 59; d = 2560, V = 45641, T = 147 86 / 69.)
     double least = 0;
     for (int mt : kQ4ManyTiles) {
         if (p.planes > 1 && mt != 2) continue;

@@ -383,7 +383,8 @@ __global__ __launch_bounds__(kQ4Threads) void tide_head_q4_join_kernel(Q4JoinPar
 // A workgroup lays the rows out once -- as fragments, 16 bytes (eight columns) of each row side by side -- and its waves then stream tiles of codes, each wave NT tiles at a
 // time, kDepth blocks of 128 columns ahead.  The scales come a kilobyte at a time through LDS (a load of each step's scales, 32 bytes of use, cost 4 of 50 us at one row, 128000 x 4096).
 // Where there are few tokens, `split` waves share the columns of a wave's tiles and add up their sums, in order, through LDS.
-// Bound by reading the codes (bf16, 128000 x 4096, groups of 128: 47 us at one row, 5.7 TB/s with the scales, 55 at 8, 57 at 16; a pure read of as much 41).
+// Bound by reading the codes and making operands of them, which take 34 of these us in vector instructions (bf16, 128000 x 4096, groups of 128: 51 us at one row, 5.3 TB/s with
+// the scales, 54 at 8, 56 at 16; a pure read of as much 41).
 struct Q4FewParams {
     Q4Rows x;
     Q4Head head;
@@ -407,7 +408,7 @@ template <int DT, int NT> __host__ __device__ inline Q4FewLds q4_few_lds(int row
     return l;
 }
 
-// (One tile a wave: 72 registers, so that seven workgroups of four waves share a CU; fp32 rows' three terms would not fit, and five do.  76: T = 1 47.3 -> 48.6 us.)
+// (One tile a wave: up to 72 registers, so that seven workgroups of four waves share a CU; fp32 rows' three terms would not fit, and five do.  With 76 one row took 3 % longer.)
 template <int DT, int kRuns, int NT, int kDepth> __global__ __launch_bounds__(kQ4FewThreads, NT == 1 && DT != kF32 ? 7 : 4) void tide_head_q4_few_kernel(Q4FewParams p) {
     constexpr int E = kQ4Elem<DT>, P = kQ4Planes<DT>, kSums = kQ4Sums<DT>, kPer = 4 / kRuns;
     constexpr int kScaleBlocks = 32 / NT / kPer;       // blocks of 128 columns whose scales a kilobyte holds
@@ -570,8 +571,9 @@ template <int DT, int kRuns, int MT> __global__ __launch_bounds__(kQ4Threads) vo
 // A workgroup has 16 MT rows and its waves NT tiles of 16 tokens each.  Everything comes to LDS by transfers that no register waits for: the rows' regions in two
 // stages, for all waves, behind a barrier for each block of 128 columns; each wave's codes in two or three stages and its scales, a kilobyte at a time, in two.  The
 // transfers are inline assembly, which the compiler does not count, and the waits for them are written out; there are no other loads from memory in the loop.
-// Some dozen rows are bound by making operands of the codes (half of the vector instructions at 48 rows) beside the matrix steps, many by the matrix steps under the power
-// limit (bf16, 128000 x 4096, groups of 128: 48 rows 69 us, 512 rows 465, 1.16 PFLOP/s; with codes and scales through registers 84 and 512).
+// Some dozen rows are bound by making operands of the codes (two thirds of the vector instructions at 48 rows, which are 38 us) beside the matrix steps (20), many by the matrix
+// steps under the power limit (bf16, 128000 x 4096, groups of 128: 48 rows 76 us, 512 rows 467, 1.15 PFLOP/s.  Codes and scales through registers took a fifth longer at
+// 48 rows, a tenth at 512).
 struct Q4ManyParams {
     const char* regions;
     Q4Head head;

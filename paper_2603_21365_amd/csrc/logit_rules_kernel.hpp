@@ -6,8 +6,8 @@
 // pass.  Integer counts do not depend on the order of their atomics and every sum has a fixed order: the results do not depend on timing.
 //
 // Small calls are bound by the launch and the latency of a few dependent loads (one row of 128000 tokens in fp32, past of 700, 8 biases, mask: 4.9 us, with the largest
-// 5.9 and 1.7 for the join), large ones by vector instructions: 256 such rows with pasts of 4096 and 16 biases take 39 us, 3.4 TB/s, of which the past's rules, which
-// some lane of a wave nearly always needs, are more than half of the instructions and the exponentials a sixth.
+// 5.9 and 1.8 for the join), large ones by vector instructions: 256 such rows with pasts of 4096 and 16 biases take 41 us, 3.3 TB/s, of which the past's rules, which
+// some lane of a wave nearly always needs, are half of the instructions and the exponentials a fifth.
 #pragma once
 #include "device_utils.hpp"
 
