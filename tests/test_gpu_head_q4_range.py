@@ -36,3 +36,31 @@ def test_magnitudes_around_the_largest(dtype, T, group):
         bad = torch.tensor([i in (0, 1, 2) if rows is x else i == 1 for i in range(len(rows))])
         assert torch.isnan(got[bad]).all(), got[bad]
         assert torch.equal(got[~bad].double(), rows[~bad].double() @ w.T)
+
+
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_an_infinity_in_any_column_even_one_without_weight(dtype, group):
+    """Row i has one in column i, whose code is 8 for every second token: none of the row's logits is a number, all of the clean rows' are what they were."""
+    V, d = 37, 200
+    g = generator(group)
+    codes = torch.randint(0, 16, (V, d), generator=g).to(torch.uint8)
+    codes[::2] = 8
+    scales = torch.pow(2.0, torch.randint(-2, 3, (V, -(-d // group)), generator=g).float())
+    w, head = weights(codes, scales, group, d), packed(codes, scales.to(torch.bfloat16))
+    x = torch.randint(-4, 5, (2 * d, d), generator=g).float()
+    want = x.double() @ w.T
+    x[torch.arange(0, 2 * d, 2), torch.arange(d)] = float("inf")
+    x[2 * 150, 150] = float("nan")
+    rows = x.to(DTYPES[dtype]).cuda()
+    for got in (tr.head_logits_q4(rows, *head, V, group), torch.cat([tr.head_logits_q4(part, *head, V, group) for part in rows.split(13)])):
+        assert torch.isnan(got[::2]).all() and torch.equal(got[1::2].cpu().double(), want[1::2])
+
+
+@pytest.mark.parametrize("T", [4194303, 4194304])
+def test_the_most_rows(T):
+    V, d = 2, 3
+    codes, scales = torch.tensor([[9, 3, 15], [0, 8, 10]], dtype=torch.uint8), torch.tensor([[2.0], [0.5]])
+    x = torch.randint(-4, 5, (T, d), generator=torch.Generator(device="cuda").manual_seed(1), device="cuda").to(torch.bfloat16)
+    got = tr.head_logits_q4(x, *packed(codes, scales.to(torch.bfloat16)), V, 32)
+    assert torch.equal(got, (x.float()[:, None, :] * weights(codes, scales, 32, d).float().cuda()).sum(2))
